@@ -555,6 +555,106 @@ size_t atom_decode_attention_kv4_workspace_bytes(int32_t B, int32_t H,
                                                  int64_t Tmax);
 
 /*
+ * Paged KV cache in 8 bits.  The paper serves from a paged cache (Section 4.5) and quantises it per attention
+ * head (Section 4.4); the INT4 cache above is one rectangle for a batch, a token of every sequence a step.  Here
+ * the cache is a pool of blocks of block_tokens tokens, shared by all sequences, in 8 bits symmetrically (the
+ * symmetric equations of Section 2) with one scale for each block of tokens and head:
+ *   codes [n_blocks, Hkv, block_tokens, D] int8, value = code * scale;   scale [n_blocks, Hkv] fp32
+ * (K and V each one such pair).  A step of any mixture of requests, with one new token each or many, is three
+ * calls: atom_kv_block_map, atom_kv8_append for every layer, atom_attention_kv8 for every layer.
+ * block_tokens is 16, 32, 64 or 128, D 64 or 128.
+ *
+ * atom_kv_block_map: the tables of a step from the requests' lengths, on the device.  With past = past_len[b] and
+ * new = new_len[b] (negative values count as 0), p(n) = min(W, ceil(n / block_tokens)):
+ *   token_start[b]  = sum of new over the requests before b, b = 0 .. B      (the step's tokens lie in this order)
+ *   seq_len[b]      = past + new
+ *   block_table[b, j]: j < p(past) kept; p(past) <= j < p(past + new) the next block of the free list; -1 beyond
+ *   slot[t]         = the cache row of token t, block * block_tokens + row of the block; -1 where it has no
+ *                     block (the free list ended, the table is full) and for t >= token_start[B]
+ * Requests take blocks in their order, request b's first one being free_blocks[cursor + blocks taken before b];
+ * past the list's end (or before its beginning) a block is -1.  Sums saturate at 2^31 - 1.
+ *
+ *   past_len, new_len  device int32 [B]
+ *   free_blocks   device int32 [n_free] block numbers; cursor: device int32, where to begin in it, or NULL for 0
+ *   block_table   device int32 [B, W], in and out
+ *   T             length of slot (of the step's padded token arrays): tokens beyond it get no slot
+ *   token_start [B + 1], seq_len [B], slot [T]   device int32, outputs, none of them an input's memory
+ *   cursor_out    device int32 or NULL: cursor + all blocks that the step wanted (more than n_free: so many are
+ *                 missing); not the memory of cursor
+ * The call with the same inputs and the table that it left gives the same again.  One launch, no workspace.
+ * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE (negative sizes, W = 0 with B > 0), ATOM_ERR_ALIGN, ATOM_ERR_UNSUPPORTED
+ * (block_tokens, B > 16384, W * block_tokens > 2^30, B * W >= 2^31, T >= 2^31 - 1).  B = 0 gives
+ * token_start[0] = 0 and slots of -1.
+ */
+atom_status atom_kv_block_map(const int32_t *past_len, const int32_t *new_len, int32_t B,
+                              int32_t block_tokens, const int32_t *free_blocks, int64_t n_free,
+                              const int32_t *cursor, int32_t *block_table, int64_t W, int64_t T,
+                              int32_t *token_start, int32_t *seq_len, int32_t *slot,
+                              int32_t *cursor_out, void *stream);
+
+/*
+ * atom_kv8_append: the step's K and V rows, quantised, into their slots.  A run is a longest piece of tokens
+ * with successive slots in one block; o is the block's row of its first token.  For every head, K and V apart:
+ *   s_old = o > 0 ? scale[block, head] : 0
+ *   s     = max(s_old, max|x| / 127)          over the run's values of the head
+ *   code  = clamp(rne(x * (1 / s)), -127, 127)        (s = 0: codes 0)
+ *   and where s > s_old > 0 the o older rows' codes become rne(code * (s_old / s)).
+ * IEEE fp32, every step rounded once: results are bit-exact.  A row is off by half a step of the block's scale when it is
+ * written, and by at most half a step of the present scale more each time that the scale has grown since.
+ * Rows of the block behind the run are left as they are.  The same call again changes nothing but older rows'
+ * scales that it raised the first time.
+ *
+ *   k_f16, v_f16   device fp16, token t's heads from t * ldk (ldv) on, [Hkv, D] each; 16-byte aligned, ld % 8 == 0: slices
+ *                  of a fused projection's output as they are
+ *   slot           device int32 [T] as atom_kv_block_map gives it; a slot outside [0, n_blocks * block_tokens)
+ *                  writes nothing, whatever its row holds
+ *   k_codes, v_codes  16-byte aligned; k_scale, v_scale
+ * The tokens that one call writes into a block have to be one run, a slot may not come twice: a block that
+ * two runs share gets undefined contents (no other block does).
+ * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE, ATOM_ERR_ALIGN, ATOM_ERR_UNSUPPORTED (block_tokens, D, n_blocks *
+ * block_tokens >= 2^31, n_blocks * Hkv * block_tokens >= 2^35, T * Hkv >= 2^31).  T = 0 returns ATOM_OK.
+ */
+atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int64_t ldk, int64_t ldv,
+                            int32_t Hkv, int32_t D, const int32_t *slot, int64_t n_blocks,
+                            int32_t block_tokens, void *k_codes, float *k_scale, void *v_codes,
+                            float *v_scale, void *stream);
+
+/*
+ * atom_attention_kv8: causal attention of the step's queries over the cache, which already holds the step's own
+ * tokens.  Request b's queries are tokens token_start[b] .. token_start[b + 1] - 1; with n of them and
+ * L = seq_len[b], query i is at position L - n + i and sees the keys 0 .. L - n + i:
+ *   out[t, h, :] = softmax_s( sm_scale * q[t, h, :] . K[s] ) V[s],  K, V of cache head h / (H / Hkv)
+ * fp32 softmax and sums; queries and codes meet exactly in the fp16 matrix cores, the softmax weights travel as fp16.
+ * Keys of a block number outside [0, n_blocks) (-1: none) and beyond W * block_tokens do not exist; a query
+ * that sees no key gives zeros.  Rows of out behind token_start[B], and of tokens beyond max_new of a request, are left as
+ * they were; rows of q there are not read.
+ *
+ *   q_f16          device fp16, token t's heads [H, D] from t * ldq on; out_f16 likewise with ldo.  16-byte aligned, ld % 8 == 0
+ *   max_new        no request has more new tokens (T if nothing is known: the call is sized by it, 1 for a decoding step)
+ *   token_start, seq_len, block_table [B, W]   device int32, as atom_kv_block_map gives them
+ *   workspace      device scratch of atom_attention_kv8_workspace_bytes(...) bytes, 16-byte aligned (NULL when that
+ *                  is 0): where the tiles of query rows alone cannot fill the GPU the keys are shared out among
+ *                  more workgroups, evenly over all sequences whatever their lengths, whose partial results meet in a second kernel.
+ *                  Contents need no initialisation and are dead after the call.
+ * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE (H % Hkv, negative sizes, W = 0 with B > 0, ld), ATOM_ERR_ALIGN,
+ * ATOM_ERR_UNSUPPORTED (block_tokens, D, sm_scale negative, above 1e6 or no number, W * block_tokens > 2^30, a cache that
+ * atom_kv8_append does not take, T * H >= 2^31, more than 2^31 - 1 workgroups), ATOM_ERR_WORKSPACE.
+ * T = 0, B = 0 or max_new = 0 returns ATOM_OK.
+ */
+atom_status atom_attention_kv8(const void *q_f16, int64_t T, int64_t ldq, int32_t B, int32_t H,
+                               int32_t Hkv, int32_t D, int32_t max_new,
+                               const int32_t *token_start, const int32_t *seq_len,
+                               const int32_t *block_table, int64_t W, int64_t n_blocks,
+                               int32_t block_tokens, const void *k_codes, const float *k_scale,
+                               const void *v_codes, const float *v_scale, float sm_scale,
+                               void *out_f16, int64_t ldo, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/* Scratch atom_attention_kv8 needs for these sizes (0 when none, and for sizes that it refuses). */
+size_t atom_attention_kv8_workspace_bytes(int64_t T, int32_t B, int32_t H, int32_t Hkv, int32_t D,
+                                          int32_t max_new, int64_t W, int32_t block_tokens);
+
+/*
  * MX variant of the path.  The paper also runs its recipe with FP4 codes and
  * names the MX formats, whose group scaling new hardware applies by itself and
  * which it expects to remove the group-dequantisation overhead of the fused

@@ -23,6 +23,11 @@ from .binding import (  # noqa: F401
     atom_decode_attention_kv4_workspace_bytes,
     atom_decode_attention_kv4_static,
     atom_static_scratch_bytes,
+    atom_kv_block_map,
+    atom_kv8_cache,
+    atom_kv8_append,
+    atom_attention_kv8,
+    atom_attention_kv8_workspace_bytes,
     atom_status_string,
     atom_mfma_rate_probe,
     atom_w4a4_gemm,

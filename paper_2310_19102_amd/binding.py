@@ -54,6 +54,10 @@ EXPORTS = (
     "atom_decode_attention_kv4_workspace_bytes",
     "atom_decode_attention_kv4_static",
     "atom_static_scratch_bytes",
+    "atom_kv_block_map",
+    "atom_kv8_append",
+    "atom_attention_kv8",
+    "atom_attention_kv8_workspace_bytes",
     "atom_mfma_rate_probe",
     "atom_check_reorder_idx",
     "atom_status_string",
@@ -164,6 +168,15 @@ def load_library():
                                                    f32, vp, vp]
     L.atom_static_scratch_bytes.restype = sz
     L.atom_static_scratch_bytes.argtypes = []
+    L.atom_kv_block_map.restype = ctypes.c_int
+    L.atom_kv_block_map.argtypes = [vp, vp, i32, i32, vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, vp]
+    L.atom_kv8_append.restype = ctypes.c_int
+    L.atom_kv8_append.argtypes = [vp, vp, i64, i64, i64, i32, i32, vp, i64, i32, vp, vp, vp, vp, vp]
+    L.atom_attention_kv8.restype = ctypes.c_int
+    L.atom_attention_kv8.argtypes = [vp, i64, i64, i32, i32, i32, i32, i32, vp, vp, vp, i64, i64, i32, vp, vp, vp, vp, f32,
+                                     vp, i64, vp, sz, vp]
+    L.atom_attention_kv8_workspace_bytes.restype = sz
+    L.atom_attention_kv8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i64, i32]
     L.atom_mfma_rate_probe.restype = ctypes.c_double
     L.atom_mfma_rate_probe.argtypes = [i32, i32, vp, vp, ctypes.POINTER(ctypes.c_int)]
     L.atom_check_reorder_idx.restype = ctypes.c_int
@@ -522,6 +535,53 @@ def atom_decode_attention_kv4_static(q: torch.Tensor, k_cache: Tuple[torch.Tenso
     if out is None:
         raise ValueError("out must be given: this call allocates nothing")
     return _run().decode_attention_kv4_static(q, k_cache, v_cache, seq_len, sm_scale, out)
+
+
+def atom_kv8_cache(n_blocks: int, n_heads: int, head_dim: int, block_tokens: int = 64, device="cuda"):
+    """A pool of empty blocks of the paged 8-bit cache, ``(codes, scale)``: int8
+    [n_blocks, n_heads, block_tokens, head_dim] and float32 [n_blocks, n_heads].  One for K, one for V, per layer."""
+    return (torch.zeros((n_blocks, n_heads, block_tokens, head_dim), dtype=torch.int8, device=device),
+            torch.zeros((n_blocks, n_heads), dtype=torch.float32, device=device))
+
+
+def atom_kv_block_map(past_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Tensor,
+                      free_blocks: torch.Tensor, n_tokens: int, block_tokens: int = 64,
+                      cursor: Optional[torch.Tensor] = None, out: Optional[Tuple[torch.Tensor, ...]] = None):
+    """Tables of a step from the requests' lengths (device int32 ``past_len``, ``new_len`` [B]), one launch.
+    ``block_table`` [B, W] is brought up to date in place with blocks from ``free_blocks`` (from ``cursor`` on, a
+    device int32 of one element; None: from its beginning); -1 where a request has none.  Returns
+    ``(token_start [B + 1], seq_len [B], slot [n_tokens], cursor_out [1])``, int32: ``n_tokens`` is the length of
+    the step's (possibly padded) token arrays, tokens without a row of the cache have slot -1, ``cursor_out`` is
+    the next step's ``cursor`` (above ``free_blocks.numel()``: that many blocks were missing).  ``out``: the four
+    outputs' memory; none may be an input's."""
+    return _run().kv_block_map(past_len, new_len, block_table, free_blocks, n_tokens, block_tokens, cursor, out)
+
+
+def atom_kv8_append(k: torch.Tensor, v: torch.Tensor, k_cache: Tuple[torch.Tensor, ...],
+                    v_cache: Tuple[torch.Tensor, ...], slot: torch.Tensor):
+    """The step's K and V rows ([T, Hkv, D] fp16, each token's heads contiguous, any stride between tokens) quantised into
+    the blocks of their caches ``(codes, scale)`` (``atom_kv8_cache``) at ``slot`` [T] (``atom_kv_block_map``; -1: not
+    stored).  A block's scale grows with its contents; older rows are brought to it.  Returns
+    ``(k_cache, v_cache)``, updated in place."""
+    return _run().kv8_append(k, v, k_cache, v_cache, slot)
+
+
+def atom_attention_kv8_workspace_bytes(T: int, B: int, H: int, Hkv: int, D: int, max_new: int, W: int,
+                                       block_tokens: int = 64) -> int:
+    return int(load_library().atom_attention_kv8_workspace_bytes(T, B, H, Hkv, D, max_new, W, block_tokens))
+
+
+def atom_attention_kv8(q: torch.Tensor, k_cache: Tuple[torch.Tensor, ...], v_cache: Tuple[torch.Tensor, ...],
+                       block_table: torch.Tensor, token_start: torch.Tensor, seq_len: torch.Tensor, sm_scale: float,
+                       max_new: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None):
+    """Causal attention of a step's queries ``q`` [T, H, D] fp16 over the paged 8-bit cache: request b's tokens are
+    ``token_start[b] .. token_start[b + 1]``, the last ones of its ``seq_len[b]`` positions, and the cache holds them
+    already.  ``max_new``: no request has more new tokens (None: unknown; 1 for a decoding step).  Returns [T, H, D] fp16 (``out``
+    if given; rows behind the last request are left as they were).  In a capture that was not begun by torch.cuda.graph a
+    ``workspace`` has to be given where ``atom_attention_kv8_workspace_bytes`` is not 0."""
+    return _run().attention_kv8(q, k_cache, v_cache, block_table, token_start, seq_len, sm_scale,
+                                q.shape[0] if max_new is None else max_new, out, workspace)
 
 
 def _mx_outputs(rows: int, K: int, n_outlier: int, device):

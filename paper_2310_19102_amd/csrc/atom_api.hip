@@ -88,6 +88,25 @@ atom_status quantize_packed_common(const void *x, int64_t rows, int64_t ld, int 
     return err == hipSuccess ? ATOM_OK : ATOM_ERR_HIP;
 }
 
+// The paged 8-bit cache: its block sizes, what one cache may be, and the sizes of an attention call.
+bool kv8_block(int32_t block_tokens) { return block_tokens == 16 || block_tokens == 32 || block_tokens == 64 || block_tokens == 128; }
+
+bool kv8_cache(int64_t n_blocks, int32_t Hkv, int32_t D, int32_t block_tokens)
+{
+    return (D == 64 || D == 128) && kv8_block(block_tokens) && n_blocks <= 0x7fffffffLL / block_tokens &&
+           n_blocks * (block_tokens / 16) <= 0x7fffffffLL / Hkv;     // slots, and the blocks of 16 rows that the kernels count
+}
+
+atom_status kv8_attention(int64_t T, int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t max_new, int64_t W, int32_t block_tokens)
+{
+    if (T < 0 || B < 0 || H <= 0 || Hkv <= 0 || H % Hkv || D <= 0 || max_new < 0 || W < 0 || (B > 0 && W == 0)) return ATOM_ERR_SHAPE;
+    if ((D != 64 && D != 128) || !kv8_block(block_tokens) || T > 0x7ffffffeLL || W > 0x40000000LL / block_tokens ||
+        B > 0x3fffffff || T * H > 0x7fffffffLL || (int64_t)max_new * (H / Hkv) > 0x7fffffffLL ||
+        !atom_internal::attention_kv8_fits(T, B, H, Hkv, max_new, W, block_tokens))
+        return ATOM_ERR_UNSUPPORTED;
+    return ATOM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -562,6 +581,76 @@ atom_status atom_decode_attention_kv4_static(const void *q_f16, int32_t B, int32
     return atom_decode_attention_kv4(q_f16, B, H, Hkv, D, Tmax, seq_len, k_codes, k_scale, k_zero, v_codes,
                                      v_scale, v_zero, sm_scale, out_f16, ws,
                                      atom_internal::static_scratch_bytes(), stream);
+}
+
+atom_status atom_kv_block_map(const int32_t *past_len, const int32_t *new_len, int32_t B, int32_t block_tokens,
+                              const int32_t *free_blocks, int64_t n_free, const int32_t *cursor, int32_t *block_table,
+                              int64_t W, int64_t T, int32_t *token_start, int32_t *seq_len, int32_t *slot,
+                              int32_t *cursor_out, void *stream)
+{
+    if (B < 0 || W < 0 || T < 0 || n_free < 0 || (B > 0 && W == 0)) return ATOM_ERR_SHAPE;
+    if (!kv8_block(block_tokens) || B > atom_internal::kMaxMapRequests || T > 0x7ffffffeLL || W > (0x40000000LL / block_tokens) ||
+        (int64_t)B * W > 0x7fffffffLL)
+        return ATOM_ERR_UNSUPPORTED;
+    if (!token_start || (B > 0 && (!past_len || !new_len || !block_table || !seq_len)) || (T > 0 && !slot) ||
+        (n_free > 0 && !free_blocks))
+        return ATOM_ERR_NULL;
+    if (!aligned(past_len, 4) || !aligned(new_len, 4) || !aligned(free_blocks, 4) || !aligned(cursor, 4) ||
+        !aligned(block_table, 4) || !aligned(token_start, 4) || !aligned(seq_len, 4) || !aligned(slot, 4) ||
+        !aligned(cursor_out, 4))
+        return ATOM_ERR_ALIGN;
+    hipError_t err = atom_internal::launch_kv_block_map(past_len, new_len, B, block_tokens, free_blocks, n_free, cursor,
+                                                        block_table, W, T, token_start, seq_len, slot, cursor_out,
+                                                        static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? ATOM_OK : ATOM_ERR_HIP;
+}
+
+atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int64_t ldk, int64_t ldv, int32_t Hkv, int32_t D,
+                            const int32_t *slot, int64_t n_blocks, int32_t block_tokens, void *k_codes, float *k_scale,
+                            void *v_codes, float *v_scale, void *stream)
+{
+    if (T < 0 || Hkv <= 0 || D <= 0 || n_blocks <= 0 || ldk < (int64_t)Hkv * D || ldv < (int64_t)Hkv * D) return ATOM_ERR_SHAPE;
+    if (!kv8_cache(n_blocks, Hkv, D, block_tokens) || T > 0x7fffffffLL || T * Hkv > 0x7fffffffLL) return ATOM_ERR_UNSUPPORTED;
+    if (T == 0) return ATOM_OK;
+    if (!k_f16 || !v_f16 || !slot || !k_codes || !k_scale || !v_codes || !v_scale) return ATOM_ERR_NULL;
+    if (!aligned(k_f16, 16) || !aligned(v_f16, 16) || (ldk % 8) || (ldv % 8) || !aligned(slot, 4) || !aligned(k_codes, 16) ||
+        !aligned(v_codes, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4))
+        return ATOM_ERR_ALIGN;
+    hipError_t err = atom_internal::launch_kv8_append(k_f16, v_f16, T, ldk, ldv, Hkv, D, slot, n_blocks, block_tokens, k_codes,
+                                                      k_scale, v_codes, v_scale, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? ATOM_OK : ATOM_ERR_HIP;
+}
+
+size_t atom_attention_kv8_workspace_bytes(int64_t T, int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t max_new, int64_t W,
+                                          int32_t block_tokens)
+{
+    if (kv8_attention(T, B, H, Hkv, D, max_new, W, block_tokens) != ATOM_OK) return 0;
+    return atom_internal::attention_kv8_workspace_bytes(T, B, H, Hkv, D, max_new, W, block_tokens);
+}
+
+atom_status atom_attention_kv8(const void *q_f16, int64_t T, int64_t ldq, int32_t B, int32_t H, int32_t Hkv, int32_t D,
+                               int32_t max_new, const int32_t *token_start, const int32_t *seq_len, const int32_t *block_table,
+                               int64_t W, int64_t n_blocks, int32_t block_tokens, const void *k_codes, const float *k_scale,
+                               const void *v_codes, const float *v_scale, float sm_scale, void *out_f16, int64_t ldo,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    const atom_status st = kv8_attention(T, B, H, Hkv, D, max_new, W, block_tokens);
+    if (st != ATOM_OK) return st;
+    if (n_blocks <= 0 || ldq < (int64_t)H * D || ldo < (int64_t)H * D) return ATOM_ERR_SHAPE;
+    if (!kv8_cache(n_blocks, Hkv, D, block_tokens) || !(sm_scale >= 0.0f && sm_scale <= 1e6f)) return ATOM_ERR_UNSUPPORTED;
+    if (T == 0 || B == 0 || max_new == 0) return ATOM_OK;
+    if (!q_f16 || !token_start || !seq_len || !block_table || !k_codes || !k_scale || !v_codes || !v_scale || !out_f16)
+        return ATOM_ERR_NULL;
+    if (!aligned(q_f16, 16) || (ldq % 8) || !aligned(out_f16, 16) || (ldo % 8) || !aligned(k_codes, 16) || !aligned(v_codes, 16) ||
+        !aligned(k_scale, 4) || !aligned(v_scale, 4) || !aligned(token_start, 4) || !aligned(seq_len, 4) ||
+        !aligned(block_table, 4) || !aligned(workspace, 16))
+        return ATOM_ERR_ALIGN;
+    const size_t need = atom_internal::attention_kv8_workspace_bytes(T, B, H, Hkv, D, max_new, W, block_tokens);
+    if (need && (!workspace || workspace_bytes < need)) return ATOM_ERR_WORKSPACE;
+    const atom_internal::AttentionKv8 a = {q_f16, T, ldq, B, H, Hkv, D, max_new, token_start, seq_len, block_table, W, n_blocks,
+                                           block_tokens, k_codes, k_scale, v_codes, v_scale, sm_scale, out_f16, ldo, workspace};
+    hipError_t err = atom_internal::launch_attention_kv8(a, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? ATOM_OK : ATOM_ERR_HIP;
 }
 
 size_t atom_decode_attention_kv4_workspace_bytes(int32_t B, int32_t H, int32_t Hkv, int32_t D,

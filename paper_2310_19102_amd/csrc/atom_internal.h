@@ -124,6 +124,27 @@ hipError_t launch_decode_attention_kv4(const void *q, int B, int H, int Hkv, int
                                        const void *vz, float sm_scale, void *out, void *workspace,
                                        hipStream_t stream);
 size_t     decode_attention_workspace_bytes(int B, int H, int Hkv, int64_t Tmax);
+// Paged 8-bit KV cache (atom_kv8.hip, atom_kv8_attention.hip).
+constexpr int kMaxMapRequests = 16384;     // two int32 each in one workgroup's LDS
+hipError_t launch_kv_block_map(const int32_t *past, const int32_t *fresh, int B, int block_tokens, const int32_t *free_blocks,
+                               int64_t n_free, const int32_t *cursor, int32_t *table, int64_t W, int64_t T,
+                               int32_t *token_start, int32_t *seq_len, int32_t *slot, int32_t *cursor_out, hipStream_t stream);
+hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ldk, int64_t ldv, int Hkv, int D,
+                             const int32_t *slot, int64_t n_blocks, int block_tokens, void *k_codes, float *k_scale,
+                             void *v_codes, float *v_scale, hipStream_t stream);
+struct AttentionKv8 {
+    const void *q; int64_t T, ldq;
+    int B, H, Hkv, D, max_new;
+    const int32_t *token_start, *seq_len, *block_table; int64_t W, n_blocks; int block_tokens;
+    const void *k_codes; const float *k_scale; const void *v_codes; const float *v_scale;
+    float sm_scale;
+    void *out; int64_t ldo;
+    void *workspace;
+};
+size_t     attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, int max_new, int64_t W, int block_tokens);
+bool       attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new, int64_t W, int block_tokens);   // its grid
+hipError_t launch_attention_kv8(const AttentionKv8 &a, hipStream_t stream);
+
 // The library's own per-GPU scratch array (for the entry point that allocates nothing): its size,
 // and its device address on the current device (looked up on the first call per device).
 size_t     static_scratch_bytes();

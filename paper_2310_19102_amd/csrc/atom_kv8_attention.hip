@@ -1,0 +1,522 @@
+// Attention over the paged 8-bit KV cache for gfx950 (Section 4.4 of the paper: the cache is loaded in its low
+// precision and dequantised inside the attention operator, whose arithmetic stays in floating point; Section 4.5);
+// atom_kv8.hip fills the cache and has its layout.
+
+#include <hip/hip_runtime.h>
+#include <hip/hip_fp16.h>
+#include <stdint.h>
+
+#include "atom_internal.h"
+#include "atom_launch.h"
+
+namespace {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e   = 1.4426950408889634f;
+constexpr float kNoScore = -1e30f;                // the running maximum before the first key: below every score, and finite
+
+// What all kernels of a call are told.
+struct Args {
+    const __half *q; int T; int64_t ldq;
+    int B, H, Hkv, group;                         // group = H / Hkv query heads to a cache head
+    int max_new;
+    const int32_t *token_start, *seq_len, *table;
+    int W, shift;                                 // table columns; block_tokens = 1 << shift
+    int64_t capacity;                             // W * block_tokens
+    int32_t n_blocks;
+    const int8_t *kq; const float *ks; const int8_t *vq; const float *vs;
+    float sm_scale;
+    __half *out; int64_t ldo;
+    float *part;                                  // NULL: no tile's keys are split
+    int part_rows;                                // rows of a split's record
+    int target;                                   // splits wanted for each cache head (0: none)
+};
+
+// A request's share of the call.
+struct Request {
+    int start, n;                                 // its first token, its tokens that are computed
+    int before;                                   // position of its first token (may be negative: such a row sees nothing)
+    int keys;                                     // keys that exist for it
+};
+
+__device__ __forceinline__ Request request(const Args &a, int b)
+{
+    Request r;
+    const int first = a.token_start[b], end = a.token_start[b + 1], len = a.seq_len[b];
+    r.start = min(max(first, 0), a.T);
+    const int e = min(max(end, r.start), a.T);
+    r.n = min(e - r.start, a.max_new);
+    const int64_t before = (int64_t)len - max((int64_t)end - first, (int64_t)0);
+    r.before = (int)min(max(before, (int64_t)-0x40000000), (int64_t)0x3fffffff);        // (there are at most 2^30 keys)
+    r.keys = (int)min((int64_t)max(len, 0), a.capacity);
+    return r;
+}
+
+// ---- which part of the work a workgroup has
+//
+// The query rows of a request and cache head (token after token, the group's heads of each) come in tiles of ROWS.  A tile's keys are cut into
+// pieces of the same number of keys in the whole call, so that `target` pieces (more by one a tile at most) hold all of them: sequences of
+// any lengths keep the card evenly busy, and the pieces of a tile meet in the merge kernel.  Every wavefront finds its place from the
+// lengths by itself, 64 requests at a time: for as many it is one read, which it needs anyway.
+struct Place { int b, tile, split, splits, keys_per, first_slot; bool found; };
+
+__device__ __forceinline__ int64_t wave_sum(int64_t v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// FROM_TILE: `index` counts tiles (all of a tile's pieces are meant), else pieces.  few / many: only requests with at most / more rows.
+template <int ROWS, bool FROM_TILE>
+__device__ __forceinline__ Place place(const Args &a, int index, int rows_min, int rows_max)
+{
+    const int lane = threadIdx.x & 63;
+    auto tiles_keys = [&](int base, int &tiles, int &keys) {
+        tiles = 0;
+        keys = 0;
+        if (base + lane < a.B) {
+            const Request r = request(a, base + lane);
+            const int64_t rows = (int64_t)r.n * a.group;
+            if (rows >= rows_min && rows <= rows_max) {
+                tiles = (int)((rows + ROWS - 1) / ROWS);
+                keys = r.keys;
+            }
+        }
+    };
+    Place p;
+    p.found = false;
+    int tiles, keys;
+    tiles_keys(0, tiles, keys);
+    int per = 0x7fffff80;
+    if (a.target) {                               // a whole number of 128 keys: one step of 32 for each of four wavefronts
+        int64_t all = (int64_t)tiles * keys;
+        for (int base = 64; base < a.B; base += 64) {
+            int t2, k2;
+            tiles_keys(base, t2, k2);
+            all += (int64_t)t2 * k2;
+        }
+        all = wave_sum(all);
+        const float want = ceilf((float)all * 1.00001f / (128.0f * (float)a.target));
+        per = want < 1.0f ? 128 : want < 8388607.0f ? 128 * (int)want : 0x3fffff80;
+    }
+    int count = 0, slots = 0;                     // tiles and pieces of the requests before
+    for (int base = 0; base < a.B; base += 64) {
+        if (base) tiles_keys(base, tiles, keys);
+        const int splits = keys > per ? (keys + per - 1) / per : 1;
+        int ct = tiles, cs = tiles * splits;      // inclusive sums over the 64
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int vt = __shfl_up(ct, d, 64), vs = __shfl_up(cs, d, 64);
+            if (lane >= d) { ct += vt; cs += vs; }
+        }
+        const int mine = FROM_TILE ? count + ct : slots + cs;
+        const uint64_t past = __ballot(index < mine);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            p.found = true;
+            p.b = base + l;
+            p.splits = __builtin_amdgcn_readlane(splits, l);
+            const int t0 = count + __builtin_amdgcn_readlane(ct - tiles, l);
+            const int s0 = slots + __builtin_amdgcn_readlane(cs - tiles * splits, l);
+            if (FROM_TILE) {
+                p.tile = index - t0;
+                p.split = 0;
+            } else {
+                p.tile = (index - s0) / p.splits;
+                p.split = (index - s0) - p.tile * p.splits;
+            }
+            p.keys_per = per;
+            p.first_slot = s0 + p.tile * p.splits;
+            return p;
+        }
+        count += __builtin_amdgcn_readlane(ct, 63);
+        slots += __builtin_amdgcn_readlane(cs, 63);
+    }
+    return p;
+}
+
+// ---- codes to fp16
+//
+// A code with its sign bit flipped is u = code + 128.  As the low byte of a half it is the subnormal number u * 2^-24 exactly, which the
+// matrix instructions take: a byte selection makes two of them.
+__device__ __forceinline__ uint32_t flip(uint32_t w) { return w ^ 0x80808080u; }
+
+// bytes i of lo and of hi as one pair of subnormal halves
+template <int i>
+__device__ __forceinline__ uint32_t pair_of(uint32_t lo, uint32_t hi)
+{
+    return __builtin_amdgcn_perm(hi, lo, 0x0c000c00u | ((4u + i) << 16) | i);
+}
+
+// u * 2^-24 to (u - 128) * 2^-9, exactly: the values' side keeps no offset that a long sum would have to carry.
+__device__ __forceinline__ uint32_t centred(uint32_t pair)
+{
+    const h2 v = __builtin_elementwise_fma(__builtin_bit_cast(h2, pair), h2{(_Float16)32768.0f, (_Float16)32768.0f},
+                                           h2{(_Float16)-0.25f, (_Float16)-0.25f});
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+__device__ __forceinline__ h8 halves(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_bit_cast(h8, u4{a, b, c, d});
+}
+
+// max over the lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float max_of_chunks(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float sum_of_chunks(float v)
+{
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+// ---------------------------------------------------------------- few query rows
+//
+// One workgroup of four wavefronts for a tile of 16 query rows of a (request, cache head) and a piece of its keys; the
+// wavefronts take steps of 32 keys in turn, each with a softmax of its own, and meet in LDS.
+//
+//   scores: S^T = K Q^T on 16x16x32 fp16 matrix instructions.  Keys are the rows, so that a lane holds four keys of ONE query row.  Lane (l & 15, c =
+//           l >> 4) loads the D / 4 dimensions from c D / 4 on of key l & 15 as they lie in the cache; the order of the dimensions within a product is
+//           free as long as Q has the same.  The offset of u = code + 128 leaves through the accumulator's start, -128 sum(q) 2^-24.
+//   softmax: e = score * log2(e) * sm_scale * k_scale + log2(v_scale), p = 2^(e - M) with M a bound on e so far: the block's value scale sits in the
+//           weight, so the matrix instruction adds codes of blocks of different scales, and the weights are near one where
+//           they count, whatever the scales are.  The sum of the softmax takes p / v_scale.  M moves only where some e passes it by 8 (p <= 2^8 then).
+//   values: O^T = V^T P^T.  The weights lie in the registers of the scores as the second operand wants them when its order of keys is
+//           that of the scores' rows; V's rows are loaded in that order, D / 16 bytes a lane, and the byte selection that makes halves also
+//           transposes.  No LDS, no lane exchange in the loop.  The weights travel as fp16 (rounded to nearest even: 2^-12 of themselves).
+//   loads: the next step's 32 rows of K and V are in flight while one is computed; block numbers and scales of 64 blocks of 16 keys are
+//           read at once, a lane each.
+constexpr int kWaves = 4, kStep = 32, kTileRows = 16;
+
+template <int D>
+__global__ __launch_bounds__(kWaves * 64)
+void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
+{
+    constexpr int KB = D / 4, VB = D / 16;            // bytes of a K row and of a V row in a lane
+    constexpr int KS = D / 32;                        // matrix instructions for 16 keys' scores
+    __shared__ alignas(16) float s_acc[kWaves][kTileRows][D + 4];
+    __shared__ float s_m[kWaves][kTileRows], s_l[kWaves][kTileRows];
+
+    const int h = blockIdx.x % a.Hkv;
+    const Place w = place<kTileRows, false>(a, blockIdx.x / a.Hkv, rows_min, rows_max);
+    if (!w.found) return;
+    const Request r = request(a, w.b);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int m = lane & 15, c = lane >> 4;           // query row (or key) of the tile, chunk
+    const int rows = min(kTileRows, r.n * a.group - w.tile * kTileRows);
+    const int row = w.tile * kTileRows + min(m, rows - 1);
+    const int token = row / a.group, head = h * a.group + row - token * a.group;
+    // keys that this lane's row sees, and the fewest and the most of the tile
+    const int sees = min(max(r.before + token + 1, 0), r.keys);
+    const int sees_least = min(max(r.before + w.tile * kTileRows / a.group + 1, 0), r.keys);
+    const int sees_most = min(max(r.before + (w.tile * kTileRows + rows - 1) / a.group + 1, 0), r.keys);
+    const int key0 = w.split * w.keys_per, key1 = min(sees_most, key0 + w.keys_per);     // (a split below 2^31: keys_per is at most keys)
+
+    h8 q[KS];
+    float qsum = 0.0f;
+    {
+        const __half *qp = a.q + (int64_t)(r.start + token) * a.ldq + (int64_t)head * D + c * KB;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const u4 v = *reinterpret_cast<const u4 *>(qp + 8 * s);
+            q[s] = __builtin_bit_cast(h8, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) qsum += (float)q[s][i];
+        }
+        qsum = sum_of_chunks(qsum);
+    }
+    const float start = qsum * (-128.0f * 5.9604644775390625e-08f);
+    const float to_e = a.sm_scale * kLog2e * 16777216.0f;
+
+    f4 acc[VB];
+#pragma unroll
+    for (int e = 0; e < VB; ++e) acc[e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    float M = kNoScore, l = 0.0f;
+
+    struct Rows { u4 k[2][KB / 16]; uint32_t v[8][VB / 4]; };
+    // lane i: block of 16 keys number i of this wavefront's (two to a step)
+    int   unit = -1;
+    float b_scale = 0.0f, b_log = 0.0f, b_inv = 0.0f;
+    const int32_t *table = a.table + (int64_t)w.b * a.W;
+    auto key_of = [&](int step) { return key0 + (step * kWaves + wave) * kStep; };
+    auto look_up = [&](int step) {                    // the blocks of 32 steps from `step` on
+        const int key = key_of(step + (lane >> 1)) + 16 * (lane & 1);
+        unit = -1;
+        b_scale = b_log = b_inv = 0.0f;
+        if (key < key1) {
+            const int32_t page = table[key >> a.shift];
+            if (page >= 0 && page < a.n_blocks) {
+                const int64_t at = (int64_t)page * a.Hkv + h;
+                unit = (int)(at << (a.shift - 4)) + ((key & ((1 << a.shift) - 1)) >> 4);
+                // (never zero: a masked score of minus infinity stays one, and a block of zeros has a weight to be divided out again)
+                b_scale = fmaxf(a.ks[at] * to_e, 1e-37f);
+                const float v = fmaxf(a.vs[at], 2.3283064365386963e-10f);
+                b_log = __builtin_amdgcn_logf(v);
+                b_inv = __builtin_amdgcn_rcpf(v);
+            }
+        }
+    };
+    auto fetch = [&](int step, Rows &x) {             // (blocks past the end or without a page: the cache's first rows, masked)
+        const int at = 2 * (step & 31);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t base = (int64_t)max(__builtin_amdgcn_readlane(unit, at + u), 0) * (16 * D);
+            const int8_t *kp = a.kq + base + (uint32_t)(m * D + c * KB);
+#pragma unroll
+            for (int i = 0; i < KB / 16; ++i) x.k[u][i] = *reinterpret_cast<const u4 *>(kp + 16 * i);
+            const int8_t *vp = a.vq + base + (uint32_t)(4 * c * D + m * VB);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (VB == 8) {
+                    const u2 v = *reinterpret_cast<const u2 *>(vp + i * D);
+                    x.v[4 * u + i][0] = v[0];
+                    x.v[4 * u + i][1] = v[1];
+                } else {
+                    x.v[4 * u + i][0] = *reinterpret_cast<const uint32_t *>(vp + i * D);
+                }
+            }
+        }
+    };
+    auto compute = [&](int step, const Rows &x) {
+        const int at = 2 * (step & 31), key = key_of(step);
+        float e[8];
+        float log_v[2], inv_v[2], top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f4 s = f4{start, start, start, start};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const uint32_t w0 = flip(x.k[u][i >> 1][(2 * i) & 3]), w1 = flip(x.k[u][i >> 1][(2 * i + 1) & 3]);
+                const h8 k = halves(__builtin_amdgcn_perm(0, w0, 0x0c010c00u), __builtin_amdgcn_perm(0, w0, 0x0c030c02u),
+                                    __builtin_amdgcn_perm(0, w1, 0x0c010c00u), __builtin_amdgcn_perm(0, w1, 0x0c030c02u));
+                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i], s, 0, 0, 0);
+            }
+            const int  id = __builtin_amdgcn_readlane(unit, at + u);
+            const bool whole = id >= 0 && key + 16 * u + 16 <= min(sees_least, key1);
+            if (!whole) {
+                const int room = id < 0 ? 0 : min(sees, key1) - (key + 16 * u + 4 * c);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = i < room ? s[i] : -INFINITY;
+            }
+            const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_scale), at + u));
+            log_v[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_log), at + u));
+            inv_v[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_inv), at + u));
+            const float f1 = id < 0 ? 1.0f : f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e[4 * u + i] = fmaf(s[i], f1, log_v[u]);
+                top = fmaxf(top, e[4 * u + i]);
+            }
+        }
+        if (__ballot(top > M + 8.0f)) {               // rare after the first steps
+            const float to = fmaxf(M, max_of_chunks(top));
+            const float down = __builtin_amdgcn_exp2f(M - to);
+            M = to;
+            l *= down;
+#pragma unroll
+            for (int i = 0; i < VB; ++i) acc[i] *= down;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e[4 * u + i] = __builtin_amdgcn_exp2f(e[4 * u + i] - M);
+                sum += e[4 * u + i];
+            }
+            l = fmaf(sum, inv_v[u], l);
+        }
+        h8 p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = (_Float16)e[i];
+        uint32_t v[8][VB / 4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < VB / 4; ++j) v[i][j] = flip(x.v[i][j]);
+#define ATOM_VALUES(j, n)                                                                                                    \
+        acc[4 * (j) + (n)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(                                                         \
+            halves(centred(pair_of<n>(v[0][j], v[1][j])), centred(pair_of<n>(v[2][j], v[3][j])),                             \
+                   centred(pair_of<n>(v[4][j], v[5][j])), centred(pair_of<n>(v[6][j], v[7][j]))), p, acc[4 * (j) + (n)], 0, 0, 0)
+#pragma unroll
+        for (int j = 0; j < VB / 4; ++j) {
+            ATOM_VALUES(j, 0);
+            ATOM_VALUES(j, 1);
+            ATOM_VALUES(j, 2);
+            ATOM_VALUES(j, 3);
+        }
+#undef ATOM_VALUES
+    };
+
+    if (key_of(0) < key1) {                           // (the same in all lanes)
+        const int steps = (key1 - key_of(0) + kWaves * kStep - 1) / (kWaves * kStep);
+        Rows x, y;
+        look_up(0);
+        fetch(0, x);
+        for (int s = 0; s < steps; s += 2) {
+            // (32 steps to a look-up, an even number: both steps of a round have theirs in the lanes)
+            if (s + 1 < steps) fetch(s + 1, y);
+            compute(s, x);
+            const bool more = s + 2 < steps, turn = ((s + 2) & 31) == 0;
+            if (more && !turn) fetch(s + 2, x);
+            if (s + 1 < steps) compute(s + 1, y);
+            if (more && turn) {
+                look_up(s + 2);
+                fetch(s + 2, x);
+            }
+        }
+    }
+
+    // ---- the four wavefronts meet
+    l = sum_of_chunks(l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < VB; ++e) s_acc[wave][m][VB * (4 * c + i) + e] = acc[e][i];
+    if (c == 0) {
+        s_m[wave][m] = M;
+        s_l[wave][m] = l;
+    }
+    __syncthreads();
+    const bool whole = w.splits == 1;
+    const int64_t record = whole ? 0 : ((int64_t)(w.first_slot + w.split) * a.Hkv + h) * a.part_rows;
+    for (int i = tid; i < rows * (D / 4); i += kWaves * 64) {
+        const int rr = i / (D / 4), d = 4 * (i % (D / 4));
+        float top = s_m[0][rr];
+#pragma unroll
+        for (int k = 1; k < kWaves; ++k) top = fmaxf(top, s_m[k][rr]);
+        float sum = 0.0f;
+        f4 o = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const float f = __builtin_amdgcn_exp2f(s_m[k][rr] - top);
+            sum = fmaf(s_l[k][rr], f, sum);
+            const f4 v = *reinterpret_cast<const f4 *>(&s_acc[k][rr][d]);
+            o += v * f;
+        }
+        if (whole) {
+            const float f = sum > 0.0f ? 512.0f / sum : 0.0f;         // (values were 2^-9 of the codes)
+            const int rw = w.tile * kTileRows + rr, t = rw / a.group;
+            __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + rw - t * a.group) * D + d;
+            const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
+            *reinterpret_cast<u2 *>(to) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+        } else {
+            float *to = a.part + (record + rr) * (D + 4);
+            *reinterpret_cast<f4 *>(to + 4 + d) = o;
+            if (d == 0) {
+                to[0] = top;
+                to[1] = sum;
+            }
+        }
+    }
+}
+
+// The pieces of a tile, in their order.  One workgroup for a tile and cache head.
+template <int D, int ROWS>
+__global__ __launch_bounds__(256)
+void attention_kv8_merge_kernel(const Args a, int rows_min, int rows_max)
+{
+    const int h = blockIdx.x % a.Hkv;
+    const Place w = place<ROWS, true>(a, blockIdx.x / a.Hkv, rows_min, rows_max);
+    if (!w.found || w.splits == 1) return;
+    const Request r = request(a, w.b);
+    const int rows = min(ROWS, r.n * a.group - w.tile * ROWS);
+    const int64_t stride = (int64_t)a.Hkv * a.part_rows * (D + 4);
+    for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
+        const int rr = i / (D / 4), d = 4 * (i % (D / 4));
+        const float *from = a.part + (((int64_t)w.first_slot * a.Hkv + h) * a.part_rows + rr) * (D + 4);
+        float top = kNoScore;
+        for (int s = 0; s < w.splits; ++s) top = fmaxf(top, from[s * stride]);
+        float sum = 0.0f;
+        f4 o = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < w.splits; ++s) {
+            const float f = __builtin_amdgcn_exp2f(from[s * stride] - top);
+            sum = fmaf(from[s * stride + 1], f, sum);
+            o += *reinterpret_cast<const f4 *>(from + s * stride + 4 + d) * f;
+        }
+        const float f = sum > 0.0f ? 512.0f / sum : 0.0f;
+        const int rw = w.tile * ROWS + rr, t = rw / a.group;
+        __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + rw - t * a.group) * D + d;
+        const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
+        *reinterpret_cast<u2 *>(to) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+    }
+}
+
+// ---------------------------------------------------------------- shape of a call
+
+// Tiles of `rows` query rows, at most: of B requests with together T tokens, each with max_new at most.
+int64_t most_tiles(int64_t T, int B, int group, int max_new, int rows)
+{
+    const int64_t each = ((int64_t)max_new * group + rows - 1) / rows, by_request = each * B, by_token = T * group / rows + B;
+    return by_request < by_token ? by_request : by_token;
+}
+
+struct Shape { int64_t slots; int target, part_rows; int64_t tiles; };
+
+Shape rows_shape(int64_t T, int B, int Hkv, int group, int max_new, int64_t capacity)
+{
+    Shape s;
+    s.tiles = most_tiles(T, B, group, max_new, kTileRows);
+    int64_t target = (1024 + Hkv - 1) / Hkv;
+    const int64_t most = s.tiles * ((capacity + 127) / 128);          // no piece below 128 keys
+    if (target > most) target = most;
+    s.target = s.tiles >= 2 * target || most == s.tiles ? 0 : (int)target;
+    s.slots = s.tiles + s.target;
+    s.part_rows = (int)((int64_t)max_new * group < kTileRows ? (int64_t)max_new * group : kTileRows);
+    return s;
+}
+
+}  // namespace
+
+namespace atom_internal {
+
+size_t attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, int max_new, int64_t W, int block_tokens)
+{
+    if (T == 0 || B == 0 || max_new == 0) return 0;
+    const Shape s = rows_shape(T, B, Hkv, H / Hkv, max_new, W * block_tokens);
+    return s.target ? (size_t)(s.slots * Hkv * s.part_rows) * (size_t)(D + 4) * sizeof(float) : 0;
+}
+
+bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new, int64_t W, int block_tokens)
+{
+    if (T == 0 || B == 0 || max_new == 0) return true;
+    const Shape s = rows_shape(T, B, Hkv, H / Hkv, max_new, W * block_tokens);
+    return s.slots * Hkv <= 0x7fffffffLL;
+}
+
+hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)
+{
+    Args a;
+    a.q = (const __half *)c.q; a.T = (int)c.T; a.ldq = c.ldq;
+    a.B = c.B; a.H = c.H; a.Hkv = c.Hkv; a.group = c.H / c.Hkv;
+    a.max_new = c.max_new;
+    a.token_start = c.token_start; a.seq_len = c.seq_len; a.table = c.block_table;
+    a.W = (int)c.W; a.shift = __builtin_ctz((unsigned)c.block_tokens);
+    a.capacity = c.W * c.block_tokens;
+    a.n_blocks = (int32_t)c.n_blocks;
+    a.kq = (const int8_t *)c.k_codes; a.ks = c.k_scale; a.vq = (const int8_t *)c.v_codes; a.vs = c.v_scale;
+    a.sm_scale = c.sm_scale;
+    a.out = (__half *)c.out; a.ldo = c.ldo;
+    const Shape s = rows_shape(c.T, c.B, c.Hkv, a.group, c.max_new, a.capacity);
+    a.target = s.target;
+    a.part = s.target ? (float *)c.workspace : nullptr;
+    a.part_rows = s.part_rows;
+    auto rows = c.D == 128 ? &attention_kv8_rows_kernel<128> : &attention_kv8_rows_kernel<64>;
+    hipLaunchKernelGGL(rows, dim3((unsigned)(s.slots * c.Hkv)), dim3(kWaves * 64), 0, stream, a, 1, 0x7fffffff);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess || !s.target) return err;
+    auto merge = c.D == 128 ? &attention_kv8_merge_kernel<128, kTileRows> : &attention_kv8_merge_kernel<64, kTileRows>;
+    hipLaunchKernelGGL(merge, dim3((unsigned)(s.tiles * c.Hkv)), dim3(256), 0, stream, a, 1, 0x7fffffff);
+    return hipGetLastError();
+}
+
+}  // namespace atom_internal

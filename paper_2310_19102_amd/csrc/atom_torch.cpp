@@ -13,6 +13,7 @@
 #include <ATen/hip/EmptyTensor.h>
 #include <ATen/hip/HIPContext.h>
 #include <c10/hip/HIPCachingAllocator.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -55,7 +56,7 @@ const Tensor &tensor(PyObject *o, const char *name)
 struct Kind { at::ScalarType type; const char *name; };
 constexpr Kind kHalf = {at::kHalf, "torch.float16"}, kByte = {at::kByte, "torch.uint8"},
                kChar = {at::kChar, "torch.int8"}, kInt = {at::kInt, "torch.int32"},
-               kShort = {at::kShort, "torch.int16"};
+               kShort = {at::kShort, "torch.int16"}, kFloat = {at::kFloat, "torch.float32"};
 
 // A device tensor of the given type (what binding.py has always asked of its arguments).
 const Tensor &device(PyObject *o, Kind k, const char *name)
@@ -704,6 +705,184 @@ PyObject *attention(Args a, bool fixed)
 PyObject *decode_attention_kv4(Args a) { return attention(a, false); }
 PyObject *decode_attention_kv4_static(Args a) { return attention(a, true); }
 
+// All of a call's tensors are on one device, which is the current one while this lives.
+struct OnDevice {
+    c10::DeviceIndex index;
+    c10::hip::HIPGuard guard;
+    explicit OnDevice(const Tensor &t) : index(t.device().index()), guard(index) {}
+    void with(std::initializer_list<const Tensor *> others) const
+    {
+        for (const Tensor *t : others)
+            if (t->device().index() != index) value_error("all tensors of a call must be on one device");
+    }
+};
+
+const Tensor &vector(PyObject *o, int64_t n, const char *name)
+{
+    const Tensor &t = contiguous(o, kInt, name);
+    if (t.dim() != 1 || t.size(0) != n) {
+        PyErr_Format(PyExc_ValueError, "%s must be int32 [%lld]", name, (long long)n);
+        throw Raised();
+    }
+    return t;
+}
+
+// A 32-bit argument of the library (a larger one would arrive as another number).
+int32_t narrow(int64_t v, const char *name)
+{
+    if (v < INT32_MIN || v > INT32_MAX) value_error(name, "does not fit 32 bits");
+    return (int32_t)v;
+}
+
+PyObject *kv_block_map(Args a)
+{
+    const Tensor &past = device(a[0], kInt, "past_len");
+    if (past.dim() != 1 || !past.is_contiguous()) value_error("past_len must be contiguous int32 [B]");
+    const int64_t B = past.size(0), T = whole(a[4]);
+    const Tensor &fresh = vector(a[1], B, "new_len"), &table = contiguous(a[2], kInt, "block_table"),
+                 &blocks = contiguous(a[3], kInt, "free_blocks");
+    if (table.dim() != 2 || table.size(0) != B) value_error("block_table must be int32 [B, W]");
+    if (blocks.dim() != 1) value_error("free_blocks must have one dimension");
+    const int32_t bs = narrow(whole(a[5]), "block_tokens");
+    const OnDevice on(past);
+    on.with({&fresh, &table, &blocks});
+    const int32_t *cursor = nullptr;
+    if (a[6] != Py_None) {
+        const Tensor &c = vector(a[6], 1, "cursor");
+        on.with({&c});
+        cursor = (const int32_t *)data(c);
+    }
+    if (T < 0) value_error("n_tokens must not be negative");
+    Out out[4];
+    const int64_t sizes[] = {B + 1, B, T, 1};
+    const char *names[] = {"token_start", "seq_len", "slot", "cursor_out"};
+    if (a[7] == Py_None) {
+        for (int i = 0; i < 4; ++i) out[i].fresh(make({sizes[i]}, kInt, past));
+    } else {
+        PyObject *seq = PySequence_Tuple(a[7]);
+        if (!seq) throw Raised();
+        const bool four = PyTuple_GET_SIZE(seq) == 4;
+        for (int i = 0; four && i < 4; ++i) {
+            PyObject *item = PyTuple_GET_ITEM(seq, i);
+            if (THPVariable_Check(item)) out[i].given(item, names[i]);
+        }
+        Py_DECREF(seq);
+        if (!four) value_error("out must be four tensors");
+        for (int i = 0; i < 4; ++i) {
+            if (!out[i].t) value_error(names[i], "must be a tensor");
+            on.with({&vector(out[i].o, sizes[i], names[i])});
+            // every workgroup reads the lengths while the first one writes these
+            for (const Tensor *in : {&past, &fresh, &table, &blocks})
+                if (in->numel() && out[i].t->numel() && out[i].t->is_alias_of(*in) &&
+                    (char *)data(*out[i].t) < (char *)data(*in) + bytes(*in) && (char *)data(*in) < (char *)data(*out[i].t) + bytes(*out[i].t))
+                    value_error(names[i], "must not be an input's memory");
+            if (cursor && out[i].t->numel() && cursor >= (const int32_t *)data(*out[i].t) &&
+                cursor < (const int32_t *)data(*out[i].t) + out[i].t->numel())
+                value_error(names[i], "must not be an input's memory");
+        }
+    }
+    ATOM_CALL(atom_kv_block_map, (const int32_t *)data(past), (const int32_t *)data(fresh), narrow(B, "B"), bs,
+              (const int32_t *)data(blocks), blocks.size(0), cursor, (int32_t *)data(table), table.size(1), T,
+              (int32_t *)out[0].data(), (int32_t *)out[1].data(), (int32_t *)out[2].data(), (int32_t *)out[3].data());
+    return tuple({&out[0], &out[1], &out[2], &out[3]});
+}
+
+// Rows [T, heads, D] of a step: each token's heads contiguous.  The stride between tokens (of one token: any that the library takes).
+void token_rows(const Tensor &t, const char *name)
+{
+    if (t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2)))
+        value_error(name, "must be [T, heads, D] with contiguous heads");
+}
+int64_t token_stride(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2); }
+
+// A paged cache of one tensor: codes [n_blocks, Hkv, block_tokens, D], scales [n_blocks, Hkv].
+struct Pages {
+    PyObject *seq;
+    const Tensor *codes = nullptr, *scale = nullptr;
+    Pages(PyObject *o, const char *n0, const char *n1) : seq(PySequence_Tuple(o))
+    {
+        if (!seq) throw Raised();
+        try {
+            if (PyTuple_GET_SIZE(seq) != 2) value_error("a cache must be (codes, scale)");
+            codes = &contiguous(PyTuple_GET_ITEM(seq, 0), kChar, n0);
+            scale = &contiguous(PyTuple_GET_ITEM(seq, 1), kFloat, n1);
+            if (codes->dim() != 4) value_error(n0, "must be int8 [n_blocks, Hkv, block_tokens, D]");
+            if (scale->dim() != 2 || scale->size(0) != codes->size(0) || scale->size(1) != codes->size(1))
+                value_error(n1, "must be float32 [n_blocks, Hkv]");
+        } catch (...) {
+            Py_DECREF(seq);
+            throw;
+        }
+    }
+    ~Pages() { Py_DECREF(seq); }
+    Pages(const Pages &) = delete;
+    Pages &operator=(const Pages &) = delete;
+};
+
+PyObject *kv8_append(Args a)
+{
+    const Tensor &k = device(a[0], kHalf, "k"), &v = device(a[1], kHalf, "v");
+    token_rows(k, "k");
+    token_rows(v, "v");
+    if (v.sizes() != k.sizes()) value_error("k and v shapes disagree");
+    const int64_t T = k.size(0), Hkv = k.size(1), D = k.size(2);
+    const Pages kc(a[2], "k codes", "k scale"), vc(a[3], "v codes", "v scale");
+    const Tensor &slot = vector(a[4], T, "slot");
+    if (vc.codes->sizes() != kc.codes->sizes() || kc.codes->size(1) != Hkv || kc.codes->size(3) != D)
+        value_error("cache and row shapes disagree");
+    const OnDevice on(k);
+    on.with({&v, kc.codes, kc.scale, vc.codes, vc.scale, &slot});
+    ATOM_CALL(atom_kv8_append, data(k), data(v), T, token_stride(k), token_stride(v), narrow(Hkv, "Hkv"), narrow(D, "D"),
+              (const int32_t *)data(slot), kc.codes->size(0), narrow(kc.codes->size(2), "block_tokens"), data(*kc.codes),
+              (float *)data(*kc.scale), data(*vc.codes), (float *)data(*vc.scale));
+    return PyTuple_Pack(2, a[2], a[3]);
+}
+
+// a: q, k_cache, v_cache, block_table, token_start, seq_len, sm_scale, max_new, out, workspace
+PyObject *attention_kv8(Args a)
+{
+    const Tensor &q = device(a[0], kHalf, "q");
+    token_rows(q, "q");
+    const int64_t T = q.size(0), H = q.size(1), D = q.size(2);
+    const Pages kc(a[1], "k codes", "k scale"), vc(a[2], "v codes", "v scale");
+    const Tensor &table = contiguous(a[3], kInt, "block_table");
+    if (table.dim() != 2) value_error("block_table must be int32 [B, W]");
+    const int64_t B = table.size(0), W = table.size(1);
+    const Tensor &first = vector(a[4], B + 1, "token_start"), &len = vector(a[5], B, "seq_len");
+    if (vc.codes->sizes() != kc.codes->sizes() || kc.codes->size(3) != D) value_error("cache and query shapes disagree");
+    const float sm = real(a[6]);
+    const int64_t asked = whole(a[7]);
+    if (asked < 0) value_error("max_new must not be negative");
+    const int32_t max_new = narrow(std::min(asked, T), "max_new"), b = narrow(B, "B"), h = narrow(H, "H"),
+                  hkv = narrow(kc.codes->size(1), "Hkv"), d = narrow(D, "D"), bs = narrow(kc.codes->size(2), "block_tokens");
+    const OnDevice on(q);
+    on.with({kc.codes, kc.scale, vc.codes, vc.scale, &table, &first, &len});
+    Out out;
+    out.take(a[8], "out", {T, H, D}, kHalf, q);
+    if (out.o) {
+        device(out.o, kHalf, "out");
+        token_rows(*out.t, "out");
+        if (out.t->sizes() != q.sizes()) value_error("out must be [T, H, D]");
+        on.with({out.t});
+    }
+    const size_t need = atom_attention_kv8_workspace_bytes(T, b, h, hkv, d, max_new, W, bs);
+    Tensor own;
+    const Tensor *w = a[9] == Py_None ? nullptr : &tensor(a[9], "workspace");
+    if (w && (!w->is_cuda() || w->device().index() != on.index || !w->is_contiguous()))
+        value_error("workspace must be a contiguous tensor on the device of q");
+    if (need && (!w || bytes(*w) < need)) {
+        own = make({(int64_t)need}, kByte, q);
+        if (!safe_to_capture(own))
+            value_error("workspace of atom_attention_kv8_workspace_bytes needed: PyTorch's allocator does not know of this capture");
+        w = &own;
+    }
+    ATOM_CALL(atom_attention_kv8, data(q), T, token_stride(q), b, h, hkv, d, max_new, (const int32_t *)data(first),
+              (const int32_t *)data(len), (const int32_t *)data(table), W, kc.codes->size(0), bs, data(*kc.codes),
+              (const float *)data(*kc.scale), data(*vc.codes), (const float *)data(*vc.scale), sm, out.data(),
+              token_stride(*out.t), w ? data(*w) : nullptr, w ? bytes(*w) : 0);
+    return out.give();
+}
+
 PyObject *mx_quantize_act(Args a)
 {
     const Tensor &x = device(a[0], kHalf, "x"), &idx = device(a[3], kInt, "reorder_idx");
@@ -780,6 +959,7 @@ PyMethodDef methods[] = {
     ENTRY(w4a4_gemm_decode_tiled, 8), ENTRY(decode_linear, 12), ENTRY(decode_linear_coop, 13), ENTRY(pack_act, 5),
     ENTRY(quantize_act_packed, 9), ENTRY(add_quantize_act_packed, 11), ENTRY(swiglu_quantize_act_packed, 8),
     ENTRY(w4a4_gemm_prepacked, 9), ENTRY(w4a4_gemm_packed, 9), ENTRY(kv_quantize, 4), ENTRY(kv_quantize_pair, 6),
+    ENTRY(kv_block_map, 8), ENTRY(kv8_append, 5), ENTRY(attention_kv8, 10),
     ENTRY(decode_attention_kv4, 7), ENTRY(decode_attention_kv4_static, 6), ENTRY(mx_quantize_act, 7), ENTRY(mx_gemm, 7),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,476 @@
+"""The paged 8-bit KV cache on the GPU against plain implementations: tables, codes and scales bit for bit, attention in 64
+bits within the rounding of its fp16 weights and output."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_19102_amd as atom
+import _kv8_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def i32(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def npy(t):
+    return t.detach().cpu().numpy()
+
+
+def tables(past, new, table, free, T, bs, cursor=None):
+    """One call and the definition's outcome, compared."""
+    want = ref.block_map(npy(past), npy(new), npy(table), npy(free), T, bs, 0 if cursor is None else int(cursor))
+    got = atom.atom_kv_block_map(past, new, table, free, T, bs, cursor=cursor)
+    for g, w, name in zip((*got, table), want, ("token_start", "seq_len", "slot", "cursor", "table")):
+        assert np.array_equal(npy(g), w), name
+    return got
+
+
+# ---------------------------------------------------------------- block tables and slot maps
+
+
+@pytest.mark.parametrize("B,bs,W,past,new,T", [
+    (1, 64, 1, 0, 1, 1), (1, 16, 5, 33, 7, 7), (1, 128, 4, 128, 0, 0), (2, 16, 3, 16, 20, 50), (7, 32, 9, 100, 60, 333),
+    (63, 64, 40, 2000, 1, 64), (65, 16, 70, 900, 9, 700), (300, 16, 13, 120, 80, 30000), (1025, 32, 6, 60, 40, 41000),
+    (2500, 128, 3, 300, 2, 5000)])
+def test_block_map(B, bs, W, past, new, T):
+    """Odd batches, tables that are too narrow for some, padded and cut token arrays, requests without tokens, negative lengths."""
+    g = torch.Generator().manual_seed(B + W)
+    p = torch.randint(0, past + 1, (B,), generator=g).to(torch.int32)
+    n = torch.randint(0, new + 1, (B,), generator=g).to(torch.int32)
+    if B > 6:
+        p[3], n[3], p[5], n[5] = -4, 2, 6, -9
+    ids = torch.randperm(B * (W + 2), generator=g).to(torch.int32)
+    table = ids[:B * W].view(B, W).clone().cuda()
+    free = ids[B * W:].cuda()
+    first = tables(p.cuda(), n.cuda(), table, free, T, bs)
+    # the same call on the table that it left
+    again = tables(p.cuda(), n.cuda(), table, free, T, bs)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_block_map_where_the_free_list_ends():
+    past, new = i32(0, 5, 64, 0), i32(40, 30, 1, 33)
+    for cursor, n_free in ((None, 4), (i32(2), 4), (i32(9), 4), (i32(-2), 4), (None, 0)):
+        table = torch.full((4, 6), 77, dtype=torch.int32, device="cuda")
+        tables(past, new, table, torch.arange(10, 10 + n_free, dtype=torch.int32, device="cuda"), 110, 16, cursor)
+
+
+def test_block_map_of_no_request_and_of_huge_lengths():
+    free = torch.arange(8, dtype=torch.int32, device="cuda")
+    start, length, slot, cursor = atom.atom_kv_block_map(i32(), i32(), torch.empty((0, 4), dtype=torch.int32, device="cuda"), free, 5,
+                                                         16, cursor=i32(3))
+    assert start.tolist() == [0] and length.numel() == 0 and slot.tolist() == [-1] * 5 and cursor.tolist() == [3]
+    big = 2 ** 31 - 1                                       # sums saturate
+    table = torch.full((3, 2), -1, dtype=torch.int32, device="cuda")
+    start, length, slot, cursor = atom.atom_kv_block_map(i32(big, 0, 0), i32(5, big, big), table, free, 40, 16)
+    assert start.tolist() == [0, 5, big, big] and length.tolist() == [big, big, big]
+    assert slot.tolist() == [-1] * 5 + list(range(32)) + [-1] * 3 and cursor.tolist() == [4]
+    assert table.tolist() == [[-1, -1], [0, 1], [2, 3]]
+
+
+def test_block_map_cursor_chains_steps():
+    """Steps that hand the cursor on take every block once."""
+    B, bs, W = 5, 16, 8
+    table = torch.full((B, W), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(64, generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()
+    past, cursor = torch.zeros(B, dtype=torch.int32, device="cuda"), i32(0)
+    for new in (i32(40, 0, 16, 1, 17), i32(1, 1, 1, 0, 15), i32(8, 30, 1, 2, 1)):
+        _, past, _, cursor = tables(past, new, table, free, 80, bs, cursor)
+    used = table[table >= 0].tolist()
+    assert len(used) == len(set(used)) == int(cursor)
+
+
+# ---------------------------------------------------------------- append
+
+
+def caches(n, Hkv, bs, D, seed=0, fill=True):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    got = []
+    for _ in "kv":
+        codes, scale = atom.atom_kv8_cache(n, Hkv, D, bs)
+        if fill:                                            # contents of earlier steps
+            codes.random_(-127, 128, generator=g)
+            scale.uniform_(0.001, 0.02, generator=g)
+        got.append((codes, scale))
+    return got
+
+
+def check_append(k, v, kc, vc, slot):
+    want = [ref.append(npy(x), npy(c), npy(s), npy(slot)) for x, (c, s) in ((k, kc), (v, vc))]
+    atom.atom_kv8_append(k, v, kc, vc, slot)
+    for (c, s), (wc, ws), name in zip((kc, vc), want, "kv"):
+        assert np.array_equal(npy(s).view(np.uint32), ws.view(np.uint32)), name + " scales"
+        assert np.array_equal(npy(c), wc), name + " codes"
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bs", [16, 32, 64, 128])
+@pytest.mark.parametrize("Hkv,past,new", [(1, [0], [1]), (3, [0, 5, 130], [1, 1, 1]), (2, [0, 0, 7], [200, 16, 0]),
+                                          (5, [3, 64, 127, 0, 50], [140, 1, 2, 1, 90]), (8, [0] * 40, [3] * 40)])
+def test_append(D, bs, Hkv, past, new):
+    """Whole caches before and after, bit for bit: fresh blocks, growing and unchanged scales, runs across blocks; nothing
+    else is touched."""
+    g = torch.Generator(device="cuda").manual_seed(D + bs + Hkv)
+    need = [-(-(p + n) // bs) for p, n in zip(past, new)]
+    blocks, W, T = sum(need) + 3, max(need) + 1, sum(new) + 2
+    free = torch.randperm(blocks, generator=g, device="cuda").to(torch.int32)
+    table = free.flip(0)[:1].repeat(len(past), W)
+    used = 0
+    for b, p in enumerate(past):                            # blocks that the requests hold already
+        have = -(-p // bs)
+        table[b, :have] = free[used:used + have]
+        used += have
+    start, length, slot, _ = tables(i32(*past), i32(*new), table, free[used:].contiguous(), T, bs)
+    kc, vc = caches(blocks, Hkv, bs, D, seed=1)
+    k, v = (torch.randn((T, Hkv, D), generator=g, device="cuda").to(torch.float16) for _ in "kv")
+    k[:, 0] *= 8.0
+    k[-2:], v[-2:] = float("nan"), float("inf")             # padding: slot -1
+    check_append(k, v, kc, vc, slot)
+    kept = [t.clone() for t in (*kc, *vc)]
+    atom.atom_kv8_append(k, v, kc, vc, slot)                # the same again
+    assert all(torch.equal(a, b) for a, b in zip(kept, (*kc, *vc)))
+
+
+@pytest.mark.parametrize("D,bs", [(64, 16), (128, 64), (128, 128)])
+def test_append_token_by_token(D, bs):
+    """A block that fills one token at a time, its scale growing on the way; ends within the stated distance of the rows."""
+    g = torch.Generator(device="cuda").manual_seed(bs)
+    Hkv, n = 3, 2 * bs
+    kc, vc = caches(4, Hkv, bs, D, seed=2)
+    k, v = (torch.randn((n, Hkv, D), generator=g, device="cuda") for _ in "kv")
+    k *= torch.linspace(0.1, 3.0, n, device="cuda")[:, None, None]
+    k, v = k.to(torch.float16), v.to(torch.float16)
+    grown = torch.zeros((n, Hkv), device="cuda")            # how often a row's scale has grown since
+    blocks = (3, 1)
+    for t in range(n):
+        slot = i32(blocks[t // bs] * bs + t % bs)
+        before = kc[1][blocks[t // bs]].clone()
+        check_append(k[t:t + 1], v[t:t + 1], kc, vc, slot)
+        if t % bs:
+            grown[t - t % bs:t] += (kc[1][blocks[t // bs]] > before).float()
+    codes, scale = kc
+    back = torch.cat([codes[b].float() * scale[b][:, None, None] for b in blocks], 1).transpose(0, 1)
+    step = torch.cat([scale[b].expand(bs, Hkv) for b in blocks])
+    # half a step a rounding (and what fp32 adds to a quotient of up to 127: 2^-22 of it twice)
+    assert ((back - k.float()).abs() <= (step * (0.5 + 0.0001) * (1 + grown))[:, :, None]).all()
+
+
+def test_append_zeros_and_extremes():
+    D, bs = 128, 16
+    kc, vc = caches(5, 2, bs, D, fill=False)
+    k = torch.zeros((40, 2, D), dtype=torch.float16, device="cuda")
+    v = torch.full_like(k, 65504.0)
+    v[:, 1] = 5.9604645e-08                                 # fp16's smallest number
+    v[5:9, 1] = -v[5:9, 1]
+    slot = torch.arange(7, 47, dtype=torch.int32, device="cuda")
+    check_append(k, v, kc, vc, slot)
+    assert (kc[0] == 0).all() and (kc[1] == 0).all()
+    k[3, 0, 5] = -2.0                                       # a block of zeros gets its first value
+    check_append(k, v, kc, vc, slot)
+    # ties: codes of a half between two numbers go to the even one
+    x = torch.zeros((1, 2, D), dtype=torch.float16, device="cuda")
+    x[0, :, 0] = 127.0
+    x[0, :, 1:64] = torch.arange(63, device="cuda") + 0.5
+    x[0, :, 64:] = -(torch.arange(64, device="cuda") + 0.5)
+    check_append(x, x, kc, vc, i32(0))
+
+
+def test_append_takes_slices_of_a_projection_and_any_slots():
+    D, bs, Hkv, T = 64, 32, 4, 77
+    g = torch.Generator(device="cuda").manual_seed(9)
+    qkv = torch.randn((T, 3 * Hkv, D), generator=g, device="cuda").to(torch.float16)
+    wide = torch.randn((T, Hkv + 2, D), generator=g, device="cuda").to(torch.float16)
+    kc, vc = caches(9, Hkv, bs, D, seed=4)
+    slot = torch.cat([torch.arange(40, 90), torch.tensor([-1, 9 * bs, 2 ** 31 - 1, -2 ** 31, 5]), torch.arange(128, 150)])
+    check_append(qkv[:, Hkv:2 * Hkv], wide[:, :Hkv], kc, vc, slot.to(torch.int32).cuda())
+    # rows of no tokens
+    atom.atom_kv8_append(qkv[:0, :Hkv], qkv[:0, :Hkv], kc, vc, i32())
+
+
+def test_append_large_and_long_runs():
+    """Enough tokens for every number of tokens to a wavefront that the call picks."""
+    for T, Hkv in ((1500, 2), (3000, 8), (9000, 16)):
+        D, bs = 64, 128
+        g = torch.Generator(device="cuda").manual_seed(T)
+        k, v = (torch.randn((T, Hkv, D), generator=g, device="cuda").to(torch.float16) for _ in "kv")
+        kc, vc = caches(T // bs + 60, Hkv, bs, D, seed=T)
+        slot = torch.arange(31, 31 + T, dtype=torch.int32, device="cuda")
+        slot[200:240] = torch.arange(40, dtype=torch.int32, device="cuda") * bs + (T // bs + 5) * bs     # single tokens in between
+        slot[240:] += bs                                    # (the run of before ended inside its block)
+        check_append(k, v, kc, vc, slot)
+
+
+# ---------------------------------------------------------------- attention
+
+
+class Case:
+    """A cache with contents, requests on it and their queries."""
+
+    def __init__(self, H, Hkv, D, bs, past, new, seed=0, pad=0, extra=1, spare=2):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        need = [-(-(p + n) // bs) for p, n in zip(past, new)]
+        self.blocks, self.W = sum(need) + spare, max([1, *need]) + extra
+        self.kc, self.vc = caches(self.blocks, Hkv, bs, D, seed=seed)
+        for c, s in (self.kc, self.vc):
+            c.copy_((torch.randn(c.shape, generator=g, device="cuda") * 40).round_().clamp_(-127, 127))
+            s.mul_(2.0)
+        ids = torch.randperm(self.blocks, generator=g, device="cuda").to(torch.int32)
+        self.table = torch.full((len(past), self.W), -1, dtype=torch.int32, device="cuda")
+        used = 0
+        for b, n in enumerate(need):
+            self.table[b, :n] = ids[used:used + n]
+            used += n
+        self.unused = ids[used:].long()
+        self.start = i32(*np.concatenate([[0], np.cumsum(new)]).astype(int).tolist())
+        self.len = i32(*[p + n for p, n in zip(past, new)])
+        self.T = sum(new) + pad
+        self.q = torch.randn((self.T, H, D), generator=g, device="cuda").to(torch.float16)
+        self.sm = D ** -0.5
+        self.max_new = max(new, default=0)
+
+    def call(self, **kw):
+        return atom.atom_attention_kv8(kw.pop("q", self.q), self.kc, self.vc, self.table, self.start, self.len, self.sm,
+                                       **{"max_new": self.max_new, **kw})
+
+    def check(self, got=None, **kw):
+        got = self.call(**kw) if got is None else got
+        want, tol, done = ref.attention(npy(self.q), [npy(t) for t in self.kc], [npy(t) for t in self.vc], npy(self.table),
+                                        npy(self.start), npy(self.len), self.sm)
+        off = np.abs(npy(got).astype(np.float64) - want)
+        assert np.isfinite(npy(got)[done]).all()
+        worst = (off / np.maximum(tol, 1e-30))[done]
+        assert worst.size == 0 or worst.max() <= 1.0, f"{worst.max():.2f} of the bound at {np.unravel_index(worst.argmax(), worst.shape)}"
+        return got
+
+
+HEADS = [(1, 1), (4, 4), (8, 2), (16, 1), (20, 1), (6, 2), (40, 1)]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bs", [16, 32, 64, 128])
+@pytest.mark.parametrize("H,Hkv", HEADS)
+def test_attention_single_tokens(D, bs, H, Hkv):
+    """One new token each over contexts from none to some hundred keys, on both sides of every block and step."""
+    past = [0, 1, 14, 15, 16, 30, 31, 32, 63, 64, 127, 128, 129, 255, 300]
+    Case(H, Hkv, D, bs, past, [1] * len(past), seed=bs + H).check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bs", [16, 64, 128])
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (8, 2), (5, 1)])
+def test_attention_several_tokens(D, bs, H, Hkv):
+    """Ragged numbers of new tokens, none among them, with and without a context: prompts, chunks, drafts, single tokens."""
+    past, new = [0, 0, 7, 100, 64, 0, 33, 250], [1, 37, 0, 5, 1, 130, 70, 3]
+    Case(H, Hkv, D, bs, past, new, seed=D + H).check()
+    Case(H, Hkv, D, bs, past, new, seed=D + H).check(max_new=None)
+
+
+@pytest.mark.parametrize("H,Hkv,D,bs,past,new", [
+    (32, 32, 128, 64, [1000], [1]), (64, 8, 128, 16, [5000, 17], [1, 1]), (8, 1, 64, 32, [20000], [1]), (4, 4, 128, 128, [4000, 3], [2, 9]),
+    (64, 8, 128, 64, [0], [300]), (16, 4, 64, 16, [3000], [64]), (16, 16, 128, 32, [10, 2000, 0], [1, 200, 90])])
+def test_attention_long(H, Hkv, D, bs, past, new):
+    Case(H, Hkv, D, bs, past, new, seed=len(past)).check()
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 130, 200])
+def test_attention_many_requests(B):
+    """More requests than a wavefront has lanes, some without tokens or keys."""
+    g = torch.Generator().manual_seed(B)
+    past = torch.randint(0, 90, (B,), generator=g).tolist()
+    new = torch.randint(0, 3, (B,), generator=g).tolist()
+    past[1] = new[1] = 0
+    Case(4, 2, 64, 16, past, new, seed=B).check()
+
+
+def test_attention_rows_that_see_nothing_and_rows_that_are_left():
+    """More new tokens than positions (the first ones see no key), lengths of zero, padded rows of NaN, a max_new below a
+    request's tokens: zeros where the mask leaves nothing, everything behind as it was."""
+    c = Case(4, 2, 128, 16, [0, 20, 5], [6, 3, 9], seed=3, pad=5)
+    c.len = i32(2, 0, 14)
+    c.q[18:] = float("nan")
+    out = torch.full_like(c.q, 7.0)
+    c.check(out=out, max_new=None)
+    assert (out[18:] == 7.0).all() and (out[:4] == 0).all() and (out[6:9] == 0).all()
+    out = torch.full_like(c.q, 7.0)
+    full = c.call(max_new=None)
+    c.call(out=out, max_new=4)
+    for b, n in ((0, 6), (1, 3), (2, 9)):
+        s = int(c.start[b])
+        assert torch.equal(out[s:s + min(n, 4)], full[s:s + min(n, 4)]) and (out[s + 4:s + n] == 7.0).all()
+
+
+def test_attention_pages_that_do_not_exist():
+    """-1, numbers past the pool and columns past the table hold no keys; blocks of nobody may hold anything."""
+    c = Case(8, 2, 64, 16, [100, 40, 70], [3, 1, 1], seed=5, spare=6)
+    for _, s in (c.kc, c.vc):
+        s[c.unused] = float("nan")
+    c.table[0, 2] = -1
+    c.table[0, 3] = c.blocks
+    c.table[0, 5] = 2 ** 31 - 1
+    c.table[1, :] = -1                                      # nothing at all
+    c.check()
+    c.len = i32(500, 41, 71)                                # longer than its table row
+    c.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_scales_far_apart(D):
+    """Blocks whose scales differ by many orders of magnitude, zeros among them: the weights keep their precision wherever the
+    mass lies."""
+    c = Case(4, 2, D, 16, [200, 333], [2, 1], seed=11)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for i, (_, s) in enumerate((c.kc, c.vc)):
+        s.copy_(torch.pow(10.0, torch.empty(s.shape, device="cuda").uniform_(-9 + 5 * i, -1 + 2 * i, generator=g)))
+    c.vc[1][::5] = 0
+    c.vc[0][::5] = 0
+    c.check()
+    c.sm = 0.0                                              # plain means
+    c.check()
+    c.sm = 30.0                                             # nearly one key each
+    c.kc[1].fill_(0.02)
+    c.check()
+
+
+def test_attention_strides_and_given_memory():
+    """Queries as a slice of the projection's output, outputs into a wider array, a workspace of the caller."""
+    c = Case(8, 4, 64, 32, [700, 50], [1, 3], seed=8)
+    want = c.check()
+    qkv = torch.randn((c.T, 16, 64), device="cuda").to(torch.float16)
+    qkv[:, 4:12] = c.q
+    wide = torch.full((c.T, 11, 64), 3.0, dtype=torch.float16, device="cuda")
+    need = atom.atom_attention_kv8_workspace_bytes(c.T, 2, 8, 4, 64, c.max_new, c.W, 32)
+    assert need > 0
+    ws = torch.full((need + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+    got = c.call(q=qkv[:, 4:12], out=wide[:, 2:10], workspace=ws[:need])
+    assert torch.equal(got, want) and (wide[:, :2] == 3.0).all() and (wide[:, 10:] == 3.0).all() and (ws[need:] == 0xA5).all()
+
+
+def test_attention_runs_twice_alike():
+    c = Case(32, 8, 128, 64, [900, 4000, 20], [1, 1, 1], seed=2)
+    assert torch.equal(c.call(), c.call())
+
+
+def test_cache_offsets_past_32_bits():
+    """Blocks beyond 4 GiB of codes, appended to and read."""
+    D, bs, Hkv = 128, 128, 8
+    n = (5 << 30) // (Hkv * bs * D)
+    kc = atom.atom_kv8_cache(n, Hkv, D, bs)
+    vc = atom.atom_kv8_cache(n, Hkv, D, bs)
+    past, new = i32(0, 0), i32(200, 140)
+    table = torch.full((2, 2), -1, dtype=torch.int32, device="cuda")
+    ids = [n - 1, 3, n // 2 + 11, n - 2]
+    start, length, slot, _ = tables(past, new, table, i32(*ids), 340, bs)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    q, k, v = (torch.randn((340, Hkv, D), generator=g, device="cuda").to(torch.float16) for _ in "qkv")
+    atom.atom_kv8_append(k, v, kc, vc, slot)
+    out = atom.atom_attention_kv8(q, kc, vc, table, start, length, D ** -0.5, max_new=200)
+    small = [(c[ids], s[ids]) for c, s in (kc, vc)]         # the same blocks as a cache of their own
+    at = torch.tensor([[0, 1], [2, 3]], dtype=torch.int32, device="cuda")
+    want = atom.atom_attention_kv8(q, small[0], small[1], at, start, length, D ** -0.5, max_new=200)
+    assert torch.equal(out, want)
+    want_k = ref.append(npy(k), np.zeros((4, Hkv, bs, D), np.int8), np.zeros((4, Hkv), np.float32),
+                        npy(torch.cat([torch.arange(0, 200), torch.arange(256, 396)])))
+    assert np.array_equal(npy(small[0][0]), want_k[0]) and np.array_equal(npy(small[0][1]), want_k[1])
+    assert int((kc[0] != 0).any((1, 2, 3)).sum()) == 4
+
+
+# ---------------------------------------------------------------- together
+
+
+def _step(s):
+    start, length, slot, cursor = atom.atom_kv_block_map(s["past"], s["new"], s["table"], s["free"], s["T"], s["bs"], cursor=s["cursor"])
+    atom.atom_kv8_append(s["k"], s["v"], s["kc"], s["vc"], slot)
+    out = atom.atom_attention_kv8(s["q"], s["kc"], s["vc"], s["table"], start, length, s["sm"], max_new=s["max_new"], out=s["out"])
+    return out, length, cursor
+
+
+def _state(B, T, max_new, H=8, Hkv=2, D=64, bs=16, W=40, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = lambda *n, **k: torch.zeros(n, device="cuda", **k)          # noqa: E731
+    return {"g": g, "bs": bs, "T": T, "sm": D ** -0.5, "max_new": max_new, "past": z(B, dtype=torch.int32), "new": z(B, dtype=torch.int32),
+            "table": torch.full((B, W), -1, dtype=torch.int32, device="cuda"), "cursor": z(1, dtype=torch.int32),
+            "free": torch.randperm(B * W, generator=g, device="cuda").to(torch.int32), "kc": atom.atom_kv8_cache(B * W, Hkv, D, bs),
+            "vc": atom.atom_kv8_cache(B * W, Hkv, D, bs), "q": z(T, H, D, dtype=torch.float16), "k": z(T, Hkv, D, dtype=torch.float16),
+            "v": z(T, Hkv, D, dtype=torch.float16), "out": z(T, H, D, dtype=torch.float16)}
+
+
+def _inputs(s, new):
+    s["new"].copy_(i32(*new))
+    for n in "qkv":
+        s[n].copy_(torch.randn(s[n].shape, generator=s["g"], device="cuda"))
+
+
+def test_steps_of_a_server():
+    """Prompts, then steps that mix decoding requests with chunks: every step's attention against 64 bits over what the cache
+    holds, and against the keys and values as they were (within the cache's steps)."""
+    s = _state(4, 120, 90)
+    kept = [[] for _ in range(4)]
+    for new in ([90, 3, 0, 17], [1, 1, 40, 1], [1, 1, 1, 1], [1, 60, 1, 0], [1, 1, 1, 1]):
+        _inputs(s, new)
+        out, length, cursor = _step(s)
+        at = 0
+        for b, n in enumerate(new):
+            kept[b].append(npy(s["k"][at:at + n]))
+            at += n
+        start = np.concatenate([[0], np.cumsum(new)])
+        want, tol, done = ref.attention(npy(s["q"]), [npy(t) for t in s["kc"]], [npy(t) for t in s["vc"]], npy(s["table"]), start,
+                                        npy(length), s["sm"])
+        assert (np.abs(npy(out) - want) <= tol)[done].all() and done[:sum(new)].all()
+        s["past"].copy_(length)
+        s["cursor"].copy_(cursor)
+    for b in range(4):                                      # the keys that the cache stands for
+        k = np.concatenate(kept[b]).astype(np.float64)
+        pages = npy(s["table"])[b, :-(-len(k) // 16)]
+        c, sc = npy(s["kc"][0])[pages].astype(np.float64), npy(s["kc"][1])[pages].astype(np.float64)
+        rows = (c * sc[:, :, None, None]).transpose(0, 2, 1, 3).reshape(-1, 2, 64)[:len(k)]
+        step = np.repeat(sc, 16, 0)[:len(k)]
+        assert (np.abs(rows - k) <= 16 * 0.51 * step[:, :, None]).all()
+
+
+def test_a_captured_step_replays():
+    """A step captured once with padded arrays and replayed with other lengths, eager steps of another state in between; each
+    replay against the eager calls."""
+    a, e, other = _state(3, 64, 64, seed=4), _state(3, 64, 64, seed=4), _state(5, 32, 32, seed=5)
+    _inputs(other, [9, 0, 3, 4, 5])
+    for s in (a, e):
+        _inputs(s, [2, 2, 2])
+        _step(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, length, cursor = _step(a)
+        a["past"].copy_(length)
+        a["cursor"].copy_(cursor)
+    for s in (a, e):                                        # both from the beginning
+        s["past"].zero_()
+        s["cursor"].zero_()
+    for new in ([30, 1, 0], [1, 1, 33], [1, 1, 1], [1, 40, 1], [1, 1, 1]):
+        for s in (a, e):
+            s["g"].manual_seed(sum(new))
+            _inputs(s, new)
+            s["out"].fill_(5.0)
+        _step(other)
+        graph.replay()
+        _, length, cursor = _step(e)
+        torch.cuda.synchronize()
+        e["past"].copy_(length)
+        e["cursor"].copy_(cursor)
+        for n in ("out", "table", "past", "cursor"):
+            assert torch.equal(a[n], e[n]), n
+        for c in ("kc", "vc"):
+            assert torch.equal(a[c][0], e[c][0]) and torch.equal(a[c][1], e[c][1])
+
+
+def test_calls_on_another_stream():
+    s = _state(3, 64, 64, seed=7)
+    _inputs(s, [20, 1, 43])
+    want = _step(s)[0].clone()
+    s["out"].zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        _step(s)
+    side.synchronize()
+    assert torch.equal(s["out"], want)
