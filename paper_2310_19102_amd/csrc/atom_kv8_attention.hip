@@ -14,6 +14,7 @@ namespace {
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 typedef unsigned u2 __attribute__((ext_vector_type(2)));
 
@@ -420,6 +421,246 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
     }
 }
 
+// ---------------------------------------------------------------- many query rows
+//
+// One workgroup of four wavefronts for a tile of 128 query rows of a (request, cache head) and a piece of its keys; a wavefront has
+// 32 rows, and all four read the same 64 keys from LDS.  The arithmetic is that of the kernel above on 32x32x16 matrix instructions: S^T = K Q^T, so that
+// a lane has one query row and 16 of 32 keys, and O^T = V^T P^T with the weights where the scores were.
+//
+//   LDS:   the four wavefronts turn 64 rows of codes into halves once for all 128 query rows (each for itself it would be
+//          four times the work: 256 vector instructions a tile).  K as [key][D]; V as [D][key], its keys in the order of the scores' rows, so that
+//          an operand is one 16-byte read: byte selection makes the halves and transposes.  Rows are padded by 16 bytes, which spreads the reads (16 lanes,
+//          16 rows) and V's writes (16 groups of keys of two dimensions) over all banks.
+//   loads: codes of the next tile but one are on their way, and their block numbers a tile earlier, while one is computed; two buffers, a barrier a tile.
+//   order: the last tiles of a request, which see the most keys, first.
+constexpr int kTile = 128, kKeys = 64;
+
+template <int D>
+struct TileLds {
+    static constexpr int kPitch = 2 * D + 16, vPitch = 2 * kKeys + 16;          // bytes
+    static constexpr int k = 0, v = kKeys * kPitch, scales = v + D * vPitch, bytes = scales + 64;   // of one buffer; scales: f4 x 4 blocks of 16 keys
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2)
+void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
+{
+    typedef TileLds<D> L;
+    constexpr int KS = D / 16, DB = D / 32;           // matrix instructions for 32 keys' scores; blocks of 32 output dimensions
+    constexpr int KL = D / 64, VB = D / 16;           // 16-byte loads of K, bytes of a V row in a lane
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+
+    const int h = blockIdx.x % a.Hkv;
+    const Place w = place<kTile, false>(a, blockIdx.x / a.Hkv, rows_min, rows_max);
+    if (!w.found) return;
+    const Request r = request(a, w.b);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, hh = lane >> 5;
+    const int all = r.n * a.group;
+    const int tile = (all + kTile - 1) / kTile - 1 - w.tile;
+    const int row0 = tile * kTile + wave * 32, rows = min(32, all - row0);      // of this wavefront; none: rows <= 0
+    const int row = min(row0 + n, all - 1);
+    const int token = row / a.group, head = h * a.group + row - token * a.group;
+    auto keys_of = [&](int row_) { return min(max(r.before + min(row_, all - 1) / a.group + 1, 0), r.keys); };
+    const int sees = keys_of(row), key0 = w.split * w.keys_per;
+    const int key1 = min(keys_of(tile * kTile + kTile - 1), key0 + w.keys_per);           // of the workgroup
+    const int wave1 = rows > 0 ? min(keys_of(row0 + rows - 1), key1) : 0, least = min(keys_of(row0), key1);
+
+    h8 q[KS];
+    float start = 0.0f;
+    {
+        const __half *qp = a.q + (int64_t)(r.start + token) * a.ldq + (int64_t)head * D + 8 * hh;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            q[s] = __builtin_bit_cast(h8, *reinterpret_cast<const u4 *>(qp + 16 * s));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) start += (float)q[s][i];
+        }
+        start += __shfl_xor(start, 32, 64);
+        start *= -128.0f * 5.9604644775390625e-08f;
+    }
+    const float to_e = a.sm_scale * kLog2e * 16777216.0f;
+    f16v o[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+    float M = kNoScore, l = 0.0f;
+
+    // ---- loading: a thread has 16 (or 32) codes of one key of K, and D / 16 of four keys of V
+    const int32_t *table = a.table + (int64_t)w.b * a.W;
+    const int kt = tid >> 2, vt = 4 * (lane & 15), vd = VB * (4 * wave + (lane >> 4));
+    auto page_of = [&](int key) {                     // -1: none
+        if (key >= key1) return -1;
+        const int32_t p = table[key >> a.shift];
+        return p >= 0 && p < a.n_blocks ? p : -1;
+    };
+    auto row_of = [&](int page, int key) {            // of the whole cache; without a page its first rows, which are masked
+        return page < 0 ? (int64_t)(key & 15) : (((int64_t)page * a.Hkv + h) << a.shift) + (key & ((1 << a.shift) - 1));
+    };
+    u4 kr[KL];
+    uint32_t vr[4][VB / 4];
+    f4 sc;
+    int k_page, v_page, s_page;                       // of the tile to be loaded next
+    auto pages = [&](int key) {
+        k_page = page_of(key + kt);
+        v_page = page_of(key + vt);
+        s_page = tid < 4 ? page_of(key + 16 * tid) : -1;
+    };
+    auto fetch = [&](int key) {
+        const int8_t *kp = a.kq + row_of(k_page, key + kt) * D + 16 * (tid & 3);
+#pragma unroll
+        for (int i = 0; i < KL; ++i) kr[i] = *reinterpret_cast<const u4 *>(kp + 64 * i);
+        const int8_t *vp = a.vq + row_of(v_page, key + vt) * D + vd;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (VB == 8) {
+                const u2 v = *reinterpret_cast<const u2 *>(vp + i * D);
+                vr[i][0] = v[0];
+                vr[i][1] = v[1];
+            } else {
+                vr[i][0] = *reinterpret_cast<const uint32_t *>(vp + i * D);
+            }
+        }
+        if (tid < 4) {
+            sc = f4{1.0f, 0.0f, 0.0f, 0.0f};          // no page: a factor that keeps minus infinity, no weight
+            if (s_page >= 0) {
+                const int64_t at = (int64_t)s_page * a.Hkv + h;
+                const float v = fmaxf(a.vs[at], 2.3283064365386963e-10f);
+                sc = f4{fmaxf(a.ks[at] * to_e, 1e-37f), __builtin_amdgcn_logf(v), __builtin_amdgcn_rcpf(v), 1.0f};
+            }
+        }
+    };
+    auto stage = [&](unsigned char *buf) {
+        unsigned char *kp = buf + L::k + kt * L::kPitch + 32 * (tid & 3);
+#pragma unroll
+        for (int i = 0; i < KL; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t w0 = flip(kr[i][2 * j]), w1 = flip(kr[i][2 * j + 1]);
+                *reinterpret_cast<u4 *>(kp + 128 * i + 16 * j) =
+                    u4{__builtin_amdgcn_perm(0, w0, 0x0c010c00u), __builtin_amdgcn_perm(0, w0, 0x0c030c02u),
+                       __builtin_amdgcn_perm(0, w1, 0x0c010c00u), __builtin_amdgcn_perm(0, w1, 0x0c030c02u)};
+            }
+        // keys vt .. vt + 3: step u = vt / 16 of 16 keys, half-wave (vt / 4) & 1, its first or second four
+        const int tq = lane & 15;
+        unsigned char *vp = buf + L::v + vd * L::vPitch + 16 * (2 * (tq >> 2) + (tq & 1)) + 8 * ((tq >> 1) & 1);
+#pragma unroll
+        for (int j = 0; j < VB / 4; ++j) {
+            const uint32_t w0 = flip(vr[0][j]), w1 = flip(vr[1][j]), w2 = flip(vr[2][j]), w3 = flip(vr[3][j]);
+#define ATOM_STAGE(e) *reinterpret_cast<u2 *>(vp + (4 * j + (e)) * L::vPitch) = u2{centred(pair_of<e>(w0, w1)), centred(pair_of<e>(w2, w3))}
+            ATOM_STAGE(0);
+            ATOM_STAGE(1);
+            ATOM_STAGE(2);
+            ATOM_STAGE(3);
+#undef ATOM_STAGE
+        }
+        if (tid < 4) *reinterpret_cast<f4 *>(buf + L::scales + 16 * tid) = sc;
+    };
+    auto compute = [&](const unsigned char *buf, int key) {
+        f16v s[2];
+        const unsigned char *kp = buf + L::k + n * L::kPitch + 16 * hh;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] = start;
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(kp + 32 * t * L::kPitch + 32 * i), q[i], s[t], 0, 0, 0);
+        }
+        f4 c[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) c[b] = *reinterpret_cast<const f4 *>(buf + L::scales + 16 * b);
+        const bool there = c[0][3] * c[1][3] * c[2][3] * c[3][3] != 0.0f;
+        if (key + kKeys > least || !there) {          // (the same in all lanes)
+            const int room = min(sees, key1) - (key + 4 * hh);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (32 * t + 8 * (i >> 2) + (i & 3) >= room || c[2 * t + (i >> 3)][3] == 0.0f) s[t][i] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            float m = s[b >> 1][8 * (b & 1)];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) m = fmaxf(m, s[b >> 1][8 * (b & 1) + i]);
+            top = fmaxf(top, fmaf(m, c[b][0], c[b][1]));
+        }
+        if (__ballot(top > M + 8.0f)) {               // rare after the first tiles
+            const float to = fmaxf(M, fmaxf(top, __shfl_xor(top, 32, 64)));
+            const float down = __builtin_amdgcn_exp2f(M - to);
+            M = to;
+            l *= down;
+#pragma unroll
+            for (int i = 0; i < DB; ++i) o[i] *= down;
+        }
+        h8 p[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const float shift = c[b][1] - M;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[b >> 1][8 * (b & 1) + i], c[b][0], shift));
+                sum += e;
+                p[b][i] = (_Float16)e;
+            }
+            l = fmaf(sum, c[b][2], l);
+        }
+        const unsigned char *vp = buf + L::v + n * L::vPitch + 16 * hh;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(vp + 32 * i * L::vPitch + 32 * u), p[u], o[i], 0, 0, 0);
+    };
+
+    if (key0 < key1) {                                // (the same in all threads)
+        pages(key0);
+        fetch(key0);
+        pages(key0 + kKeys);
+        stage(lds);
+        fetch(key0 + kKeys);
+        pages(key0 + 2 * kKeys);
+        __syncthreads();
+        int at = 0;
+        for (int key = key0; key < key1; key += kKeys, at ^= L::bytes) {
+            if (key < wave1) compute(lds + at, key);
+            if (key + kKeys < key1) {
+                stage(lds + (at ^ L::bytes));
+                fetch(key + 2 * kKeys);
+                pages(key + 3 * kKeys);
+            }
+            __syncthreads();
+        }
+    }
+
+    l += __shfl_xor(l, 32, 64);
+    if (n >= rows) return;
+    const bool whole = w.splits == 1;
+    const float f = whole ? (l > 0.0f ? 512.0f / l : 0.0f) : 1.0f;            // (values were 2^-9 of the codes)
+    __half *to = a.out + (int64_t)(r.start + token) * a.ldo + (int64_t)head * D + 4 * hh;
+    float *part = whole ? nullptr : a.part + (((int64_t)(w.first_slot + w.split) * a.Hkv + h) * a.part_rows + wave * 32 + n) * (D + 4);
+    if (!whole && hh == 0) {
+        part[0] = M;
+        part[1] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f4 v = f4{o[i][4 * j] * f, o[i][4 * j + 1] * f, o[i][4 * j + 2] * f, o[i][4 * j + 3] * f};
+            if (whole) {
+                const __half2 lo = __floats2half2_rn(v[0], v[1]), hi = __floats2half2_rn(v[2], v[3]);
+                *reinterpret_cast<u2 *>(to + 32 * i + 8 * j) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+            } else {
+                *reinterpret_cast<f4 *>(part + 4 + 32 * i + 8 * j + 4 * hh) = v;
+            }
+        }
+}
+
 // The pieces of a tile, in their order.  One workgroup for a tile and cache head.
 template <int D, int ROWS>
 __global__ __launch_bounds__(256)
@@ -429,7 +670,9 @@ void attention_kv8_merge_kernel(const Args a, int rows_min, int rows_max)
     const Place w = place<ROWS, true>(a, blockIdx.x / a.Hkv, rows_min, rows_max);
     if (!w.found || w.splits == 1) return;
     const Request r = request(a, w.b);
-    const int rows = min(ROWS, r.n * a.group - w.tile * ROWS);
+    // (the kernel of many rows takes a request's tiles from the last one on)
+    const int tile = ROWS == kTile ? (r.n * a.group + ROWS - 1) / ROWS - 1 - w.tile : w.tile;
+    const int rows = min(ROWS, r.n * a.group - tile * ROWS);
     const int64_t stride = (int64_t)a.Hkv * a.part_rows * (D + 4);
     for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
         const int rr = i / (D / 4), d = 4 * (i % (D / 4));
@@ -444,7 +687,7 @@ void attention_kv8_merge_kernel(const Args a, int rows_min, int rows_max)
             o += *reinterpret_cast<const f4 *>(from + s * stride + 4 + d) * f;
         }
         const float f = sum > 0.0f ? 512.0f / sum : 0.0f;
-        const int rw = w.tile * ROWS + rr, t = rw / a.group;
+        const int rw = tile * ROWS + rr, t = rw / a.group;
         __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + rw - t * a.group) * D + d;
         const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
         *reinterpret_cast<u2 *>(to) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
@@ -453,26 +696,80 @@ void attention_kv8_merge_kernel(const Args a, int rows_min, int rows_max)
 
 // ---------------------------------------------------------------- shape of a call
 
-// Tiles of `rows` query rows, at most: of B requests with together T tokens, each with max_new at most.
-int64_t most_tiles(int64_t T, int B, int group, int max_new, int rows)
+// Requests of up to kFew query rows (tokens times the heads of a group) go to the first kernel, larger ones to the second.
+constexpr int kFew = 64;
+
+struct Part { int64_t tiles, slots; int target, part_rows; size_t floats; };     // no tiles: no launch
+struct Shape { Part few, many; int few_most; };      // few_most: rows that the first kernel takes at most
+
+// Pieces of keys: `want` workgroups for each cache head, none below 128 keys, no cutting where the tiles alone are twice as many.
+Part part_of(int64_t tiles, int part_rows, int64_t want, int Hkv, int D, int64_t capacity)
 {
-    const int64_t each = ((int64_t)max_new * group + rows - 1) / rows, by_request = each * B, by_token = T * group / rows + B;
-    return by_request < by_token ? by_request : by_token;
+    Part p = {tiles, tiles, 0, part_rows, 0};
+    const int64_t most = tiles * ((capacity + 127) / 128);
+    if (want > most) want = most;
+    if (tiles > 0 && tiles < 2 * want && most > tiles) {
+        p.target = (int)want;
+        p.slots += want;
+        p.floats = (size_t)(p.slots * Hkv * part_rows) * (size_t)(D + 4);
+    }
+    return p;
 }
 
-struct Shape { int64_t slots; int target, part_rows; int64_t tiles; };
-
-Shape rows_shape(int64_t T, int B, int Hkv, int group, int max_new, int64_t capacity)
+Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t capacity)
 {
-    Shape s;
-    s.tiles = most_tiles(T, B, group, max_new, kTileRows);
-    int64_t target = (1024 + Hkv - 1) / Hkv;
-    const int64_t most = s.tiles * ((capacity + 127) / 128);          // no piece below 128 keys
-    if (target > most) target = most;
-    s.target = s.tiles >= 2 * target || most == s.tiles ? 0 : (int)target;
-    s.slots = s.tiles + s.target;
-    s.part_rows = (int)((int64_t)max_new * group < kTileRows ? (int64_t)max_new * group : kTileRows);
+    Shape s = {};
+    if (T == 0 || B == 0 || max_new == 0) return s;
+    const int64_t rows = (int64_t)max_new * group;   // of one request, at most
+    const bool many = rows > kFew;
+    s.few_most = (int)(many ? (B > 1 ? kFew : 0) : rows);
+    if (s.few_most) {
+        const int64_t each = (int64_t)B * ((s.few_most + kTileRows - 1) / kTileRows), by_token = T * group / kTileRows + B;
+        s.few = part_of(each < by_token ? each : by_token, s.few_most < kTileRows ? s.few_most : kTileRows, (1024 + Hkv - 1) / Hkv, Hkv, D,
+                        capacity);
+    }
+    if (many) {                                      // (one request goes there whatever its size)
+        const int64_t least = s.few_most + 1, each = (int64_t)B * ((rows + kTile - 1) / kTile);
+        const int64_t requests = T * group / least < B ? T * group / least : B, by_token = T * group / kTile + requests;
+        s.many = part_of(each < by_token ? each : by_token, kTile, (512 + Hkv - 1) / Hkv, Hkv, D, capacity);
+    }
     return s;
+}
+
+template <int D>
+hipError_t launch(Args a, const Shape &s, float *workspace, hipStream_t stream)
+{
+    if (s.few.tiles) {
+        a.target = s.few.target;
+        a.part = workspace;
+        a.part_rows = s.few.part_rows;
+        hipLaunchKernelGGL((attention_kv8_rows_kernel<D>), dim3((unsigned)(s.few.slots * a.Hkv)), dim3(kWaves * 64), 0, stream, a, 1, s.few_most);
+        hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+        if (s.few.target) {
+            hipLaunchKernelGGL((attention_kv8_merge_kernel<D, kTileRows>), dim3((unsigned)(s.few.tiles * a.Hkv)), dim3(256), 0, stream, a, 1,
+                               s.few_most);
+            if ((err = hipGetLastError()) != hipSuccess) return err;
+        }
+    }
+    if (s.many.tiles) {
+        static atom_launch::LdsOptIn opt;
+        constexpr int bytes = 2 * TileLds<D>::bytes;
+        hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(&attention_kv8_tile_kernel<D>), bytes);
+        if (err != hipSuccess) return err;
+        a.target = s.many.target;
+        a.part = workspace + s.few.floats;
+        a.part_rows = s.many.part_rows;
+        hipLaunchKernelGGL((attention_kv8_tile_kernel<D>), dim3((unsigned)(s.many.slots * a.Hkv)), dim3(256), bytes, stream, a, s.few_most + 1,
+                           0x7fffffff);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+        if (s.many.target) {
+            hipLaunchKernelGGL((attention_kv8_merge_kernel<D, kTile>), dim3((unsigned)(s.many.tiles * a.Hkv)), dim3(256), 0, stream, a,
+                               s.few_most + 1, 0x7fffffff);
+            return hipGetLastError();
+        }
+    }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -481,16 +778,14 @@ namespace atom_internal {
 
 size_t attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, int max_new, int64_t W, int block_tokens)
 {
-    if (T == 0 || B == 0 || max_new == 0) return 0;
-    const Shape s = rows_shape(T, B, Hkv, H / Hkv, max_new, W * block_tokens);
-    return s.target ? (size_t)(s.slots * Hkv * s.part_rows) * (size_t)(D + 4) * sizeof(float) : 0;
+    const Shape s = shape(T, B, Hkv, H / Hkv, D, max_new, W * block_tokens);
+    return (s.few.floats + s.many.floats) * sizeof(float);
 }
 
 bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new, int64_t W, int block_tokens)
 {
-    if (T == 0 || B == 0 || max_new == 0) return true;
-    const Shape s = rows_shape(T, B, Hkv, H / Hkv, max_new, W * block_tokens);
-    return s.slots * Hkv <= 0x7fffffffLL;
+    const Shape s = shape(T, B, Hkv, H / Hkv, 128, max_new, W * block_tokens);
+    return s.few.slots * Hkv <= 0x7fffffffLL && s.many.slots * Hkv <= 0x7fffffffLL;
 }
 
 hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)
@@ -506,17 +801,8 @@ hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)
     a.kq = (const int8_t *)c.k_codes; a.ks = c.k_scale; a.vq = (const int8_t *)c.v_codes; a.vs = c.v_scale;
     a.sm_scale = c.sm_scale;
     a.out = (__half *)c.out; a.ldo = c.ldo;
-    const Shape s = rows_shape(c.T, c.B, c.Hkv, a.group, c.max_new, a.capacity);
-    a.target = s.target;
-    a.part = s.target ? (float *)c.workspace : nullptr;
-    a.part_rows = s.part_rows;
-    auto rows = c.D == 128 ? &attention_kv8_rows_kernel<128> : &attention_kv8_rows_kernel<64>;
-    hipLaunchKernelGGL(rows, dim3((unsigned)(s.slots * c.Hkv)), dim3(kWaves * 64), 0, stream, a, 1, 0x7fffffff);
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess || !s.target) return err;
-    auto merge = c.D == 128 ? &attention_kv8_merge_kernel<128, kTileRows> : &attention_kv8_merge_kernel<64, kTileRows>;
-    hipLaunchKernelGGL(merge, dim3((unsigned)(s.tiles * c.Hkv)), dim3(256), 0, stream, a, 1, 0x7fffffff);
-    return hipGetLastError();
+    const Shape s = shape(c.T, c.B, c.Hkv, a.group, c.D, c.max_new, a.capacity);
+    return c.D == 128 ? launch<128>(a, s, (float *)c.workspace, stream) : launch<64>(a, s, (float *)c.workspace, stream);
 }
 
 }  // namespace atom_internal
