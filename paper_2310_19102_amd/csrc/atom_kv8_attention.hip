@@ -13,6 +13,7 @@ namespace {
 
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
@@ -35,7 +36,7 @@ struct Args {
     __half *out; int64_t ldo;
     float *part;                                  // NULL: no tile's keys are split
     int part_rows;                                // rows of a split's record
-    int target;                                   // splits wanted for each cache head (0: none)
+    int budget;                                   // workgroups for each cache head that tiles may be cut into (0: none is cut)
 };
 
 // A request's share of the call.
@@ -60,10 +61,10 @@ __device__ __forceinline__ Request request(const Args &a, int b)
 
 // ---- which part of the work a workgroup has
 //
-// The query rows of a request and cache head (token after token, the group's heads of each) come in tiles of ROWS.  A tile's keys are cut into
-// pieces of the same number of keys in the whole call, so that `target` pieces (more by one a tile at most) hold all of them: sequences of
-// any lengths keep the card evenly busy, and the pieces of a tile meet in the merge kernel.  Every wavefront finds its place from the
-// lengths by itself, 64 requests at a time: for as many it is one read, which it needs anyway.
+// The query rows of a request and cache head (token after token, the group's heads of each) come in tiles of 1 << LOG rows.  Where the tiles are
+// fewer than the workgroups that a call is to have for each cache head (budget), their keys are cut into pieces of about one size in the whole call:
+// sequences of any lengths keep the card evenly busy, and the pieces of a tile meet in the merge kernel.  Every wavefront
+// finds its place from the lengths by itself, 64 requests at a time: for as many it is one read, which it needs anyway.
 struct Place { int b, tile, split, splits, keys_per, first_slot; bool found; };
 
 __device__ __forceinline__ int64_t wave_sum(int64_t v)
@@ -73,9 +74,9 @@ __device__ __forceinline__ int64_t wave_sum(int64_t v)
     return v;
 }
 
-// FROM_TILE: `index` counts tiles (all of a tile's pieces are meant), else pieces.  few / many: only requests with at most / more rows.
-template <int ROWS, bool FROM_TILE>
-__device__ __forceinline__ Place place(const Args &a, int index, int rows_min, int rows_max)
+// FROM_TILE: `index` counts tiles (all of a tile's pieces are meant), else pieces.  Requests of rows_min to rows_max rows count.
+template <int LOG, bool FROM_TILE>
+__device__ __forceinline__ Place place(const Args &a, int index, int budget, int rows_min, int rows_max)
 {
     const int lane = threadIdx.x & 63;
     auto tiles_keys = [&](int base, int &tiles, int &keys) {
@@ -85,7 +86,7 @@ __device__ __forceinline__ Place place(const Args &a, int index, int rows_min, i
             const Request r = request(a, base + lane);
             const int64_t rows = (int64_t)r.n * a.group;
             if (rows >= rows_min && rows <= rows_max) {
-                tiles = (int)((rows + ROWS - 1) / ROWS);
+                tiles = (int)((rows + (1 << LOG) - 1) >> LOG);
                 keys = r.keys;
             }
         }
@@ -94,17 +95,29 @@ __device__ __forceinline__ Place place(const Args &a, int index, int rows_min, i
     p.found = false;
     int tiles, keys;
     tiles_keys(0, tiles, keys);
-    int per = 0x7fffff80;
-    if (a.target) {                               // a whole number of 128 keys: one step of 32 for each of four wavefronts
-        int64_t all = (int64_t)tiles * keys;
+    int per = 0x3fffff80;                         // keys of a piece at most, a multiple of 128: one step of 32 for each of four wavefronts
+    if (budget) {
+        // sum over tiles of ceil(keys / per) is below tiles + all / per
+        int64_t all = (int64_t)tiles * keys, count = tiles;
         for (int base = 64; base < a.B; base += 64) {
             int t2, k2;
             tiles_keys(base, t2, k2);
             all += (int64_t)t2 * k2;
+            count += t2;
         }
         all = wave_sum(all);
-        const float want = ceilf((float)all * 1.00001f / (128.0f * (float)a.target));
-        per = want < 1.0f ? 128 : want < 8388607.0f ? 128 * (int)want : 0x3fffff80;
+        count = wave_sum(count);
+        auto share = [&](float pieces) {
+            const float want = ceilf((float)all * 1.00001f / (128.0f * pieces));
+            return want < 1.0f ? 128 : want < 8388607.0f ? 128 * (int)want : 0x3fffff80;
+        };
+        if (count < budget) {
+            per = share((float)(budget - count));
+            if (a.B <= 64) {                      // mostly it is half a piece a tile less
+                const int tight = share((float)budget - 0.5f * (float)count);
+                if (wave_sum((int64_t)tiles * (keys > tight ? (keys + tight - 1) / tight : 1)) <= budget) per = tight;
+            }
+        }
     }
     int count = 0, slots = 0;                     // tiles and pieces of the requests before
     for (int base = 0; base < a.B; base += 64) {
@@ -132,7 +145,8 @@ __device__ __forceinline__ Place place(const Args &a, int index, int rows_min, i
                 p.tile = (index - s0) / p.splits;
                 p.split = (index - s0) - p.tile * p.splits;
             }
-            p.keys_per = per;
+            const int all = __builtin_amdgcn_readlane(keys, l);
+            p.keys_per = p.splits == 1 ? 0x3fffff80 : ((all + p.splits - 1) / p.splits + 127) & ~127;      // even pieces
             p.first_slot = s0 + p.tile * p.splits;
             return p;
         }
@@ -168,6 +182,14 @@ __device__ __forceinline__ h8 halves(uint32_t a, uint32_t b, uint32_t c, uint32_
     return __builtin_bit_cast(h8, u4{a, b, c, d});
 }
 
+// Part of a row of codes.  ONCE: with the hint that nothing reads it again.
+template <bool ONCE, class V>
+__device__ __forceinline__ V load(const int8_t *p)
+{
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+    else return *reinterpret_cast<const V *>(p);
+}
+
 // max over the lanes l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ float max_of_chunks(float v)
 {
@@ -194,12 +216,12 @@ __device__ __forceinline__ float sum_of_chunks(float v)
 //   values: O^T = V^T P^T.  The weights lie in the registers of the scores as the second operand wants them when its order of keys is
 //           that of the scores' rows; V's rows are loaded in that order, D / 16 bytes a lane, and the byte selection that makes halves also
 //           transposes.  No LDS, no lane exchange in the loop.  The weights travel as fp16 (rounded to nearest even: 2^-12 of themselves).
-//   loads: the next step's 32 rows of K and V are in flight while one is computed; block numbers and scales of 64 blocks of 16 keys are
-//           read at once, a lane each.
-constexpr int kWaves = 4, kStep = 32, kTileRows = 16;
+//   loads: the next step's rows of K are asked for once the scores have used this step's, those of V after the values: half the registers of two
+//           buffers.  Block numbers and scales of 64 blocks of 16 keys are read at once, a lane each.
+constexpr int kWaves = 4, kStep = 32, kRowsLog = 4, kTileRows = 1 << kRowsLog;
 
-template <int D>
-__global__ __launch_bounds__(kWaves * 64)
+template <int D, bool ONCE>
+__global__ __launch_bounds__(kWaves * 64, 4)
 void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
 {
     constexpr int KB = D / 4, VB = D / 16;            // bytes of a K row and of a V row in a lane
@@ -208,7 +230,7 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
     __shared__ float s_m[kWaves][kTileRows], s_l[kWaves][kTileRows];
 
     const int h = blockIdx.x % a.Hkv;
-    const Place w = place<kTileRows, false>(a, blockIdx.x / a.Hkv, rows_min, rows_max);
+    const Place w = place<kRowsLog, false>(a, blockIdx.x / a.Hkv, a.budget, rows_min, rows_max);
     if (!w.found) return;
     const Request r = request(a, w.b);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -243,7 +265,8 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
     for (int e = 0; e < VB; ++e) acc[e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
     float M = kNoScore, l = 0.0f;
 
-    struct Rows { u4 k[2][KB / 16]; uint32_t v[8][VB / 4]; };
+    u4 kr[2][KB / 16];
+    uint32_t vr[8][VB / 4];
     // lane i: block of 16 keys number i of this wavefront's (two to a step)
     int   unit = -1;
     float b_scale = 0.0f, b_log = 0.0f, b_inv = 0.0f;
@@ -266,37 +289,44 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
             }
         }
     };
-    auto fetch = [&](int step, Rows &x) {             // (blocks past the end or without a page: the cache's first rows, masked)
-        const int at = 2 * (step & 31);
+    // (blocks past the end or without a page: the cache's first rows, masked)
+    auto block_at = [&](int step, int u) { return (int64_t)max(__builtin_amdgcn_readlane(unit, 2 * (step & 31) + u), 0) * (16 * D); };
+    auto fetch_k = [&](int step) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int64_t base = (int64_t)max(__builtin_amdgcn_readlane(unit, at + u), 0) * (16 * D);
-            const int8_t *kp = a.kq + base + (uint32_t)(m * D + c * KB);
+            const int8_t *kp = a.kq + block_at(step, u) + (uint32_t)(m * D + c * KB);
 #pragma unroll
-            for (int i = 0; i < KB / 16; ++i) x.k[u][i] = *reinterpret_cast<const u4 *>(kp + 16 * i);
-            const int8_t *vp = a.vq + base + (uint32_t)(4 * c * D + m * VB);
+            for (int i = 0; i < KB / 16; ++i) kr[u][i] = load<ONCE, u4>(kp + 16 * i);
+        }
+    };
+    auto fetch_v = [&](int step) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int8_t *vp = a.vq + block_at(step, u) + (uint32_t)(4 * c * D + m * VB);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if constexpr (VB == 8) {
-                    const u2 v = *reinterpret_cast<const u2 *>(vp + i * D);
-                    x.v[4 * u + i][0] = v[0];
-                    x.v[4 * u + i][1] = v[1];
+                    const u2 v = load<ONCE, u2>(vp + i * D);
+                    vr[4 * u + i][0] = v[0];
+                    vr[4 * u + i][1] = v[1];
                 } else {
-                    x.v[4 * u + i][0] = *reinterpret_cast<const uint32_t *>(vp + i * D);
+                    vr[4 * u + i][0] = load<ONCE, uint32_t>(vp + i * D);
                 }
             }
         }
     };
-    auto compute = [&](int step, const Rows &x) {
+    // the blocks of the next step: of this look-up, or (`turn`) still to be looked up
+    auto compute = [&](int step, bool more) __attribute__((always_inline)) {
         const int at = 2 * (step & 31), key = key_of(step);
+        const bool turn = ((step + 1) & 31) == 0;
         float e[8];
-        float log_v[2], inv_v[2], top = -INFINITY;
+        float inv_v[2], top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f4 s = f4{start, start, start, start};
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
-                const uint32_t w0 = flip(x.k[u][i >> 1][(2 * i) & 3]), w1 = flip(x.k[u][i >> 1][(2 * i + 1) & 3]);
+                const uint32_t w0 = flip(kr[u][i >> 1][(2 * i) & 3]), w1 = flip(kr[u][i >> 1][(2 * i + 1) & 3]);
                 const h8 k = halves(__builtin_amdgcn_perm(0, w0, 0x0c010c00u), __builtin_amdgcn_perm(0, w0, 0x0c030c02u),
                                     __builtin_amdgcn_perm(0, w1, 0x0c010c00u), __builtin_amdgcn_perm(0, w1, 0x0c030c02u));
                 s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i], s, 0, 0, 0);
@@ -309,15 +339,16 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
                 for (int i = 0; i < 4; ++i) s[i] = i < room ? s[i] : -INFINITY;
             }
             const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_scale), at + u));
-            log_v[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_log), at + u));
+            const float log_v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_log), at + u));
             inv_v[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_inv), at + u));
             const float f1 = id < 0 ? 1.0f : f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                e[4 * u + i] = fmaf(s[i], f1, log_v[u]);
+                e[4 * u + i] = fmaf(s[i], f1, log_v);
                 top = fmaxf(top, e[4 * u + i]);
             }
         }
+        if (more && !turn) fetch_k(step + 1);
         if (__ballot(top > M + 8.0f)) {               // rare after the first steps
             const float to = fmaxf(M, max_of_chunks(top));
             const float down = __builtin_amdgcn_exp2f(M - to);
@@ -339,17 +370,15 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
         h8 p;
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i] = (_Float16)e[i];
-        uint32_t v[8][VB / 4];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < VB / 4; ++j) v[i][j] = flip(x.v[i][j]);
+        __builtin_amdgcn_sched_barrier(0);            // (or registers for all of it at once)
 #define ATOM_VALUES(j, n)                                                                                                    \
         acc[4 * (j) + (n)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(                                                         \
-            halves(centred(pair_of<n>(v[0][j], v[1][j])), centred(pair_of<n>(v[2][j], v[3][j])),                             \
-                   centred(pair_of<n>(v[4][j], v[5][j])), centred(pair_of<n>(v[6][j], v[7][j]))), p, acc[4 * (j) + (n)], 0, 0, 0)
+            halves(centred(pair_of<n>(vr[0][j], vr[1][j])), centred(pair_of<n>(vr[2][j], vr[3][j])),                         \
+                   centred(pair_of<n>(vr[4][j], vr[5][j])), centred(pair_of<n>(vr[6][j], vr[7][j]))), p, acc[4 * (j) + (n)], 0, 0, 0)
 #pragma unroll
         for (int j = 0; j < VB / 4; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vr[i][j] = flip(vr[i][j]);
             ATOM_VALUES(j, 0);
             ATOM_VALUES(j, 1);
             ATOM_VALUES(j, 2);
@@ -360,19 +389,18 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
 
     if (key_of(0) < key1) {                           // (the same in all lanes)
         const int steps = (key1 - key_of(0) + kWaves * kStep - 1) / (kWaves * kStep);
-        Rows x, y;
         look_up(0);
-        fetch(0, x);
-        for (int s = 0; s < steps; s += 2) {
-            // (32 steps to a look-up, an even number: both steps of a round have theirs in the lanes)
-            if (s + 1 < steps) fetch(s + 1, y);
-            compute(s, x);
-            const bool more = s + 2 < steps, turn = ((s + 2) & 31) == 0;
-            if (more && !turn) fetch(s + 2, x);
-            if (s + 1 < steps) compute(s + 1, y);
-            if (more && turn) {
-                look_up(s + 2);
-                fetch(s + 2, x);
+        fetch_k(0);
+        fetch_v(0);
+        for (int step = 0; step < steps; ++step) {
+            const bool more = step + 1 < steps;
+            compute(step, more);
+            if (more) {
+                if (((step + 1) & 31) == 0) {
+                    look_up(step + 1);
+                    fetch_k(step + 1);
+                }
+                fetch_v(step + 1);
             }
         }
     }
@@ -433,7 +461,7 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
 //          16 rows) and V's writes (16 groups of keys of two dimensions) over all banks.
 //   loads: codes of the next tile but one are on their way, and their block numbers a tile earlier, while one is computed; two buffers, a barrier a tile.
 //   order: the last tiles of a request, which see the most keys, first.
-constexpr int kTile = 128, kKeys = 64;
+constexpr int kTileLog = 7, kTile = 1 << kTileLog, kKeys = 64;
 
 template <int D>
 struct TileLds {
@@ -451,7 +479,7 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
 
     const int h = blockIdx.x % a.Hkv;
-    const Place w = place<kTile, false>(a, blockIdx.x / a.Hkv, rows_min, rows_max);
+    const Place w = place<kTileLog, false>(a, blockIdx.x / a.Hkv, a.budget, rows_min, rows_max);
     if (!w.found) return;
     const Request r = request(a, w.b);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -661,34 +689,72 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
         }
 }
 
-// The pieces of a tile, in their order.  One workgroup for a tile and cache head.
-template <int D, int ROWS>
+// The pieces of tiles, in their order: 16 rows of a tile and cache head for a workgroup, first (the first `few_groups` workgroups) those of the kernel
+// of few rows, then eight for each tile of the other.  What bounds it is its chain of reads (lengths, then the pieces), so eight pieces are read at once.
+struct Parts { int few_groups, few_most, few_budget, few_rows, many_budget; const float *few, *many; };
+
+template <int D>
 __global__ __launch_bounds__(256)
-void attention_kv8_merge_kernel(const Args a, int rows_min, int rows_max)
+void attention_kv8_merge_kernel(const Args a, const Parts parts)
 {
-    const int h = blockIdx.x % a.Hkv;
-    const Place w = place<ROWS, true>(a, blockIdx.x / a.Hkv, rows_min, rows_max);
+    const bool is_few = (int)blockIdx.x < parts.few_groups;
+    const int  index = is_few ? blockIdx.x : blockIdx.x - parts.few_groups, h = index % a.Hkv;
+    Place w;
+    int sub = 0, rows_log, part_rows;
+    const float *part;
+    if (is_few) {
+        w = place<kRowsLog, true>(a, index / a.Hkv, parts.few_budget, 1, parts.few_most);
+        rows_log = kRowsLog;
+        part = parts.few;
+        part_rows = parts.few_rows;
+    } else {
+        constexpr int kSubs = kTile / kTileRows;
+        sub = index / a.Hkv % kSubs;
+        w = place<kTileLog, true>(a, index / a.Hkv / kSubs, parts.many_budget, parts.few_most + 1, 0x7fffffff);
+        rows_log = kTileLog;
+        part = parts.many;
+        part_rows = kTile;
+    }
     if (!w.found || w.splits == 1) return;
     const Request r = request(a, w.b);
+    const int all = r.n * a.group;
     // (the kernel of many rows takes a request's tiles from the last one on)
-    const int tile = ROWS == kTile ? (r.n * a.group + ROWS - 1) / ROWS - 1 - w.tile : w.tile;
-    const int rows = min(ROWS, r.n * a.group - tile * ROWS);
-    const int64_t stride = (int64_t)a.Hkv * a.part_rows * (D + 4);
+    const int tile = is_few ? w.tile : ((all - 1) >> rows_log) - w.tile;
+    const int first = (tile << rows_log) + sub * kTileRows, rows = min(kTileRows, all - first);
+    const int64_t stride = (int64_t)a.Hkv * part_rows * (D + 4);
     for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
         const int rr = i / (D / 4), d = 4 * (i % (D / 4));
-        const float *from = a.part + (((int64_t)w.first_slot * a.Hkv + h) * a.part_rows + rr) * (D + 4);
-        float top = kNoScore;
-        for (int s = 0; s < w.splits; ++s) top = fmaxf(top, from[s * stride]);
-        float sum = 0.0f;
+        const float *from = part + (((int64_t)w.first_slot * a.Hkv + h) * part_rows + sub * kTileRows + rr) * (D + 4);
+        float top = kNoScore, sum = 0.0f;
         f4 o = f4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = 0; s < w.splits; ++s) {
-            const float f = __builtin_amdgcn_exp2f(from[s * stride] - top);
-            sum = fmaf(from[s * stride + 1], f, sum);
-            o += *reinterpret_cast<const f4 *>(from + s * stride + 4 + d) * f;
+        for (int s = 0; s < w.splits; s += 8) {
+            float m[8], l[8];
+            f4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float *piece = from + min(s + k, w.splits - 1) * stride;
+                const f2 ml = *reinterpret_cast<const f2 *>(piece);
+                m[k] = s + k < w.splits ? ml[0] : kNoScore;
+                l[k] = s + k < w.splits ? ml[1] : 0.0f;
+                v[k] = *reinterpret_cast<const f4 *>(piece + 4 + d);
+            }
+            float to = top;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) to = fmaxf(to, m[k]);
+            const float down = __builtin_amdgcn_exp2f(top - to);
+            top = to;
+            sum *= down;
+            o *= down;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float f = s + k < w.splits ? __builtin_amdgcn_exp2f(m[k] - top) : 0.0f;
+                sum = fmaf(l[k], f, sum);
+                o += v[k] * f;
+            }
         }
         const float f = sum > 0.0f ? 512.0f / sum : 0.0f;
-        const int rw = tile * ROWS + rr, t = rw / a.group;
-        __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + rw - t * a.group) * D + d;
+        const int row = first + rr, t = row / a.group;
+        __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + row - t * a.group) * D + d;
         const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
         *reinterpret_cast<u2 *>(to) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
     }
@@ -698,20 +764,22 @@ void attention_kv8_merge_kernel(const Args a, int rows_min, int rows_max)
 
 // Requests of up to kFew query rows (tokens times the heads of a group) go to the first kernel, larger ones to the second.
 constexpr int kFew = 64;
+constexpr int kFewWorkgroups = 1024, kManyWorkgroups = 512;      // what the card has room for at once
 
-struct Part { int64_t tiles, slots; int target, part_rows; size_t floats; };     // no tiles: no launch
+struct Part { int64_t tiles, groups; int budget, part_rows; size_t floats; };    // no tiles: no launch
 struct Shape { Part few, many; int few_most; };      // few_most: rows that the first kernel takes at most
 
-// Pieces of keys: `want` workgroups for each cache head, none below 128 keys, no cutting where the tiles alone are twice as many.
+// `want` workgroups together, for each cache head: where there are fewer tiles (and 128 keys to a piece) they are cut.
 Part part_of(int64_t tiles, int part_rows, int64_t want, int Hkv, int D, int64_t capacity)
 {
     Part p = {tiles, tiles, 0, part_rows, 0};
     const int64_t most = tiles * ((capacity + 127) / 128);
-    if (want > most) want = most;
-    if (tiles > 0 && tiles < 2 * want && most > tiles) {
-        p.target = (int)want;
-        p.slots += want;
-        p.floats = (size_t)(p.slots * Hkv * part_rows) * (size_t)(D + 4);
+    int64_t budget = (want + Hkv - 1) / Hkv;
+    if (budget > most) budget = most;
+    if (budget > tiles) {
+        p.budget = (int)budget;
+        p.groups = budget;
+        p.floats = (size_t)(p.groups * Hkv * part_rows) * (size_t)(D + 4);
     }
     return p;
 }
@@ -725,51 +793,67 @@ Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t ca
     s.few_most = (int)(many ? (B > 1 ? kFew : 0) : rows);
     if (s.few_most) {
         const int64_t each = (int64_t)B * ((s.few_most + kTileRows - 1) / kTileRows), by_token = T * group / kTileRows + B;
-        s.few = part_of(each < by_token ? each : by_token, s.few_most < kTileRows ? s.few_most : kTileRows, (1024 + Hkv - 1) / Hkv, Hkv, D,
-                        capacity);
+        s.few = part_of(each < by_token ? each : by_token, s.few_most < kTileRows ? s.few_most : kTileRows, kFewWorkgroups, Hkv, D, capacity);
     }
     if (many) {                                      // (one request goes there whatever its size)
         const int64_t least = s.few_most + 1, each = (int64_t)B * ((rows + kTile - 1) / kTile);
         const int64_t requests = T * group / least < B ? T * group / least : B, by_token = T * group / kTile + requests;
-        s.many = part_of(each < by_token ? each : by_token, kTile, (512 + Hkv - 1) / Hkv, Hkv, D, capacity);
+        s.many = part_of(each < by_token ? each : by_token, kTile, kManyWorkgroups, Hkv, D, capacity);
     }
     return s;
+}
+
+// A cache that the last-level cache (256 MB) does not keep until the next step is read with the hint that nothing reads it again, where a row is read
+// by one workgroup only.
+bool reads_once(const Args &a, int rows)
+{
+    return rows <= kTileRows && (int64_t)a.B * a.Hkv * a.capacity * 128 >= (int64_t)1 << 27;
 }
 
 template <int D>
 hipError_t launch(Args a, const Shape &s, float *workspace, hipStream_t stream)
 {
+    hipError_t err = hipSuccess;
+    Parts parts = {};
+    parts.few_most = s.few_most;
+    int64_t merges = 0;
     if (s.few.tiles) {
-        a.target = s.few.target;
+        a.budget = s.few.budget;
         a.part = workspace;
         a.part_rows = s.few.part_rows;
-        hipLaunchKernelGGL((attention_kv8_rows_kernel<D>), dim3((unsigned)(s.few.slots * a.Hkv)), dim3(kWaves * 64), 0, stream, a, 1, s.few_most);
-        hipError_t err = hipGetLastError();
-        if (err != hipSuccess) return err;
-        if (s.few.target) {
-            hipLaunchKernelGGL((attention_kv8_merge_kernel<D, kTileRows>), dim3((unsigned)(s.few.tiles * a.Hkv)), dim3(256), 0, stream, a, 1,
-                               s.few_most);
-            if ((err = hipGetLastError()) != hipSuccess) return err;
+        auto kern = reads_once(a, s.few_most) ? &attention_kv8_rows_kernel<D, true> : &attention_kv8_rows_kernel<D, false>;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(s.few.groups * a.Hkv)), dim3(kWaves * 64), 0, stream, a, 1, s.few_most);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+        if (s.few.budget) {
+            merges = s.few.tiles * a.Hkv;
+            parts.few_groups = (int)merges;
+            parts.few_budget = s.few.budget;
+            parts.few_rows = s.few.part_rows;
+            parts.few = workspace;
         }
     }
     if (s.many.tiles) {
         static atom_launch::LdsOptIn opt;
         constexpr int bytes = 2 * TileLds<D>::bytes;
-        hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(&attention_kv8_tile_kernel<D>), bytes);
+        err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(&attention_kv8_tile_kernel<D>), bytes);
         if (err != hipSuccess) return err;
-        a.target = s.many.target;
+        a.budget = s.many.budget;
         a.part = workspace + s.few.floats;
         a.part_rows = s.many.part_rows;
-        hipLaunchKernelGGL((attention_kv8_tile_kernel<D>), dim3((unsigned)(s.many.slots * a.Hkv)), dim3(256), bytes, stream, a, s.few_most + 1,
+        hipLaunchKernelGGL((attention_kv8_tile_kernel<D>), dim3((unsigned)(s.many.groups * a.Hkv)), dim3(256), bytes, stream, a, s.few_most + 1,
                            0x7fffffff);
         if ((err = hipGetLastError()) != hipSuccess) return err;
-        if (s.many.target) {
-            hipLaunchKernelGGL((attention_kv8_merge_kernel<D, kTile>), dim3((unsigned)(s.many.tiles * a.Hkv)), dim3(256), 0, stream, a,
-                               s.few_most + 1, 0x7fffffff);
-            return hipGetLastError();
+        if (s.many.budget) {
+            merges += s.many.tiles * (kTile / kTileRows) * a.Hkv;
+            parts.many_budget = s.many.budget;
+            parts.many = workspace + s.few.floats;
         }
     }
-    return hipSuccess;
+    if (merges) {
+        hipLaunchKernelGGL((attention_kv8_merge_kernel<D>), dim3((unsigned)merges), dim3(256), 0, stream, a, parts);
+        err = hipGetLastError();
+    }
+    return err;
 }
 
 }  // namespace
@@ -785,7 +869,7 @@ size_t attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, in
 bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new, int64_t W, int block_tokens)
 {
     const Shape s = shape(T, B, Hkv, H / Hkv, 128, max_new, W * block_tokens);
-    return s.few.slots * Hkv <= 0x7fffffffLL && s.many.slots * Hkv <= 0x7fffffffLL;
+    return (s.few.groups + 8 * s.many.groups) * Hkv <= 0x7fffffffLL;
 }
 
 hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)
