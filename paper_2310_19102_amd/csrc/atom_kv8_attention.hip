@@ -67,11 +67,25 @@ __device__ __forceinline__ Request request(const Args &a, int b)
 // finds its place from the lengths by itself, 64 requests at a time: for as many it is one read, which it needs anyway.
 struct Place { int b, tile, split, splits, keys_per, first_slot; bool found; };
 
-__device__ __forceinline__ int64_t wave_sum(int64_t v)
+// Sum over the lanes up to this one, on the vector unit (lane exchanges through LDS cost a microsecond in front of the first load).
+template <class V>
+__device__ __forceinline__ V running(V v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+#define ATOM_STEP(ctrl, rows) \
+    v += __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, rows, 0xF, false))
+    ATOM_STEP(0x111, 0xF);                        // one, two, four, eight lanes below in the row of 16
+    ATOM_STEP(0x112, 0xF);
+    ATOM_STEP(0x114, 0xF);
+    ATOM_STEP(0x118, 0xF);
+    ATOM_STEP(0x142, 0xA);                        // the row below's last lane, into rows 1 and 3
+    ATOM_STEP(0x143, 0xC);                        // the lower half's, into the upper
+#undef ATOM_STEP
     return v;
+}
+__device__ __forceinline__ int total(int v) { return __builtin_amdgcn_readlane(running(v), 63); }
+__device__ __forceinline__ float total(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, running(v)), 63));
 }
 
 // FROM_TILE: `index` counts tiles (all of a tile's pieces are meant), else pieces.  Requests of rows_min to rows_max rows count.
@@ -98,24 +112,25 @@ __device__ __forceinline__ Place place(const Args &a, int index, int budget, int
     int per = 0x3fffff80;                         // keys of a piece at most, a multiple of 128: one step of 32 for each of four wavefronts
     if (budget) {
         // sum over tiles of ceil(keys / per) is below tiles + all / per
-        int64_t all = (int64_t)tiles * keys, count = tiles;
+        int64_t mine = (int64_t)tiles * keys;
+        int     count = tiles;
         for (int base = 64; base < a.B; base += 64) {
             int t2, k2;
             tiles_keys(base, t2, k2);
-            all += (int64_t)t2 * k2;
+            mine += (int64_t)t2 * k2;
             count += t2;
         }
-        all = wave_sum(all);
-        count = wave_sum(count);
-        auto share = [&](float pieces) {
-            const float want = ceilf((float)all * 1.00001f / (128.0f * pieces));
-            return want < 1.0f ? 128 : want < 8388607.0f ? 128 * (int)want : 0x3fffff80;
-        };
+        count = total(count);
         if (count < budget) {
+            const float all = total((float)mine) * 1.00001f;          // (64 values: rounded by less than that)
+            auto share = [&](float pieces) {
+                const float want = ceilf(all / (128.0f * pieces));
+                return want < 1.0f ? 128 : want < 8388607.0f ? 128 * (int)want : 0x3fffff80;
+            };
             per = share((float)(budget - count));
             if (a.B <= 64) {                      // mostly it is half a piece a tile less
                 const int tight = share((float)budget - 0.5f * (float)count);
-                if (wave_sum((int64_t)tiles * (keys > tight ? (keys + tight - 1) / tight : 1)) <= budget) per = tight;
+                if (total(tiles * (keys > tight ? (keys + tight - 1) / tight : 1)) <= budget) per = tight;
             }
         }
     }
@@ -123,12 +138,7 @@ __device__ __forceinline__ Place place(const Args &a, int index, int budget, int
     for (int base = 0; base < a.B; base += 64) {
         if (base) tiles_keys(base, tiles, keys);
         const int splits = keys > per ? (keys + per - 1) / per : 1;
-        int ct = tiles, cs = tiles * splits;      // inclusive sums over the 64
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int vt = __shfl_up(ct, d, 64), vs = __shfl_up(cs, d, 64);
-            if (lane >= d) { ct += vt; cs += vs; }
-        }
+        const int ct = running(tiles), cs = running(tiles * splits);
         const int mine = FROM_TILE ? count + ct : slots + cs;
         const uint64_t past = __ballot(index < mine);
         if (past) {
@@ -274,8 +284,10 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
     auto key_of = [&](int step) { return key0 + (step * kWaves + wave) * kStep; };
     auto look_up = [&](int step) {                    // the blocks of 32 steps from `step` on
         const int key = key_of(step + (lane >> 1)) + 16 * (lane & 1);
-        unit = -1;
-        b_scale = b_log = b_inv = 0.0f;
+        unit = -1;                                    // (no such keys: e is minus infinity)
+        b_scale = 1.0f;
+        b_log = -INFINITY;
+        b_inv = 0.0f;
         if (key < key1) {
             const int32_t page = table[key >> a.shift];
             if (page >= 0 && page < a.n_blocks) {
@@ -331,20 +343,17 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
                                     __builtin_amdgcn_perm(0, w1, 0x0c010c00u), __builtin_amdgcn_perm(0, w1, 0x0c030c02u));
                 s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i], s, 0, 0, 0);
             }
-            const int  id = __builtin_amdgcn_readlane(unit, at + u);
-            const bool whole = id >= 0 && key + 16 * u + 16 <= min(sees_least, key1);
-            if (!whole) {
-                const int room = id < 0 ? 0 : min(sees, key1) - (key + 16 * u + 4 * c);
+            if (key + 16 * u + 16 > min(sees_least, key1)) {
+                const int room = min(sees, key1) - (key + 16 * u + 4 * c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[i] = i < room ? s[i] : -INFINITY;
             }
             const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_scale), at + u));
             const float log_v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_log), at + u));
             inv_v[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_inv), at + u));
-            const float f1 = id < 0 ? 1.0f : f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                e[4 * u + i] = fmaf(s[i], f1, log_v);
+                e[4 * u + i] = fmaf(s[i], f, log_v);
                 top = fmaxf(top, e[4 * u + i]);
             }
         }
@@ -461,12 +470,19 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
 //          16 rows) and V's writes (16 groups of keys of two dimensions) over all banks.
 //   loads: codes of the next tile but one are on their way, and their block numbers a tile earlier, while one is computed; two buffers, a barrier a tile.
 //   order: the last tiles of a request, which see the most keys, first.
+constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100;                    // kinds of instructions, for the order of a loop's body
+
+__device__ __forceinline__ float larger(float a, float b, float c)
+{
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 constexpr int kTileLog = 7, kTile = 1 << kTileLog, kKeys = 64;
 
 template <int D>
 struct TileLds {
     static constexpr int kPitch = 2 * D + 16, vPitch = 2 * kKeys + 16;          // bytes
-    static constexpr int k = 0, v = kKeys * kPitch, scales = v + D * vPitch, bytes = scales + 64;   // of one buffer; scales: f4 x 4 blocks of 16 keys
+    static constexpr int k = 0, v = kKeys * kPitch, bytes = v + D * vPitch;     // of one buffer
 };
 
 template <int D>
@@ -505,7 +521,7 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
             for (int i = 0; i < 8; ++i) start += (float)q[s][i];
         }
         start += __shfl_xor(start, 32, 64);
-        start *= -128.0f * 5.9604644775390625e-08f;
+        start *= -128.0f * 5.9604644775390625e-08f;    // what u = code + 128 adds to a score, negated
     }
     const float to_e = a.sm_scale * kLog2e * 16777216.0f;
     f16v o[DB];
@@ -515,31 +531,39 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
         for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
     float M = kNoScore, l = 0.0f;
 
-    // ---- loading: a thread has 16 (or 32) codes of one key of K, and D / 16 of four keys of V
+    // ---- blocks: lane i has the block of 16 keys number i of 16 tiles, its place and its scales
     const int32_t *table = a.table + (int64_t)w.b * a.W;
-    const int kt = tid >> 2, vt = 4 * (lane & 15), vd = VB * (4 * wave + (lane >> 4));
-    auto page_of = [&](int key) {                     // -1: none
-        if (key >= key1) return -1;
-        const int32_t p = table[key >> a.shift];
-        return p >= 0 && p < a.n_blocks ? p : -1;
+    int   page = -1, unit = -1;                       // block number of the table; rows / 16 in the whole cache, -1: no such keys
+    float ks = 0.0f, vs = 0.0f, b_scale, b_log, b_inv;
+    auto read_pages = [&](int tile) {
+        const int key = key0 + tile * kKeys + 16 * lane;
+        page = key < key1 ? table[key >> a.shift] : -1;
     };
-    auto row_of = [&](int page, int key) {            // of the whole cache; without a page its first rows, which are masked
-        return page < 0 ? (int64_t)(key & 15) : (((int64_t)page * a.Hkv + h) << a.shift) + (key & ((1 << a.shift) - 1));
+    auto take_units = [&](int tile) {                 // a tile later: the scales are on their way
+        const int key = key0 + tile * kKeys + 16 * lane;
+        const bool there = page >= 0 && page < a.n_blocks;
+        const int64_t at = there ? (int64_t)page * a.Hkv + h : 0;
+        unit = there ? (int)(at << (a.shift - 4)) + ((key & ((1 << a.shift) - 1)) >> 4) : -1;
+        ks = a.ks[at];
+        vs = a.vs[at];
     };
+    auto take_scales = [&]() {
+        const float v = fmaxf(vs, 2.3283064365386963e-10f);
+        // (never zero: a masked score of minus infinity stays one, and a block of zeros has a weight to be divided out again)
+        b_scale = unit < 0 ? 1.0f : fmaxf(ks * to_e, 1e-37f);
+        b_log = unit < 0 ? -INFINITY : __builtin_amdgcn_logf(v);
+        b_inv = unit < 0 ? 0.0f : __builtin_amdgcn_rcpf(v);
+    };
+    // ---- loading: a thread has 16 (or 32) codes of one key of K, and D / 16 of four keys of V
+    const int kt = tid >> 2, tq = lane & 15, vd = VB * (4 * wave + (lane >> 4));
     u4 kr[KL];
     uint32_t vr[4][VB / 4];
-    f4 sc;
-    int k_page, v_page, s_page;                       // of the tile to be loaded next
-    auto pages = [&](int key) {
-        k_page = page_of(key + kt);
-        v_page = page_of(key + vt);
-        s_page = tid < 4 ? page_of(key + 16 * tid) : -1;
-    };
-    auto fetch = [&](int key) {
-        const int8_t *kp = a.kq + row_of(k_page, key + kt) * D + 16 * (tid & 3);
+    auto fetch = [&](int tile) {                      // (no such keys: the cache's first rows, masked)
+        const int at = 4 * (tile & 15);
+        const int8_t *kp = a.kq + (int64_t)max(__builtin_amdgcn_readlane(unit, at + wave), 0) * (16 * D) + (uint32_t)((kt & 15) * D + 16 * (tid & 3));
 #pragma unroll
         for (int i = 0; i < KL; ++i) kr[i] = *reinterpret_cast<const u4 *>(kp + 64 * i);
-        const int8_t *vp = a.vq + row_of(v_page, key + vt) * D + vd;
+        const int8_t *vp = a.vq + (int64_t)max(__shfl(unit, at + (tq >> 2), 64), 0) * (16 * D) + (uint32_t)((4 * tq & 15) * D + vd);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (VB == 8) {
@@ -548,14 +572,6 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
                 vr[i][1] = v[1];
             } else {
                 vr[i][0] = *reinterpret_cast<const uint32_t *>(vp + i * D);
-            }
-        }
-        if (tid < 4) {
-            sc = f4{1.0f, 0.0f, 0.0f, 0.0f};          // no page: a factor that keeps minus infinity, no weight
-            if (s_page >= 0) {
-                const int64_t at = (int64_t)s_page * a.Hkv + h;
-                const float v = fmaxf(a.vs[at], 2.3283064365386963e-10f);
-                sc = f4{fmaxf(a.ks[at] * to_e, 1e-37f), __builtin_amdgcn_logf(v), __builtin_amdgcn_rcpf(v), 1.0f};
             }
         }
     };
@@ -570,8 +586,7 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
                     u4{__builtin_amdgcn_perm(0, w0, 0x0c010c00u), __builtin_amdgcn_perm(0, w0, 0x0c030c02u),
                        __builtin_amdgcn_perm(0, w1, 0x0c010c00u), __builtin_amdgcn_perm(0, w1, 0x0c030c02u)};
             }
-        // keys vt .. vt + 3: step u = vt / 16 of 16 keys, half-wave (vt / 4) & 1, its first or second four
-        const int tq = lane & 15;
+        // keys 4 tq .. 4 tq + 3: step u = tq / 4 of 16 keys, half-wave tq & 1, its first or second four
         unsigned char *vp = buf + L::v + vd * L::vPitch + 16 * (2 * (tq >> 2) + (tq & 1)) + 8 * ((tq >> 1) & 1);
 #pragma unroll
         for (int j = 0; j < VB / 4; ++j) {
@@ -583,38 +598,53 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
             ATOM_STAGE(3);
 #undef ATOM_STAGE
         }
-        if (tid < 4) *reinterpret_cast<f4 *>(buf + L::scales + 16 * tid) = sc;
     };
-    auto compute = [&](const unsigned char *buf, int key) {
+    auto compute = [&](const unsigned char *buf, int tile) __attribute__((always_inline)) {
+        const int key = key0 + tile * kKeys;
+        // scores: two chains of products, operands read six ahead of their use
         f16v s[2];
         const unsigned char *kp = buf + L::k + n * L::kPitch + 16 * hh;
+        h8 kf[2 * KS];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int i = 0; i < 2 * KS; ++i) kf[i] = *reinterpret_cast<const h8 *>(kp + 32 * (i & 1) * L::kPitch + 32 * (i >> 1));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = start;
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < KS; ++i)
-                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(kp + 32 * t * L::kPitch + 32 * i), q[i], s[t], 0, 0, 0);
+            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], q[i >> 1], s[i & 1], 0, 0, 0);
+        constexpr int kAhead = 6;
+        __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
         }
-        f4 c[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) c[b] = *reinterpret_cast<const f4 *>(buf + L::scales + 16 * b);
-        const bool there = c[0][3] * c[1][3] * c[2][3] * c[3][3] != 0.0f;
-        if (key + kKeys > least || !there) {          // (the same in all lanes)
+        __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
+        __builtin_amdgcn_sched_barrier(0);
+
+        if (key + kKeys > least) {                    // (the same in all lanes)
             const int room = min(sees, key1) - (key + 4 * hh);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (32 * t + 8 * (i >> 2) + (i & 3) >= room || c[2 * t + (i >> 3)][3] == 0.0f) s[t][i] = -INFINITY;
+                    if (32 * t + 8 * (i >> 2) + (i & 3) >= room) s[t][i] = -INFINITY;
         }
-        float top = -INFINITY;
+        const int at = 4 * (tile & 15);
+        auto of_block = [&](float v, int b) {
+            return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), at + b));
+        };
+        // e = s * factor + shift, the offset of the codes in the shift
+        float factor[4], shift[4], top = -INFINITY;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            float m = s[b >> 1][8 * (b & 1)];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) m = fmaxf(m, s[b >> 1][8 * (b & 1) + i]);
-            top = fmaxf(top, fmaf(m, c[b][0], c[b][1]));
+            const f16v &x = s[b >> 1];
+            const int  i = 8 * (b & 1);
+            const float m = larger(larger(larger(x[i], x[i + 1], x[i + 2]), x[i + 3], x[i + 4]), x[i + 5], larger(x[i + 6], x[i + 7], x[i + 7]));
+            factor[b] = of_block(b_scale, b);
+            shift[b] = fmaf(start, factor[b], of_block(b_log, b));
+            top = fmaxf(top, fmaf(m, factor[b], shift[b]));
         }
         if (__ballot(top > M + 8.0f)) {               // rare after the first tiles
             const float to = fmaxf(M, fmaxf(top, __shfl_xor(top, 32, 64)));
@@ -624,42 +654,59 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
 #pragma unroll
             for (int i = 0; i < DB; ++i) o[i] *= down;
         }
-        h8 p[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const float shift = c[b][1] - M;
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[b >> 1][8 * (b & 1) + i], c[b][0], shift));
-                sum += e;
-                p[b][i] = (_Float16)e;
-            }
-            l = fmaf(sum, c[b][2], l);
-        }
         const unsigned char *vp = buf + L::v + n * L::vPitch + 16 * hh;
+        h8 vf[4][DB];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int i = 0; i < DB; ++i)
-                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(vp + 32 * i * L::vPitch + 32 * u), p[u], o[i], 0, 0, 0);
+            for (int i = 0; i < DB; ++i) vf[u][i] = *reinterpret_cast<const h8 *>(vp + 32 * i * L::vPitch + 32 * u);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const float to_p = shift[b] - M;
+            float sum = 0.0f;
+            h8 p;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[b >> 1][8 * (b & 1) + i], factor[b], to_p));
+                sum += e;
+                p[i] = (_Float16)e;
+            }
+            l = fmaf(sum, of_block(b_inv, b), l);
+#pragma unroll
+            for (int i = 0; i < DB; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[b][i], p, o[i], 0, 0, 0);
+        }
+        // the weights of a block between the products of the one before
+        __builtin_amdgcn_sched_group_barrier(kDsRead, DB, 1);
+        __builtin_amdgcn_sched_group_barrier(kValu, 28, 1);
+#pragma unroll
+        for (int u = 0; u < 3; ++u)
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(kValu, 28 / DB, 1);
+            }
+        __builtin_amdgcn_sched_group_barrier(kMfma, DB, 1);
+        __builtin_amdgcn_sched_barrier(0);
     };
 
     if (key0 < key1) {                                // (the same in all threads)
-        pages(key0);
-        fetch(key0);
-        pages(key0 + kKeys);
+        const int tiles = (key1 - key0 + kKeys - 1) / kKeys;
+        read_pages(0);
+        take_units(0);
+        fetch(0);
         stage(lds);
-        fetch(key0 + kKeys);
-        pages(key0 + 2 * kKeys);
+        if (tiles > 1) fetch(1);
         __syncthreads();
         int at = 0;
-        for (int key = key0; key < key1; key += kKeys, at ^= L::bytes) {
-            if (key < wave1) compute(lds + at, key);
-            if (key + kKeys < key1) {
-                stage(lds + (at ^ L::bytes));
-                fetch(key + 2 * kKeys);
-                pages(key + 3 * kKeys);
+        for (int t = 0; t < tiles; ++t, at ^= L::bytes) {
+            if ((t & 15) == 0) take_scales();
+            if (key0 + t * kKeys < wave1) compute(lds + at, t);
+            if (t + 1 < tiles) stage(lds + (at ^ L::bytes));
+            if (t + 2 < tiles) {
+                if (((t + 2) & 15) == 0) take_units(t + 2);
+                fetch(t + 2);
+                if (((t + 3) & 15) == 0) read_pages(t + 3);
             }
             __syncthreads();
         }
