@@ -468,9 +468,11 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
 //          four times the work: 256 vector instructions a tile).  K as [key][D]; V as [D][key], its keys in the order of the scores' rows, so that
 //          an operand is one 16-byte read: byte selection makes the halves and transposes.  Rows are padded by 16 bytes, which spreads the reads (16 lanes,
 //          16 rows) and V's writes (16 groups of keys of two dimensions) over all banks.
+//   order of work: 32 keys at a time; the scores of the next 32 are multiplied while the vector unit makes weights of the last ones and halves of the next
+//          tile's codes, so that the matrix unit and the vector unit of a lone wavefront work at the same time.  The tiles of K lie 32 keys behind those of V for that:
+//          the scores of keys 32 .. 95 of a tile of V are multiplied with it.
 //   loads: codes of the next tile but one are on their way, and their block numbers a tile earlier, while one is computed; two buffers, a barrier a tile.
 //   order: the last tiles of a request, which see the most keys, first.
-constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100;                    // kinds of instructions, for the order of a loop's body
 
 __device__ __forceinline__ float larger(float a, float b, float c)
 {
@@ -531,19 +533,25 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
         for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
     float M = kNoScore, l = 0.0f;
 
-    // ---- blocks: lane i has the block of 16 keys number i of 16 tiles, its place and its scales
+    // ---- blocks: lane i has the block of 16 keys number i of 16 tiles, its place and its scales; another register the blocks of K's tiles
     const int32_t *table = a.table + (int64_t)w.b * a.W;
-    int   page = -1, unit = -1;                       // block number of the table; rows / 16 in the whole cache, -1: no such keys
+    int   page = -1, page_k = -1, unit = -1, unit_k = -1;      // block numbers of the table; rows / 16 in the whole cache, -1: no such keys
     float ks = 0.0f, vs = 0.0f, b_scale, b_log, b_inv;
+    auto key_of = [&](int tile) { return key0 + tile * kKeys + 16 * lane; };
+    auto exists = [&](int p) { return p >= 0 && p < a.n_blocks; };
+    auto place_of = [&](int p, int key) {
+        return exists(p) ? (int)(((int64_t)p * a.Hkv + h) << (a.shift - 4)) + ((key & ((1 << a.shift) - 1)) >> 4) : -1;
+    };
     auto read_pages = [&](int tile) {
-        const int key = key0 + tile * kKeys + 16 * lane;
+        const int key = key_of(tile);
         page = key < key1 ? table[key >> a.shift] : -1;
+        page_k = key + 32 < key1 ? table[(key + 32) >> a.shift] : -1;
     };
     auto take_units = [&](int tile) {                 // a tile later: the scales are on their way
-        const int key = key0 + tile * kKeys + 16 * lane;
-        const bool there = page >= 0 && page < a.n_blocks;
-        const int64_t at = there ? (int64_t)page * a.Hkv + h : 0;
-        unit = there ? (int)(at << (a.shift - 4)) + ((key & ((1 << a.shift) - 1)) >> 4) : -1;
+        const int key = key_of(tile);
+        unit = place_of(page, key);
+        unit_k = place_of(page_k, key + 32);
+        const int64_t at = exists(page) ? (int64_t)page * a.Hkv + h : 0;
         ks = a.ks[at];
         vs = a.vs[at];
     };
@@ -558,11 +566,12 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
     const int kt = tid >> 2, tq = lane & 15, vd = VB * (4 * wave + (lane >> 4));
     u4 kr[KL];
     uint32_t vr[4][VB / 4];
-    auto fetch = [&](int tile) {                      // (no such keys: the cache's first rows, masked)
-        const int at = 4 * (tile & 15);
-        const int8_t *kp = a.kq + (int64_t)max(__builtin_amdgcn_readlane(unit, at + wave), 0) * (16 * D) + (uint32_t)((kt & 15) * D + 16 * (tid & 3));
+    auto fetch_k = [&](int unit_, int at, u4 (&to)[KL]) {       // (no such keys: the cache's first rows, masked)
+        const int8_t *kp = a.kq + (int64_t)max(__builtin_amdgcn_readlane(unit_, at + wave), 0) * (16 * D) + (uint32_t)((kt & 15) * D + 16 * (tid & 3));
 #pragma unroll
-        for (int i = 0; i < KL; ++i) kr[i] = *reinterpret_cast<const u4 *>(kp + 64 * i);
+        for (int i = 0; i < KL; ++i) to[i] = *reinterpret_cast<const u4 *>(kp + 64 * i);
+    };
+    auto fetch_v = [&](int at) {
         const int8_t *vp = a.vq + (int64_t)max(__shfl(unit, at + (tq >> 2), 64), 0) * (16 * D) + (uint32_t)((4 * tq & 15) * D + vd);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -575,75 +584,93 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
             }
         }
     };
-    auto stage = [&](unsigned char *buf) {
-        unsigned char *kp = buf + L::k + kt * L::kPitch + 32 * (tid & 3);
+    constexpr int kPieces = 2 * KL, vPieces = VB;      // of a thread's staging
+    auto stage_k = [&](unsigned char *buf, const u4 (&kr)[KL], int piece) __attribute__((always_inline)) {
+        const uint32_t w0 = flip(kr[piece >> 1][2 * (piece & 1)]), w1 = flip(kr[piece >> 1][2 * (piece & 1) + 1]);
+        *reinterpret_cast<u4 *>(buf + L::k + kt * L::kPitch + 32 * (tid & 3) + 128 * (piece >> 1) + 16 * (piece & 1)) =
+            u4{__builtin_amdgcn_perm(0, w0, 0x0c010c00u), __builtin_amdgcn_perm(0, w0, 0x0c030c02u),
+               __builtin_amdgcn_perm(0, w1, 0x0c010c00u), __builtin_amdgcn_perm(0, w1, 0x0c030c02u)};
+    };
+    auto stage_v = [&](unsigned char *buf, int piece) __attribute__((always_inline)) {
+        // one dimension of keys 4 tq .. 4 tq + 3: step u = tq / 4 of 16 keys, half-wave tq & 1, its first or second four
+        const int j = piece >> 2;
+        const uint32_t sel = 0x0c040c00u + (piece & 3) * 0x00010001u;
+        if ((piece & 3) == 0)
 #pragma unroll
-        for (int i = 0; i < KL; ++i)
+            for (int i = 0; i < 4; ++i) vr[i][j] = flip(vr[i][j]);
+        *reinterpret_cast<u2 *>(buf + L::v + (vd + piece) * L::vPitch + 16 * (2 * (tq >> 2) + (tq & 1)) + 8 * ((tq >> 1) & 1)) =
+            u2{centred(__builtin_amdgcn_perm(vr[1][j], vr[0][j], sel)), centred(__builtin_amdgcn_perm(vr[3][j], vr[2][j], sel))};
+    };
+    // ---- computing, 32 keys: e = score * factor + shift (the offset of the codes in the shift), the weights to be divided by 1 / inv
+    float factor[2], shift[2], inv[2];
+    // Half a tile: the scores of the next 32 keys (K's rows 32 half ..) and between their products the weights of the last ones, `now`; then the weights'
+    // products with V, and between them `pieces` of staging.  Operands are read from LDS three products ahead.  The order is the one written.
+    auto half_tile = [&](const unsigned char *buf, int half, const f16v &now, f16v &then, auto stage, int pieces) __attribute__((always_inline)) {
+        constexpr int kAhead = 3, per = 16 / KS;
+        const unsigned char *kp = buf + L::k + (32 * half + n) * L::kPitch + 16 * hh;
+        const unsigned char *vp = buf + L::v + n * L::vPitch + 16 * hh + 64 * half;
+        h8 f[KS + 2 * DB];
+        auto read = [&](int i) __attribute__((always_inline)) {
+            f[i] = i < KS ? *reinterpret_cast<const h8 *>(kp + 32 * i)
+                          : *reinterpret_cast<const h8 *>(vp + 32 * ((i - KS) % DB) * L::vPitch + 32 * ((i - KS) / DB));
+        };
+        h8 p[2];
+        float sum[2] = {0.0f, 0.0f};
+        const float to_p[2] = {shift[0] - M, shift[1] - M};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t w0 = flip(kr[i][2 * j]), w1 = flip(kr[i][2 * j + 1]);
-                *reinterpret_cast<u4 *>(kp + 128 * i + 16 * j) =
-                    u4{__builtin_amdgcn_perm(0, w0, 0x0c010c00u), __builtin_amdgcn_perm(0, w0, 0x0c030c02u),
-                       __builtin_amdgcn_perm(0, w1, 0x0c010c00u), __builtin_amdgcn_perm(0, w1, 0x0c030c02u)};
+        for (int i = 0; i < 16; ++i) then[i] = 0.0f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read(i);
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            read(i + kAhead);
+            then = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i], q[i], then, 0, 0, 0);
+#pragma unroll
+            for (int k = per * i; k < per * (i + 1); ++k) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(now[k], factor[k >> 3], to_p[k >> 3]));
+                sum[k >> 3] += e;
+                p[k >> 3][k & 7] = (_Float16)e;
             }
-        // keys 4 tq .. 4 tq + 3: step u = tq / 4 of 16 keys, half-wave tq & 1, its first or second four
-        unsigned char *vp = buf + L::v + vd * L::vPitch + 16 * (2 * (tq >> 2) + (tq & 1)) + 8 * ((tq >> 1) & 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l = fmaf(sum[0], inv[0], l);
+        l = fmaf(sum[1], inv[1], l);
 #pragma unroll
-        for (int j = 0; j < VB / 4; ++j) {
-            const uint32_t w0 = flip(vr[0][j]), w1 = flip(vr[1][j]), w2 = flip(vr[2][j]), w3 = flip(vr[3][j]);
-#define ATOM_STAGE(e) *reinterpret_cast<u2 *>(vp + (4 * j + (e)) * L::vPitch) = u2{centred(pair_of<e>(w0, w1)), centred(pair_of<e>(w2, w3))}
-            ATOM_STAGE(0);
-            ATOM_STAGE(1);
-            ATOM_STAGE(2);
-            ATOM_STAGE(3);
-#undef ATOM_STAGE
+        for (int i = 0; i < 2 * DB; ++i) {
+            if (i + kAhead < 2 * DB) read(KS + i + kAhead);
+            o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[KS + i], p[i / DB], o[i % DB], 0, 0, 0);
+#pragma unroll
+            for (int k = pieces * i / (2 * DB); k < pieces * (i + 1) / (2 * DB); ++k) stage(k);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto compute = [&](const unsigned char *buf, int tile) __attribute__((always_inline)) {
-        const int key = key0 + tile * kKeys;
-        // scores: two chains of products, operands read six ahead of their use
-        f16v s[2];
-        const unsigned char *kp = buf + L::k + n * L::kPitch + 16 * hh;
-        h8 kf[2 * KS];
+    auto first_scores = [&](const unsigned char *buf, f16v &s) {
 #pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) kf[i] = *reinterpret_cast<const h8 *>(kp + 32 * (i & 1) * L::kPitch + 32 * (i >> 1));
+        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], q[i >> 1], s[i & 1], 0, 0, 0);
-        constexpr int kAhead = 6;
-        __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
-#pragma unroll
-        for (int i = 0; i < 2 * KS - kAhead; ++i) {
-            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
-        __builtin_amdgcn_sched_barrier(0);
-
-        if (key + kKeys > least) {                    // (the same in all lanes)
+        for (int i = 0; i < KS; ++i)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(buf + L::k + (32 + n) * L::kPitch + 16 * hh + 32 * i), q[i], s, 0, 0, 0);
+    };
+    // the largest e of 32 keys from `key` on (block `at` of the lanes' and the one behind it)
+    auto look = [&](int key, int at, f16v &s) __attribute__((always_inline)) {
+        if (key + 32 > least) {                       // (the same in all lanes)
             const int room = min(sees, key1) - (key + 4 * hh);
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (32 * t + 8 * (i >> 2) + (i & 3) >= room) s[t][i] = -INFINITY;
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + (i & 3) >= room) s[i] = -INFINITY;
         }
-        const int at = 4 * (tile & 15);
         auto of_block = [&](float v, int b) {
             return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), at + b));
         };
-        // e = s * factor + shift, the offset of the codes in the shift
-        float factor[4], shift[4], top = -INFINITY;
+        float top = -INFINITY;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const f16v &x = s[b >> 1];
-            const int  i = 8 * (b & 1);
-            const float m = larger(larger(larger(x[i], x[i + 1], x[i + 2]), x[i + 3], x[i + 4]), x[i + 5], larger(x[i + 6], x[i + 7], x[i + 7]));
+        for (int b = 0; b < 2; ++b) {
+            const int i = 8 * b;
+            const float m = larger(larger(larger(s[i], s[i + 1], s[i + 2]), s[i + 3], s[i + 4]), s[i + 5], larger(s[i + 6], s[i + 7], s[i + 7]));
             factor[b] = of_block(b_scale, b);
             shift[b] = fmaf(start, factor[b], of_block(b_log, b));
+            inv[b] = of_block(b_inv, b);
             top = fmaxf(top, fmaf(m, factor[b], shift[b]));
         }
         if (__ballot(top > M + 8.0f)) {               // rare after the first tiles
@@ -654,60 +681,57 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
 #pragma unroll
             for (int i = 0; i < DB; ++i) o[i] *= down;
         }
-        const unsigned char *vp = buf + L::v + n * L::vPitch + 16 * hh;
-        h8 vf[4][DB];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int i = 0; i < DB; ++i) vf[u][i] = *reinterpret_cast<const h8 *>(vp + 32 * i * L::vPitch + 32 * u);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const float to_p = shift[b] - M;
-            float sum = 0.0f;
-            h8 p;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[b >> 1][8 * (b & 1) + i], factor[b], to_p));
-                sum += e;
-                p[i] = (_Float16)e;
-            }
-            l = fmaf(sum, of_block(b_inv, b), l);
-#pragma unroll
-            for (int i = 0; i < DB; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[b][i], p, o[i], 0, 0, 0);
-        }
-        // the weights of a block between the products of the one before
-        __builtin_amdgcn_sched_group_barrier(kDsRead, DB, 1);
-        __builtin_amdgcn_sched_group_barrier(kValu, 28, 1);
-#pragma unroll
-        for (int u = 0; u < 3; ++u)
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(kValu, 28 / DB, 1);
-            }
-        __builtin_amdgcn_sched_group_barrier(kMfma, DB, 1);
-        __builtin_amdgcn_sched_barrier(0);
     };
-
     if (key0 < key1) {                                // (the same in all threads)
         const int tiles = (key1 - key0 + kKeys - 1) / kKeys;
+        u4 kr0[KL];
         read_pages(0);
+        const int key_first = key0 - 32 + 16 * lane;  // the first 32 keys: as the last ones of a tile of K
+        const int page_first = key_first >= key0 && key_first < key1 ? table[key_first >> a.shift] : -1;
         take_units(0);
-        fetch(0);
-        stage(lds);
-        if (tiles > 1) fetch(1);
+        fetch_k(place_of(page_first, key_first), 0, kr0);
+        fetch_k(unit_k, 0, kr);
+        fetch_v(0);
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) stage_k(lds + L::bytes, kr0, k);
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) stage_k(lds, kr, k);
+#pragma unroll
+        for (int k = 0; k < vPieces; ++k) stage_v(lds, k);
+        fetch_k(unit_k, 4, kr);
+        fetch_v(4);
+        take_scales();
+        __syncthreads();
+        f16v x, y;
+        first_scores(lds + L::bytes, x);
+        look(key0, 0, x);
         __syncthreads();
         int at = 0;
         for (int t = 0; t < tiles; ++t, at ^= L::bytes) {
-            if ((t & 15) == 0) take_scales();
-            if (key0 + t * kKeys < wave1) compute(lds + at, t);
-            if (t + 1 < tiles) stage(lds + (at ^ L::bytes));
-            if (t + 2 < tiles) {
-                if (((t + 2) & 15) == 0) take_units(t + 2);
-                fetch(t + 2);
-                if (((t + 3) & 15) == 0) read_pages(t + 3);
+            unsigned char *here = lds + at, *next = lds + (at ^ L::bytes);
+            const int key = key0 + t * kKeys, block = 4 * (t & 15), ahead = 4 * ((t + 2) & 15);
+            auto next_k = [&](int k) __attribute__((always_inline)) { stage_k(next, kr, k); };
+            auto next_v = [&](int k) __attribute__((always_inline)) { stage_v(next, k); };
+            if (key < wave1) {                        // (the same in all lanes)
+                half_tile(here, 0, x, y, next_k, kPieces);
+                look(key + 32, block + 2, y);
+            } else {
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) next_k(k);
             }
+            if (ahead == 0) take_units(t + 2);
+            fetch_k(unit_k, ahead, kr);
+            if (key + 32 < wave1) {
+                half_tile(here, 1, y, x, next_v, vPieces);
+                if (block == 60) take_scales();
+                look(key + 64, (block + 4) & 63, x);
+            } else {
+#pragma unroll
+                for (int k = 0; k < vPieces; ++k) next_v(k);
+                if (block == 60) take_scales();
+            }
+            fetch_v(ahead);
+            if (ahead == 60) read_pages(t + 3);
             __syncthreads();
         }
     }
