@@ -26,6 +26,7 @@ constexpr float kNoScore = -1e30f;                // the running maximum before 
 struct Args {
     const __half *q; int T; int64_t ldq;
     int B, H, Hkv, group;                         // group = H / Hkv query heads to a cache head
+    uint32_t div_mul; int div_shift;              // n / group = n * div_mul >> div_shift for n below 2^31
     int max_new;
     const int32_t *token_start, *seq_len, *table;
     int W, shift;                                 // table columns; block_tokens = 1 << shift
@@ -38,6 +39,8 @@ struct Args {
     int part_rows;                                // rows of a split's record
     int budget;                                   // workgroups for each cache head that tiles may be cut into (0: none is cut)
 };
+
+__device__ __forceinline__ int by_group(const Args &a, int n) { return (int)(((uint64_t)(uint32_t)n * a.div_mul) >> a.div_shift); }
 
 // A request's share of the call.
 struct Request {
@@ -65,7 +68,7 @@ __device__ __forceinline__ Request request(const Args &a, int b)
 // fewer than the workgroups that a call is to have for each cache head (budget), their keys are cut into pieces of about one size in the whole call:
 // sequences of any lengths keep the card evenly busy, and the pieces of a tile meet in the merge kernel.  Every wavefront
 // finds its place from the lengths by itself, 64 requests at a time: for as many it is one read, which it needs anyway.
-struct Place { int b, tile, split, splits, keys_per, first_slot; bool found; };
+struct Place { int b, tile, split, splits, keys_per, first_slot; Request r; bool found; };
 
 // Sum over the lanes up to this one, on the vector unit (lane exchanges through LDS cost a microsecond in front of the first load).
 template <class V>
@@ -93,11 +96,12 @@ template <int LOG, bool FROM_TILE>
 __device__ __forceinline__ Place place(const Args &a, int index, int budget, int rows_min, int rows_max)
 {
     const int lane = threadIdx.x & 63;
+    Request r = {0, 0, 0, 0};
     auto tiles_keys = [&](int base, int &tiles, int &keys) {
         tiles = 0;
         keys = 0;
         if (base + lane < a.B) {
-            const Request r = request(a, base + lane);
+            r = request(a, base + lane);
             const int64_t rows = (int64_t)r.n * a.group;
             if (rows >= rows_min && rows <= rows_max) {
                 tiles = (int)((rows + (1 << LOG) - 1) >> LOG);
@@ -110,7 +114,7 @@ __device__ __forceinline__ Place place(const Args &a, int index, int budget, int
     int tiles, keys;
     tiles_keys(0, tiles, keys);
     int per = 0x3fffff80;                         // keys of a piece at most, a multiple of 128: one step of 32 for each of four wavefronts
-    if (budget) {
+    if (budget) {                                 // (with more than 64 requests r is read again below)
         // sum over tiles of ceil(keys / per) is below tiles + all / per
         int64_t mine = (int64_t)tiles * keys;
         int     count = tiles;
@@ -136,7 +140,7 @@ __device__ __forceinline__ Place place(const Args &a, int index, int budget, int
     }
     int count = 0, slots = 0;                     // tiles and pieces of the requests before
     for (int base = 0; base < a.B; base += 64) {
-        if (base) tiles_keys(base, tiles, keys);
+        if (base || (budget && a.B > 64)) tiles_keys(base, tiles, keys);
         const int splits = keys > per ? (keys + per - 1) / per : 1;
         const int ct = running(tiles), cs = running(tiles * splits);
         const int mine = FROM_TILE ? count + ct : slots + cs;
@@ -145,6 +149,8 @@ __device__ __forceinline__ Place place(const Args &a, int index, int budget, int
             const int l = __builtin_ctzll(past);
             p.found = true;
             p.b = base + l;
+            p.r = Request{__builtin_amdgcn_readlane(r.start, l), __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.before, l),
+                          __builtin_amdgcn_readlane(r.keys, l)};
             p.splits = __builtin_amdgcn_readlane(splits, l);
             const int t0 = count + __builtin_amdgcn_readlane(ct - tiles, l);
             const int s0 = slots + __builtin_amdgcn_readlane(cs - tiles * splits, l);
@@ -185,6 +191,16 @@ __device__ __forceinline__ uint32_t centred(uint32_t pair)
     const h2 v = __builtin_elementwise_fma(__builtin_bit_cast(h2, pair), h2{(_Float16)32768.0f, (_Float16)32768.0f},
                                            h2{(_Float16)-0.25f, (_Float16)-0.25f});
     return __builtin_bit_cast(uint32_t, v);
+}
+
+// v + the sum of eight halves
+__device__ __forceinline__ float add8(const h8 &x, float v)
+{
+    const u4 w = __builtin_bit_cast(u4, x);
+    const h2 one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, (uint32_t)w[i]), one, v, false);
+    return v;
 }
 
 __device__ __forceinline__ h8 halves(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
@@ -242,38 +258,25 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
     const int h = blockIdx.x % a.Hkv;
     const Place w = place<kRowsLog, false>(a, blockIdx.x / a.Hkv, a.budget, rows_min, rows_max);
     if (!w.found) return;
-    const Request r = request(a, w.b);
+    const Request r = w.r;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, c = lane >> 4;           // query row (or key) of the tile, chunk
     const int rows = min(kTileRows, r.n * a.group - w.tile * kTileRows);
     const int row = w.tile * kTileRows + min(m, rows - 1);
-    const int token = row / a.group, head = h * a.group + row - token * a.group;
+    const int token = by_group(a, row), head = h * a.group + row - token * a.group;
     // keys that this lane's row sees, and the fewest and the most of the tile
     const int sees = min(max(r.before + token + 1, 0), r.keys);
-    const int sees_least = min(max(r.before + w.tile * kTileRows / a.group + 1, 0), r.keys);
-    const int sees_most = min(max(r.before + (w.tile * kTileRows + rows - 1) / a.group + 1, 0), r.keys);
+    const int sees_least = min(max(r.before + by_group(a, w.tile * kTileRows) + 1, 0), r.keys);
+    const int sees_most = min(max(r.before + by_group(a, w.tile * kTileRows + rows - 1) + 1, 0), r.keys);
     const int key0 = w.split * w.keys_per, key1 = min(sees_most, key0 + w.keys_per);     // (a split below 2^31: keys_per is at most keys)
 
     h8 q[KS];
-    float qsum = 0.0f;
-    {
-        const __half *qp = a.q + (int64_t)(r.start + token) * a.ldq + (int64_t)head * D + c * KB;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const u4 v = *reinterpret_cast<const u4 *>(qp + 8 * s);
-            q[s] = __builtin_bit_cast(h8, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) qsum += (float)q[s][i];
-        }
-        qsum = sum_of_chunks(qsum);
-    }
-    const float start = qsum * (-128.0f * 5.9604644775390625e-08f);
     const float to_e = a.sm_scale * kLog2e * 16777216.0f;
 
     f4 acc[VB];
 #pragma unroll
     for (int e = 0; e < VB; ++e) acc[e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    float M = kNoScore, l = 0.0f;
+    float M = kNoScore, l = 0.0f, start = 0.0f;       // start: what u = code + 128 adds to a score, negated
 
     u4 kr[2][KB / 16];
     uint32_t vr[8][VB / 4];
@@ -282,24 +285,22 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
     float b_scale = 0.0f, b_log = 0.0f, b_inv = 0.0f;
     const int32_t *table = a.table + (int64_t)w.b * a.W;
     auto key_of = [&](int step) { return key0 + (step * kWaves + wave) * kStep; };
-    auto look_up = [&](int step) {                    // the blocks of 32 steps from `step` on
-        const int key = key_of(step + (lane >> 1)) + 16 * (lane & 1);
-        unit = -1;                                    // (no such keys: e is minus infinity)
-        b_scale = 1.0f;
-        b_log = -INFINITY;
-        b_inv = 0.0f;
-        if (key < key1) {
-            const int32_t page = table[key >> a.shift];
-            if (page >= 0 && page < a.n_blocks) {
-                const int64_t at = (int64_t)page * a.Hkv + h;
-                unit = (int)(at << (a.shift - 4)) + ((key & ((1 << a.shift) - 1)) >> 4);
-                // (never zero: a masked score of minus infinity stays one, and a block of zeros has a weight to be divided out again)
-                b_scale = fmaxf(a.ks[at] * to_e, 1e-37f);
-                const float v = fmaxf(a.vs[at], 2.3283064365386963e-10f);
-                b_log = __builtin_amdgcn_logf(v);
-                b_inv = __builtin_amdgcn_rcpf(v);
-            }
-        }
+    auto block_key = [&](int step) { return key_of(step + (lane >> 1)) + 16 * (lane & 1); };
+    auto page_of = [&](int step) { const int key = block_key(step); return key < key1 ? table[key >> a.shift] : -1; };
+    auto look_up = [&](int step, int page) {          // the blocks of 32 steps from `step` on; their scales are on the way
+        const int  key = block_key(step);
+        const bool there = page >= 0 && page < a.n_blocks;
+        const int64_t at = there ? (int64_t)page * a.Hkv + h : 0;
+        unit = there ? (int)(at << (a.shift - 4)) + ((key & ((1 << a.shift) - 1)) >> 4) : -1;
+        b_scale = a.ks[at];
+        b_log = a.vs[at];
+    };
+    auto take_scales = [&]() {                        // (no such keys: e is minus infinity)
+        const float v = fmaxf(b_log, 2.3283064365386963e-10f);
+        // (never zero: a masked score of minus infinity stays one, and a block of zeros has a weight to be divided out again)
+        b_scale = unit < 0 ? 1.0f : fmaxf(b_scale * to_e, 1e-37f);
+        b_log = unit < 0 ? -INFINITY : __builtin_amdgcn_logf(v);
+        b_inv = unit < 0 ? 0.0f : __builtin_amdgcn_rcpf(v);
     };
     // (blocks past the end or without a page: the cache's first rows, masked)
     auto block_at = [&](int step, int u) { return (int64_t)max(__builtin_amdgcn_readlane(unit, 2 * (step & 31) + u), 0) * (16 * D); };
@@ -398,18 +399,27 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
 
     if (key_of(0) < key1) {                           // (the same in all lanes)
         const int steps = (key1 - key_of(0) + kWaves * kStep - 1) / (kWaves * kStep);
-        look_up(0);
+        const int page = page_of(0);
+        const __half *qp = a.q + (int64_t)(r.start + token) * a.ldq + (int64_t)head * D + c * KB;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = __builtin_bit_cast(h8, *reinterpret_cast<const u4 *>(qp + 8 * s));
+        look_up(0, page);
         fetch_k(0);
         fetch_v(0);
+        take_scales();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) start = add8(q[s], start);
+        start = sum_of_chunks(start) * (-128.0f * 5.9604644775390625e-08f);
         for (int step = 0; step < steps; ++step) {
             const bool more = step + 1 < steps;
             compute(step, more);
             if (more) {
                 if (((step + 1) & 31) == 0) {
-                    look_up(step + 1);
+                    look_up(step + 1, page_of(step + 1));
                     fetch_k(step + 1);
                 }
                 fetch_v(step + 1);
+                if (((step + 1) & 31) == 0) take_scales();
             }
         }
     }
@@ -443,7 +453,7 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
         }
         if (whole) {
             const float f = sum > 0.0f ? 512.0f / sum : 0.0f;         // (values were 2^-9 of the codes)
-            const int rw = w.tile * kTileRows + rr, t = rw / a.group;
+            const int rw = w.tile * kTileRows + rr, t = by_group(a, rw);
             __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + rw - t * a.group) * D + d;
             const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
             *reinterpret_cast<u2 *>(to) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
@@ -499,32 +509,26 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
     const int h = blockIdx.x % a.Hkv;
     const Place w = place<kTileLog, false>(a, blockIdx.x / a.Hkv, a.budget, rows_min, rows_max);
     if (!w.found) return;
-    const Request r = request(a, w.b);
+    const Request r = w.r;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, hh = lane >> 5;
     const int all = r.n * a.group;
     const int tile = (all + kTile - 1) / kTile - 1 - w.tile;
     const int row0 = tile * kTile + wave * 32, rows = min(32, all - row0);      // of this wavefront; none: rows <= 0
     const int row = min(row0 + n, all - 1);
-    const int token = row / a.group, head = h * a.group + row - token * a.group;
-    auto keys_of = [&](int row_) { return min(max(r.before + min(row_, all - 1) / a.group + 1, 0), r.keys); };
+    const int token = by_group(a, row), head = h * a.group + row - token * a.group;
+    auto keys_of = [&](int row_) { return min(max(r.before + by_group(a, min(row_, all - 1)) + 1, 0), r.keys); };
     const int sees = keys_of(row), key0 = w.split * w.keys_per;
     const int key1 = min(keys_of(tile * kTile + kTile - 1), key0 + w.keys_per);           // of the workgroup
     const int wave1 = rows > 0 ? min(keys_of(row0 + rows - 1), key1) : 0, least = min(keys_of(row0), key1);
 
     h8 q[KS];
-    float start = 0.0f;
-    {
+    float start = 0.0f;                               // what u = code + 128 adds to a score, negated
+    auto read_q = [&]() {
         const __half *qp = a.q + (int64_t)(r.start + token) * a.ldq + (int64_t)head * D + 8 * hh;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            q[s] = __builtin_bit_cast(h8, *reinterpret_cast<const u4 *>(qp + 16 * s));
-#pragma unroll
-            for (int i = 0; i < 8; ++i) start += (float)q[s][i];
-        }
-        start += __shfl_xor(start, 32, 64);
-        start *= -128.0f * 5.9604644775390625e-08f;    // what u = code + 128 adds to a score, negated
-    }
+        for (int s = 0; s < KS; ++s) q[s] = __builtin_bit_cast(h8, *reinterpret_cast<const u4 *>(qp + 16 * s));
+    };
     const float to_e = a.sm_scale * kLog2e * 16777216.0f;
     f16v o[DB];
 #pragma unroll
@@ -603,9 +607,25 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
     };
     // ---- computing, 32 keys: e = score * factor + shift (the offset of the codes in the shift), the weights to be divided by 1 / inv
     float factor[2], shift[2], inv[2];
+    auto scales_of = [&](int at) __attribute__((always_inline)) {              // block `at` of the lanes' and the one behind it
+        auto of_block = [&](float v, int b) {
+            return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), at + b));
+        };
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            factor[b] = of_block(b_scale, b);
+            shift[b] = fmaf(start, factor[b], of_block(b_log, b));
+            inv[b] = of_block(b_inv, b);
+        }
+    };
+    auto largest = [&](const f16v &s, int b) __attribute__((always_inline)) {
+        const int i = 8 * b;
+        const float m = larger(larger(larger(s[i], s[i + 1], s[i + 2]), s[i + 3], s[i + 4]), s[i + 5], larger(s[i + 6], s[i + 7], s[i + 7]));
+        return fmaf(m, factor[b], shift[b]);
+    };
     // Half a tile: the scores of the next 32 keys (K's rows 32 half ..) and between their products the weights of the last ones, `now`; then the weights'
     // products with V, and between them `pieces` of staging.  Operands are read from LDS three products ahead.  The order is the one written.
-    auto half_tile = [&](const unsigned char *buf, int half, const f16v &now, f16v &then, auto stage, int pieces) __attribute__((always_inline)) {
+    auto half_tile = [&](const unsigned char *buf, int half, const f16v &now, f16v &then, int at, auto stage, int pieces) __attribute__((always_inline)) {
         constexpr int kAhead = 3, per = 16 / KS;
         const unsigned char *kp = buf + L::k + (32 * half + n) * L::kPitch + 16 * hh;
         const unsigned char *vp = buf + L::v + n * L::vPitch + 16 * hh + 64 * half;
@@ -636,14 +656,19 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
         }
         l = fmaf(sum[0], inv[0], l);
         l = fmaf(sum[1], inv[1], l);
+        float top[2];
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) {
             if (i + kAhead < 2 * DB) read(KS + i + kAhead);
             o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[KS + i], p[i / DB], o[i % DB], 0, 0, 0);
 #pragma unroll
             for (int k = pieces * i / (2 * DB); k < pieces * (i + 1) / (2 * DB); ++k) stage(k);
+            if (i == 0) scales_of(at);
+            if (i == 2 * DB - 3) top[0] = largest(then, 0);
+            if (i == 2 * DB - 2) top[1] = largest(then, 1);
             __builtin_amdgcn_sched_barrier(0);
         }
+        return fmaxf(top[0], top[1]);
     };
     auto first_scores = [&](const unsigned char *buf, f16v &s) {
 #pragma unroll
@@ -652,26 +677,14 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
         for (int i = 0; i < KS; ++i)
             s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(buf + L::k + (32 + n) * L::kPitch + 16 * hh + 32 * i), q[i], s, 0, 0, 0);
     };
-    // the largest e of 32 keys from `key` on (block `at` of the lanes' and the one behind it)
-    auto look = [&](int key, int at, f16v &s) __attribute__((always_inline)) {
+    // Scores of the 32 keys from `key` on: those that a row does not see, and M where some e passes it by 8.
+    auto look = [&](int key, f16v &s, float top) __attribute__((always_inline)) {
         if (key + 32 > least) {                       // (the same in all lanes)
             const int room = min(sees, key1) - (key + 4 * hh);
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (8 * (i >> 2) + (i & 3) >= room) s[i] = -INFINITY;
-        }
-        auto of_block = [&](float v, int b) {
-            return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), at + b));
-        };
-        float top = -INFINITY;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int i = 8 * b;
-            const float m = larger(larger(larger(s[i], s[i + 1], s[i + 2]), s[i + 3], s[i + 4]), s[i + 5], larger(s[i + 6], s[i + 7], s[i + 7]));
-            factor[b] = of_block(b_scale, b);
-            shift[b] = fmaf(start, factor[b], of_block(b_log, b));
-            inv[b] = of_block(b_inv, b);
-            top = fmaxf(top, fmaf(m, factor[b], shift[b]));
+            top = fmaxf(largest(s, 0), largest(s, 1));
         }
         if (__ballot(top > M + 8.0f)) {               // rare after the first tiles
             const float to = fmaxf(M, fmaxf(top, __shfl_xor(top, 32, 64)));
@@ -682,12 +695,14 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
             for (int i = 0; i < DB; ++i) o[i] *= down;
         }
     };
+
     if (key0 < key1) {                                // (the same in all threads)
         const int tiles = (key1 - key0 + kKeys - 1) / kKeys;
         u4 kr0[KL];
         read_pages(0);
         const int key_first = key0 - 32 + 16 * lane;  // the first 32 keys: as the last ones of a tile of K
         const int page_first = key_first >= key0 && key_first < key1 ? table[key_first >> a.shift] : -1;
+        read_q();                                     // (behind the block numbers, which the codes wait for)
         take_units(0);
         fetch_k(place_of(page_first, key_first), 0, kr0);
         fetch_k(unit_k, 0, kr);
@@ -700,11 +715,16 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
         for (int k = 0; k < vPieces; ++k) stage_v(lds, k);
         fetch_k(unit_k, 4, kr);
         fetch_v(4);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) start = add8(q[s], start);
+        start += __shfl_xor(start, 32, 64);
+        start *= -128.0f * 5.9604644775390625e-08f;
         take_scales();
         __syncthreads();
         f16v x, y;
         first_scores(lds + L::bytes, x);
-        look(key0, 0, x);
+        scales_of(0);
+        look(key0, x, fmaxf(largest(x, 0), largest(x, 1)));
         __syncthreads();
         int at = 0;
         for (int t = 0; t < tiles; ++t, at ^= L::bytes) {
@@ -713,22 +733,21 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
             auto next_k = [&](int k) __attribute__((always_inline)) { stage_k(next, kr, k); };
             auto next_v = [&](int k) __attribute__((always_inline)) { stage_v(next, k); };
             if (key < wave1) {                        // (the same in all lanes)
-                half_tile(here, 0, x, y, next_k, kPieces);
-                look(key + 32, block + 2, y);
+                const float top = half_tile(here, 0, x, y, block + 2, next_k, kPieces);
+                look(key + 32, y, top);
             } else {
 #pragma unroll
                 for (int k = 0; k < kPieces; ++k) next_k(k);
             }
             if (ahead == 0) take_units(t + 2);
+            if (block == 60) take_scales();
             fetch_k(unit_k, ahead, kr);
             if (key + 32 < wave1) {
-                half_tile(here, 1, y, x, next_v, vPieces);
-                if (block == 60) take_scales();
-                look(key + 64, (block + 4) & 63, x);
+                const float top = half_tile(here, 1, y, x, (block + 4) & 63, next_v, vPieces);
+                look(key + 64, x, top);
             } else {
 #pragma unroll
                 for (int k = 0; k < vPieces; ++k) next_v(k);
-                if (block == 60) take_scales();
             }
             fetch_v(ahead);
             if (ahead == 60) read_pages(t + 3);
@@ -737,27 +756,37 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
     }
 
     l += __shfl_xor(l, 32, 64);
-    if (n >= rows) return;
-    const bool whole = w.splits == 1;
-    const float f = whole ? (l > 0.0f ? 512.0f / l : 0.0f) : 1.0f;            // (values were 2^-9 of the codes)
-    __half *to = a.out + (int64_t)(r.start + token) * a.ldo + (int64_t)head * D + 4 * hh;
-    float *part = whole ? nullptr : a.part + (((int64_t)(w.first_slot + w.split) * a.Hkv + h) * a.part_rows + wave * 32 + n) * (D + 4);
-    if (!whole && hh == 0) {
-        part[0] = M;
-        part[1] = l;
-    }
+    if (w.splits == 1) {
+        // by way of this wavefront's own part of LDS, so that a store has whole rows (nobody reads codes there any more)
+        constexpr int pitch = 2 * D + 16, lanes = D / 8;      // lanes of a row
+        unsigned char *mine = lds + wave * 32 * pitch;
+        const float f = l > 0.0f ? 512.0f / l : 0.0f;         // (values were 2^-9 of the codes)
 #pragma unroll
-    for (int i = 0; i < DB; ++i)
+        for (int i = 0; i < DB; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const f4 v = f4{o[i][4 * j] * f, o[i][4 * j + 1] * f, o[i][4 * j + 2] * f, o[i][4 * j + 3] * f};
-            if (whole) {
-                const __half2 lo = __floats2half2_rn(v[0], v[1]), hi = __floats2half2_rn(v[2], v[3]);
-                *reinterpret_cast<u2 *>(to + 32 * i + 8 * j) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
-            } else {
-                *reinterpret_cast<f4 *>(part + 4 + 32 * i + 8 * j + 4 * hh) = v;
+            for (int j = 0; j < 4; ++j) {
+                const __half2 lo = __floats2half2_rn(o[i][4 * j] * f, o[i][4 * j + 1] * f), hi = __floats2half2_rn(o[i][4 * j + 2] * f, o[i][4 * j + 3] * f);
+                *reinterpret_cast<u2 *>(mine + n * pitch + 64 * i + 16 * j + 8 * hh) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+            }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 32 * lanes / 64; ++i) {
+            const int rr = i * (64 / lanes) + lane / lanes;
+            if (rr < rows) {
+                const int t = by_group(a, row0 + rr);
+                __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + row0 + rr - t * a.group) * D + 8 * (lane % lanes);
+                *reinterpret_cast<u4 *>(to) = *reinterpret_cast<const u4 *>(mine + rr * pitch + 16 * (lane % lanes));
             }
         }
+    } else if (n < rows) {
+        float *part = a.part + (((int64_t)(w.first_slot + w.split) * a.Hkv + h) * a.part_rows + wave * 32 + n) * (D + 4);
+        if (hh == 0) *reinterpret_cast<f2 *>(part) = f2{M, l};
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<f4 *>(part + 4 + 32 * i + 8 * j + 4 * hh) = f4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
+    }
 }
 
 // The pieces of tiles, in their order: 16 rows of a tile and cache head for a workgroup, first (the first `few_groups` workgroups) those of the kernel
@@ -787,7 +816,7 @@ void attention_kv8_merge_kernel(const Args a, const Parts parts)
         part_rows = kTile;
     }
     if (!w.found || w.splits == 1) return;
-    const Request r = request(a, w.b);
+    const Request r = w.r;
     const int all = r.n * a.group;
     // (the kernel of many rows takes a request's tiles from the last one on)
     const int tile = is_few ? w.tile : ((all - 1) >> rows_log) - w.tile;
@@ -824,7 +853,7 @@ void attention_kv8_merge_kernel(const Args a, const Parts parts)
             }
         }
         const float f = sum > 0.0f ? 512.0f / sum : 0.0f;
-        const int row = first + rr, t = row / a.group;
+        const int row = first + rr, t = by_group(a, row);
         __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + row - t * a.group) * D + d;
         const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
         *reinterpret_cast<u2 *>(to) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
@@ -835,7 +864,7 @@ void attention_kv8_merge_kernel(const Args a, const Parts parts)
 
 // Requests of up to kFew query rows (tokens times the heads of a group) go to the first kernel, larger ones to the second.
 constexpr int kFew = 64;
-constexpr int kFewWorkgroups = 1024, kManyWorkgroups = 512;      // what the card has room for at once
+constexpr int kFewWorkgroups = 1024, kManyWorkgroups = 256;      // what the card has room for at once
 
 struct Part { int64_t tiles, groups; int budget, part_rows; size_t floats; };    // no tiles: no launch
 struct Shape { Part few, many; int few_most; };      // few_most: rows that the first kernel takes at most
@@ -948,6 +977,9 @@ hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)
     Args a;
     a.q = (const __half *)c.q; a.T = (int)c.T; a.ldq = c.ldq;
     a.B = c.B; a.H = c.H; a.Hkv = c.Hkv; a.group = c.H / c.Hkv;
+    const int log = a.group > 1 ? 32 - __builtin_clz((unsigned)(a.group - 1)) : 0;
+    a.div_shift = 31 + log;
+    a.div_mul = (uint32_t)(((uint64_t)1 << a.div_shift) / (unsigned)a.group + 1);
     a.max_new = c.max_new;
     a.token_start = c.token_start; a.seq_len = c.seq_len; a.table = c.block_table;
     a.W = (int)c.W; a.shift = __builtin_ctz((unsigned)c.block_tokens);
