@@ -35,9 +35,14 @@ struct Args {
     const int8_t *kq; const float *ks; const int8_t *vq; const float *vs;
     float sm_scale;
     __half *out; int64_t ldo;
-    float *part;                                  // NULL: no tile's keys are split
-    int part_rows;                                // rows of a split's record
+};
+
+// One of the two kinds of work of a call, by the rows (tokens times heads of a group) of a request.
+struct Job {
+    int rows_min, rows_max;
     int budget;                                   // workgroups for each cache head that tiles may be cut into (0: none is cut)
+    float *part; int part_rows;                   // records of the pieces, and rows of a record
+    int groups, merges;                           // workgroups for each cache head of the kernel, of the merge
 };
 
 __device__ __forceinline__ int by_group(const Args &a, int n) { return (int)(((uint64_t)(uint32_t)n * a.div_mul) >> a.div_shift); }
@@ -91,10 +96,11 @@ __device__ __forceinline__ float total(float v)
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, running(v)), 63));
 }
 
-// FROM_TILE: `index` counts tiles (all of a tile's pieces are meant), else pieces.  Requests of rows_min to rows_max rows count.
+// FROM_TILE: `index` counts tiles (all of a tile's pieces are meant), else pieces.
 template <int LOG, bool FROM_TILE>
-__device__ __forceinline__ Place place(const Args &a, int index, int budget, int rows_min, int rows_max)
+__device__ __forceinline__ Place place(const Args &a, const Job &job, int index)
 {
+    const int budget = job.budget;
     const int lane = threadIdx.x & 63;
     Request r = {0, 0, 0, 0};
     auto tiles_keys = [&](int base, int &tiles, int &keys) {
@@ -103,7 +109,7 @@ __device__ __forceinline__ Place place(const Args &a, int index, int budget, int
         if (base + lane < a.B) {
             r = request(a, base + lane);
             const int64_t rows = (int64_t)r.n * a.group;
-            if (rows >= rows_min && rows <= rows_max) {
+            if (rows >= job.rows_min && rows <= job.rows_max) {
                 tiles = (int)((rows + (1 << LOG) - 1) >> LOG);
                 keys = r.keys;
             }
@@ -258,17 +264,19 @@ __device__ __forceinline__ float sum_of_chunks(float v)
 //           buffers.  Block numbers and scales of 64 blocks of 16 keys are read at once, a lane each.
 constexpr int kWaves = 4, kStep = 32, kRowsLog = 4, kTileRows = 1 << kRowsLog;
 
+template <int D>
+struct RowsLds { float acc[kWaves][kTileRows][D + 4], m[kWaves][kTileRows], l[kWaves][kTileRows]; };
+
 template <int D, bool ONCE>
-__global__ __launch_bounds__(kWaves * 64, 4)
-void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
+__device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int index, RowsLds<D> &lds)
 {
     constexpr int KB = D / 4, VB = D / 16;            // bytes of a K row and of a V row in a lane
     constexpr int KS = D / 32;                        // matrix instructions for 16 keys' scores
-    __shared__ alignas(16) float s_acc[kWaves][kTileRows][D + 4];
-    __shared__ float s_m[kWaves][kTileRows], s_l[kWaves][kTileRows];
+    auto &s_acc = lds.acc;
+    auto &s_m = lds.m, &s_l = lds.l;
 
-    const int h = blockIdx.x % a.Hkv;
-    const Place w = place<kRowsLog, false>(a, blockIdx.x / a.Hkv, a.budget, rows_min, rows_max);
+    const int h = index % a.Hkv;
+    const Place w = place<kRowsLog, false>(a, job, index / a.Hkv);
     if (!w.found) return;
     const Request r = w.r;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -449,7 +457,7 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
     }
     __syncthreads();
     const bool whole = w.splits == 1;
-    const int64_t record = whole ? 0 : ((int64_t)(w.first_slot + w.split) * a.Hkv + h) * a.part_rows;
+    const int64_t record = whole ? 0 : ((int64_t)(w.first_slot + w.split) * a.Hkv + h) * job.part_rows;
     for (int i = tid; i < rows * (D / 4); i += kWaves * 64) {
         const int rr = i / (D / 4), d = 4 * (i % (D / 4));
         float top = s_m[0][rr];
@@ -471,7 +479,7 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
             const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
             *reinterpret_cast<u2 *>(to) = u2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
         } else {
-            float *to = a.part + (record + rr) * (D + 4);
+            float *to = job.part + (record + rr) * (D + 4);
             *reinterpret_cast<f4 *>(to + 4 + d) = o;
             if (d == 0) {
                 to[0] = top;
@@ -479,6 +487,14 @@ void attention_kv8_rows_kernel(const Args a, int rows_min, int rows_max)
             }
         }
     }
+}
+
+template <int D, bool ONCE>
+__global__ __launch_bounds__(kWaves * 64, 4)
+void attention_kv8_rows_kernel(const Args a, const Job few)
+{
+    __shared__ alignas(16) RowsLds<D> lds;
+    rows_tile<D, ONCE>(a, few, blockIdx.x, lds);
 }
 
 // ---------------------------------------------------------------- many query rows
@@ -511,16 +527,14 @@ struct TileLds {
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 2)
-void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
+__device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, int index, unsigned char *lds)
 {
     typedef TileLds<D> L;
     constexpr int KS = D / 16, DB = D / 32;           // matrix instructions for 32 keys' scores; blocks of 32 output dimensions
     constexpr int KL = D / 64, VB = D / 16;           // 16-byte loads of K, bytes of a V row in a lane
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
 
-    const int h = blockIdx.x % a.Hkv;
-    const Place w = place<kTileLog, false>(a, blockIdx.x / a.Hkv, a.budget, rows_min, rows_max);
+    const int h = index % a.Hkv;
+    const Place w = place<kTileLog, false>(a, job, index / a.Hkv);
     if (!w.found) return;
     const Request r = w.r;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -792,7 +806,7 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
             }
         }
     } else if (n < rows) {
-        float *part = a.part + (((int64_t)(w.first_slot + w.split) * a.Hkv + h) * a.part_rows + wave * 32 + n) * (D + 4);
+        float *part = job.part + (((int64_t)(w.first_slot + w.split) * a.Hkv + h) * job.part_rows + wave * 32 + n) * (D + 4);
         if (hh == 0) *reinterpret_cast<f2 *>(part) = f2{M, l};
 #pragma unroll
         for (int i = 0; i < DB; ++i)
@@ -802,31 +816,42 @@ void attention_kv8_tile_kernel(const Args a, int rows_min, int rows_max)
     }
 }
 
-// The pieces of tiles, in their order: 16 rows of a tile and cache head for a workgroup, first (the first `few_groups` workgroups) those of the kernel
-// of few rows, then eight for each tile of the other.  What bounds it is its chain of reads (lengths, then the pieces), so eight pieces are read at once.
-struct Parts { int few_groups, few_most, few_budget, few_rows, many_budget; const float *few, *many; };
+// A step with requests of many rows: its few-row requests, which wait for memory, run beside the tiles of the others, which keep the matrix units
+// busy (one launch after the other, 32 single tokens and two chunks of 125 and 318 tokens took 27 + 45 us).
+template <int D>
+__global__ __launch_bounds__(256, 2)
+void attention_kv8_step_kernel(const Args a, const Job few, const Job many)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    static_assert(sizeof(RowsLds<D>) <= 2 * TileLds<D>::bytes, "one workgroup's LDS");
+    const int first = few.groups * a.Hkv;
+    if ((int)blockIdx.x < first) rows_tile<D, false>(a, few, blockIdx.x, *reinterpret_cast<RowsLds<D> *>(lds));
+    else                         many_rows_tile<D>(a, many, blockIdx.x - first, lds);
+}
 
+// The pieces of tiles, in their order: 16 rows of a tile and cache head for a workgroup, first those of few rows, then eight for each tile of
+// many.  What bounds it is its chain of reads (lengths, then the pieces), so eight pieces are read at once.
 template <int D>
 __global__ __launch_bounds__(256)
-void attention_kv8_merge_kernel(const Args a, const Parts parts)
+void attention_kv8_merge_kernel(const Args a, const Job few, const Job many)
 {
-    const bool is_few = (int)blockIdx.x < parts.few_groups;
-    const int  index = is_few ? blockIdx.x : blockIdx.x - parts.few_groups, h = index % a.Hkv;
+    constexpr int kSubs = kTile / kTileRows;
+    const bool is_few = (int)blockIdx.x < few.merges * a.Hkv;
+    const int  index = is_few ? blockIdx.x : blockIdx.x - few.merges * a.Hkv, h = index % a.Hkv;
     Place w;
     int sub = 0, rows_log, part_rows;
     const float *part;
     if (is_few) {
-        w = place<kRowsLog, true>(a, index / a.Hkv, parts.few_budget, 1, parts.few_most);
+        w = place<kRowsLog, true>(a, few, index / a.Hkv);
         rows_log = kRowsLog;
-        part = parts.few;
-        part_rows = parts.few_rows;
+        part = few.part;
+        part_rows = few.part_rows;
     } else {
-        constexpr int kSubs = kTile / kTileRows;
         sub = index / a.Hkv % kSubs;
-        w = place<kTileLog, true>(a, index / a.Hkv / kSubs, parts.many_budget, parts.few_most + 1, 0x7fffffff);
+        w = place<kTileLog, true>(a, many, index / a.Hkv / kSubs);
         rows_log = kTileLog;
-        part = parts.many;
-        part_rows = kTile;
+        part = many.part;
+        part_rows = many.part_rows;
     }
     if (!w.found || w.splits == 1) return;
     const Request r = w.r;
@@ -875,27 +900,29 @@ void attention_kv8_merge_kernel(const Args a, const Parts parts)
 
 // ---------------------------------------------------------------- shape of a call
 
-// Requests of up to kFew query rows (tokens times the heads of a group) go to the first kernel, larger ones to the second.
+// Requests of up to kFew query rows (tokens times the heads of a group) are work of the first kind, larger ones of the second.
 constexpr int kFew = 64;
-constexpr int kFewWorkgroups = 1024, kManyWorkgroups = 256;      // what the card has room for at once
+// Workgroups that the card has room for at once: of the kernel of few rows; of few rows beside many; of many rows one a compute unit (two to one
+// are as fast each, and their tiles need not be cut: 28 tiles for each of 8 cache heads 45 us, cut to 512 43 us and 12 us for their merge).
+constexpr int kFewWorkgroups = 1024, kFewBeside = 512, kManyWorkgroups = 256;
+// Beside many rows, sequences of up to so many keys are not cut (a merge is a launch of 4 us).
+constexpr int kUncutBeside = 4096;
 
-struct Part { int64_t tiles, groups; int budget, part_rows; size_t floats; };    // no tiles: no launch
-struct Shape { Part few, many; int few_most; };      // few_most: rows that the first kernel takes at most
+struct Shape { Job few, many; size_t floats; };
 
 // `want` workgroups together, for each cache head: where there are fewer tiles (and 128 keys to a piece) they are cut.
-Part part_of(int64_t tiles, int part_rows, int64_t want, int Hkv, int D, int64_t capacity)
+void size_job(Job &job, int64_t tiles, int part_rows, int64_t want, int Hkv, int64_t capacity, int subs)
 {
-    Part p = {tiles, tiles, 0, part_rows, 0};
     const int64_t most = tiles * ((capacity + 127) / 128);
     int64_t budget = (want + Hkv - 1) / Hkv;
     if (budget > most) budget = most;
-    if (budget > tiles) {
-        p.budget = (int)budget;
-        p.groups = budget;
-        p.floats = (size_t)(p.groups * Hkv * part_rows) * (size_t)(D + 4);
-    }
-    return p;
+    job.budget = budget > tiles ? (int)budget : 0;
+    job.groups = (int)(job.budget ? budget : tiles);
+    job.merges = job.budget ? (int)(tiles * subs) : 0;
+    job.part_rows = part_rows;
 }
+
+size_t records(const Job &job, int Hkv, int D) { return job.budget ? (size_t)job.groups * Hkv * job.part_rows * (D + 4) : 0; }
 
 Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t capacity)
 {
@@ -903,16 +930,22 @@ Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t ca
     if (T == 0 || B == 0 || max_new == 0) return s;
     const int64_t rows = (int64_t)max_new * group;   // of one request, at most
     const bool many = rows > kFew;
-    s.few_most = (int)(many ? (B > 1 ? kFew : 0) : rows);
-    if (s.few_most) {
-        const int64_t each = (int64_t)B * ((s.few_most + kTileRows - 1) / kTileRows), by_token = T * group / kTileRows + B;
-        s.few = part_of(each < by_token ? each : by_token, s.few_most < kTileRows ? s.few_most : kTileRows, kFewWorkgroups, Hkv, D, capacity);
+    const int  few_most = (int)(many ? (B > 1 ? kFew : 0) : rows);       // (one request is work of the second kind whatever its size)
+    s.few.rows_min = 1;
+    s.few.rows_max = few_most;
+    s.many.rows_min = few_most + 1;
+    s.many.rows_max = 0x7fffffff;
+    if (few_most) {
+        const int64_t each = (int64_t)B * ((few_most + kTileRows - 1) / kTileRows), by_token = T * group / kTileRows + B;
+        size_job(s.few, each < by_token ? each : by_token, few_most < kTileRows ? few_most : kTileRows,
+                 !many ? kFewWorkgroups : capacity > kUncutBeside ? kFewBeside : 0, Hkv, capacity, 1);
     }
-    if (many) {                                      // (one request goes there whatever its size)
-        const int64_t least = s.few_most + 1, each = (int64_t)B * ((rows + kTile - 1) / kTile);
+    if (many) {
+        const int64_t least = few_most + 1, each = (int64_t)B * ((rows + kTile - 1) / kTile);
         const int64_t requests = T * group / least < B ? T * group / least : B, by_token = T * group / kTile + requests;
-        s.many = part_of(each < by_token ? each : by_token, kTile, kManyWorkgroups, Hkv, D, capacity);
+        size_job(s.many, each < by_token ? each : by_token, kTile, kManyWorkgroups, Hkv, capacity, kTile / kTileRows);
     }
+    s.floats = records(s.few, Hkv, D) + records(s.many, Hkv, D);
     return s;
 }
 
@@ -924,49 +957,27 @@ bool reads_once(const Args &a, int rows)
 }
 
 template <int D>
-hipError_t launch(Args a, const Shape &s, float *workspace, hipStream_t stream)
+hipError_t launch(const Args &a, Shape s, float *workspace, hipStream_t stream)
 {
-    hipError_t err = hipSuccess;
-    Parts parts = {};
-    parts.few_most = s.few_most;
-    int64_t merges = 0;
-    if (s.few.tiles) {
-        a.budget = s.few.budget;
-        a.part = workspace;
-        a.part_rows = s.few.part_rows;
-        auto kern = reads_once(a, s.few_most) ? &attention_kv8_rows_kernel<D, true> : &attention_kv8_rows_kernel<D, false>;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(s.few.groups * a.Hkv)), dim3(kWaves * 64), 0, stream, a, 1, s.few_most);
-        if ((err = hipGetLastError()) != hipSuccess) return err;
-        if (s.few.budget) {
-            merges = s.few.tiles * a.Hkv;
-            parts.few_groups = (int)merges;
-            parts.few_budget = s.few.budget;
-            parts.few_rows = s.few.part_rows;
-            parts.few = workspace;
-        }
-    }
-    if (s.many.tiles) {
+    s.few.part = workspace;
+    s.many.part = workspace + records(s.few, a.Hkv, D);
+    if (!s.many.groups) {
+        if (!s.few.groups) return hipSuccess;
+        auto kern = reads_once(a, s.few.rows_max) ? &attention_kv8_rows_kernel<D, true> : &attention_kv8_rows_kernel<D, false>;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(s.few.groups * a.Hkv)), dim3(kWaves * 64), 0, stream, a, s.few);
+    } else {
         static atom_launch::LdsOptIn opt;
         constexpr int bytes = 2 * TileLds<D>::bytes;
-        err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(&attention_kv8_tile_kernel<D>), bytes);
+        hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(&attention_kv8_step_kernel<D>), bytes);
         if (err != hipSuccess) return err;
-        a.budget = s.many.budget;
-        a.part = workspace + s.few.floats;
-        a.part_rows = s.many.part_rows;
-        hipLaunchKernelGGL((attention_kv8_tile_kernel<D>), dim3((unsigned)(s.many.groups * a.Hkv)), dim3(256), bytes, stream, a, s.few_most + 1,
-                           0x7fffffff);
-        if ((err = hipGetLastError()) != hipSuccess) return err;
-        if (s.many.budget) {
-            merges += s.many.tiles * (kTile / kTileRows) * a.Hkv;
-            parts.many_budget = s.many.budget;
-            parts.many = workspace + s.few.floats;
-        }
+        hipLaunchKernelGGL((attention_kv8_step_kernel<D>), dim3((unsigned)((s.few.groups + s.many.groups) * a.Hkv)), dim3(256), bytes, stream, a,
+                           s.few, s.many);
     }
-    if (merges) {
-        hipLaunchKernelGGL((attention_kv8_merge_kernel<D>), dim3((unsigned)merges), dim3(256), 0, stream, a, parts);
-        err = hipGetLastError();
-    }
-    return err;
+    hipError_t err = hipGetLastError();
+    const int merges = (s.few.merges + s.many.merges) * a.Hkv;
+    if (err != hipSuccess || !merges) return err;
+    hipLaunchKernelGGL((attention_kv8_merge_kernel<D>), dim3((unsigned)merges), dim3(256), 0, stream, a, s.few, s.many);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -975,14 +986,16 @@ namespace atom_internal {
 
 size_t attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, int max_new, int64_t W, int block_tokens)
 {
-    const Shape s = shape(T, B, Hkv, H / Hkv, D, max_new, W * block_tokens);
-    return (s.few.floats + s.many.floats) * sizeof(float);
+    return shape(T, B, Hkv, H / Hkv, D, max_new, W * block_tokens).floats * sizeof(float);
 }
 
 bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new, int64_t W, int block_tokens)
 {
-    const Shape s = shape(T, B, Hkv, H / Hkv, 128, max_new, W * block_tokens);
-    return (s.few.groups + 8 * s.many.groups) * Hkv <= 0x7fffffffLL;
+    // every count is below (rows / 16 + B) * blocks of 128 rows and the workgroups wanted, as doubles here
+    const double group = H / Hkv, rows = (double)max_new * group, tiles = (double)T * group / kTileRows + B, each = (double)B * (rows / kTileRows + 1);
+    const double most = (tiles < each ? tiles : each) + kFewWorkgroups;
+    (void)W; (void)block_tokens;
+    return 2.0 * most * Hkv < 2147483647.0;
 }
 
 hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)
