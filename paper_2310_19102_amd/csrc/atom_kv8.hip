@@ -17,23 +17,50 @@ namespace {
 
 // ---------------------------------------------------------------- block tables and slot maps
 
-constexpr int kMapThreads = 1024;
+constexpr int kMapKept = 8192;                               // requests whose lengths a workgroup keeps
 
 __device__ __forceinline__ int32_t saturate(int64_t v) { return v > 0x7fffffffLL ? 0x7fffffff : (int32_t)v; }
 
-// One launch; every workgroup scans all B requests by itself (two int32 per request in its LDS: first token, first taken
-// block) and then writes its share of the table and of the slots, so nothing waits for another workgroup.  A slot whose
+// Sum over the lanes up to this one, on the vector unit.
+__device__ __forceinline__ int64_t running(int64_t v)
+{
+#define ATOM_STEP(ctrl, rows)                                                                                        \
+    {                                                                                                                \
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, ctrl, rows, 0xF, false);      \
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), ctrl, rows, 0xF, false);        \
+        v += (int64_t)(((uint64_t)hi << 32) | lo);                                                                   \
+    }
+    ATOM_STEP(0x111, 0xF)                                    // one, two, four, eight lanes below in the row of 16
+    ATOM_STEP(0x112, 0xF)
+    ATOM_STEP(0x114, 0xF)
+    ATOM_STEP(0x118, 0xF)
+    ATOM_STEP(0x142, 0xA)                                    // the row below's last lane, into rows 1 and 3
+    ATOM_STEP(0x143, 0xC)                                    // the lower half's, into the upper
+#undef ATOM_STEP
+    return v;
+}
+__device__ __forceinline__ int64_t of_lane(int64_t v, int lane)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane);
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// One launch; every workgroup scans all B requests by itself (per request its first token, its first taken block and, of up to 8192, both
+// lengths in its LDS) and then writes its share of the table and of the slots, so nothing waits for another workgroup.  A slot whose
 // page is a new one reads the free list, not the table, which another workgroup may be writing.
-// Bound by its own latency: two dependent reads and the scan, 1024 requests a round.
-__global__ __launch_bounds__(kMapThreads)
+// Bound by its latency: the lengths, one barrier (three in a round of many requests), the search in LDS, the free list.  200 requests with a table of 300 columns: with a
+// scan by lane exchanges through LDS, lengths read again for each entry and four entries a thread in turn 7.7 us, 4.6 so.
+template <int THREADS, bool KEPT>
+__global__ __launch_bounds__(THREADS)
 void kv_block_map_kernel(const int32_t *__restrict__ past, const int32_t *__restrict__ fresh, int B, int shift,
                          const int32_t *__restrict__ free_blocks, int64_t n_free, const int32_t *__restrict__ cursor,
-                         int32_t *table, int W, int T, int32_t *__restrict__ token_start, int32_t *__restrict__ seq_len,
+                         int32_t *table, int W, uint32_t w_mul, int w_shift, int T, int32_t *__restrict__ token_start, int32_t *__restrict__ seq_len,
                          int32_t *__restrict__ slot, int32_t *__restrict__ cursor_out)
 {
-    extern __shared__ int32_t s_first[];                     // [B + 1] first token, [B] first taken block
-    __shared__ int64_t s_wave[2][kMapThreads / 64];
-    int32_t *s_token = s_first, *s_taken = s_first + B + 1;
+    constexpr int kWaves = THREADS / 64;
+    extern __shared__ int32_t s_first[];                     // [B + 1] first token, [B] first taken block, and of KEPT [B] past, [B] new
+    __shared__ int64_t s_wave[2][kWaves];
+    int32_t *s_token = s_first, *s_taken = s_first + B + 1, *s_past = s_taken + B, *s_new = s_past + B;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int bs = 1 << shift;
     const int64_t start = cursor ? *cursor : 0;
@@ -41,36 +68,39 @@ void kv_block_map_kernel(const int32_t *__restrict__ past, const int32_t *__rest
 
     auto pages = [&](int64_t tokens) -> int { const int64_t n = (tokens + bs - 1) >> shift; return n < W ? (int)n : W; };
     int64_t tokens = 0, taken = 0;                           // of the requests before this round
-    for (int base = 0; base < B; base += kMapThreads) {
+    for (int base = 0; base < B; base += THREADS) {
         const int b = base + tid;
         const int64_t p = b < B ? max(past[b], 0) : 0, n = b < B ? max(fresh[b], 0) : 0;
-        const int64_t mine[2] = {n, pages(p + n) - pages(p)};
-        int64_t sum[2] = {mine[0], mine[1]};                 // inclusive over the wavefront, then exclusive over all
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int64_t v = __shfl_up(sum[k], d, 64);
-                if (lane >= d) sum[k] += v;
+        const int64_t blocks = pages(p + n) - pages(p);
+        const int64_t sum0 = running(n), sum1 = running(blocks);         // inclusive over the wavefront
+        int64_t before0 = tokens, before1 = taken;
+        if constexpr (kWaves > 1) {
+            if (base) __syncthreads();                       // (the last round's sums are read)
+            if (lane == 63) {
+                s_wave[0][wave] = sum0;
+                s_wave[1][wave] = sum1;
             }
-        __syncthreads();                                     // (the last round's sums are read)
-        if (lane == 63) {
-            s_wave[0][wave] = sum[0];
-            s_wave[1][wave] = sum[1];
-        }
-        __syncthreads();
-        int64_t before[2] = {tokens, taken};
-#pragma unroll 2
-        for (int w = 0; w < kMapThreads / 64; ++w) {
-            const int64_t v0 = s_wave[0][w], v1 = s_wave[1][w];
-            if (w < wave) { before[0] += v0; before[1] += v1; }
-            tokens += v0;
-            taken += v1;
+            __syncthreads();
+            const int64_t all0 = running(lane < kWaves ? s_wave[0][lane] : 0), all1 = running(lane < kWaves ? s_wave[1][lane] : 0);
+            const int w = __builtin_amdgcn_readfirstlane(wave);
+            if (w) {
+                before0 += of_lane(all0, w - 1);
+                before1 += of_lane(all1, w - 1);
+            }
+            tokens += of_lane(all0, kWaves - 1);
+            taken += of_lane(all1, kWaves - 1);
+        } else {
+            tokens += of_lane(sum0, 63);
+            taken += of_lane(sum1, 63);
         }
         if (b < B) {
-            const int32_t at = saturate(before[0] + sum[0] - mine[0]);
+            const int32_t at = saturate(before0 + sum0 - n);
             s_token[b] = at;
-            s_taken[b] = saturate(before[1] + sum[1] - mine[1]);
+            s_taken[b] = saturate(before1 + sum1 - blocks);
+            if constexpr (KEPT) {
+                s_past[b] = (int32_t)p;
+                s_new[b] = (int32_t)n;
+            }
             if (first_group) {
                 token_start[b] = at;
                 seq_len[b] = saturate(p + n);
@@ -87,17 +117,14 @@ void kv_block_map_kernel(const int32_t *__restrict__ past, const int32_t *__rest
     }
     __syncthreads();
 
+    auto past_of = [&](int b) -> int64_t { if constexpr (KEPT) return s_past[b]; else return max(past[b], 0); };
+    auto new_of = [&](int b) -> int64_t { if constexpr (KEPT) return s_new[b]; else return max(fresh[b], 0); };
     auto taken_block = [&](int b, int nth) -> int32_t {      // the nth block that request b takes
         const int64_t f = start + s_taken[b] + nth;
         return f >= 0 && f < n_free ? free_blocks[f] : -1;
     };
-    const int64_t step = (int64_t)gridDim.x * kMapThreads, me = (int64_t)blockIdx.x * kMapThreads + tid;
-    for (int64_t e = me; e < (int64_t)B * W; e += step) {
-        const int b = (int)((uint32_t)e / (uint32_t)W), j = (int)((uint32_t)e - (uint32_t)b * (uint32_t)W);
-        const int64_t p = max(past[b], 0), n = max(fresh[b], 0);
-        const int have = pages(p);
-        if (j >= have) table[e] = j < pages(p + n) ? taken_block(b, j - have) : -1;
-    }
+    const int64_t step = (int64_t)gridDim.x * THREADS, me = (int64_t)blockIdx.x * THREADS + tid, entries = (int64_t)B * W;
+    // slots first: their chain of reads is the longer one
     for (int64_t t = me; t < T; t += step) {
         int32_t where = -1;
         if (t < total) {
@@ -107,7 +134,7 @@ void kv_block_map_kernel(const int32_t *__restrict__ past, const int32_t *__rest
                 if (s_token[mid] <= t) lo = mid;
                 else hi = mid;
             }
-            const int64_t p0 = max(past[lo], 0), p = p0 + (t - s_token[lo]);
+            const int64_t p0 = past_of(lo), p = p0 + (t - s_token[lo]);
             const int64_t j = p >> shift;
             if (j < W) {
                 const int have = pages(p0);
@@ -117,6 +144,12 @@ void kv_block_map_kernel(const int32_t *__restrict__ past, const int32_t *__rest
             }
         }
         slot[t] = where;
+    }
+    for (int64_t e = me; e < entries; e += step) {
+        const int b = (int)(((uint64_t)(uint32_t)e * w_mul) >> w_shift), j = (int)e - b * W;
+        const int64_t p = past_of(b);
+        const int have = pages(p);
+        if (j >= have) table[e] = j < pages(p + new_of(b)) ? taken_block(b, j - have) : -1;
     }
 }
 
@@ -134,6 +167,20 @@ __device__ __forceinline__ uint32_t magnitudes(const uint4 &v)
 {
     constexpr uint32_t m = 0x7fff7fffu;
     return pair_max_u16(pair_max_u16(v.x & m, v.y & m), pair_max_u16(v.z & m, v.w & m));
+}
+
+// The largest of the wavefront's values (none is below zero), in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+#define ATOM_STEP(ctrl, rows) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xF, false))
+    ATOM_STEP(0x111, 0xF);
+    ATOM_STEP(0x112, 0xF);
+    ATOM_STEP(0x114, 0xF);
+    ATOM_STEP(0x118, 0xF);
+    ATOM_STEP(0x142, 0xA);
+    ATOM_STEP(0x143, 0xC);
+#undef ATOM_STEP
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 // clamp(rne(v), -127, 127) in the low byte: adding 1.5 * 2^23 rounds to the nearest even integer and leaves it there.
@@ -158,85 +205,108 @@ __device__ __forceinline__ uint32_t recode4(uint32_t w, float ratio)
     return pack4(c(0), c(1), c(2), c(3));
 }
 
-// One wavefront for a head (of K or of V) and `slab` tokens: it finds the runs that begin among them (a run: tokens whose
-// slots follow one another inside one block) and writes each whole, also past the slab's end.  A run's scale is the larger of the block's
+// What a call writes to and from, of K or of V.
+struct Side { const __half *x; int64_t ld; int8_t *codes; float *scale; };
+
+// A wavefront's window of 64 slots: which of the first `slab` tokens begin a run (a run: tokens whose slots follow one another inside one block).
+struct Window { int32_t got; bool valid; uint64_t leaders; };
+
+__device__ __forceinline__ Window window(const int32_t *__restrict__ slot, int32_t slots, int T, int64_t t_first, int slab, int bs)
+{
+    const int lane = threadIdx.x & 63;
+    Window w;
+    w.got = slot[min(t_first + lane, (int64_t)T - 1)];
+    const int32_t before = slot[max(t_first - 1, (int64_t)0)];
+    w.valid = t_first + lane < T && w.got >= 0 && w.got < slots;
+    int32_t prev = __shfl_up(w.got, 1, 64);
+    if (lane == 0) prev = t_first > 0 ? before : -2;
+    const bool follows = prev >= 0 && prev < slots && w.got == prev + 1 && (w.got & (bs - 1)) != 0;
+    w.leaders = __ballot(w.valid && !follows && lane < slab);
+    return w;
+}
+
+// The run that token t_first + l0 begins: from its slots at hand, and from those beyond them if it goes on there.
+__device__ __forceinline__ int run_length(const int32_t *__restrict__ slot, int T, const Window &w, int64_t t_first, int l0, int bs)
+{
+    const int lane = threadIdx.x & 63;
+    const int32_t first = __builtin_amdgcn_readlane(w.got, l0);
+    const int o = first & (bs - 1);
+    const uint64_t same = __ballot(w.valid && lane >= l0 && w.got == first + (lane - l0) && o + (lane - l0) < bs) >> l0;
+    int len = ~same ? __builtin_ctzll(~same) : 64;
+    if (len == 64 - l0)
+        while (o + len < bs) {
+            const int64_t t = t_first + l0 + len + lane;
+            const bool ok = t < T && o + len + lane < bs && slot[min(t, (int64_t)T - 1)] == first + len + lane;
+            const uint64_t m = __ballot(ok);
+            const int more = ~m ? __builtin_ctzll(~m) : 64;
+            len += more;
+            if (more < 64) break;
+        }
+    return len;
+}
+
+// A run of one head's rows, by one wavefront.  A run's scale is the larger of the block's
 // (where the block holds older rows, those before the run's first) and max|x| / 127:
 //   s = max(s_old, max|x| / 127), r = 1 / s, code = clamp(rne(x * r), -127, 127)   IEEE fp32, every step rounded once
 // and where s grows, the older rows become rne(code * (s_old / s)).
-// Rows stay in registers between the maximum and the codes (64 rows; a longer run is read twice, the second time
+// Rows stay in registers between the maximum and the codes (64 rows; those of a longer run are read twice, the second time
 // from the cache).  16-byte loads, 8 values a lane: D / 8 lanes a row.
 template <int D>
-__global__ __launch_bounds__(256)
-void kv8_append_kernel(const __half *__restrict__ xk, const __half *__restrict__ xv, int T, int64_t ldk, int64_t ldv, int Hkv,
-                       const int32_t *__restrict__ slot, int32_t slots, int shift, int slab, int8_t *__restrict__ kq,
-                       float *__restrict__ ks, int8_t *__restrict__ vq, float *__restrict__ vs)
-{
-    constexpr int LPR = D / 8, RPL = 64 / LPR, kLoads = 64 / RPL;   // lanes a row, rows a load, loads of 64 rows
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t group = item / (2 * Hkv);
-    const int which = (int)(item - group * (2 * Hkv)), h = which % Hkv;
-    const bool is_v = which >= Hkv;
-    const int64_t t_first = group * slab;
-    if (t_first >= T) return;
-    const int bs = 1 << shift;
+struct Run {
+    static constexpr int LPR = D / 8, RPL = 64 / LPR, kLoads = 64 / RPL;    // lanes a row, rows a load, loads of 64 rows
+    uint4 raw[kLoads];
+    const __half *rows; int64_t ld;
+    int8_t *block; float *scale;
+    int o, len, g, j;
+    float s_old;
 
-    const int32_t got = slot[min(t_first + lane, (int64_t)T - 1)];
-    const bool    valid = t_first + lane < T && got >= 0 && got < slots;
-    int32_t prev = __shfl_up(got, 1, 64);
-    if (lane == 0) prev = t_first > 0 ? slot[t_first - 1] : -2;
-    const bool follows = prev >= 0 && prev < slots && got == prev + 1 && (got & (bs - 1)) != 0;
-    uint64_t leaders = __ballot(valid && !follows && lane < slab);
+    // ONCE: with the hint that nothing reads the row again
+    template <bool ONCE>
+    __device__ __forceinline__ uint4 load(int row) const
+    {
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+        const u4 *p = reinterpret_cast<const u4 *>(rows + (int64_t)min(row, len - 1) * ld);
+        const u4  v = ONCE ? __builtin_nontemporal_load(p) : *p;
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
 
-    const __half *x = (is_v ? xv : xk) + (int64_t)h * D;
-    const int64_t ld = is_v ? ldv : ldk;
-    int8_t *cq = is_v ? vq : kq;
-    float  *cs = is_v ? vs : ks;
-    const int j = lane % LPR, g = lane / LPR;
-
-    while (leaders) {
-        const int l0 = __builtin_ctzll(leaders);
-        leaders &= leaders - 1;
-        const int32_t first = __builtin_amdgcn_readlane(got, l0);
-        const int     o = first & (bs - 1);
-        // length of the run: in the slots at hand, and beyond them if it goes on there
-        const uint64_t same = __ballot(valid && lane >= l0 && got == first + (lane - l0) && o + (lane - l0) < bs) >> l0;
-        int len = ~same ? __builtin_ctzll(~same) : 64;
-        if (len == 64 - l0)
-            while (o + len < bs) {
-                const int64_t t = t_first + l0 + len + lane;
-                const bool ok = t < T && o + len + lane < bs && slot[min(t, (int64_t)T - 1)] == first + len + lane;
-                const uint64_t m = __ballot(ok);
-                const int more = ~m ? __builtin_ctzll(~m) : 64;
-                len += more;
-                if (more < 64) break;
-            }
+    // the run's rows on their way to the registers, and their largest magnitude (the bits of a half)
+    __device__ __forceinline__ uint32_t begin(const Side &side, int h, int Hkv, int32_t first, int len_, int64_t t, int shift)
+    {
+        const int lane = threadIdx.x & 63;
+        g = lane / LPR;
+        j = lane % LPR;
+        len = len_;
+        ld = side.ld;
+        o = first & ((1 << shift) - 1);
         const int64_t at = (int64_t)(first >> shift) * Hkv + h;             // block and head
-        const float   s_old = o > 0 ? cs[at] : 0.0f;
-        const __half *rows = x + (t_first + l0) * ld + 8 * j;
-        auto load = [&](int row) { return *reinterpret_cast<const uint4 *>(rows + (int64_t)min(row, len - 1) * ld); };
-
-        uint4 raw[kLoads];
+        block = side.codes + (at << shift) * D;
+        scale = side.scale + at;
+        rows = side.x + (int64_t)h * D + t * ld + 8 * j;
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u)
+            if (u * RPL < len) raw[u] = load<true>(u * RPL + g);
+        s_old = o > 0 ? *scale : 0.0f;
         uint32_t top = 0;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            if (u * RPL < len) raw[u] = load(u * RPL + g);
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) top = pair_max_u16(top, magnitudes(raw[u]));
-        for (int row = 64; row < len; row += RPL) top = pair_max_u16(top, magnitudes(load(row + g)));
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) top = pair_max_u16(top, (uint32_t)__shfl_xor((int)top, d, 64));
-        top = max(top & 0xffffu, top >> 16);
+        for (int row = 64; row < len; row += RPL) top = pair_max_u16(top, magnitudes(load<false>(row + g)));
+        return wave_max(max(top & 0xffffu, top >> 16));
+    }
+
+    __device__ __forceinline__ void store(int row, const uint4 &v, float r)
+    {
+        if (row < len)
+            *reinterpret_cast<uint2 *>(block + (o + row) * D + 8 * j) = make_uint2(codes4(v.x, v.y, r), codes4(v.z, v.w, r));
+    }
+
+    __device__ __forceinline__ void end(uint32_t top)                   
+    {
+        const int lane = threadIdx.x & 63;
         const float amax = __half2float(__ushort_as_half((unsigned short)top));
         const float s_new = amax / 127.0f, s = s_new > s_old ? s_new : s_old;
         const float r = s > 0.0f ? 1.0f / s : 0.0f;
-
-        int8_t *block = cq + (at << shift) * D;
-        auto store = [&](int row, const uint4 &v) {
-            if (row < len)
-                *reinterpret_cast<uint2 *>(block + (o + row) * D + 8 * j) = make_uint2(codes4(v.x, v.y, r), codes4(v.z, v.w, r));
-        };
         if (s > s_old && s_old > 0.0f) {                                    // the older rows on the new scale
             const float ratio = s_old / s;
             for (int i = 16 * lane; i < o * D; i += 1024) {
@@ -247,9 +317,30 @@ void kv8_append_kernel(const __half *__restrict__ xk, const __half *__restrict__
         }
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            if (u * RPL < len) store(u * RPL + g, raw[u]);
-        for (int row = 64; row < len; row += RPL) store(row + g, load(row + g));
-        if (lane == 0) cs[at] = s;
+            if (u * RPL < len) store(u * RPL + g, raw[u], r);
+        for (int row = 64; row < len; row += RPL) store(row + g, load<false>(row + g), r);
+        if (lane == 0) *scale = s;
+    }
+};
+
+// One wavefront for a head (of K or of V) and `slab` tokens (ONE: one): it writes the runs that begin among them, each whole, also past the slab's end.
+// The wavefronts of a workgroup have neighbouring heads, whose rows lie side by side.  Bound by memory where there is much to write: 10240 tokens of 32 heads
+// of 128 (252 MB) 44.7 us, 5.6 TB/s; without the hint on the loads 52; all four wavefronts on one head's run 69.
+template <int D, bool ONE>
+__global__ __launch_bounds__(256)
+void kv8_append_kernel(Side k, Side v, int T, int Hkv, const int32_t *__restrict__ slot, int32_t slots, int shift, int slab)
+{
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t group = item / (2 * Hkv), t_first = ONE ? group : group * slab;
+    const int which = (int)(item - group * (2 * Hkv)), h = which % Hkv;
+    if (t_first >= T) return;
+    const Window w = window(slot, slots, T, t_first, ONE ? 1 : slab, 1 << shift);
+    for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1) {
+        const int l0 = ONE ? 0 : __builtin_ctzll(leaders);
+        const int len = run_length(slot, T, w, t_first, l0, 1 << shift);
+        Run<D> run;
+        run.end(run.begin(which < Hkv ? k : v, h, Hkv, __builtin_amdgcn_readlane(w.got, l0), len, t_first + l0, shift));
+        if constexpr (ONE) break;
     }
 }
 
@@ -261,19 +352,32 @@ hipError_t launch_kv_block_map(const int32_t *past, const int32_t *fresh, int B,
                                int64_t n_free, const int32_t *cursor, int32_t *table, int64_t W, int64_t T,
                                int32_t *token_start, int32_t *seq_len, int32_t *slot, int32_t *cursor_out, hipStream_t stream)
 {
-    const size_t lds = (size_t)(2 * B + 1) * sizeof(int32_t);
-    static atom_launch::LdsOptIn opt;
-    if (lds > 60 * 1024) {
-        hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(&kv_block_map_kernel), lds);
-        if (err != hipSuccess) return err;
-    }
+    const bool   kept = B <= kMapKept;
+    const size_t lds = (size_t)((kept ? 4 : 2) * B + 1) * sizeof(int32_t);
+    const int    log = W > 1 ? 64 - __builtin_clzll((uint64_t)(W - 1)) : 0;
+    const uint32_t w_mul = W > 0 ? (uint32_t)(((uint64_t)1 << (31 + log)) / (uint64_t)W + 1) : 0;       // n / W = n * w_mul >> 31 + log below 2^31
+    // Entries and tokens one to a thread as long as the card has room for the workgroups at once.  A lone wavefront needs no barrier for
+    // the scan: up to 64 requests and little to write.
     const int64_t work = (int64_t)B * W + T;
-    int64_t grid = (work + 4 * kMapThreads - 1) / (4 * kMapThreads);
-    if (grid > 256) grid = 256;
-    if (grid < 1) grid = 1;
-    hipLaunchKernelGGL(kv_block_map_kernel, dim3((unsigned)grid), dim3(kMapThreads), lds, stream, past, fresh, B,
-                       __builtin_ctz((unsigned)block_tokens), free_blocks, n_free, cursor, table, (int)W, (int)T, token_start,
-                       seq_len, slot, cursor_out);
+#define ATOM_MAP(THREADS, KEPT)                                                                                                      \
+    do {                                                                                                                             \
+        auto kern = &kv_block_map_kernel<THREADS, KEPT>;                                                                             \
+        static atom_launch::LdsOptIn opt;                                                                                            \
+        if (lds > 60 * 1024) {                                                                                                       \
+            hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(kern), lds);                        \
+            if (err != hipSuccess) return err;                                                                                       \
+        }                                                                                                                            \
+        int64_t grid = (work + THREADS - 1) / THREADS;                                                                               \
+        if (grid > 512) grid = 512;                                                                                                  \
+        if (grid < 1) grid = 1;                                                                                                      \
+        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(THREADS), lds, stream, past, fresh, B, __builtin_ctz((unsigned)block_tokens), \
+                           free_blocks, n_free, cursor, table, (int)W, w_mul, 31 + log, (int)T, token_start, seq_len, slot, cursor_out); \
+    } while (0)
+    if (!kept)                             ATOM_MAP(1024, false);
+    else if (B > 256 || work > 64 * 1024)  ATOM_MAP(1024, true);
+    else if (B > 64 || work > 1024)        ATOM_MAP(256, true);
+    else                                   ATOM_MAP(64, true);
+#undef ATOM_MAP
     return hipGetLastError();
 }
 
@@ -282,13 +386,17 @@ hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ld
                              void *v_codes, float *v_scale, hipStream_t stream)
 {
     const int64_t heads = 2 * (int64_t)Hkv;
-    const int     slab = T * heads <= 16384 ? 1 : T * heads <= 131072 ? 4 : 16;
-    const int64_t waves = (T + slab - 1) / slab * heads, grid = (waves + 3) / 4;
+    const Side ks = {(const __half *)k, ldk, (int8_t *)k_codes, k_scale}, vs = {(const __half *)v, ldv, (int8_t *)v_codes, v_scale};
+    const int32_t slots = (int32_t)(n_blocks * block_tokens);
+    const int     shift = __builtin_ctz((unsigned)block_tokens);
+    // Tokens to a wavefront: one up to as many wavefronts as the card has places for (64 sequences of 32 heads: 4096), then 8 and 64, so that
+    // those that find no run's beginning are few: a step of so many tokens has long runs.
+    const int     slab = T * heads <= 16384 ? 1 : T * heads <= 131072 ? 8 : 64;
+    const int64_t grid = ((T + slab - 1) / slab * heads + 3) / 4;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-    auto kern = D == 128 ? &kv8_append_kernel<128> : &kv8_append_kernel<64>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, stream, (const __half *)k, (const __half *)v, (int)T, ldk, ldv,
-                       Hkv, slot, (int32_t)(n_blocks * block_tokens), __builtin_ctz((unsigned)block_tokens), slab,
-                       (int8_t *)k_codes, k_scale, (int8_t *)v_codes, v_scale);
+    auto kern = slab == 1 ? (D == 128 ? &kv8_append_kernel<128, true> : &kv8_append_kernel<64, true>)
+                          : (D == 128 ? &kv8_append_kernel<128, false> : &kv8_append_kernel<64, false>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, stream, ks, vs, (int)T, Hkv, slot, slots, shift, slab);
     return hipGetLastError();
 }
 

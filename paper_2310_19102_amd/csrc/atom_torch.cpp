@@ -757,7 +757,17 @@ PyObject *kv_block_map(Args a)
     const int64_t sizes[] = {B + 1, B, T, 1};
     const char *names[] = {"token_start", "seq_len", "slot", "cursor_out"};
     if (a[7] == Py_None) {
-        for (int i = 0; i < 4; ++i) out[i].fresh(make({sizes[i]}, kInt, past));
+        // four tensors in one allocation, each from a 128-byte boundary (an allocation takes 0.6 us, a tensor in one 0.2)
+        const auto up = [](int64_t n) { return (n + 31) / 32 * 32; };
+        const Tensor all = make({up(B + 1) + up(B) + up(T) + 1}, kInt, past);
+        int64_t at = 0;
+        for (int i = 0; i < 4; ++i) {
+            auto impl = c10::make_intrusive<at::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+            impl->set_storage_offset(at);
+            impl->set_sizes_contiguous(at::IntArrayRef(&sizes[i], 1));
+            out[i].fresh(Tensor(std::move(impl)));
+            at += up(sizes[i]);
+        }
     } else {
         PyObject *seq = PySequence_Tuple(a[7]);
         if (!seq) throw Raised();
