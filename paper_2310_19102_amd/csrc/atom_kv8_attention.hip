@@ -262,13 +262,13 @@ __device__ __forceinline__ float sum_of_chunks(float v)
 //           transposes.  No LDS, no lane exchange in the loop.  The weights travel as fp16 (rounded to nearest even: 2^-12 of themselves).
 //   loads: the next step's rows of K are asked for once the scores have used this step's, those of V after the values: half the registers of two
 //           buffers.  Block numbers and scales of 64 blocks of 16 keys are read at once, a lane each.
-constexpr int kWaves = 4, kStep = 32, kRowsLog = 4, kTileRows = 1 << kRowsLog;
+constexpr int kStep = 32, kRowsLog = 4, kTileRows = 1 << kRowsLog;
 
-template <int D>
+template <int D, int kWaves>
 struct RowsLds { float acc[kWaves][kTileRows][D + 4], m[kWaves][kTileRows], l[kWaves][kTileRows]; };
 
-template <int D, bool ONCE>
-__device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int index, RowsLds<D> &lds)
+template <int D, bool ONCE, int kWaves>
+__device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int index, RowsLds<D, kWaves> &lds)
 {
     constexpr int KB = D / 4, VB = D / 16;            // bytes of a K row and of a V row in a lane
     constexpr int KS = D / 32;                        // matrix instructions for 16 keys' scores
@@ -489,12 +489,12 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
     }
 }
 
-template <int D, bool ONCE>
+template <int D, bool ONCE, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, 4)
 void attention_kv8_rows_kernel(const Args a, const Job few)
 {
-    __shared__ alignas(16) RowsLds<D> lds;
-    rows_tile<D, ONCE>(a, few, blockIdx.x, lds);
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    rows_tile<D, ONCE, kWaves>(a, few, blockIdx.x, *reinterpret_cast<RowsLds<D, kWaves> *>(lds));
 }
 
 // ---------------------------------------------------------------- many query rows
@@ -823,9 +823,9 @@ __global__ __launch_bounds__(256, 2)
 void attention_kv8_step_kernel(const Args a, const Job few, const Job many)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    static_assert(sizeof(RowsLds<D>) <= 2 * TileLds<D>::bytes, "one workgroup's LDS");
+    static_assert(sizeof(RowsLds<D, 4>) <= 2 * TileLds<D>::bytes, "one workgroup's LDS");
     const int first = few.groups * a.Hkv;
-    if ((int)blockIdx.x < first) rows_tile<D, false>(a, few, blockIdx.x, *reinterpret_cast<RowsLds<D> *>(lds));
+    if ((int)blockIdx.x < first) rows_tile<D, false, 4>(a, few, blockIdx.x, *reinterpret_cast<RowsLds<D, 4> *>(lds));
     else                         many_rows_tile<D>(a, many, blockIdx.x - first, lds);
 }
 
@@ -907,8 +907,22 @@ constexpr int kFew = 64;
 constexpr int kFewWorkgroups = 1024, kFewBeside = 512, kManyWorkgroups = 256;
 // Beside many rows, sequences of up to so many keys are not cut (a merge is a launch of 4 us).
 constexpr int kUncutBeside = 4096;
+// Few rows alone, uncut: workgroups of 4, 8 or 16 wavefronts (the most that run at once and have a step each), where the longest sequence costs less than a
+// merge.  Its compute unit reads 50 bytes a ns; of a full card the shorter sequences of a batch leave it a part of what they would read.
+// Uncut / cut, us, the longest sequence 500, 1000, 2000 (lengths from a quarter of it): 32 cache heads of 128, one sequence 8.1 / 10.0, 10.6 / 10.0, 16.7 / 10.3;
+// 8 sequences 9.2 / 12.2, 13.1 / 15.5, 19.3 / 21.4; 8 cache heads, 64 sequences 12.6 / 17.2, 18.7 / 23.9, -; 4 of 64, one of 1000 6.8 / 8.2.
+constexpr double kUncutBytes = 205e3;
+int wavefronts(int64_t tiles, int Hkv, int D, int64_t capacity)              // 0: cut
+{
+    const int64_t groups = tiles * Hkv;
+    if (groups > kFewWorkgroups || capacity <= 128) return 4;
+    const int    room = groups <= kFewWorkgroups / 4 ? 16 : groups <= kFewWorkgroups / 2 ? 8 : 4;
+    const double full = (double)groups * room / (4 * kFewWorkgroups);
+    if ((double)capacity * 2 * D * (16 / room) * (1.0 - 0.75 * full) >= kUncutBytes) return 0;
+    return capacity <= 256 && room > 8 ? 8 : room;
+}
 
-struct Shape { Job few, many; size_t floats; };
+struct Shape { Job few, many; size_t floats; int waves; };    // waves: of a workgroup of few rows
 
 // `want` workgroups together, for each cache head: where there are fewer tiles (and 128 keys to a piece) they are cut.
 void size_job(Job &job, int64_t tiles, int part_rows, int64_t want, int Hkv, int64_t capacity, int subs)
@@ -937,8 +951,11 @@ Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t ca
     s.many.rows_max = 0x7fffffff;
     if (few_most) {
         const int64_t each = (int64_t)B * ((few_most + kTileRows - 1) / kTileRows), by_token = T * group / kTileRows + B;
-        size_job(s.few, each < by_token ? each : by_token, few_most < kTileRows ? few_most : kTileRows,
-                 !many ? kFewWorkgroups : capacity > kUncutBeside ? kFewBeside : 0, Hkv, capacity, 1);
+        const int64_t tiles = each < by_token ? each : by_token;
+        const int waves = many ? 4 : wavefronts(tiles, Hkv, D, capacity);
+        s.waves = waves ? waves : 4;
+        size_job(s.few, tiles, few_most < kTileRows ? few_most : kTileRows,
+                 !many ? (waves ? 0 : kFewWorkgroups) : capacity > kUncutBeside ? kFewBeside : 0, Hkv, capacity, 1);
     }
     if (many) {
         const int64_t least = few_most + 1, each = (int64_t)B * ((rows + kTile - 1) / kTile);
@@ -956,6 +973,21 @@ bool reads_once(const Args &a, int rows)
     return rows <= kTileRows && (int64_t)a.B * a.Hkv * a.capacity * 128 >= (int64_t)1 << 27;
 }
 
+template <int D, int kWaves>
+hipError_t launch_rows(const Args &a, const Job &few, dim3 grid, hipStream_t stream)
+{
+    constexpr int bytes = sizeof(RowsLds<D, kWaves>);
+    const bool once = reads_once(a, few.rows_max);
+    auto kern = once ? &attention_kv8_rows_kernel<D, true, kWaves> : &attention_kv8_rows_kernel<D, false, kWaves>;
+    if (bytes > 60 * 1024) {
+        static atom_launch::LdsOptIn opt[2];
+        hipError_t err = atom_launch::ensure_dynamic_lds(opt[once], reinterpret_cast<const void *>(kern), bytes);
+        if (err != hipSuccess) return err;
+    }
+    hipLaunchKernelGGL(kern, grid, dim3(kWaves * 64), bytes, stream, a, few);
+    return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch(const Args &a, Shape s, float *workspace, hipStream_t stream)
 {
@@ -963,8 +995,10 @@ hipError_t launch(const Args &a, Shape s, float *workspace, hipStream_t stream)
     s.many.part = workspace + records(s.few, a.Hkv, D);
     if (!s.many.groups) {
         if (!s.few.groups) return hipSuccess;
-        auto kern = reads_once(a, s.few.rows_max) ? &attention_kv8_rows_kernel<D, true> : &attention_kv8_rows_kernel<D, false>;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(s.few.groups * a.Hkv)), dim3(kWaves * 64), 0, stream, a, s.few);
+        const dim3 grid((unsigned)(s.few.groups * a.Hkv));
+        hipError_t err = s.waves == 16 ? launch_rows<D, 16>(a, s.few, grid, stream)
+                         : s.waves == 8 ? launch_rows<D, 8>(a, s.few, grid, stream) : launch_rows<D, 4>(a, s.few, grid, stream);
+        if (err != hipSuccess) return err;
     } else {
         static atom_launch::LdsOptIn opt;
         constexpr int bytes = 2 * TileLds<D>::bytes;

@@ -274,6 +274,38 @@ def test_attention_long(H, Hkv, D, bs, past, new):
     Case(H, Hkv, D, bs, past, new, seed=len(past)).check()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,Hkv,bs,past,new", [
+    (8, 2, 16, [3000, 0, 2100, 7, 900], [1, 1, 1, 1, 1]),                # pieces of several sequences, one of them none
+    (3, 3, 64, [2500, 1, 4100], [3, 2, 1]), (20, 1, 32, [2000, 3000], [2, 3]),
+    (4, 1, 128, [5000, 2999, 40], [1, 30, 16]),                          # beside requests of many rows, cut as well
+    (8, 8, 32, [4500, 100, 4200], [1, 200, 2]),
+    (2, 2, 16, [9000], [100])])                                          # tiles of many rows in pieces
+def test_attention_in_pieces(D, H, Hkv, bs, past, new):
+    """Keys cut into pieces that a second kernel merges, the pieces of each sequence about as long as the others'."""
+    c = Case(H, Hkv, D, bs, past, new, seed=H + bs)
+    assert atom.atom_attention_kv8_workspace_bytes(c.T, len(past), H, Hkv, D, c.max_new, c.W, bs) > 0
+    out = torch.empty_like(c.q)
+    for _ in range(2):                                      # (records of the first call are what the second finds)
+        c.check(out=out.fill_(float("nan")))
+
+
+@pytest.mark.parametrize("B,Hkv,past", [(3, 2, 600), (30, 8, 700), (40, 8, 300), (100, 8, 260), (140, 8, 100), (2, 1, 130)])
+def test_attention_workgroups_of_all_sizes(B, Hkv, past):
+    """16, 8 and 4 wavefronts to a tile of few rows."""
+    g = torch.Generator().manual_seed(B)
+    Case(Hkv, Hkv, 128, 32, torch.randint(0, past + 1, (B,), generator=g).tolist(), [1] * B, seed=B).check()
+
+
+def test_attention_pieces_of_many_requests():
+    """More than 64 requests, their keys in pieces."""
+    g = torch.Generator().manual_seed(9)
+    past = (torch.rand(70, generator=g) ** 4 * 3000).int().tolist()
+    c = Case(2, 1, 64, 16, past, [1] * 70, seed=70)
+    assert atom.atom_attention_kv8_workspace_bytes(70, 70, 2, 1, 64, 1, c.W, 16) > 0
+    c.check()
+
+
 @pytest.mark.parametrize("B", [63, 64, 65, 130, 200])
 def test_attention_many_requests(B):
     """More requests than a wavefront has lanes, some without tokens or keys."""
@@ -335,7 +367,7 @@ def test_attention_scales_far_apart(D):
 
 def test_attention_strides_and_given_memory():
     """Queries as a slice of the projection's output, outputs into a wider array, a workspace of the caller."""
-    c = Case(8, 4, 64, 32, [700, 50], [1, 3], seed=8)
+    c = Case(8, 4, 64, 32, [7000, 50], [1, 3], seed=8)
     want = c.check()
     qkv = torch.randn((c.T, 16, 64), device="cuda").to(torch.float16)
     qkv[:, 4:12] = c.q

@@ -40,7 +40,7 @@ def test_append_refusals(want, changed):
     assert atom.load_library().atom_kv8_append(*{**a, **changed}.values(), None) == want
 
 
-ATTENTION = dict(q=P, T=5, ldq=1024, B=3, H=8, Hkv=4, D=128, max_new=5, start=P, length=P, table=P, W=8, n=100, bs=64, kc=P, ks=P,
+ATTENTION = dict(q=P, T=5, ldq=1024, B=3, H=8, Hkv=4, D=128, max_new=5, start=P, length=P, table=P, W=99, n=100, bs=64, kc=P, ks=P,
                  vc=P, vs=P, sm=0.1, out=P, ldo=1024, ws=P, ws_bytes=1 << 30)
 
 
@@ -56,7 +56,7 @@ ATTENTION = dict(q=P, T=5, ldq=1024, B=3, H=8, Hkv=4, D=128, max_new=5, start=P,
     (ALIGN, dict(ldq=1028)), (ALIGN, dict(ldo=1026)), (WORKSPACE, dict(ws=None)), (WORKSPACE, dict(ws_bytes=4))])
 def test_attention_refusals(want, changed):
     lib = atom.load_library()
-    assert atom.atom_attention_kv8_workspace_bytes(5, 3, 8, 4, 128, 5, 8, 64) > 4
+    assert atom.atom_attention_kv8_workspace_bytes(5, 3, 8, 4, 128, 5, 99, 64) > 4
     assert lib.atom_attention_kv8(*{**ATTENTION, **changed}.values(), None) == want
 
 
@@ -65,6 +65,11 @@ def test_workspace_of_refused_and_of_unsplit_calls():
     assert need(1, 1, 32, 32, 128, 1, 16, 64) > 0
     assert need(4096, 4096, 32, 32, 128, 1, 16, 64) == 0                 # enough workgroups as it is
     assert need(1, 1, 32, 32, 128, 1, 2, 64) == 0                       # too few keys to share out
+    # uncut in workgroups of 16, 8 and 4 wavefronts as long as the longest sequence costs less than a merge
+    for B, Hkv, D, bs, W, cut in ((1, 32, 128, 64, 8, False), (1, 32, 128, 64, 16, True), (8, 32, 128, 64, 33, False), (8, 32, 128, 64, 60, True),
+                                  (1, 4, 64, 16, 70, False), (1, 4, 64, 16, 150, True), (64, 8, 128, 64, 16, False), (64, 8, 128, 64, 60, True),
+                                  (100, 8, 128, 128, 1, False), (100, 8, 128, 128, 20, True)):
+        assert (need(B, B, Hkv, Hkv, D, 1, W, bs) > 0) == cut, (B, Hkv, D, bs, W)
     for bad in ((1, 1, 32, 5, 128, 1, 16, 64), (1, 1, 32, 32, 96, 1, 16, 64), (1, 1, 32, 32, 128, 1, 16, 60), (-1, 1, 32, 32, 128, 1, 16, 64),
                 (0, 1, 32, 32, 128, 1, 16, 64), (1, 0, 32, 32, 128, 1, 16, 64), (1, 1, 32, 32, 128, 0, 16, 64)):
         assert need(*bad) == 0
