@@ -900,7 +900,7 @@ void attention_kv8_merge_kernel(const Args a, const Job few, const Job many)
 
 // ---------------------------------------------------------------- shape of a call
 
-// Requests of up to kFew query rows (tokens times the heads of a group) are work of the first kind, larger ones of the second.
+// Requests of up to kFew query rows (tokens times the heads of a group) are work of the first kind, larger ones of the second if the call has enough of that.
 constexpr int kFew = 64;
 // Workgroups that the card has room for at once: of the kernel of few rows; of few rows beside many; of many rows one a compute unit (two to one
 // are as fast each, and their tiles need not be cut: 28 tiles for each of 8 cache heads 45 us, cut to 512 43 us and 12 us for their merge).
@@ -938,13 +938,34 @@ void size_job(Job &job, int64_t tiles, int part_rows, int64_t want, int Hkv, int
 
 size_t records(const Job &job, int Hkv, int D) { return job.budget ? (size_t)job.groups * Hkv * job.part_rows * (D + 4) : 0; }
 
+int64_t many_tiles(int64_t T, int B, int group, int64_t rows, int few_most)
+{
+    const int64_t each = (int64_t)B * ((rows + kTile - 1) / kTile), requests = T * group / (few_most + 1) < B ? T * group / (few_most + 1) : B;
+    return each < T * group / kTile + requests ? each : T * group / kTile + requests;
+}
+
+// Whether a call's requests of more than kFew rows are better tiles of 128 rows, in us, by what the host knows (tables may be wider than they are full).
+// 16 rows at a time the work spreads over the card, but turns each code into halves eight times as often: 1.8 us for a million pairs of rows and keys (D = 64:
+// 0.85).  128 at a time a tile takes 1.5 us for 64 keys, 1.85 where two share a compute unit, and where the tiles are fewer than the compute units their pieces and
+// the merge take 18.  Tiles / 16 rows, measured (tokens, earlier keys): heads 64 on 8: 1000 33.1 / 60.7 us, 2000 88.9 / 193, 299 (229) 22.3 / 20.5, 100 (3000) 34.1 / 47.8,
+// 65 (679) 19.0 / 17.3; 32 on 32: 1000 29.6 / 34.0; 16 on 4: 1046 (398) 40.3 / 34.0, 2 x 470 20.6 / 13.0; 20 on 1: 3 x 353 20.4 / 10.5, 3000 77 / 138; 12 on 12: 2 x 196 16.0 / 6.2;
+// of 64: 16 on 4: 3000 59.8 / 53.5, 12 on 12: 2000 (1000) 62.3 / 38.2, 64 on 8: 4 x 706 28.2 / 39.1.
+bool worth_tiles(int64_t T, int64_t tiles, int Hkv, int group, int D, int max_new, int64_t capacity)
+{
+    const double keys = max_new < capacity ? (double)capacity - 0.5 * max_new : 0.5 * (double)capacity, steps = (double)capacity / 64, n = (double)tiles * Hkv;
+    const double few = 6 + (double)T * group * Hkv * keys * 1e-6 * (D == 128 ? 1.8 : 0.85);
+    const double shared = n * keys / 64 * 0.0048, alone = steps * (n > 256 ? 1.85 : 1.5);
+    const double many = (kManyWorkgroups + Hkv - 1) / Hkv > tiles ? 18 + n * steps / 256 * 1.95 : 7 + (shared > alone ? shared : alone);
+    return many * (D == 128 ? 1.0 : 0.8) < few;
+}
+
 Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t capacity)
 {
     Shape s = {};
     if (T == 0 || B == 0 || max_new == 0) return s;
     const int64_t rows = (int64_t)max_new * group;   // of one request, at most
-    const bool many = rows > kFew;
-    const int  few_most = (int)(many ? (B > 1 ? kFew : 0) : rows);       // (one request is work of the second kind whatever its size)
+    const bool many = rows > kFew && worth_tiles(T, many_tiles(T, B, group, rows, B > 1 ? kFew : 0), Hkv, group, D, max_new, capacity);
+    const int  few_most = many ? (B > 1 ? kFew : 0) : (int)rows;         // (one request is work of the second kind whatever its size)
     s.few.rows_min = 1;
     s.few.rows_max = few_most;
     s.many.rows_min = few_most + 1;
@@ -958,9 +979,7 @@ Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t ca
                  !many ? (waves ? 0 : kFewWorkgroups) : capacity > kUncutBeside ? kFewBeside : 0, Hkv, capacity, 1);
     }
     if (many) {
-        const int64_t least = few_most + 1, each = (int64_t)B * ((rows + kTile - 1) / kTile);
-        const int64_t requests = T * group / least < B ? T * group / least : B, by_token = T * group / kTile + requests;
-        size_job(s.many, each < by_token ? each : by_token, kTile, kManyWorkgroups, Hkv, capacity, kTile / kTileRows);
+        size_job(s.many, many_tiles(T, B, group, rows, few_most), kTile, kManyWorkgroups, Hkv, capacity, kTile / kTileRows);
     }
     s.floats = records(s.few, Hkv, D) + records(s.many, Hkv, D);
     return s;
@@ -1030,6 +1049,14 @@ bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new, int64_t W
     const double most = (tiles < each ? tiles : each) + kFewWorkgroups;
     (void)W; (void)block_tokens;
     return 2.0 * most * Hkv < 2147483647.0;
+}
+
+// How a call of these sizes runs, as its tests ask it: wavefronts of a workgroup of few rows, 32 where those requests' keys may be cut, 64 where
+// requests of many rows are tiles of 128, 128 where those may be cut.
+extern "C" int atom_internal_attention_kv8_route(int64_t T, int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t max_new, int64_t W, int32_t block_tokens)
+{
+    const Shape s = shape(T, B, Hkv, H / Hkv, D, max_new, W * block_tokens);
+    return (s.few.groups ? (s.many.groups ? 4 : s.waves) : 0) + (s.few.budget ? 32 : 0) + (s.many.groups ? 64 : 0) + (s.many.budget ? 128 : 0);
 }
 
 hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)

@@ -1,11 +1,14 @@
 """The paged 8-bit KV cache on the GPU against plain implementations: tables, codes and scales bit for bit, attention in 64
 bits within the rounding of its fp16 weights and output."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2310_19102_amd as atom
 import _kv8_ref as ref
+from paper_2310_19102_amd import binding
 
 pytestmark = pytest.mark.gpu
 
@@ -234,6 +237,13 @@ class Case:
         return atom.atom_attention_kv8(kw.pop("q", self.q), self.kc, self.vc, self.table, self.start, self.len, self.sm,
                                        **{"max_new": self.max_new, **kw})
 
+    def route(self, max_new=-1):
+        """(wavefronts of a workgroup of few rows, their keys may be cut, tiles of many rows, theirs may be cut)"""
+        (n, Hkv, bs, D), (T, H, _) = self.kc[0].shape, self.q.shape
+        ask = ctypes.CDLL(binding._LIB_PATH).atom_internal_attention_kv8_route
+        r = ask(ctypes.c_int64(T), self.table.shape[0], H, Hkv, D, self.max_new if max_new == -1 else max_new, ctypes.c_int64(self.W), bs)
+        return r & 31, bool(r & 32), bool(r & 64), bool(r & 128)
+
     def check(self, got=None, **kw):
         got = self.call(**kw) if got is None else got
         want, tol, done = ref.attention(npy(self.q), [npy(t) for t in self.kc], [npy(t) for t in self.vc], npy(self.table),
@@ -267,6 +277,38 @@ def test_attention_several_tokens(D, bs, H, Hkv):
     Case(H, Hkv, D, bs, past, new, seed=D + H).check(max_new=None)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bs", [16, 32, 64, 128])
+@pytest.mark.parametrize("H,Hkv,past,new", [
+    (16, 2, [0, 64, 300, 7, 90], [257, 330, 170, 0, 1]), (20, 1, [31, 0, 500], [65, 129, 3]), (3, 3, [63], [1100]), (64, 4, [250], [40])])
+def test_attention_tiles_of_many_rows(D, bs, H, Hkv, past, new):
+    """The same in tiles of 128 rows, which short calls take where the tables have room for long sequences; few-row requests beside them."""
+    c = Case(H, Hkv, D, bs, past, new, seed=D + H, extra=(1 << 20) // bs)
+    assert c.route()[2]
+    c.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_tiles_that_see_nothing(D):
+    """Rows in front of the first position, keys that no block holds, padded tokens, in tiles of 128 rows."""
+    c = Case(16, 1, D, 32, [0, 100, 40], [150, 90, 200], seed=D, pad=9, extra=1 << 15)
+    c.len = i32(60, 0, 240)
+    c.q[440:] = float("inf")
+    c.table[2, 1] = -1
+    c.table[2, 4] = 2 ** 30
+    assert c.route()[2]
+    out = torch.full_like(c.q, 7.0)
+    c.check(out=out)
+    assert (out[440:] == 7.0).all() and (out[:90] == 0).all() and (out[150:240] == 0).all()
+    part = torch.full_like(c.q, 7.0)
+    c.call(out=part, max_new=100)                           # the last tokens of a request left out
+    for b, n in enumerate((150, 90, 200)):
+        s = int(c.start[b])
+        m = min(n, 100)
+        assert (part[s + m:s + n] == 7.0).all()
+        assert ((part[s:s + m].float() - out[s:s + m].float()).abs() <= 2.0 ** -9 * out[s:s + m].float().abs() + 1e-3).all()
+
+
 @pytest.mark.parametrize("H,Hkv,D,bs,past,new", [
     (32, 32, 128, 64, [1000], [1]), (64, 8, 128, 16, [5000, 17], [1, 1]), (8, 1, 64, 32, [20000], [1]), (4, 4, 128, 128, [4000, 3], [2, 9]),
     (64, 8, 128, 64, [0], [300]), (16, 4, 64, 16, [3000], [64]), (16, 16, 128, 32, [10, 2000, 0], [1, 200, 90])])
@@ -283,8 +325,8 @@ def test_attention_long(H, Hkv, D, bs, past, new):
     (2, 2, 16, [9000], [100])])                                          # tiles of many rows in pieces
 def test_attention_in_pieces(D, H, Hkv, bs, past, new):
     """Keys cut into pieces that a second kernel merges, the pieces of each sequence about as long as the others'."""
-    c = Case(H, Hkv, D, bs, past, new, seed=H + bs)
-    assert atom.atom_attention_kv8_workspace_bytes(c.T, len(past), H, Hkv, D, c.max_new, c.W, bs) > 0
+    c = Case(H, Hkv, D, bs, past, new, seed=H + bs, extra=3000)
+    assert c.route()[1] or c.route()[3]
     out = torch.empty_like(c.q)
     for _ in range(2):                                      # (records of the first call are what the second finds)
         c.check(out=out.fill_(float("nan")))
@@ -294,7 +336,9 @@ def test_attention_in_pieces(D, H, Hkv, bs, past, new):
 def test_attention_workgroups_of_all_sizes(B, Hkv, past):
     """16, 8 and 4 wavefronts to a tile of few rows."""
     g = torch.Generator().manual_seed(B)
-    Case(Hkv, Hkv, 128, 32, torch.randint(0, past + 1, (B,), generator=g).tolist(), [1] * B, seed=B).check()
+    c = Case(Hkv, Hkv, 128, 32, torch.randint(0, past + 1, (B,), generator=g).tolist(), [1] * B, seed=B)
+    assert c.route() == ({3: 16, 30: 16, 40: 8, 100: 4, 140: 4, 2: 8}[B], False, False, False)
+    c.check()
 
 
 def test_attention_pieces_of_many_requests():
@@ -347,11 +391,12 @@ def test_attention_pages_that_do_not_exist():
     c.check()
 
 
-@pytest.mark.parametrize("D", [64, 128])
-def test_attention_scales_far_apart(D):
+@pytest.mark.parametrize("D,new", [(64, [2, 1]), (128, [2, 1]), (64, [230, 240]), (128, [150, 40])])
+def test_attention_scales_far_apart(D, new):
     """Blocks whose scales differ by many orders of magnitude, zeros among them: the weights keep their precision wherever the
     mass lies."""
-    c = Case(4, 2, D, 16, [200, 333], [2, 1], seed=11)
+    c = Case(16, 2, D, 16, [200, 333], new, seed=11, extra=1 if new[0] == 2 else 1 << 16)
+    assert c.route()[2] == (new[0] > 2)
     g = torch.Generator(device="cuda").manual_seed(1)
     for i, (_, s) in enumerate((c.kc, c.vc)):
         s.copy_(torch.pow(10.0, torch.empty(s.shape, device="cuda").uniform_(-9 + 5 * i, -1 + 2 * i, generator=g)))
