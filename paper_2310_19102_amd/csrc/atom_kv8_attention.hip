@@ -681,9 +681,30 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        // M is a bound on e but for the last few binary orders: what passes it by many shows in the sums (the first keys of a row: M is none yet).  No
+        // maxima where it does not, a sixth of the vector unit's work.
+        if (__ballot(sum[0] > 1024.0f || sum[1] > 1024.0f)) {
+            const float top = fmaxf(largest(now, 0), largest(now, 1));
+            const float to = fmaxf(M, fmaxf(top, __shfl_xor(top, 32, 64)));
+            const float down = __builtin_amdgcn_exp2f(M - to);
+            M = to;
+            l *= down;
+#pragma unroll
+            for (int i = 0; i < DB; ++i) o[i] *= down;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                sum[b] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(now[8 * b + i], factor[b], shift[b] - M));
+                    sum[b] += e;
+                    p[b][i] = (_Float16)e;
+                }
+            }
+        }
         l = fmaf(sum[0], inv[0], l);
         l = fmaf(sum[1], inv[1], l);
-        float top[2];
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) {
             if (i + kAhead < 2 * DB) read(KS + i + kAhead);
@@ -691,11 +712,8 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
 #pragma unroll
             for (int k = pieces * i / (2 * DB); k < pieces * (i + 1) / (2 * DB); ++k) stage(k);
             if (i == 0) scales_of(at);
-            if (i == 2 * DB - 3) top[0] = largest(then, 0);
-            if (i == 2 * DB - 2) top[1] = largest(then, 1);
             __builtin_amdgcn_sched_barrier(0);
         }
-        return fmaxf(top[0], top[1]);
     };
     auto first_scores = [&](const unsigned char *buf, f16v &s) {
 #pragma unroll
@@ -704,22 +722,13 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
         for (int i = 0; i < KS; ++i)
             s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(buf + L::k + (32 + n) * L::kPitch + 16 * hh + 32 * i), q[i], s, 0, 0, 0);
     };
-    // Scores of the 32 keys from `key` on: those that a row does not see, and M where some e passes it by 8.
-    auto look = [&](int key, f16v &s, float top) __attribute__((always_inline)) {
+    // Scores of the 32 keys from `key` on: minus infinity where a row does not see them.
+    auto mask = [&](int key, f16v &s) __attribute__((always_inline)) {
         if (key + 32 > least) {                       // (the same in all lanes)
             const int room = min(sees, key1) - (key + 4 * hh);
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (8 * (i >> 2) + (i & 3) >= room) s[i] = -INFINITY;
-            top = fmaxf(largest(s, 0), largest(s, 1));
-        }
-        if (__ballot(top > M + 8.0f)) {               // rare after the first tiles
-            const float to = fmaxf(M, fmaxf(top, __shfl_xor(top, 32, 64)));
-            const float down = __builtin_amdgcn_exp2f(M - to);
-            M = to;
-            l *= down;
-#pragma unroll
-            for (int i = 0; i < DB; ++i) o[i] *= down;
         }
     };
 
@@ -751,7 +760,7 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
         f16v x, y;
         first_scores(lds + L::bytes, x);
         scales_of(0);
-        look(key0, x, fmaxf(largest(x, 0), largest(x, 1)));
+        mask(key0, x);
         __syncthreads();
         int at = 0;
         for (int t = 0; t < tiles; ++t, at ^= L::bytes) {
@@ -760,8 +769,8 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
             auto next_k = [&](int k) __attribute__((always_inline)) { stage_k(next, kr, k); };
             auto next_v = [&](int k) __attribute__((always_inline)) { stage_v(next, k); };
             if (key < wave1) {                        // (the same in all lanes)
-                const float top = half_tile(here, 0, x, y, block + 2, next_k, kPieces);
-                look(key + 32, y, top);
+                half_tile(here, 0, x, y, block + 2, next_k, kPieces);
+                mask(key + 32, y);
             } else {
 #pragma unroll
                 for (int k = 0; k < kPieces; ++k) next_k(k);
@@ -770,8 +779,8 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
             if (block == 60) take_scales();
             fetch_k(unit_k, ahead, kr);
             if (key + 32 < wave1) {
-                const float top = half_tile(here, 1, y, x, (block + 4) & 63, next_v, vPieces);
-                look(key + 64, x, top);
+                half_tile(here, 1, y, x, (block + 4) & 63, next_v, vPieces);
+                mask(key + 64, x);
             } else {
 #pragma unroll
                 for (int k = 0; k < vPieces; ++k) next_v(k);
