@@ -911,9 +911,12 @@ void attention_kv8_merge_kernel(const Args a, const Job few, const Job many)
 
 // Requests of up to kFew query rows (tokens times the heads of a group) are work of the first kind, larger ones of the second if the call has enough of that.
 constexpr int kFew = 64;
-// Workgroups that the card has room for at once: of the kernel of few rows; of few rows beside many; of many rows one a compute unit (two to one
-// are as fast each, and their tiles need not be cut: 28 tiles for each of 8 cache heads 45 us, cut to 512 43 us and 12 us for their merge).
+// Workgroups that the card has room for at once: of the kernel of few rows; of few rows beside many; of many rows one a compute unit, and two.
 constexpr int kFewWorkgroups = 1024, kFewBeside = 512, kManyWorkgroups = 256;
+// Tiles of many rows are cut to one workgroup a compute unit, and to two where they fill half of those at most and sequences are long: then a tile is
+// halved at least, which pays for the pieces' starts and the merge (tokens, earlier keys: heads 64 on 8, 200 (6000) 80.2 -> 69.3 us, 2 x 300 (2000) 56.1 -> 47.0; 32 on 32,
+// 400 (4000) 63.1 -> 54.9; but 32 single tokens and two chunks of 125 and 318 (2000), which share the card, 48.1 -> 57.5).
+int many_workgroups(int64_t tiles, int Hkv, int64_t capacity) { return tiles * Hkv <= kManyWorkgroups && capacity >= 1536 ? 2 * kManyWorkgroups : kManyWorkgroups; }
 // Beside many rows, sequences of up to so many keys are not cut (a merge is a launch of 4 us).
 constexpr int kUncutBeside = 4096;
 // Few rows alone, uncut: workgroups of 4, 8 or 16 wavefronts (the most that run at once and have a step each), where the longest sequence costs less than a
@@ -955,8 +958,8 @@ int64_t many_tiles(int64_t T, int B, int group, int64_t rows, int few_most)
 
 // Whether a call's requests of more than kFew rows are better tiles of 128 rows, in us, by what the host knows (tables may be wider than they are full).
 // 16 rows at a time the work spreads over the card, but turns each code into halves eight times as often: 1.8 us for a million pairs of rows and keys (D = 64:
-// 0.85).  128 at a time a tile takes 1.5 us for 64 keys, 1.85 where two share a compute unit, and where the tiles are fewer than the compute units their pieces and
-// the merge take 18.  Tiles / 16 rows, measured (tokens, earlier keys): heads 64 on 8: 1000 33.1 / 60.7 us, 2000 88.9 / 193, 299 (229) 22.3 / 20.5, 100 (3000) 34.1 / 47.8,
+// 0.85).  128 at a time a tile takes 1.5 us for 64 keys, 1.85 where two share a compute unit, and where tiles are cut
+// their pieces' starts and the merge take 18.  Tiles / 16 rows, measured (tokens, earlier keys): heads 64 on 8: 1000 33.1 / 60.7 us, 2000 88.9 / 193, 299 (229) 22.3 / 20.5, 100 (3000) 34.1 / 47.8,
 // 65 (679) 19.0 / 17.3; 32 on 32: 1000 29.6 / 34.0; 16 on 4: 1046 (398) 40.3 / 34.0, 2 x 470 20.6 / 13.0; 20 on 1: 3 x 353 20.4 / 10.5, 3000 77 / 138; 12 on 12: 2 x 196 16.0 / 6.2;
 // of 64: 16 on 4: 3000 59.8 / 53.5, 12 on 12: 2000 (1000) 62.3 / 38.2, 64 on 8: 4 x 706 28.2 / 39.1.
 bool worth_tiles(int64_t T, int64_t tiles, int Hkv, int group, int D, int max_new, int64_t capacity)
@@ -964,7 +967,8 @@ bool worth_tiles(int64_t T, int64_t tiles, int Hkv, int group, int D, int max_ne
     const double keys = max_new < capacity ? (double)capacity - 0.5 * max_new : 0.5 * (double)capacity, steps = (double)capacity / 64, n = (double)tiles * Hkv;
     const double few = 6 + (double)T * group * Hkv * keys * 1e-6 * (D == 128 ? 1.8 : 0.85);
     const double shared = n * keys / 64 * 0.0048, alone = steps * (n > 256 ? 1.85 : 1.5);
-    const double many = (kManyWorkgroups + Hkv - 1) / Hkv > tiles ? 18 + n * steps / 256 * 1.95 : 7 + (shared > alone ? shared : alone);
+    const int    want = many_workgroups(tiles, Hkv, capacity);
+    const double many = (want + Hkv - 1) / Hkv > tiles ? 18 + n * steps / 256 * (want > kManyWorkgroups ? 1.2 : 1.95) : 7 + (shared > alone ? shared : alone);
     return many * (D == 128 ? 1.0 : 0.8) < few;
 }
 
@@ -988,7 +992,8 @@ Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t ca
                  !many ? (waves ? 0 : kFewWorkgroups) : capacity > kUncutBeside ? kFewBeside : 0, Hkv, capacity, 1);
     }
     if (many) {
-        size_job(s.many, many_tiles(T, B, group, rows, few_most), kTile, kManyWorkgroups, Hkv, capacity, kTile / kTileRows);
+        const int64_t tiles = many_tiles(T, B, group, rows, few_most);
+        size_job(s.many, tiles, kTile, many_workgroups(tiles, Hkv, capacity), Hkv, capacity, kTile / kTileRows);
     }
     s.floats = records(s.few, Hkv, D) + records(s.many, Hkv, D);
     return s;
