@@ -601,8 +601,8 @@ atom_status atom_kv_block_map(const int32_t *past_len, const int32_t *new_len, i
  *   and where s > s_old > 0 the o older rows' codes become rne(code * (s_old / s)).
  * IEEE fp32, every step rounded once: results are bit-exact.  A row is off by half a step of the block's scale when it is
  * written, and by at most half a step of the present scale more each time that the scale has grown since.
- * Rows of the block behind the run are left as they are.  The same call again changes nothing but older rows'
- * scales that it raised the first time.
+ * Rows of the block behind the run are left as they are.  The same call once more changes nothing.
+ * A value that is not finite spoils its block for its head, nothing else.
  *
  *   k_f16, v_f16   device fp16, token t's heads from t * ldk (ldv) on, [Hkv, D] each; 16-byte aligned, ld % 8 == 0: slices
  *                  of a fused projection's output as they are
@@ -627,7 +627,8 @@ atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int
  * fp32 softmax and sums; queries and codes meet exactly in the fp16 matrix cores, the softmax weights travel as fp16.
  * Keys of a block number outside [0, n_blocks) (-1: none) and beyond W * block_tokens do not exist; a query
  * that sees no key gives zeros.  Rows of out behind token_start[B], and of tokens beyond max_new of a request, are left as
- * they were; rows of q there are not read.
+ * they were; rows of q there are not read.  out may be q itself (with ldo = ldq), and overlaps no input otherwise.  A block whose scale is not finite spoils the
+ * queries that see it, no other.
  *
  *   q_f16          device fp16, token t's heads [H, D] from t * ldq on; out_f16 likewise with ldo.  16-byte aligned, ld % 8 == 0
  *   max_new        no request has more new tokens (T if nothing is known: the call is sized by it, 1 for a decoding step)

@@ -578,7 +578,7 @@ def atom_attention_kv8(q: torch.Tensor, k_cache: Tuple[torch.Tensor, ...], v_cac
     """Causal attention of a step's queries ``q`` [T, H, D] fp16 over the paged 8-bit cache: request b's tokens are
     ``token_start[b] .. token_start[b + 1]``, the last ones of its ``seq_len[b]`` positions, and the cache holds them
     already.  ``max_new``: no request has more new tokens (None: unknown; 1 for a decoding step).  Returns [T, H, D] fp16 (``out``
-    if given; rows behind the last request are left as they were).  In a capture that was not begun by torch.cuda.graph a
+    if given, which may be ``q``; rows behind the last request are left as they were, of a new output without a value).  In a capture that was not begun by torch.cuda.graph a
     ``workspace`` has to be given where ``atom_attention_kv8_workspace_bytes`` is not 0."""
     return _run().attention_kv8(q, k_cache, v_cache, block_table, token_start, seq_len, sm_scale,
                                 q.shape[0] if max_new is None else max_new, out, workspace)

@@ -142,7 +142,7 @@ struct AttentionKv8 {
     void *workspace;
 };
 size_t     attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, int max_new, int64_t W, int block_tokens);
-bool       attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new, int64_t W, int block_tokens);   // its grid
+bool       attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new);   // its grid
 hipError_t launch_attention_kv8(const AttentionKv8 &a, hipStream_t stream);
 
 // The library's own per-GPU scratch array (for the entry point that allocates nothing): its size,

@@ -21,6 +21,10 @@ typedef unsigned u2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e   = 1.4426950408889634f;
 constexpr float kNoScore = -1e30f;                // the running maximum before the first key: below every score, and finite
+constexpr int   kAllKeys = 0x40000000;            // as many as a request has at most, and a multiple of 128
+// A block's factor and value scale as the kernels take them lie between these: never zero and never infinite, so that a masked score of minus infinity
+// stays one whatever the block holds, and a block of zeros has a weight to be divided out again.
+constexpr float kLeastFactor = 1e-37f, kLeastValue = 2.3283064365386963e-10f, kMost = 1e35f;
 
 // What all kernels of a call are told.
 struct Args {
@@ -119,7 +123,7 @@ __device__ __forceinline__ Place place(const Args &a, const Job &job, int index)
     p.found = false;
     int tiles, keys;
     tiles_keys(0, tiles, keys);
-    int per = 0x3fffff80;                         // keys of a piece at most, a multiple of 128: one step of 32 for each of four wavefronts
+    int per = kAllKeys;                           // keys of a piece at most, a multiple of 128: one step of 32 for each of four wavefronts
     if (budget) {                                 // (with more than 64 requests r is read again below)
         // sum over tiles of ceil(keys / per) is below tiles + all / per
         int64_t mine = (int64_t)tiles * keys;
@@ -135,7 +139,7 @@ __device__ __forceinline__ Place place(const Args &a, const Job &job, int index)
             const float all = total((float)mine) * 1.00001f;          // (64 values: rounded by less than that)
             auto share = [&](float pieces) {
                 const float want = ceilf(all / (128.0f * pieces));
-                return want < 1.0f ? 128 : want < 8388607.0f ? 128 * (int)want : 0x3fffff80;
+                return want < 1.0f ? 128 : want < 8388607.0f ? 128 * (int)want : kAllKeys;
             };
             per = share((float)(budget - count));
             if (a.B <= 64) {                      // mostly it is half a piece a tile less
@@ -168,7 +172,7 @@ __device__ __forceinline__ Place place(const Args &a, const Job &job, int index)
                 p.split = (index - s0) - p.tile * p.splits;
             }
             const int all = __builtin_amdgcn_readlane(keys, l);
-            p.keys_per = p.splits == 1 ? 0x3fffff80 : ((all + p.splits - 1) / p.splits + 127) & ~127;      // even pieces
+            p.keys_per = p.splits == 1 ? kAllKeys : ((all + p.splits - 1) / p.splits + 127) & ~127;      // even pieces
             p.first_slot = s0 + p.tile * p.splits;
             return p;
         }
@@ -316,9 +320,8 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
         b_log = a.vs[at];
     };
     auto take_scales = [&]() {                        // (no such keys: e is minus infinity)
-        const float v = fmaxf(b_log, 2.3283064365386963e-10f);
-        // (never zero: a masked score of minus infinity stays one, and a block of zeros has a weight to be divided out again)
-        b_scale = unit < 0 ? 1.0f : fmaxf(b_scale * to_e, 1e-37f);
+        const float v = fminf(fmaxf(b_log, kLeastValue), kMost);
+        b_scale = unit < 0 ? 1.0f : fminf(fmaxf(b_scale * to_e, kLeastFactor), kMost);
         b_log = unit < 0 ? -INFINITY : __builtin_amdgcn_logf(v);
         b_inv = unit < 0 ? 0.0f : __builtin_amdgcn_rcpf(v);
     };
@@ -540,7 +543,7 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, hh = lane >> 5;
     const int all = r.n * a.group;
-    const int tile = (all + kTile - 1) / kTile - 1 - w.tile;
+    const int tile = ((all - 1) >> kTileLog) - w.tile;
     const int row0 = tile * kTile + wave * 32, rows = min(32, all - row0);      // of this wavefront; none: rows <= 0
     const int row = min(row0 + n, all - 1);
     const int token = by_group(a, row), head = h * a.group + row - token * a.group;
@@ -587,9 +590,8 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
         vs = a.vs[at];
     };
     auto take_scales = [&]() {
-        const float v = fmaxf(vs, 2.3283064365386963e-10f);
-        // (never zero: a masked score of minus infinity stays one, and a block of zeros has a weight to be divided out again)
-        b_scale = unit < 0 ? 1.0f : fmaxf(ks * to_e, 1e-37f);
+        const float v = fminf(fmaxf(vs, kLeastValue), kMost);
+        b_scale = unit < 0 ? 1.0f : fminf(fmaxf(ks * to_e, kLeastFactor), kMost);
         b_log = unit < 0 ? -INFINITY : __builtin_amdgcn_logf(v);
         b_inv = unit < 0 ? 0.0f : __builtin_amdgcn_rcpf(v);
     };
@@ -1056,12 +1058,11 @@ size_t attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, in
     return shape(T, B, Hkv, H / Hkv, D, max_new, W * block_tokens).floats * sizeof(float);
 }
 
-bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new, int64_t W, int block_tokens)
+bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new)
 {
     // every count is below (rows / 16 + B) * blocks of 128 rows and the workgroups wanted, as doubles here
     const double group = H / Hkv, rows = (double)max_new * group, tiles = (double)T * group / kTileRows + B, each = (double)B * (rows / kTileRows + 1);
     const double most = (tiles < each ? tiles : each) + kFewWorkgroups;
-    (void)W; (void)block_tokens;
     return 2.0 * most * Hkv < 2147483647.0;
 }
 

@@ -192,6 +192,21 @@ def test_append_takes_slices_of_a_projection_and_any_slots():
     atom.atom_kv8_append(qkv[:0, :Hkv], qkv[:0, :Hkv], kc, vc, i32())
 
 
+def test_append_of_what_is_not_finite_spoils_its_own_block_and_head():
+    D, bs, Hkv, T = 128, 32, 3, 90
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn((T, Hkv, D), generator=g, device="cuda").to(torch.float16) for _ in "kv")
+    kc, vc = caches(5, Hkv, bs, D, seed=1)
+    slot = torch.arange(40, 40 + T, dtype=torch.int32, device="cuda")
+    want = [ref.append(npy(x), npy(c), npy(s), npy(slot)) for x, (c, s) in ((k, kc), (v, vc))]
+    k[30, 1, 7], v[60, 2, 100], v[61, 2, 3] = float("inf"), float("nan"), -float("inf")
+    atom.atom_kv8_append(k, v, kc, vc, slot)
+    for (codes, scale), (wc, ws), spoiled in ((kc, want[0], (2, 1)), (vc, want[1], (3, 2))):
+        same = np.ones((5, Hkv), bool)
+        same[spoiled] = False
+        assert np.array_equal(npy(codes)[same], wc[same]) and np.array_equal(npy(scale)[same], ws[same])
+
+
 def test_append_large_and_long_runs():
     """Enough tokens for every number of tokens to a wavefront that the call picks."""
     for T, Hkv in ((1500, 2), (3000, 8), (9000, 16)):
@@ -244,12 +259,15 @@ class Case:
         r = ask(ctypes.c_int64(T), self.table.shape[0], H, Hkv, D, self.max_new if max_new == -1 else max_new, ctypes.c_int64(self.W), bs)
         return r & 31, bool(r & 32), bool(r & 64), bool(r & 128)
 
-    def check(self, got=None, **kw):
+    def check(self, got=None, rows=None, heads=slice(None), **kw):
+        """The call (or what it gave) against 64 bits; `rows`: of these tokens only, `heads`: of these only (one cache head)."""
         got = self.call(**kw) if got is None else got
-        want, tol, done = ref.attention(npy(self.q), [npy(t) for t in self.kc], [npy(t) for t in self.vc], npy(self.table),
+        want, tol, done = ref.attention(npy(self.q[:, heads]), [npy(t) for t in self.kc], [npy(t) for t in self.vc], npy(self.table),
                                         npy(self.start), npy(self.len), self.sm)
-        off = np.abs(npy(got).astype(np.float64) - want)
-        assert np.isfinite(npy(got)[done]).all()
+        if rows is not None:
+            done &= np.isin(np.arange(self.T), rows)
+        off = np.abs(npy(got[:, heads]).astype(np.float64) - want)
+        assert np.isfinite(npy(got[:, heads])[done]).all()
         worst = (off / np.maximum(tol, 1e-30))[done]
         assert worst.size == 0 or worst.max() <= 1.0, f"{worst.max():.2f} of the bound at {np.unravel_index(worst.argmax(), worst.shape)}"
         return got
@@ -339,6 +357,59 @@ def test_attention_workgroups_of_all_sizes(B, Hkv, past):
     c = Case(Hkv, Hkv, 128, 32, torch.randint(0, past + 1, (B,), generator=g).tolist(), [1] * B, seed=B)
     assert c.route() == ({3: 16, 30: 16, 40: 8, 100: 4, 140: 4, 2: 8}[B], False, False, False)
     c.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("past,new,cut", [(1500, 260, False), (6500, 100, True)])
+def test_attention_long_tiles_of_many_rows(D, past, new, cut):
+    """More than 1024 keys to a workgroup of the tiles of 128 rows, which looks its blocks up 1024 at a time."""
+    c = Case(128, 1, D, 32, [past], [new], seed=D)
+    assert c.route()[2:] == (True, cut)
+    c.check(heads=slice(5, None, 17))
+
+
+def test_attention_of_the_longest_table():
+    """2^30 keys, the most that a table may have: 8388608 times the same block, whose own softmax it is.  A wavefront adds 2^14 sums to its total, each rounded
+    by 2^-24 of it at most, and so the values: 2^-10 for each of the two."""
+    D, bs = 64, 128
+    c = Case(1, 1, D, bs, [127], [1], seed=3)
+    one = npy(c.q), [npy(t) for t in c.kc]
+    of = lambda v: ref.attention(*one, v, npy(c.table), npy(c.start), npy(c.len), c.sm)          # noqa: E731
+    want, tol, _ = of([npy(t) for t in c.vc])
+    mass = of([np.abs(npy(t)) for t in c.vc])[0]
+    table = c.table[:, :1].expand(1, 2 ** 30 // bs).contiguous()
+    got = atom.atom_attention_kv8(c.q, c.kc, c.vc, table, c.start, i32(2 ** 30), c.sm, max_new=1)
+    assert (np.abs(npy(got) - want) <= tol + 2.0 ** -9 * mass).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("extra", [1, 1 << 16])
+def test_attention_spoiled_blocks_reach_nobody_else(D, extra):
+    """Blocks whose scales are infinite or no numbers: queries before their tokens, and other requests, do not see them."""
+    c = Case(16, 2, D, 16, [100, 30], [60, 70], seed=D, extra=extra)
+    assert c.route()[2] == (extra > 1)
+    c.kc[1][c.table[0, 7].long()] = float("inf")
+    c.vc[1][c.table[0, 8].long()] = float("inf")
+    for _, s in (c.kc, c.vc):
+        s[c.table[0, 9].long()] = float("nan")
+    c.check(rows=[*range(112 - 100), *range(60, 130)])
+
+
+def test_attention_output_over_the_queries():
+    for past, new, extra in (([70, 0], [3, 40], 1), ([9000], [2], 1), ([40, 10], [200, 1], 1 << 16), ([5000], [300], 3000)):
+        c = Case(16, 2, 64, 32, past, new, seed=len(past), extra=extra)
+        want, q = c.check(), c.q.clone()
+        assert c.call(q=q, out=q).data_ptr() == q.data_ptr() and torch.equal(q, want)
+
+
+def test_attention_of_nothing():
+    c = Case(4, 2, 64, 16, [20], [3])
+    out = torch.full_like(c.q, 7.0)
+    c.call(out=out, max_new=0)
+    none = torch.empty((0, 4, 64), dtype=torch.float16, device="cuda")
+    assert (out == 7.0).all() and c.call(q=none, max_new=None).shape == (0, 4, 64)
+    atom.atom_attention_kv8(c.q, c.kc, c.vc, c.table[:0], i32(0), i32(), 1.0, out=out)
+    assert (out == 7.0).all()
 
 
 def test_attention_pieces_of_many_requests():
@@ -551,3 +622,52 @@ def test_calls_on_another_stream():
         _step(s)
     side.synchronize()
     assert torch.equal(s["out"], want)
+
+
+def test_two_calls_at_once():
+    """Steps of two servers on two streams, launched in turn, each with workspaces of its own."""
+    states = [_state(3, 64, 64, seed=8), _state(5, 40, 20, W=400, seed=9)]
+    lengths, want = ([20, 1, 43], [9, 0, 20, 4, 5]), []
+    for s, new in zip(states, lengths):
+        _inputs(s, new)
+        want.append(_step(s)[0].clone())
+        s["out"].zero_()
+    streams = [torch.cuda.Stream() for _ in states]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, stream in zip(states, streams):
+            with torch.cuda.stream(stream):
+                _step(s)
+    torch.cuda.synchronize()
+    for s, w, new in zip(states, want, lengths):
+        assert torch.equal(s["out"][:sum(new)], w[:sum(new)])
+
+
+def test_a_capture_that_the_allocator_does_not_know_of():
+    """A capture begun on the stream itself: a workspace of the call's own would be other tensors' memory at the replays, so the call has to be
+    given one."""
+    c = Case(8, 1, 128, 64, [3000, 70], [1, 1], seed=6)
+    need = atom.atom_attention_kv8_workspace_bytes(2, 2, 8, 1, 128, 1, c.W, 64)
+    assert need > 0
+    want, out, ws = c.check(), torch.zeros_like(c.q), torch.empty(need, dtype=torch.uint8, device="cuda")
+    hip = ctypes.CDLL(next(line.split()[-1] for line in open("/proc/self/maps") if "libamdhip64" in line))
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        handle, graph, run = ctypes.c_void_p(stream.cuda_stream), ctypes.c_void_p(), ctypes.c_void_p()
+        assert hip.hipStreamBeginCapture(handle, 2) == 0    # (relaxed)
+        try:
+            with pytest.raises(ValueError, match="workspace"):
+                c.call(out=out)
+            c.call(out=out, workspace=ws)
+        finally:
+            assert hip.hipStreamEndCapture(handle, ctypes.byref(graph)) == 0
+        assert hip.hipGraphInstantiate(ctypes.byref(run), graph, None, None, ctypes.c_size_t(0)) == 0
+        for _ in range(3):
+            out.zero_()
+            ws.fill_(0xA5)
+            assert hip.hipGraphLaunch(run, handle) == 0
+            stream.synchronize()
+            assert torch.equal(out, want)
+            torch.cuda.synchronize()
+        assert hip.hipGraphExecDestroy(run) == 0 and hip.hipGraphDestroy(graph) == 0
