@@ -658,9 +658,10 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
         return fmaf(m, factor[b], shift[b]);
     };
     // Half a tile: the scores of the next 32 keys (K's rows 32 half ..) and between their products the weights of the last ones, `now`; then the weights'
-    // products with V, and between them `pieces` of staging.  Operands are read from LDS three products ahead.  The order is the one written.
+    // products with V, and between them `pieces` of staging.  Operands are read from LDS four products ahead, and a weight's argument, power of two and sum lie a product
+    // apart, so that none waits for the one before (one after the other 321 us for 316, two prompts of up to 4096 tokens).  The order is the one written.
     auto half_tile = [&](const unsigned char *buf, int half, const f16v &now, f16v &then, int at, auto stage, int pieces) __attribute__((always_inline)) {
-        constexpr int kAhead = 3, per = 16 / KS;
+        constexpr int kAhead = 4, per = 16 / KS;
         const unsigned char *kp = buf + L::k + (32 * half + n) * L::kPitch + 16 * hh;
         const unsigned char *vp = buf + L::v + n * L::vPitch + 16 * hh + 64 * half;
         h8 f[KS + 2 * DB];
@@ -674,20 +675,32 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
 #pragma unroll
         for (int i = 0; i < 16; ++i) then[i] = 0.0f;
         __builtin_amdgcn_sched_barrier(0);
+        float e[16];
+        auto arguments = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = per * i; k < per * (i + 1); ++k) e[k] = fmaf(now[k], factor[k >> 3], to_p[k >> 3]);
+        };
+        auto weights = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = per * i; k < per * (i + 1); ++k) {
+                sum[k >> 3] += e[k];
+                p[k >> 3][k & 7] = (_Float16)e[k];
+            }
+        };
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) read(i);
+        arguments(0);
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             read(i + kAhead);
             then = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i], q[i], then, 0, 0, 0);
 #pragma unroll
-            for (int k = per * i; k < per * (i + 1); ++k) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(now[k], factor[k >> 3], to_p[k >> 3]));
-                sum[k >> 3] += e;
-                p[k >> 3][k & 7] = (_Float16)e;
-            }
+            for (int k = per * i; k < per * (i + 1); ++k) e[k] = __builtin_amdgcn_exp2f(e[k]);
+            if (i + 1 < KS) arguments(i + 1);
+            if (i) weights(i - 1);
             __builtin_amdgcn_sched_barrier(0);
         }
+        weights(KS - 1);
         // M is a bound on e but for the last few binary orders: what passes it by many shows in the sums (the first keys of a row: M is none yet).  No
         // maxima where it does not, a sixth of the vector unit's work.
         if (__ballot(sum[0] > 1024.0f || sum[1] > 1024.0f)) {
