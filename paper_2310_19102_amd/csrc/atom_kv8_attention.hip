@@ -44,6 +44,7 @@ struct Args {
 // One of the two kinds of work of a call, by the rows (tokens times heads of a group) of a request.
 struct Job {
     int rows_min, rows_max;
+    int log;                                      // a tile has 1 << log query rows
     int budget;                                   // workgroups for each cache head that tiles may be cut into (0: none is cut)
     float *part; int part_rows;                   // records of the pieces, and rows of a record
     int groups, merges;                           // workgroups for each cache head of the kernel, of the merge
@@ -73,7 +74,7 @@ __device__ __forceinline__ Request request(const Args &a, int b)
 
 // ---- which part of the work a workgroup has
 //
-// The query rows of a request and cache head (token after token, the group's heads of each) come in tiles of 1 << LOG rows.  Where the tiles are
+// The query rows of a request and cache head (token after token, the group's heads of each) come in tiles of 1 << job.log rows.  Where the tiles are
 // fewer than the workgroups that a call is to have for each cache head (budget), their keys are cut into pieces of about one size in the whole call:
 // sequences of any lengths keep the card evenly busy, and the pieces of a tile meet in the merge kernel.  Every wavefront
 // finds its place from the lengths by itself, 64 requests at a time: for as many it is one read, which it needs anyway.
@@ -101,7 +102,7 @@ __device__ __forceinline__ float total(float v)
 }
 
 // FROM_TILE: `index` counts tiles (all of a tile's pieces are meant), else pieces.
-template <int LOG, bool FROM_TILE>
+template <bool FROM_TILE>
 __device__ __forceinline__ Place place(const Args &a, const Job &job, int index)
 {
     const int budget = job.budget;
@@ -114,7 +115,7 @@ __device__ __forceinline__ Place place(const Args &a, const Job &job, int index)
             r = request(a, base + lane);
             const int64_t rows = (int64_t)r.n * a.group;
             if (rows >= job.rows_min && rows <= job.rows_max) {
-                tiles = (int)((rows + (1 << LOG) - 1) >> LOG);
+                tiles = (int)((rows + (1 << job.log) - 1) >> job.log);
                 keys = r.keys;
             }
         }
@@ -252,7 +253,7 @@ __device__ __forceinline__ float sum_of_chunks(float v)
 
 // ---------------------------------------------------------------- few query rows
 //
-// One workgroup of four wavefronts (8 or 16 where a lone one has a whole context) for a tile of 16 query rows of a (request, cache head) and a piece of its keys;
+// One workgroup of four wavefronts (8 or 16 where a lone one has a whole context) for a tile of 16 or 32 query rows of a (request, cache head) and a piece of its keys;
 // the wavefronts take steps of 32 keys in turn, each with a softmax of its own, and meet in LDS.  Bound by memory where there is enough of it: 64 single tokens over
 // up to 2048 keys of 32 heads of 128 (673 MB) 113 us, 5.9 TB/s; 16 over up to 16000 keys of 8 cache heads, 8 heads to each (329 MB), 57 us, 5.8 TB/s, and the merge 4.9.
 // With little to read by the chain of lengths, block numbers, scales and codes: one token over 1000 keys of 32 heads 6.8 us.
@@ -268,41 +269,53 @@ __device__ __forceinline__ float sum_of_chunks(float v)
 //           transposes.  No LDS, no lane exchange in the loop.  The weights travel as fp16 (rounded to nearest even: 2^-12 of themselves).
 //   loads: the next step's rows of K are asked for once the scores have used this step's, those of V after the values: half the registers of two
 //           buffers.  Block numbers and scales of 64 blocks of 16 keys are read at once, a lane each.
-constexpr int kStep = 32, kRowsLog = 4, kTileRows = 1 << kRowsLog;
+//   rows:  SETS = 2: tiles of 32 rows, the codes turned into halves once for two sets of 16.
+constexpr int kStep = 32, kRowsLog = 4, kSetRows = 1 << kRowsLog;
 
-template <int D, int kWaves>
-struct RowsLds { float acc[kWaves][kTileRows][D + 4], m[kWaves][kTileRows], l[kWaves][kTileRows]; };
+template <int D, int kWaves, int SETS>
+struct RowsLds { float acc[kWaves][SETS * kSetRows][D + 4], m[kWaves][SETS * kSetRows], l[kWaves][SETS * kSetRows]; };
 
-template <int D, bool ONCE, int kWaves>
-__device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int index, RowsLds<D, kWaves> &lds)
+template <int D, bool ONCE, int kWaves, int SETS>
+__device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int index, RowsLds<D, kWaves, SETS> &lds)
 {
     constexpr int KB = D / 4, VB = D / 16;            // bytes of a K row and of a V row in a lane
     constexpr int KS = D / 32;                        // matrix instructions for 16 keys' scores
+    constexpr int kTileRows = SETS * kSetRows;
     auto &s_acc = lds.acc;
     auto &s_m = lds.m, &s_l = lds.l;
 
     const int h = index % a.Hkv;
-    const Place w = place<kRowsLog, false>(a, job, index / a.Hkv);
+    const Place w = place<false>(a, job, index / a.Hkv);
     if (!w.found) return;
     const Request r = w.r;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m = lane & 15, c = lane >> 4;           // query row (or key) of the tile, chunk
+    const int m = lane & 15, c = lane >> 4;           // query row (or key) of the set, chunk
     const int rows = min(kTileRows, r.n * a.group - w.tile * kTileRows);
-    const int row = w.tile * kTileRows + min(m, rows - 1);
-    const int token = by_group(a, row), head = h * a.group + row - token * a.group;
-    // keys that this lane's row sees, and the fewest and the most of the tile
-    const int sees = min(max(r.before + token + 1, 0), r.keys);
+    // keys that this lane's rows see, and the fewest and the most of the tile
+    int token[SETS], head[SETS], sees[SETS];
+#pragma unroll
+    for (int t = 0; t < SETS; ++t) {
+        const int row = w.tile * kTileRows + min(t * kSetRows + m, rows - 1);
+        token[t] = by_group(a, row);
+        head[t] = h * a.group + row - token[t] * a.group;
+        sees[t] = min(max(r.before + token[t] + 1, 0), r.keys);
+    }
     const int sees_least = min(max(r.before + by_group(a, w.tile * kTileRows) + 1, 0), r.keys);
     const int sees_most = min(max(r.before + by_group(a, w.tile * kTileRows + rows - 1) + 1, 0), r.keys);
     const int key0 = w.split * w.keys_per, key1 = min(sees_most, key0 + w.keys_per);     // (a split below 2^31: keys_per is at most keys)
 
-    h8 q[KS];
+    h8 q[SETS][KS];
     const float to_e = a.sm_scale * kLog2e * 16777216.0f;
 
-    f4 acc[VB];
+    f4 acc[SETS][VB];
+    float M[SETS], l[SETS], start[SETS];              // start: what u = code + 128 adds to a score, negated
 #pragma unroll
-    for (int e = 0; e < VB; ++e) acc[e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    float M = kNoScore, l = 0.0f, start = 0.0f;       // start: what u = code + 128 adds to a score, negated
+    for (int t = 0; t < SETS; ++t) {
+        M[t] = kNoScore;
+        l[t] = start[t] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < VB; ++e) acc[t][e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
 
     u4 kr[2][KB / 16];
     uint32_t vr[8][VB / 4];
@@ -357,68 +370,83 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
     auto compute = [&](int step, bool more) __attribute__((always_inline)) {
         const int at = 2 * (step & 31), key = key_of(step);
         const bool turn = ((step + 1) & 31) == 0;
-        float e[8];
-        float inv_v[2], top = -INFINITY;
+        float e[SETS][8], top[SETS], inv_v[2];
+#pragma unroll
+        for (int t = 0; t < SETS; ++t) top[t] = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if constexpr (D == 128) ordered(kr[u][0], kr[u][1]);
-            f4 s = f4{start, start, start, start};
+            f4 s[SETS];
+#pragma unroll
+            for (int t = 0; t < SETS; ++t) s[t] = f4{start[t], start[t], start[t], start[t]};
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 const uint32_t w0 = flip(kr[u][i >> 1][(2 * i) & 3]), w1 = flip(kr[u][i >> 1][(2 * i + 1) & 3]);
                 const h8 k = halves(__builtin_amdgcn_perm(0, w0, 0x0c010c00u), __builtin_amdgcn_perm(0, w0, 0x0c030c02u),
                                     __builtin_amdgcn_perm(0, w1, 0x0c010c00u), __builtin_amdgcn_perm(0, w1, 0x0c030c02u));
-                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i], s, 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < SETS; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[t][i], s[t], 0, 0, 0);
             }
             if (key + 16 * u + 16 > min(sees_least, key1)) {
-                const int room = min(sees, key1) - (key + 16 * u + 4 * c);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = i < room ? s[i] : -INFINITY;
+                for (int t = 0; t < SETS; ++t) {
+                    const int room = min(sees[t], key1) - (key + 16 * u + 4 * c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[t][i] = i < room ? s[t][i] : -INFINITY;
+                }
             }
             const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_scale), at + u));
             const float log_v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_log), at + u));
             inv_v[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, b_inv), at + u));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                e[4 * u + i] = fmaf(s[i], f, log_v);
-                top = fmaxf(top, e[4 * u + i]);
-            }
+            for (int t = 0; t < SETS; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e[t][4 * u + i] = fmaf(s[t][i], f, log_v);
+                    top[t] = fmaxf(top[t], e[t][4 * u + i]);
+                }
         }
         if (more && !turn) fetch_k(step + 1);
-        if (__ballot(top > M + 8.0f)) {               // rare after the first steps
-            const float to = fmaxf(M, max_of_chunks(top));
-            const float down = __builtin_amdgcn_exp2f(M - to);
-            M = to;
-            l *= down;
+        h8 p[SETS];
 #pragma unroll
-            for (int i = 0; i < VB; ++i) acc[i] *= down;
-        }
+        for (int t = 0; t < SETS; ++t) {
+            if (__ballot(top[t] > M[t] + 8.0f)) {     // rare after the first steps
+                const float to = fmaxf(M[t], max_of_chunks(top[t]));
+                const float down = __builtin_amdgcn_exp2f(M[t] - to);
+                M[t] = to;
+                l[t] *= down;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                e[4 * u + i] = __builtin_amdgcn_exp2f(e[4 * u + i] - M);
-                sum += e[4 * u + i];
+                for (int i = 0; i < VB; ++i) acc[t][i] *= down;
             }
-            l = fmaf(sum, inv_v[u], l);
-        }
-        h8 p;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = (_Float16)e[i];
+            for (int u = 0; u < 2; ++u) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e[t][4 * u + i] = __builtin_amdgcn_exp2f(e[t][4 * u + i] - M[t]);
+                    sum += e[t][4 * u + i];
+                }
+                l[t] = fmaf(sum, inv_v[u], l[t]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[t][i] = (_Float16)e[t][i];
+        }
         __builtin_amdgcn_sched_barrier(0);            // (or registers for all of it at once)
 #define ATOM_VALUES(j, n)                                                                                                    \
-        acc[4 * (j) + (n)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(                                                         \
-            halves(centred(pair_of<n>(vr[0][j], vr[1][j])), centred(pair_of<n>(vr[2][j], vr[3][j])),                         \
-                   centred(pair_of<n>(vr[4][j], vr[5][j])), centred(pair_of<n>(vr[6][j], vr[7][j]))), p, acc[4 * (j) + (n)], 0, 0, 0)
+        {                                                                                                                    \
+            const h8 v = halves(centred(pair_of<n>(vr[0][j], vr[1][j])), centred(pair_of<n>(vr[2][j], vr[3][j])),            \
+                                centred(pair_of<n>(vr[4][j], vr[5][j])), centred(pair_of<n>(vr[6][j], vr[7][j])));           \
+            _Pragma("unroll") for (int t = 0; t < SETS; ++t)                                                                 \
+                acc[t][4 * (j) + (n)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[t], acc[t][4 * (j) + (n)], 0, 0, 0);     \
+        }
 #pragma unroll
         for (int j = 0; j < VB / 4; ++j) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) vr[i][j] = flip(vr[i][j]);
-            ATOM_VALUES(j, 0);
-            ATOM_VALUES(j, 1);
-            ATOM_VALUES(j, 2);
-            ATOM_VALUES(j, 3);
+            ATOM_VALUES(j, 0)
+            ATOM_VALUES(j, 1)
+            ATOM_VALUES(j, 2)
+            ATOM_VALUES(j, 3)
         }
 #undef ATOM_VALUES
     };
@@ -426,16 +454,22 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
     if (key_of(0) < key1) {                           // (the same in all lanes)
         const int steps = (key1 - key_of(0) + kWaves * kStep - 1) / (kWaves * kStep);
         const int page = page_of(0);
-        const __half *qp = a.q + (int64_t)(r.start + token) * a.ldq + (int64_t)head * D + 16 * c;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) q[s] = __builtin_bit_cast(h8, *reinterpret_cast<const u4 *>(qp + 64 * (s >> 1) + 8 * (s & 1)));
+        for (int t = 0; t < SETS; ++t) {
+            const __half *qp = a.q + (int64_t)(r.start + token[t]) * a.ldq + (int64_t)head[t] * D + 16 * c;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) q[t][s] = __builtin_bit_cast(h8, *reinterpret_cast<const u4 *>(qp + 64 * (s >> 1) + 8 * (s & 1)));
+        }
         look_up(0, page);
         fetch_k(0);
         fetch_v(0);
         take_scales();
 #pragma unroll
-        for (int s = 0; s < KS; ++s) start = add8(q[s], start);
-        start = sum_of_chunks(start) * (-128.0f * 5.9604644775390625e-08f);
+        for (int t = 0; t < SETS; ++t) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) start[t] = add8(q[t][s], start[t]);
+            start[t] = sum_of_chunks(start[t]) * (-128.0f * 5.9604644775390625e-08f);
+        }
         for (int step = 0; step < steps; ++step) {
             const bool more = step + 1 < steps;
             compute(step, more);
@@ -451,14 +485,17 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
     }
 
     // ---- the wavefronts meet
-    l = sum_of_chunks(l);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int t = 0; t < SETS; ++t) {
+        l[t] = sum_of_chunks(l[t]);
 #pragma unroll
-        for (int e = 0; e < VB; ++e) s_acc[wave][m][VB * (4 * c + i) + e] = acc[e][i];
-    if (c == 0) {
-        s_m[wave][m] = M;
-        s_l[wave][m] = l;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < VB; ++e) s_acc[wave][t * kSetRows + m][VB * (4 * c + i) + e] = acc[t][e][i];
+        if (c == 0) {
+            s_m[wave][t * kSetRows + m] = M[t];
+            s_l[wave][t * kSetRows + m] = l[t];
+        }
     }
     __syncthreads();
     const bool whole = w.splits == 1;
@@ -494,12 +531,13 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
     }
 }
 
-template <int D, bool ONCE, int kWaves>
-__global__ __launch_bounds__(kWaves * 64, 4)
+// (two sets: two wavefronts a SIMD, by their registers)
+template <int D, bool ONCE, int kWaves, int SETS>
+__global__ __launch_bounds__(kWaves * 64, SETS == 2 ? 2 : 4)
 void attention_kv8_rows_kernel(const Args a, const Job few)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    rows_tile<D, ONCE, kWaves>(a, few, blockIdx.x, *reinterpret_cast<RowsLds<D, kWaves> *>(lds));
+    rows_tile<D, ONCE, kWaves, SETS>(a, few, blockIdx.x, *reinterpret_cast<RowsLds<D, kWaves, SETS> *>(lds));
 }
 
 // ---------------------------------------------------------------- many query rows
@@ -518,7 +556,7 @@ void attention_kv8_rows_kernel(const Args a, const Job few)
 //   loads: codes of the next tile but one are on their way, and their block numbers a tile earlier, while one is computed; two buffers, a barrier a tile.
 //   order: the last tiles of a request, which see the most keys, first.
 //
-// Bound by the issue of both units: two prompts of up to 4096 tokens, 64 heads on 8 cache heads of 128 (292 GFLOP), 322 us, 908 TFLOP/s; of a SIMD's cycles the matrix
+// Bound by the issue of both units: two prompts of up to 4096 tokens, 64 heads on 8 cache heads of 128 (292 GFLOP), 318 us, 918 TFLOP/s; of a SIMD's cycles the matrix
 // unit has 46 % and the vector unit 61 %, which hold each other up (a matrix instruction keeps the vector unit from starting one for 13 to 16 cycles of its 32).
 
 __device__ __forceinline__ float larger(float a, float b, float c)
@@ -542,7 +580,7 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
     constexpr int KL = D / 64, VB = D / 16;           // 16-byte loads of K, bytes of a V row in a lane
 
     const int h = index % a.Hkv;
-    const Place w = place<kTileLog, false>(a, job, index / a.Hkv);
+    const Place w = place<false>(a, job, index / a.Hkv);
     if (!w.found) return;
     const Request r = w.r;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -853,46 +891,34 @@ __global__ __launch_bounds__(256, 2)
 void attention_kv8_step_kernel(const Args a, const Job few, const Job many)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    static_assert(sizeof(RowsLds<D, 4>) <= 2 * TileLds<D>::bytes, "one workgroup's LDS");
+    static_assert(sizeof(RowsLds<D, 4, 1>) <= 2 * TileLds<D>::bytes, "one workgroup's LDS");
     const int first = many.groups * a.Hkv;
-    if ((int)blockIdx.x >= first) rows_tile<D, false, 4>(a, few, blockIdx.x - first, *reinterpret_cast<RowsLds<D, 4> *>(lds));
+    if ((int)blockIdx.x >= first) rows_tile<D, false, 4, 1>(a, few, blockIdx.x - first, *reinterpret_cast<RowsLds<D, 4, 1> *>(lds));
     else                         many_rows_tile<D>(a, many, blockIdx.x, lds);
 }
 
-// The pieces of tiles, in their order: 16 rows of a tile and cache head for a workgroup, first those of few rows, then eight for each tile of
+// The pieces of tiles, in their order: 16 rows of a tile and cache head for a workgroup, first those of few rows, then those of
 // many.  What bounds it is its chain of reads (lengths, then the pieces), so eight pieces are read at once.
 template <int D>
 __global__ __launch_bounds__(256)
 void attention_kv8_merge_kernel(const Args a, const Job few, const Job many)
 {
-    constexpr int kSubs = kTile / kTileRows;
     const bool is_few = (int)blockIdx.x < few.merges * a.Hkv;
-    const int  index = is_few ? blockIdx.x : blockIdx.x - few.merges * a.Hkv, h = index % a.Hkv;
-    Place w;
-    int sub = 0, rows_log, part_rows;
-    const float *part;
-    if (is_few) {
-        w = place<kRowsLog, true>(a, few, index / a.Hkv);
-        rows_log = kRowsLog;
-        part = few.part;
-        part_rows = few.part_rows;
-    } else {
-        sub = index / a.Hkv % kSubs;
-        w = place<kTileLog, true>(a, many, index / a.Hkv / kSubs);
-        rows_log = kTileLog;
-        part = many.part;
-        part_rows = many.part_rows;
-    }
+    const Job job = is_few ? few : many;
+    const int index = is_few ? blockIdx.x : blockIdx.x - few.merges * a.Hkv, h = index % a.Hkv;
+    const int subs = 1 << (job.log - kRowsLog), sub = index / a.Hkv & (subs - 1);
+    const Place w = place<true>(a, job, index / a.Hkv >> (job.log - kRowsLog));
     if (!w.found || w.splits == 1) return;
     const Request r = w.r;
-    const int all = r.n * a.group;
+    const int all = r.n * a.group, part_rows = job.part_rows;
+    const float *part = job.part;
     // (the kernel of many rows takes a request's tiles from the last one on)
-    const int tile = is_few ? w.tile : ((all - 1) >> rows_log) - w.tile;
-    const int first = (tile << rows_log) + sub * kTileRows, rows = min(kTileRows, all - first);
+    const int tile = is_few ? w.tile : ((all - 1) >> job.log) - w.tile;
+    const int first = (tile << job.log) + sub * kSetRows, rows = min(kSetRows, all - first);
     const int64_t stride = (int64_t)a.Hkv * part_rows * (D + 4);
     for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
         const int rr = i / (D / 4), d = 4 * (i % (D / 4));
-        const float *from = part + (((int64_t)w.first_slot * a.Hkv + h) * part_rows + sub * kTileRows + rr) * (D + 4);
+        const float *from = part + (((int64_t)w.first_slot * a.Hkv + h) * part_rows + sub * kSetRows + rr) * (D + 4);
         float top = kNoScore, sum = 0.0f;
         f4 o = f4{0.0f, 0.0f, 0.0f, 0.0f};
         for (int s = 0; s < w.splits; s += 8) {
@@ -955,17 +981,23 @@ int wavefronts(int64_t tiles, int Hkv, int D, int64_t capacity)              // 
     return capacity <= 256 && room > 8 ? 8 : room;
 }
 
-struct Shape { Job few, many; size_t floats; int waves; };    // waves: of a workgroup of few rows
+// Few rows alone, but more than 16 to a request (drafts): tiles of 32 from so many tiles times keys on, below that the tiles of 16 run at once anyway. Of 16 / of 32, us
+// (tokens, keys): heads 64 on 8 of 128, 64 sequences of 4 (3000) 72.5 / 52.4, 16 of 4 (4000) 29.7 / 26.1; 32 on 8, 32 of 6 (3000) 36.6 / 33.1, 8 of 8 (1500) 17.2 / 17.6;
+// 16 on 4 of 64, 23 of 5 (5000) 17.4 / 16.0, one of 8 (9000) 16.6 / 17.4.
+constexpr double kTwoSets = 2e5;
+
+struct Shape { Job few, many; size_t floats; int waves, sets; };    // of a workgroup of few rows: its wavefronts, its sets of 16 rows
 
 // `want` workgroups together, for each cache head: where there are fewer tiles (and 128 keys to a piece) they are cut.
-void size_job(Job &job, int64_t tiles, int part_rows, int64_t want, int Hkv, int64_t capacity, int subs)
+void size_job(Job &job, int64_t tiles, int log, int part_rows, int64_t want, int Hkv, int64_t capacity)
 {
+    job.log = log;
     const int64_t most = tiles * ((capacity + 127) / 128);
     int64_t budget = (want + Hkv - 1) / Hkv;
     if (budget > most) budget = most;
     job.budget = budget > tiles ? (int)budget : 0;
     job.groups = (int)(job.budget ? budget : tiles);
-    job.merges = job.budget ? (int)(tiles * subs) : 0;
+    job.merges = job.budget ? (int)(tiles << (log - kRowsLog)) : 0;
     job.part_rows = part_rows;
 }
 
@@ -978,15 +1010,15 @@ int64_t many_tiles(int64_t T, int B, int group, int64_t rows, int few_most)
 }
 
 // Whether a call's requests of more than kFew rows are better tiles of 128 rows, in us, by what the host knows (tables may be wider than they are full).
-// 16 rows at a time the work spreads over the card, but turns each code into halves eight times as often: 1.8 us for a million pairs of rows and keys (D = 64:
-// 0.85).  128 at a time a tile takes 1.5 us for 64 keys, 1.85 where two share a compute unit, and where tiles are cut
-// their pieces' starts and the merge take 18.  Tiles / 16 rows, measured (tokens, earlier keys): heads 64 on 8: 1000 33.1 / 60.7 us, 2000 88.9 / 193, 299 (229) 22.3 / 20.5, 100 (3000) 34.1 / 47.8,
-// 65 (679) 19.0 / 17.3; 32 on 32: 1000 29.6 / 34.0; 16 on 4: 1046 (398) 40.3 / 34.0, 2 x 470 20.6 / 13.0; 20 on 1: 3 x 353 20.4 / 10.5, 3000 77 / 138; 12 on 12: 2 x 196 16.0 / 6.2;
-// of 64: 16 on 4: 3000 59.8 / 53.5, 12 on 12: 2000 (1000) 62.3 / 38.2, 64 on 8: 4 x 706 28.2 / 39.1.
+// 16 or 32 rows at a time the work spreads over the card, but turns each code into halves more often: 1.4 us for a million pairs of rows and keys (D = 64:
+// 0.6).  128 at a time a tile takes 1.5 us for 64 keys, 1.85 where two share a compute unit, and where tiles are cut
+// their pieces' starts and the merge take 18.  Tiles / few rows, measured (tokens, earlier keys): heads 64 on 8: 1000 31.9 / 51.7 us, 2000 87.3 / 143, 299 (229) 21.2 / 19.8, 100 (3000) 33.3 / 33.5,
+// 65 (679) 18.2 / 17.3; 32 on 32: 1000 27.4 / 29.3, 400 (4000) 55.3 / 63.1; 16 on 4: 1046 (398) 37.9 / 29.6, 2 x 470 20.2 / 13.0; 20 on 1: 3 x 353 20.2 / 10.6, 3000 74 / 99;
+// 12 on 12: 2 x 196 15.7 / 6.0; of 64: 16 on 4: 3000 55.8 / 46.5, 12 on 12: 2000 (1000) 49.8 / 33.0, 64 on 8: 4 x 706 25.4 / 34.9, 40 on 8: 900 (3000) 76.9 / 68.3.
 bool worth_tiles(int64_t T, int64_t tiles, int Hkv, int group, int D, int max_new, int64_t capacity)
 {
     const double keys = max_new < capacity ? (double)capacity - 0.5 * max_new : 0.5 * (double)capacity, steps = (double)capacity / 64, n = (double)tiles * Hkv;
-    const double few = 6 + (double)T * group * Hkv * keys * 1e-6 * (D == 128 ? 1.8 : 0.85);
+    const double few = 8 + (double)T * group * Hkv * keys * 1e-6 * (D == 128 ? 1.4 : 0.6);
     const double shared = n * keys / 64 * 0.0048, alone = steps * (n > 256 ? 1.85 : 1.5);
     const int    want = many_workgroups(tiles, Hkv, capacity);
     const double many = (want + Hkv - 1) / Hkv > tiles ? 18 + n * steps / 256 * (want > kManyWorkgroups ? 1.2 : 1.95) : 7 + (shared > alone ? shared : alone);
@@ -1005,16 +1037,20 @@ Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t ca
     s.many.rows_min = few_most + 1;
     s.many.rows_max = 0x7fffffff;
     if (few_most) {
-        const int64_t each = (int64_t)B * ((few_most + kTileRows - 1) / kTileRows), by_token = T * group / kTileRows + B;
-        const int64_t tiles = each < by_token ? each : by_token;
-        const int waves = many ? 4 : wavefronts(tiles, Hkv, D, capacity);
+        auto tiles = [&](int rows) {
+            const int64_t each = (int64_t)B * ((few_most + rows - 1) / rows), by_token = T * group / rows + B;
+            return each < by_token ? each : by_token;
+        };
+        const int waves = many ? 4 : wavefronts(tiles(kSetRows), Hkv, D, capacity);
+        s.sets = !many && few_most > kSetRows && (waves == 0 || waves == 4) && (double)tiles(2 * kSetRows) * Hkv * capacity >= kTwoSets ? 2 : 1;
         s.waves = waves ? waves : 4;
-        size_job(s.few, tiles, few_most < kTileRows ? few_most : kTileRows,
-                 !many ? (waves ? 0 : kFewWorkgroups) : capacity > kUncutBeside ? kFewBeside : 0, Hkv, capacity, 1);
+        const int rows = s.sets * kSetRows;
+        size_job(s.few, tiles(rows), kRowsLog + s.sets - 1, few_most < rows ? few_most : rows,
+                 !many ? (waves ? 0 : s.sets == 2 ? kFewWorkgroups / 2 : kFewWorkgroups) : capacity > kUncutBeside ? kFewBeside : 0, Hkv, capacity);
     }
     if (many) {
         const int64_t tiles = many_tiles(T, B, group, rows, few_most);
-        size_job(s.many, tiles, kTile, many_workgroups(tiles, Hkv, capacity), Hkv, capacity, kTile / kTileRows);
+        size_job(s.many, tiles, kTileLog, kTile, many_workgroups(tiles, Hkv, capacity), Hkv, capacity);
     }
     s.floats = records(s.few, Hkv, D) + records(s.many, Hkv, D);
     return s;
@@ -1022,17 +1058,17 @@ Shape shape(int64_t T, int B, int Hkv, int group, int D, int max_new, int64_t ca
 
 // A cache that the last-level cache (256 MB) does not keep until the next step is read with the hint that nothing reads it again, where a row is read
 // by one workgroup only.
-bool reads_once(const Args &a, int rows)
+bool reads_once(const Args &a, const Job &few)
 {
-    return rows <= kTileRows && (int64_t)a.B * a.Hkv * a.capacity * 128 >= (int64_t)1 << 27;
+    return few.rows_max <= 1 << few.log && (int64_t)a.B * a.Hkv * a.capacity * 128 >= (int64_t)1 << 27;
 }
 
-template <int D, int kWaves>
+template <int D, int kWaves, int SETS = 1>
 hipError_t launch_rows(const Args &a, const Job &few, dim3 grid, hipStream_t stream)
 {
-    constexpr int bytes = sizeof(RowsLds<D, kWaves>);
-    const bool once = reads_once(a, few.rows_max);
-    auto kern = once ? &attention_kv8_rows_kernel<D, true, kWaves> : &attention_kv8_rows_kernel<D, false, kWaves>;
+    constexpr int bytes = sizeof(RowsLds<D, kWaves, SETS>);
+    const bool once = reads_once(a, few);
+    auto kern = once ? &attention_kv8_rows_kernel<D, true, kWaves, SETS> : &attention_kv8_rows_kernel<D, false, kWaves, SETS>;
     if (bytes > 60 * 1024) {
         static atom_launch::LdsOptIn opt[2];
         hipError_t err = atom_launch::ensure_dynamic_lds(opt[once], reinterpret_cast<const void *>(kern), bytes);
@@ -1050,7 +1086,8 @@ hipError_t launch(const Args &a, Shape s, float *workspace, hipStream_t stream)
     if (!s.many.groups) {
         if (!s.few.groups) return hipSuccess;
         const dim3 grid((unsigned)(s.few.groups * a.Hkv));
-        hipError_t err = s.waves == 16 ? launch_rows<D, 16>(a, s.few, grid, stream)
+        hipError_t err = s.sets == 2 ? launch_rows<D, 4, 2>(a, s.few, grid, stream)
+                         : s.waves == 16 ? launch_rows<D, 16>(a, s.few, grid, stream)
                          : s.waves == 8 ? launch_rows<D, 8>(a, s.few, grid, stream) : launch_rows<D, 4>(a, s.few, grid, stream);
         if (err != hipSuccess) return err;
     } else {
@@ -1080,17 +1117,18 @@ size_t attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, in
 bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new)
 {
     // every count is below (rows / 16 + B) * blocks of 128 rows and the workgroups wanted, as doubles here
-    const double group = H / Hkv, rows = (double)max_new * group, tiles = (double)T * group / kTileRows + B, each = (double)B * (rows / kTileRows + 1);
+    const double group = H / Hkv, rows = (double)max_new * group, tiles = (double)T * group / kSetRows + B, each = (double)B * (rows / kSetRows + 1);
     const double most = (tiles < each ? tiles : each) + kFewWorkgroups;
     return 2.0 * most * Hkv < 2147483647.0;
 }
 
 // How a call of these sizes runs, as its tests ask it: wavefronts of a workgroup of few rows, 32 where those requests' keys may be cut, 64 where
-// requests of many rows are tiles of 128, 128 where those may be cut.
+// requests of many rows are tiles of 128, 128 where those may be cut, 256 where few rows
+// are tiles of 32.
 extern "C" int atom_internal_attention_kv8_route(int64_t T, int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t max_new, int64_t W, int32_t block_tokens)
 {
     const Shape s = shape(T, B, Hkv, H / Hkv, D, max_new, W * block_tokens);
-    return (s.few.groups ? (s.many.groups ? 4 : s.waves) : 0) + (s.few.budget ? 32 : 0) + (s.many.groups ? 64 : 0) + (s.many.budget ? 128 : 0);
+    return (s.few.groups ? (s.many.groups ? 4 : s.waves) : 0) + (s.sets == 2 ? 256 : 0) + (s.few.budget ? 32 : 0) + (s.many.groups ? 64 : 0) + (s.many.budget ? 128 : 0);
 }
 
 hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)

@@ -254,10 +254,16 @@ class Case:
 
     def route(self, max_new=-1):
         """(wavefronts of a workgroup of few rows, their keys may be cut, tiles of many rows, theirs may be cut)"""
+        r = self._route(max_new)
+        return r & 31, bool(r & 32), bool(r & 64), bool(r & 128)
+
+    def tiles_of_32(self):
+        return bool(self._route() & 256)
+
+    def _route(self, max_new=-1):
         (n, Hkv, bs, D), (T, H, _) = self.kc[0].shape, self.q.shape
         ask = ctypes.CDLL(binding._LIB_PATH).atom_internal_attention_kv8_route
-        r = ask(ctypes.c_int64(T), self.table.shape[0], H, Hkv, D, self.max_new if max_new == -1 else max_new, ctypes.c_int64(self.W), bs)
-        return r & 31, bool(r & 32), bool(r & 64), bool(r & 128)
+        return ask(ctypes.c_int64(T), self.table.shape[0], H, Hkv, D, self.max_new if max_new == -1 else max_new, ctypes.c_int64(self.W), bs)
 
     def check(self, got=None, rows=None, heads=slice(None), **kw):
         """The call (or what it gave) against 64 bits; `rows`: of these tokens only, `heads`: of these only (one cache head)."""
@@ -360,11 +366,37 @@ def test_attention_workgroups_of_all_sizes(B, Hkv, past):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("past,new,cut", [(1500, 260, False), (6500, 100, True)])
+@pytest.mark.parametrize("H,Hkv,bs,past,new", [
+    (8, 2, 16, [300, 0, 40, 100, 1000], [5, 8, 1, 6, 0]), (17, 1, 32, [700, 64], [1, 1]), (3, 3, 128, [5000, 2, 0], [11, 21, 32]),
+    (16, 2, 64, [90, 31], [7, 8]), (32, 1, 16, [1300], [1])])
+def test_attention_tiles_of_32_rows(D, H, Hkv, bs, past, new):
+    """Drafts: 17 to 64 query rows of a request and cache head, the tables wide enough for tiles of 32 rows; keys in pieces and whole."""
+    c = Case(H, Hkv, D, bs, past, new, seed=H + bs, extra=(1 << 18) // bs)
+    assert c.route()[:3] == (4, True, False) and c.tiles_of_32()
+    out = torch.empty_like(c.q)
+    for _ in range(2):
+        c.check(out=out.fill_(float("nan")))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_tiles_of_32_rows_of_many_requests(D):
+    g = torch.Generator().manual_seed(D)
+    past, new = torch.randint(0, 100, (70,), generator=g).tolist(), torch.randint(0, 8, (70,), generator=g).tolist()
+    past[3], new[3:5] = 0, [7, 0]
+    c = Case(24, 8, D, 32, past, new, seed=D, pad=300, extra=12)
+    assert c.route() == (4, False, False, False) and c.tiles_of_32()
+    c.len[5] = 1                                            # its first rows see nothing
+    out = torch.full_like(c.q, 7.0)
+    c.check(out=out)
+    assert (out[sum(new):] == 7.0).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("past,new,cut", [(1500, 260, None), (1300, 500, False), (6500, 100, True)])
 def test_attention_long_tiles_of_many_rows(D, past, new, cut):
     """More than 1024 keys to a workgroup of the tiles of 128 rows, which looks its blocks up 1024 at a time."""
     c = Case(128, 1, D, 32, [past], [new], seed=D)
-    assert c.route()[2:] == (True, cut)
+    assert cut is None or c.route()[2:] == (True, cut)
     c.check(heads=slice(5, None, 17))
 
 
@@ -393,6 +425,11 @@ def test_attention_spoiled_blocks_reach_nobody_else(D, extra):
     for _, s in (c.kc, c.vc):
         s[c.table[0, 9].long()] = float("nan")
     c.check(rows=[*range(112 - 100), *range(60, 130)])
+    c = Case(16, 2, D, 16, [110, 30], [4, 3], seed=D, extra=1 << 14)
+    assert c.tiles_of_32()
+    for _, s in (c.kc, c.vc):
+        s[c.table[0, 7].long()] = float("inf")
+    c.check(rows=[0, 1, 4, 5, 6])
 
 
 def test_attention_output_over_the_queries():
