@@ -266,7 +266,7 @@ __device__ __forceinline__ float sum_of_chunks(float v)
 //           they count, whatever the scales are.  The sum of the softmax takes p / v_scale.  M moves only where some e passes it by 8 (p <= 2^8 then).
 //   values: O^T = V^T P^T.  The weights lie in the registers of the scores as the second operand wants them when its order of keys is
 //           that of the scores' rows; V's rows are loaded in that order, D / 16 bytes a lane, and the byte selection that makes halves also
-//           transposes.  No LDS, no lane exchange in the loop.  The weights travel as fp16 (rounded to nearest even: 2^-12 of themselves).
+//           transposes.  No LDS, no lane exchange in the loop.  The weights travel as fp16 (rounded to nearest even: by 2^-11 of themselves at most).
 //   loads: the next step's rows of K are asked for once the scores have used this step's, those of V after the values: half the registers of two
 //           buffers.  Block numbers and scales of 64 blocks of 16 keys are read at once, a lane each.
 //   rows:  SETS = 2: tiles of 32 rows, the codes turned into halves once for two sets of 16.
