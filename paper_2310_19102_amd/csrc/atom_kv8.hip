@@ -183,21 +183,19 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
     return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-// clamp(rne(v), -127, 127) in the low byte: adding 1.5 * 2^23 rounds to the nearest even integer and leaves it there.
-__device__ __forceinline__ uint32_t code_of(float v)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(v, -127.0f, 127.0f) + 12582912.0f);
-}
+// rne(v) in the low byte, for |v| <= 127.5: adding 1.5 * 2^23 rounds to the nearest even integer and leaves it there.  The clamp to 127 is implied: a value is at
+// most max|x|, the scale at least max|x| / 127, each of the three roundings on the way below 2^-23 of 127.
+__device__ __forceinline__ uint32_t code_of(float v) { return __builtin_bit_cast(uint32_t, v + 12582912.0f); }
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
-    const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), hi = __builtin_amdgcn_perm(d, c, 0x04000c0cu);
-    return lo | hi;
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
+// (x * r + 0 is x * r, as one instruction that takes half of a register)
 __device__ __forceinline__ uint32_t codes4(uint32_t h01, uint32_t h23, float r)
 {
     const __half2 a = __builtin_bit_cast(__half2, h01), b = __builtin_bit_cast(__half2, h23);
-    return pack4(code_of(__low2float(a) * r), code_of(__high2float(a) * r), code_of(__low2float(b) * r),
-                 code_of(__high2float(b) * r));
+    return pack4(code_of(fmaf(__low2float(a), r, 0.0f)), code_of(fmaf(__high2float(a), r, 0.0f)), code_of(fmaf(__low2float(b), r, 0.0f)),
+                 code_of(fmaf(__high2float(b), r, 0.0f)));
 }
 __device__ __forceinline__ uint32_t recode4(uint32_t w, float ratio)
 {
@@ -249,11 +247,11 @@ __device__ __forceinline__ int run_length(const int32_t *__restrict__ slot, int 
 // (where the block holds older rows, those before the run's first) and max|x| / 127:
 //   s = max(s_old, max|x| / 127), r = 1 / s, code = clamp(rne(x * r), -127, 127)   IEEE fp32, every step rounded once
 // and where s grows, the older rows become rne(code * (s_old / s)).
-// Rows stay in registers between the maximum and the codes (64 rows; those of a longer run are read twice, the second time
+// Rows stay in registers between the maximum and the codes (ROWS of them; those of a longer run are read twice, the second time
 // from the cache).  16-byte loads, 8 values a lane: D / 8 lanes a row.
-template <int D>
+template <int D, int ROWS>
 struct Run {
-    static constexpr int LPR = D / 8, RPL = 64 / LPR, kLoads = 64 / RPL;    // lanes a row, rows a load, loads of 64 rows
+    static constexpr int LPR = D / 8, RPL = 64 / LPR, kLoads = ROWS / RPL;  // lanes a row, rows a load, loads of ROWS
     uint4 raw[kLoads];
     const __half *rows; int64_t ld;
     int8_t *block; float *scale;
@@ -291,7 +289,7 @@ struct Run {
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) top = pair_max_u16(top, magnitudes(raw[u]));
-        for (int row = 64; row < len; row += RPL) top = pair_max_u16(top, magnitudes(load<false>(row + g)));
+        for (int row = ROWS; row < len; row += RPL) top = pair_max_u16(top, magnitudes(load<false>(row + g)));
         return wave_max(max(top & 0xffffu, top >> 16));
     }
 
@@ -318,15 +316,15 @@ struct Run {
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) store(u * RPL + g, raw[u], r);
-        for (int row = 64; row < len; row += RPL) store(row + g, load<false>(row + g), r);
+        for (int row = ROWS; row < len; row += RPL) store(row + g, load<false>(row + g), r);
         if (lane == 0) *scale = s;
     }
 };
 
 // One wavefront for a head (of K or of V) and `slab` tokens (ONE: one): it writes the runs that begin among them, each whole, also past the slab's end.
 // The wavefronts of a workgroup have neighbouring heads, whose rows lie side by side.  Bound by memory where there is much to write: 10240 tokens of 32 heads
-// of 128 (252 MB) 44.7 us, 5.6 TB/s; without the hint on the loads 52; all four wavefronts on one head's run 69.
-template <int D, bool ONE>
+// of 128 (252 MB) 44.3 us, 5.7 TB/s; without the hint on the loads 52; all four wavefronts on one head's run 69.
+template <int D, bool ONE, int ROWS>
 __global__ __launch_bounds__(256)
 void kv8_append_kernel(Side k, Side v, int T, int Hkv, const int32_t *__restrict__ slot, int32_t slots, int shift, int slab)
 {
@@ -338,7 +336,7 @@ void kv8_append_kernel(Side k, Side v, int T, int Hkv, const int32_t *__restrict
     for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1) {
         const int l0 = ONE ? 0 : __builtin_ctzll(leaders);
         const int len = run_length(slot, T, w, t_first, l0, 1 << shift);
-        Run<D> run;
+        Run<D, ROWS> run;
         run.end(run.begin(which < Hkv ? k : v, h, Hkv, __builtin_amdgcn_readlane(w.got, l0), len, t_first + l0, shift));
         if constexpr (ONE) break;
     }
@@ -394,8 +392,11 @@ hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ld
     const int     slab = T * heads <= 16384 ? 1 : T * heads <= 131072 ? 8 : 64;
     const int64_t grid = ((T + slab - 1) / slab * heads + 3) / 4;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-    auto kern = slab == 1 ? (D == 128 ? &kv8_append_kernel<128, true> : &kv8_append_kernel<64, true>)
-                          : (D == 128 ? &kv8_append_kernel<128, false> : &kv8_append_kernel<64, false>);
+    // Runs of up to 128 rows keep all of them, where there are many tokens (5120 of 32 heads of 128: 45.0 us with 64 rows kept, 32.3 so); few are single ones
+    // mostly, and want the wavefronts that fewer registers allow (64 single tokens 4.2 us, 7.0).
+    auto kern = slab == 1             ? (D == 128 ? &kv8_append_kernel<128, true, 64> : &kv8_append_kernel<64, true, 64>)
+                : block_tokens == 128 ? (D == 128 ? &kv8_append_kernel<128, false, 128> : &kv8_append_kernel<64, false, 128>)
+                                      : (D == 128 ? &kv8_append_kernel<128, false, 64> : &kv8_append_kernel<64, false, 64>);
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, stream, ks, vs, (int)T, Hkv, slot, slots, shift, slab);
     return hipGetLastError();
 }
