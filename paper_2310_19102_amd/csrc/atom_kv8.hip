@@ -255,7 +255,7 @@ struct Run {
     uint4 raw[kLoads];
     const __half *rows; int64_t ld;
     int8_t *block; float *scale;
-    int o, len, g, j;
+    int o, at, len, g, j;                                                   // o: older rows; at: of the block, this wavefront's first row
     float s_old;
 
     // ONCE: with the hint that nothing reads the row again
@@ -268,8 +268,8 @@ struct Run {
         return make_uint4(v[0], v[1], v[2], v[3]);
     }
 
-    // the run's rows on their way to the registers, and their largest magnitude (the bits of a half)
-    __device__ __forceinline__ uint32_t begin(const Side &side, int h, int Hkv, int32_t first, int len_, int64_t t, int shift)
+    // the run's rows (or ROWS of them from `row0` on) on their way to the registers, and their largest magnitude (the bits of a half)
+    __device__ __forceinline__ uint32_t begin(const Side &side, int h, int Hkv, int32_t first, int len_, int64_t t, int shift, int row0 = 0)
     {
         const int lane = threadIdx.x & 63;
         g = lane / LPR;
@@ -277,10 +277,11 @@ struct Run {
         len = len_;
         ld = side.ld;
         o = first & ((1 << shift) - 1);
-        const int64_t at = (int64_t)(first >> shift) * Hkv + h;             // block and head
-        block = side.codes + (at << shift) * D;
-        scale = side.scale + at;
-        rows = side.x + (int64_t)h * D + t * ld + 8 * j;
+        at = o + row0;
+        const int64_t head = (int64_t)(first >> shift) * Hkv + h;           // block and head
+        block = side.codes + (head << shift) * D;
+        scale = side.scale + head;
+        rows = side.x + (int64_t)h * D + (t + row0) * ld + 8 * j;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) raw[u] = load<true>(u * RPL + g);
@@ -296,18 +297,18 @@ struct Run {
     __device__ __forceinline__ void store(int row, const uint4 &v, float r)
     {
         if (row < len)
-            *reinterpret_cast<uint2 *>(block + (o + row) * D + 8 * j) = make_uint2(codes4(v.x, v.y, r), codes4(v.z, v.w, r));
+            *reinterpret_cast<uint2 *>(block + (at + row) * D + 8 * j) = make_uint2(codes4(v.x, v.y, r), codes4(v.z, v.w, r));
     }
 
-    __device__ __forceinline__ void end(uint32_t top)                   
+    // `top` of the whole run; `thread` of `threads` that have one: the older rows are theirs in turn
+    __device__ __forceinline__ void end(uint32_t top, int thread, int threads)
     {
-        const int lane = threadIdx.x & 63;
         const float amax = __half2float(__ushort_as_half((unsigned short)top));
         const float s_new = amax / 127.0f, s = s_new > s_old ? s_new : s_old;
         const float r = s > 0.0f ? 1.0f / s : 0.0f;
         if (s > s_old && s_old > 0.0f) {                                    // the older rows on the new scale
             const float ratio = s_old / s;
-            for (int i = 16 * lane; i < o * D; i += 1024) {
+            for (int i = 16 * thread; i < o * D; i += 16 * threads) {
                 uint4 w = *reinterpret_cast<const uint4 *>(block + i);
                 w = make_uint4(recode4(w.x, ratio), recode4(w.y, ratio), recode4(w.z, ratio), recode4(w.w, ratio));
                 *reinterpret_cast<uint4 *>(block + i) = w;
@@ -317,28 +318,53 @@ struct Run {
         for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) store(u * RPL + g, raw[u], r);
         for (int row = ROWS; row < len; row += RPL) store(row + g, load<false>(row + g), r);
-        if (lane == 0) *scale = s;
+        if (thread == 0) *scale = s;
     }
 };
 
-// One wavefront for a head (of K or of V) and `slab` tokens (ONE: one): it writes the runs that begin among them, each whole, also past the slab's end.
-// The wavefronts of a workgroup have neighbouring heads, whose rows lie side by side.  Bound by memory where there is much to write: 10240 tokens of 32 heads
-// of 128 (252 MB) 44.3 us, 5.7 TB/s; without the hint on the loads 52; all four wavefronts on one head's run 69.
-template <int D, bool ONE, int ROWS>
+// Few tokens: one wavefront for a head (of K or of V) and a token; where a run begins with that token it writes the run, whole.
+template <int D>
 __global__ __launch_bounds__(256)
-void kv8_append_kernel(Side k, Side v, int T, int Hkv, const int32_t *__restrict__ slot, int32_t slots, int shift, int slab)
+void kv8_append_kernel(Side k, Side v, int T, int Hkv, const int32_t *__restrict__ slot, int32_t slots, int shift)
 {
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t group = item / (2 * Hkv), t_first = ONE ? group : group * slab;
-    const int which = (int)(item - group * (2 * Hkv)), h = which % Hkv;
-    if (t_first >= T) return;
-    const Window w = window(slot, slots, T, t_first, ONE ? 1 : slab, 1 << shift);
-    for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1) {
-        const int l0 = ONE ? 0 : __builtin_ctzll(leaders);
-        const int len = run_length(slot, T, w, t_first, l0, 1 << shift);
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = item / (2 * Hkv);
+    const int which = (int)(item - t * (2 * Hkv)), h = which % Hkv;
+    if (t >= T) return;
+    const Window w = window(slot, slots, T, t, 1, 1 << shift);
+    if (!w.leaders) return;
+    Run<D, 64> run;
+    run.end(run.begin(which < Hkv ? k : v, h, Hkv, __builtin_amdgcn_readlane(w.got, 0), run_length(slot, T, w, t, 0, 1 << shift), t, shift),
+            threadIdx.x & 63, 64);
+}
+
+// Many tokens: a workgroup of four wavefronts for a head and `slab` tokens writes the runs that begin among them, each whole, also past the slab's end.  Up to three
+// runs are written by all four, ROWS rows each; more of them, and runs of ROWS at most, one by each in turn.  A lone wavefront's code for 64 rows is 9 KB that it goes through once, at the
+// pace of the instructions' way from the L2: 9 us for a chunk of 512 tokens of 8 heads where four together take 4.1, and 30 for 5120 tokens in blocks of 128 where they take
+// 9.6.  Bound by memory where there is much to write: 10240 tokens of 32 heads of 128 (252 MB) 43.4 us, 5.8 TB/s; without the hint on the loads 52.
+template <int D, int ROWS>
+__global__ __launch_bounds__(256)
+void kv8_append_many_kernel(Side k, Side v, int T, int Hkv, const int32_t *__restrict__ slot, int32_t slots, int shift, int slab)
+{
+    __shared__ uint32_t s_top[2][4];
+    const int64_t group = blockIdx.x / (2 * Hkv), t_first = group * slab;
+    const int which = (int)(blockIdx.x - group * (2 * Hkv)), h = which % Hkv, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Side side = which < Hkv ? k : v;
+    const Window w = window(slot, slots, T, t_first, slab, 1 << shift);        // (the same in all four)
+    const bool alone = __builtin_popcountll(w.leaders) > 3 || 1 << shift <= ROWS;
+    int turn = 0;                                                            // of the runs; nobody writes maxima before all have read the last but one's
+    for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1, ++turn) {
+        if (alone && (turn & 3) != wave) continue;
+        const int l0 = __builtin_ctzll(leaders), len = run_length(slot, T, w, t_first, l0, 1 << shift);
+        const int row0 = alone ? 0 : wave * ROWS, rows = alone ? len : min(max(len - row0, 0), ROWS);
         Run<D, ROWS> run;
-        run.end(run.begin(which < Hkv ? k : v, h, Hkv, __builtin_amdgcn_readlane(w.got, l0), len, t_first + l0, shift));
-        if constexpr (ONE) break;
+        uint32_t top = run.begin(side, h, Hkv, __builtin_amdgcn_readlane(w.got, l0), rows, t_first + l0, shift, row0);
+        if (!alone) {
+            uint32_t *tops = s_top[turn & 1];
+            if ((threadIdx.x & 63) == 0) tops[wave] = top;
+            __syncthreads();
+            top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+        }
+        run.end(top, alone ? threadIdx.x & 63 : threadIdx.x, alone ? 64 : 256);
     }
 }
 
@@ -379,6 +405,8 @@ hipError_t launch_kv_block_map(const int32_t *past, const int32_t *fresh, int B,
     return hipGetLastError();
 }
 
+constexpr int64_t kManyTokens = 256;
+
 hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ldk, int64_t ldv, int Hkv, int D,
                              const int32_t *slot, int64_t n_blocks, int block_tokens, void *k_codes, float *k_scale,
                              void *v_codes, float *v_scale, hipStream_t stream)
@@ -387,16 +415,20 @@ hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ld
     const Side ks = {(const __half *)k, ldk, (int8_t *)k_codes, k_scale}, vs = {(const __half *)v, ldv, (int8_t *)v_codes, v_scale};
     const int32_t slots = (int32_t)(n_blocks * block_tokens);
     const int     shift = __builtin_ctz((unsigned)block_tokens);
-    // Tokens to a wavefront: one up to as many wavefronts as the card has places for (64 sequences of 32 heads: 4096), then 8 and 64, so that
-    // those that find no run's beginning are few: a step of so many tokens has long runs.
-    const int     slab = T * heads <= 16384 ? 1 : T * heads <= 131072 ? 8 : 64;
-    const int64_t grid = ((T + slab - 1) / slab * heads + 3) / 4;
+    // Blocks of 64 tokens and more have long runs, which want four wavefronts; short ones a lone wavefront writes as fast, so the many of a workgroup start later there
+    // (16 cache heads of 64, blocks of 16, 331 tokens 4.4 us, 5.5 the other way; 8 of 128, blocks of 64, a chunk of 512 9.0 and 4.3).
+    const bool long_runs = block_tokens >= 64;
+    if (long_runs ? T < kManyTokens : T * heads <= 16384) {
+        const int64_t grid = (T * heads + 3) / 4;
+        hipLaunchKernelGGL((D == 128 ? &kv8_append_kernel<128> : &kv8_append_kernel<64>), dim3((unsigned)grid), dim3(256), 0, stream, ks, vs, (int)T, Hkv, slot, slots, shift);
+        return hipGetLastError();
+    }
+    // 8 tokens to a workgroup, and 64 from as many on as fill the card so (a workgroup that finds no run's beginning costs more than several runs in one).
+    const int     slab = T * heads <= 16384 ? 8 : 64;
+    const int64_t grid = (T + slab - 1) / slab * heads;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-    // Runs of up to 128 rows keep all of them, where there are many tokens (5120 of 32 heads of 128: 45.0 us with 64 rows kept, 32.3 so); few are single ones
-    // mostly, and want the wavefronts that fewer registers allow (64 single tokens 4.2 us, 7.0).
-    auto kern = slab == 1             ? (D == 128 ? &kv8_append_kernel<128, true, 64> : &kv8_append_kernel<64, true, 64>)
-                : block_tokens == 128 ? (D == 128 ? &kv8_append_kernel<128, false, 128> : &kv8_append_kernel<64, false, 128>)
-                                      : (D == 128 ? &kv8_append_kernel<128, false, 64> : &kv8_append_kernel<64, false, 64>);
+    auto kern = block_tokens == 128 || block_tokens == 32 ? (D == 128 ? &kv8_append_many_kernel<128, 32> : &kv8_append_many_kernel<64, 32>)
+                                     : (D == 128 ? &kv8_append_many_kernel<128, 16> : &kv8_append_many_kernel<64, 16>);
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, stream, ks, vs, (int)T, Hkv, slot, slots, shift, slab);
     return hipGetLastError();
 }

@@ -192,6 +192,24 @@ def test_append_takes_slices_of_a_projection_and_any_slots():
     atom.atom_kv8_append(qkv[:0, :Hkv], qkv[:0, :Hkv], kc, vc, i32())
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bs", [16, 32, 64, 128])
+@pytest.mark.parametrize("Hkv", [3, 20])
+def test_append_of_many_tokens(D, bs, Hkv):
+    """Prompts, chunks and single tokens in one call of so many tokens that workgroups share runs and take several: runs of all lengths, in
+    blocks with and without older rows."""
+    g = torch.Generator(device="cuda").manual_seed(bs + Hkv)
+    past, new = [0, 7, bs - 1, 2 * bs + 3, 1, 0, 0, bs] + [5 * i for i in range(40)], [400, 3, 2, 150, bs, 0, 1, 65] + [1 + i % 4 for i in range(40)]
+    W = 40 + 400 // bs
+    table = torch.randperm(48 * W, generator=g, device="cuda").view(48, W).cpu()
+    T = sum(new) + 9
+    rows = [int(table[b, (n + i) // bs]) * bs + (n + i) % bs for b, n in enumerate(past) for i in range(new[b])]
+    slot = i32(*rows, *[-1] * 9)
+    k, v = (torch.randn((T, Hkv, D), generator=g, device="cuda").to(torch.float16) for _ in "kv")
+    kc, vc = caches(48 * W, Hkv, bs, D, seed=bs)
+    check_append(k, v, kc, vc, slot)
+
+
 def test_append_of_what_is_not_finite_spoils_its_own_block_and_head():
     D, bs, Hkv, T = 128, 32, 3, 90
     g = torch.Generator(device="cuda").manual_seed(2)
