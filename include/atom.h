@@ -602,7 +602,9 @@ atom_status atom_kv_block_map(const int32_t *past_len, const int32_t *new_len, i
  * IEEE fp32, every step rounded once: results are bit-exact.  A row is off by half a step of the block's scale when it is
  * written, and by at most half a step of the present scale more each time that the scale has grown since.
  * Rows of the block behind the run are left as they are.  The same call once more changes nothing.
- * A value that is not finite spoils its block for its head, nothing else.
+ * A value that is not finite spoils its block for its head, nothing else, and shows: max here is NaN if either side is, so the scale
+ * becomes NaN or infinite and stays so until the block is begun anew (o = 0).  Codes written under such a scale are 0; older rows' codes are left as
+ * they are under NaN (no scale has grown) and become 0 under infinity.
  *
  *   k_f16, v_f16   device fp16, token t's heads from t * ldk (ldv) on, [Hkv, D] each; 16-byte aligned, ld % 8 == 0: slices
  *                  of a fused projection's output as they are

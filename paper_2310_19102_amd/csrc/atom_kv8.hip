@@ -162,7 +162,7 @@ __device__ __forceinline__ uint32_t pair_max_u16(uint32_t a, uint32_t b)
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
 }
 
-// The larger magnitude of each half (of finite numbers: their bits without the sign are in order).
+// The larger magnitude of each half: their bits without the sign are in order, infinity above all numbers and NaN above that.
 __device__ __forceinline__ uint32_t magnitudes(const uint4 &v)
 {
     constexpr uint32_t m = 0x7fff7fffu;
@@ -184,7 +184,8 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 }
 
 // rne(v) in the low byte, for |v| <= 127.5: adding 1.5 * 2^23 rounds to the nearest even integer and leaves it there.  The clamp to 127 is implied: a value is at
-// most max|x|, the scale at least max|x| / 127, each of the three roundings on the way below 2^-23 of 127.
+// most max|x|, the scale at least max|x| / 127, each of the three roundings on the way below 2^-23 of 127.  Under a scale that is not finite the factor is 0, and
+// so are the codes: also of NaN, whose low byte is 0 when it comes from a half (the low 13 bits of its significand are).
 __device__ __forceinline__ uint32_t code_of(float v) { return __builtin_bit_cast(uint32_t, v + 12582912.0f); }
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
@@ -246,7 +247,8 @@ __device__ __forceinline__ int run_length(const int32_t *__restrict__ slot, int 
 // A run of one head's rows, by one wavefront.  A run's scale is the larger of the block's
 // (where the block holds older rows, those before the run's first) and max|x| / 127:
 //   s = max(s_old, max|x| / 127), r = 1 / s, code = clamp(rne(x * r), -127, 127)   IEEE fp32, every step rounded once
-// and where s grows, the older rows become rne(code * (s_old / s)).
+// and where s grows, the older rows become rne(code * (s_old / s)).  The maximum of a NaN and anything is NaN, so what is not finite stays in
+// the scale, where readers find it.
 // Rows stay in registers between the maximum and the codes (ROWS of them; those of a longer run are read twice, the second time
 // from the cache).  16-byte loads, 8 values a lane: D / 8 lanes a row.
 template <int D, int ROWS>
@@ -304,7 +306,7 @@ struct Run {
     __device__ __forceinline__ void end(uint32_t top, int thread, int threads)
     {
         const float amax = __half2float(__ushort_as_half((unsigned short)top));
-        const float s_new = amax / 127.0f, s = s_new > s_old ? s_new : s_old;
+        const float s_new = amax / 127.0f, s = s_new > s_old || s_new != s_new ? s_new : s_old;      // (NaN if either is)
         const float r = s > 0.0f ? 1.0f / s : 0.0f;
         if (s > s_old && s_old > 0.0f) {                                    // the older rows on the new scale
             const float ratio = s_old / s;
