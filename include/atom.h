@@ -629,8 +629,8 @@ atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int
  * fp32 softmax and sums; queries and codes meet exactly in the fp16 matrix cores, the softmax weights travel as fp16.
  * Keys of a block number outside [0, n_blocks) (-1: none) and beyond W * block_tokens do not exist; a query
  * that sees no key gives zeros.  Rows of out behind token_start[B], and of tokens beyond max_new of a request, are left as
- * they were; rows of q there are not read.  out may be q itself (with ldo = ldq), and overlaps no input otherwise.  A block whose scale is not finite spoils the
- * queries that see it, no other.
+ * they were; rows of q there are not read.  out may be q itself (with ldo = ldq), and overlaps no input otherwise.  Queries that
+ * see a key of a block whose scale is not finite give NaN, no others do.
  *
  *   q_f16          device fp16, token t's heads [H, D] from t * ldq on; out_f16 likewise with ldo.  16-byte aligned, ld % 8 == 0
  *   max_new        no request has more new tokens (T if nothing is known: the call is sized by it, 1 for a decoding step)

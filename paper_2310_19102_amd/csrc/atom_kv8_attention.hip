@@ -25,6 +25,18 @@ constexpr int   kAllKeys = 0x40000000;            // as many as a request has at
 // A block's factor and value scale as the kernels take them lie between these: never zero and never infinite, so that a masked score of minus infinity
 // stays one whatever the block holds, and a block of zeros has a weight to be divided out again.
 constexpr float kLeastFactor = 1e-37f, kLeastValue = 2.3283064365386963e-10f, kMost = 1e35f;
+// A block whose scale is not finite gives NaN to the rows that see it: their sum is made NaN at the end, by the first key of such a block (0x7fffffff: none), so
+// that masked rows of the same tile keep finite numbers all the way and the loops carry nothing for it.
+constexpr int kNoKey = 0x7fffffff;
+
+// The first lane's `key` (they ascend) whose block exists (unit) and has a scale that is not finite.
+__device__ __forceinline__ int first_spoiled(int key, int unit, float k_scale, float v_scale)
+{
+    const uint64_t bad = __ballot(unit >= 0 && !(__builtin_isfinite(k_scale) && __builtin_isfinite(v_scale)));
+    return bad ? __builtin_amdgcn_readlane(key, __builtin_ctzll(bad)) : kNoKey;
+}
+// What a row's accumulators are multiplied by (values were 2^-9 of the codes): 0 for a row that sees no key, NaN for a NaN sum.
+__device__ __forceinline__ float quotient(float sum) { return sum == 0.0f ? 0.0f : 512.0f / sum; }
 
 // What all kernels of a call are told.
 struct Args {
@@ -320,7 +332,7 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
     u4 kr[2][KB / 16];
     uint32_t vr[8][VB / 4];
     // lane i: block of 16 keys number i of this wavefront's (two to a step)
-    int   unit = -1;
+    int   unit = -1, spoiled = kNoKey;
     float b_scale = 0.0f, b_log = 0.0f, b_inv = 0.0f;
     const int32_t *table = a.table + (int64_t)w.b * a.W;
     auto key_of = [&](int step) { return key0 + (step * kWaves + wave) * kStep; };
@@ -334,7 +346,8 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
         b_scale = a.ks[at];
         b_log = a.vs[at];
     };
-    auto take_scales = [&]() {                        // (no such keys: e is minus infinity)
+    auto take_scales = [&](int step) {                // (no such keys: e is minus infinity)
+        spoiled = min(spoiled, first_spoiled(block_key(step), unit, b_scale, b_log));
         const float v = fminf(fmaxf(b_log, kLeastValue), kMost);
         b_scale = unit < 0 ? 1.0f : fminf(fmaxf(b_scale * to_e, kLeastFactor), kMost);
         b_log = unit < 0 ? -INFINITY : __builtin_amdgcn_logf(v);
@@ -463,7 +476,7 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
         look_up(0, page);
         fetch_k(0);
         fetch_v(0);
-        take_scales();
+        take_scales(0);
 #pragma unroll
         for (int t = 0; t < SETS; ++t) {
 #pragma unroll
@@ -479,7 +492,7 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
                     fetch_k(step + 1);
                 }
                 fetch_v(step + 1);
-                if (((step + 1) & 31) == 0) take_scales();
+                if (((step + 1) & 31) == 0) take_scales(step + 1);
             }
         }
     }
@@ -487,7 +500,7 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
     // ---- the wavefronts meet
 #pragma unroll
     for (int t = 0; t < SETS; ++t) {
-        l[t] = sum_of_chunks(l[t]);
+        l[t] = sees[t] > spoiled ? NAN : sum_of_chunks(l[t]);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -515,7 +528,7 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
             o += v * f;
         }
         if (whole) {
-            const float f = sum > 0.0f ? 512.0f / sum : 0.0f;         // (values were 2^-9 of the codes)
+            const float f = quotient(sum);
             const int rw = w.tile * kTileRows + rr, t = by_group(a, rw);
             __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + rw - t * a.group) * D + d;
             const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
@@ -612,6 +625,7 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
 
     // ---- blocks: lane i has the block of 16 keys number i of 16 tiles, its place and its scales; another register the blocks of K's tiles
     const int32_t *table = a.table + (int64_t)w.b * a.W;
+    int   spoiled = kNoKey;
     int   page = -1, page_k = -1, unit = -1, unit_k = -1;      // block numbers of the table; rows / 16 in the whole cache, -1: no such keys
     float ks = 0.0f, vs = 0.0f, b_scale, b_log, b_inv;
     auto key_of = [&](int tile) { return key0 + tile * kKeys + 16 * lane; };
@@ -632,7 +646,8 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
         ks = a.ks[at];
         vs = a.vs[at];
     };
-    auto take_scales = [&]() {
+    auto take_scales = [&](int tile) {
+        spoiled = min(spoiled, first_spoiled(key_of(tile), unit, ks, vs));
         const float v = fminf(fmaxf(vs, kLeastValue), kMost);
         b_scale = unit < 0 ? 1.0f : fminf(fmaxf(ks * to_e, kLeastFactor), kMost);
         b_log = unit < 0 ? -INFINITY : __builtin_amdgcn_logf(v);
@@ -813,7 +828,7 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
         for (int s = 0; s < KS; ++s) start = add8(q[s], start);
         start += __shfl_xor(start, 32, 64);
         start *= -128.0f * 5.9604644775390625e-08f;
-        take_scales();
+        take_scales(0);
         __syncthreads();
         f16v x, y;
         first_scores(lds + L::bytes, x);
@@ -834,7 +849,7 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
                 for (int k = 0; k < kPieces; ++k) next_k(k);
             }
             if (ahead == 0) take_units(t + 2);
-            if (block == 60) take_scales();
+            if (block == 60) take_scales(t + 1);
             fetch_k(unit_k, ahead, kr);
             if (key + 32 < wave1) {
                 half_tile(here, 1, y, x, (block + 4) & 63, next_v, vPieces);
@@ -850,11 +865,12 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
     }
 
     l += __shfl_xor(l, 32, 64);
+    if (sees > spoiled) l = NAN;
     if (w.splits == 1) {
         // by way of this wavefront's own part of LDS, so that a store has whole rows (nobody reads codes there any more)
         constexpr int pitch = 2 * D + 16, lanes = D / 8;      // lanes of a row
         unsigned char *mine = lds + wave * 32 * pitch;
-        const float f = l > 0.0f ? 512.0f / l : 0.0f;         // (values were 2^-9 of the codes)
+        const float f = quotient(l);
 #pragma unroll
         for (int i = 0; i < DB; ++i)
 #pragma unroll
@@ -946,7 +962,7 @@ void attention_kv8_merge_kernel(const Args a, const Job few, const Job many)
                 o += v[k] * f;
             }
         }
-        const float f = sum > 0.0f ? 512.0f / sum : 0.0f;
+        const float f = quotient(sum);
         const int row = first + rr, t = by_group(a, row);
         __half *to = a.out + (int64_t)(r.start + t) * a.ldo + (int64_t)(h * a.group + row - t * a.group) * D + d;
         const __half2 lo = __floats2half2_rn(o[0] * f, o[1] * f), hi = __floats2half2_rn(o[2] * f, o[3] * f);
