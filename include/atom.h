@@ -626,7 +626,8 @@ atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int
  * tokens.  Request b's queries are tokens token_start[b] .. token_start[b + 1] - 1; with n of them and
  * L = seq_len[b], query i is at position L - n + i and sees the keys 0 .. L - n + i:
  *   out[t, h, :] = softmax_s( sm_scale * q[t, h, :] . K[s] ) V[s],  K, V of cache head h / (H / Hkv)
- * fp32 softmax and sums; queries and codes meet exactly in the fp16 matrix cores, the softmax weights travel as fp16.
+ * fp32 softmax and sums; queries and codes meet exactly in the fp16 matrix cores.  The softmax weights (times their blocks' value scales) travel as
+ * fp16: each is off by 2^-11 of itself, or by 2^-30 of the query's largest where that is more.
  * Keys of a block number outside [0, n_blocks) (-1: none) and beyond W * block_tokens do not exist; a query
  * that sees no key gives zeros.  Rows of out behind token_start[B], and of tokens beyond max_new of a request, are left as
  * they were; rows of q there are not read.  out may be q itself (with ldo = ldq), and overlaps no input otherwise.  Queries that

@@ -20,7 +20,10 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 typedef unsigned u2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e   = 1.4426950408889634f;
-constexpr float kNoScore = -1e30f;                // the running maximum before the first key: below every score, and finite
+constexpr float kNoScore = -1e30f;                // the running bound M before the first key: below every score, and finite
+// Weights are 2^(e - M) up to 2^kLargest, inside fp16's range (M: so far below the largest e when it is set).  A row's M moves when its e have grown by 2^8 (few
+// rows) or a sum of eight weights by 2^10 (many rows) since.
+constexpr float kLargest = 15.0f, kMostSum = 32768.0f, kRaisedFew = 7.0f, kRaisedMany = 5.0f;
 constexpr int   kAllKeys = 0x40000000;            // as many as a request has at most, and a multiple of 128
 // A block's factor and value scale as the kernels take them lie between these: never zero and never infinite, so that a masked score of minus infinity
 // stays one whatever the block holds, and a block of zeros has a weight to be divided out again.
@@ -273,12 +276,14 @@ __device__ __forceinline__ float sum_of_chunks(float v)
 //   scores: S^T = K Q^T on 16x16x32 fp16 matrix instructions.  Keys are the rows, so that a lane holds four keys of ONE query row.  Lane (l & 15, c =
 //           l >> 4) has the 16 dimensions from 16 c on of every 64 of key l & 15; the order of the dimensions within a product is free as long as Q has the
 //           same.  A load of 1 KB takes eight whole rows of 128 dimensions (half rows of 16 keys: 6.1 TB/s became 5.6), and lanes eight apart then trade halves.  The offset of u = code + 128 leaves through the accumulator's start, -128 sum(q) 2^-24.
-//   softmax: e = score * log2(e) * sm_scale * k_scale + log2(v_scale), p = 2^(e - M) with M a bound on e so far: the block's value scale sits in the
-//           weight, so the matrix instruction adds codes of blocks of different scales, and the weights are near one where
-//           they count, whatever the scales are.  The sum of the softmax takes p / v_scale.  M moves only where some e passes it by 8 (p <= 2^8 then).
+//   softmax: e = score * log2(e) * sm_scale * k_scale + log2(v_scale), p = 2^(e - M) with M seven below the largest e so far: the block's value scale sits in the
+//           weight, so the matrix instruction adds codes of blocks of different scales, and the weights are in one range where
+//           they count, whatever the scales are.  The sum of the softmax takes p / v_scale.  M moves only where some e passes it by 15 (p <= 2^15 then).
 //   values: O^T = V^T P^T.  The weights lie in the registers of the scores as the second operand wants them when its order of keys is
 //           that of the scores' rows; V's rows are loaded in that order, D / 16 bytes a lane, and the byte selection that makes halves also
-//           transposes.  No LDS, no lane exchange in the loop.  The weights travel as fp16 (rounded to nearest even: by 2^-11 of themselves at most).
+//           transposes.  No LDS in the loop, and no lane exchange but ordered()'s.  The weights travel as fp16 (fp32 products run at a sixteenth of the rate): rounded to nearest
+//           even, by 2^-11 of themselves, or by 2^-25 below 2^-14.  The largest one is 2^7 at least, so that is 2^-32 of it (2^-30 with
+//           many rows): with the largest at one, a context of small weights beside it (a first key that all attend to, 65536 others of 2^-22.7) was 20 % off.
 //   loads: the next step's rows of K are asked for once the scores have used this step's, those of V after the values: half the registers of two
 //           buffers.  Block numbers and scales of 64 blocks of 16 keys are read at once, a lane each.
 //   rows:  SETS = 2: tiles of 32 rows, the codes turned into halves once for two sets of 16.
@@ -423,8 +428,8 @@ __device__ __forceinline__ void rows_tile(const Args &a, const Job &job, int ind
         h8 p[SETS];
 #pragma unroll
         for (int t = 0; t < SETS; ++t) {
-            if (__ballot(top[t] > M[t] + 8.0f)) {     // rare after the first steps
-                const float to = fmaxf(M[t], max_of_chunks(top[t]));
+            if (__ballot(top[t] > M[t] + kLargest)) { // rare after the first steps
+                const float to = fmaxf(M[t], max_of_chunks(top[t]) - kRaisedFew);
                 const float down = __builtin_amdgcn_exp2f(M[t] - to);
                 M[t] = to;
                 l[t] *= down;
@@ -754,11 +759,11 @@ __device__ __forceinline__ void many_rows_tile(const Args &a, const Job &job, in
             __builtin_amdgcn_sched_barrier(0);
         }
         weights(KS - 1);
-        // M is a bound on e but for the last few binary orders: what passes it by many shows in the sums (the first keys of a row: M is none yet).  No
+        // M is five below the largest e, or up to ten lower: what passes it by more shows in the sums (the first keys of a row: M is none yet).  No
         // maxima where it does not, a sixth of the vector unit's work.
-        if (__ballot(sum[0] > 1024.0f || sum[1] > 1024.0f)) {
+        if (__ballot(sum[0] > kMostSum || sum[1] > kMostSum)) {
             const float top = fmaxf(largest(now, 0), largest(now, 1));
-            const float to = fmaxf(M, fmaxf(top, __shfl_xor(top, 32, 64)));
+            const float to = fmaxf(M, fmaxf(top, __shfl_xor(top, 32, 64)) - kRaisedMany);
             const float down = __builtin_amdgcn_exp2f(M - to);
             M = to;
             l *= down;

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_kv8 import Case, npy
+from test_gpu_kv8 import Case, i32, npy
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +85,32 @@ def test_a_query_finds_its_key(H, Hkv, D, bs, past, new, extra):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,Hkv,past,new,few", [(8, 8, 1 << 16, [1] * 140, True), (64, 8, 65000, [1100], False)])
+def test_many_small_weights_beside_a_large_one(H, Hkv, past, new, few, D):
+    """A first key that every query attends to and whose value is zero, and 65000 others with weights of 2^-22.68 of its: the output is what these add up to, 1 % of their
+    value.  A weight travels as fp16, off by 2^-11 of itself or 2^-30 of the largest; here 2^-30 / 2^-22.68 = 0.6 %, the same for all of them.  The output's own
+    rounding is 2^-11, of the exponents 24 * 2^-23 at most, the sums' 2^-12 of a chain of 2048 additions."""
+    bs, keys = 128, past + max(new)
+    c = Case(H, Hkv, D, bs, [bs], [0], seed=1)              # two blocks: the first keys, and one that stands for all others
+    q0 = 15.71875
+    B, T = len(new), sum(new)
+    table = torch.ones((B, -(-keys // bs)), dtype=torch.int32, device="cuda")
+    table[:, 0] = 0
+    c.kc[0].zero_()
+    c.kc[0][0, :, 0, 0] = 64                                # its score is q0, theirs 0
+    c.kc[1].fill_(2.0 ** -6)
+    c.vc[0].fill_(100)
+    c.vc[0][0, :, 0] = 0
+    c.vc[1].fill_(2.0 ** -6)
+    c.q = torch.zeros((T, H, D), dtype=torch.float16, device="cuda")
+    c.q[:, :, 0] = q0
+    c.table, c.T, c.max_new, c.sm, c.W = table, T, max(new), 1.0, table.shape[1]
+    c.start = i32(*np.concatenate([[0], np.cumsum(new)]).tolist())
+    c.len = i32(*[past + n for n in new])
+    assert c.route()[1:] == (False, not few, False)
+    got = npy(c.call()).astype(np.float64)
+    seen = np.concatenate([past + 1 + np.arange(n) for n in new])
+    others = (seen - 1) * np.exp(-q0)
+    want = (others / (1 + others) * 100 * 2.0 ** -6)[:, None, None]
+    rel = 2.0 ** -11 + 2.0 ** -30 * np.exp(q0) + 2.0 ** -11 + 24 * 2.0 ** -23 + 2.0 ** -12
+    assert (np.abs(got - want) <= rel * want).all(), np.abs(got / want - 1).max()
