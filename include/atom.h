@@ -614,7 +614,8 @@ atom_status atom_kv_block_map(const int32_t *past_len, const int32_t *new_len, i
  * The tokens that one call writes into a block have to be one run, a slot may not come twice: a block that
  * two runs share gets undefined contents (no other block does).
  * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE, ATOM_ERR_ALIGN, ATOM_ERR_UNSUPPORTED (block_tokens, D, n_blocks *
- * block_tokens >= 2^31, n_blocks * Hkv * block_tokens >= 2^35, T * Hkv >= 2^31).  T = 0 returns ATOM_OK.
+ * block_tokens >= 2^31, n_blocks * Hkv * block_tokens >= 2^35, a launch of 2^32 threads or more: 512 Hkv for 64 tokens, or for
+ * fewer than 256 tokens in blocks of 64 and more 128 Hkv for each).  T = 0 returns ATOM_OK.
  */
 atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int64_t ldk, int64_t ldv,
                             int32_t Hkv, int32_t D, const int32_t *slot, int64_t n_blocks,
@@ -642,7 +643,8 @@ atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int
  *                  Contents need no initialisation and are dead after the call.
  * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE (H % Hkv, negative sizes, W = 0 with B > 0, ld), ATOM_ERR_ALIGN,
  * ATOM_ERR_UNSUPPORTED (block_tokens, D, sm_scale negative, above 1e6 or no number, W * block_tokens > 2^30, a cache that
- * atom_kv8_append does not take, T * H >= 2^31, more than 2^31 - 1 workgroups), ATOM_ERR_WORKSPACE.
+ * atom_kv8_append does not take, T * H >= 2^31, a launch of 2^32 threads or more: as 2^24 single tokens times cache heads would be),
+ * ATOM_ERR_WORKSPACE.
  * T = 0, B = 0 or max_new = 0 returns ATOM_OK.
  */
 atom_status atom_attention_kv8(const void *q_f16, int64_t T, int64_t ldq, int32_t B, int32_t H,

@@ -102,7 +102,7 @@ atom_status kv8_attention(int64_t T, int32_t B, int32_t H, int32_t Hkv, int32_t 
     if (T < 0 || B < 0 || H <= 0 || Hkv <= 0 || H % Hkv || D <= 0 || max_new < 0 || W < 0 || (B > 0 && W == 0)) return ATOM_ERR_SHAPE;
     if ((D != 64 && D != 128) || !kv8_block(block_tokens) || T > 0x7ffffffeLL || W > 0x40000000LL / block_tokens ||
         B > 0x3fffffff || T * H > 0x7fffffffLL || (int64_t)max_new * (H / Hkv) > 0x7fffffffLL ||
-        !atom_internal::attention_kv8_fits(T, B, H, Hkv, max_new))
+        !atom_internal::attention_kv8_fits(T, B, H, Hkv, D, max_new, W, block_tokens))
         return ATOM_ERR_UNSUPPORTED;
     return ATOM_OK;
 }
@@ -610,7 +610,9 @@ atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int
                             void *v_codes, float *v_scale, void *stream)
 {
     if (T < 0 || Hkv <= 0 || D <= 0 || n_blocks <= 0 || ldk < (int64_t)Hkv * D || ldv < (int64_t)Hkv * D) return ATOM_ERR_SHAPE;
-    if (!kv8_cache(n_blocks, Hkv, D, block_tokens) || T > 0x7fffffffLL || T * Hkv > 0x7fffffffLL) return ATOM_ERR_UNSUPPORTED;
+    if (!kv8_cache(n_blocks, Hkv, D, block_tokens) || T > 0x7fffffffLL || T * Hkv > 0x7fffffffLL ||
+        !atom_internal::kv8_append_fits(T, Hkv, block_tokens))
+        return ATOM_ERR_UNSUPPORTED;
     if (T == 0) return ATOM_OK;
     if (!k_f16 || !v_f16 || !slot || !k_codes || !k_scale || !v_codes || !v_scale) return ATOM_ERR_NULL;
     if (!aligned(k_f16, 16) || !aligned(v_f16, 16) || (ldk % 8) || (ldv % 8) || !aligned(slot, 4) || !aligned(k_codes, 16) ||

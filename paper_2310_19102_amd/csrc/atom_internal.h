@@ -129,6 +129,7 @@ constexpr int kMaxMapRequests = 16384;     // two int32 each in one workgroup's 
 hipError_t launch_kv_block_map(const int32_t *past, const int32_t *fresh, int B, int block_tokens, const int32_t *free_blocks,
                                int64_t n_free, const int32_t *cursor, int32_t *table, int64_t W, int64_t T,
                                int32_t *token_start, int32_t *seq_len, int32_t *slot, int32_t *cursor_out, hipStream_t stream);
+bool       kv8_append_fits(int64_t T, int Hkv, int block_tokens);               // its grid
 hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ldk, int64_t ldv, int Hkv, int D,
                              const int32_t *slot, int64_t n_blocks, int block_tokens, void *k_codes, float *k_scale,
                              void *v_codes, float *v_scale, hipStream_t stream);
@@ -142,7 +143,7 @@ struct AttentionKv8 {
     void *workspace;
 };
 size_t     attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, int max_new, int64_t W, int block_tokens);
-bool       attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new);   // its grid
+bool       attention_kv8_fits(int64_t T, int B, int H, int Hkv, int D, int max_new, int64_t W, int block_tokens);   // its grids
 hipError_t launch_attention_kv8(const AttentionKv8 &a, hipStream_t stream);
 
 // The library's own per-GPU scratch array (for the entry point that allocates nothing): its size,

@@ -409,29 +409,38 @@ hipError_t launch_kv_block_map(const int32_t *past, const int32_t *fresh, int B,
 
 constexpr int64_t kManyTokens = 256;
 
+// How a call runs: tokens to a workgroup and head (0: a wavefront for each of them), and workgroups.
+struct AppendShape { int slab; int64_t groups; };
+
+static AppendShape append_shape(int64_t T, int Hkv, int block_tokens)
+{
+    const int64_t heads = 2 * (int64_t)Hkv;
+    // Blocks of 64 tokens and more have long runs, which want four wavefronts; short ones a lone wavefront writes as fast, so the many of a workgroup start later there
+    // (16 cache heads of 64, blocks of 16, 331 tokens 4.4 us, 5.5 the other way; 8 of 128, blocks of 64, a chunk of 512 9.0 and 4.3).
+    const bool long_runs = block_tokens >= 64;
+    if (long_runs ? T < kManyTokens : T * heads <= 16384) return {0, (T * heads + 3) / 4};
+    // 8 tokens to a workgroup, and 64 from as many on as fill the card so (a workgroup that finds no run's beginning costs more than several runs in one).
+    const int slab = T * heads <= 16384 ? 8 : 64;
+    return {slab, (T + slab - 1) / slab * heads};
+}
+
+bool kv8_append_fits(int64_t T, int Hkv, int block_tokens) { return append_shape(T, Hkv, block_tokens).groups <= atom_launch::kMostThreads / 256; }
+
 hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ldk, int64_t ldv, int Hkv, int D,
                              const int32_t *slot, int64_t n_blocks, int block_tokens, void *k_codes, float *k_scale,
                              void *v_codes, float *v_scale, hipStream_t stream)
 {
-    const int64_t heads = 2 * (int64_t)Hkv;
     const Side ks = {(const __half *)k, ldk, (int8_t *)k_codes, k_scale}, vs = {(const __half *)v, ldv, (int8_t *)v_codes, v_scale};
     const int32_t slots = (int32_t)(n_blocks * block_tokens);
     const int     shift = __builtin_ctz((unsigned)block_tokens);
-    // Blocks of 64 tokens and more have long runs, which want four wavefronts; short ones a lone wavefront writes as fast, so the many of a workgroup start later there
-    // (16 cache heads of 64, blocks of 16, 331 tokens 4.4 us, 5.5 the other way; 8 of 128, blocks of 64, a chunk of 512 9.0 and 4.3).
-    const bool long_runs = block_tokens >= 64;
-    if (long_runs ? T < kManyTokens : T * heads <= 16384) {
-        const int64_t grid = (T * heads + 3) / 4;
-        hipLaunchKernelGGL((D == 128 ? &kv8_append_kernel<128> : &kv8_append_kernel<64>), dim3((unsigned)grid), dim3(256), 0, stream, ks, vs, (int)T, Hkv, slot, slots, shift);
+    const AppendShape s = append_shape(T, Hkv, block_tokens);
+    if (!s.slab) {
+        hipLaunchKernelGGL((D == 128 ? &kv8_append_kernel<128> : &kv8_append_kernel<64>), dim3((unsigned)s.groups), dim3(256), 0, stream, ks, vs, (int)T, Hkv, slot, slots, shift);
         return hipGetLastError();
     }
-    // 8 tokens to a workgroup, and 64 from as many on as fill the card so (a workgroup that finds no run's beginning costs more than several runs in one).
-    const int     slab = T * heads <= 16384 ? 8 : 64;
-    const int64_t grid = (T + slab - 1) / slab * heads;
-    if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
     auto kern = block_tokens == 128 || block_tokens == 32 ? (D == 128 ? &kv8_append_many_kernel<128, 32> : &kv8_append_many_kernel<64, 32>)
                                      : (D == 128 ? &kv8_append_many_kernel<128, 16> : &kv8_append_many_kernel<64, 16>);
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, stream, ks, vs, (int)T, Hkv, slot, slots, shift, slab);
+    hipLaunchKernelGGL(kern, dim3((unsigned)s.groups), dim3(256), 0, stream, ks, vs, (int)T, Hkv, slot, slots, shift, s.slab);
     return hipGetLastError();
 }
 

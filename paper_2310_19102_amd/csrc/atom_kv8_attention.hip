@@ -1135,12 +1135,15 @@ size_t attention_kv8_workspace_bytes(int64_t T, int B, int H, int Hkv, int D, in
     return shape(T, B, Hkv, H / Hkv, D, max_new, W * block_tokens).floats * sizeof(float);
 }
 
-bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int max_new)
+bool attention_kv8_fits(int64_t T, int B, int H, int Hkv, int D, int max_new, int64_t W, int block_tokens)
 {
-    // every count is below (rows / 16 + B) * blocks of 128 rows and the workgroups wanted, as doubles here
+    // first, that shape() can count in 32 bits: every count is below (rows / 16 + B) * blocks of 128 rows and the workgroups wanted, as doubles here
     const double group = H / Hkv, rows = (double)max_new * group, tiles = (double)T * group / kSetRows + B, each = (double)B * (rows / kSetRows + 1);
     const double most = (tiles < each ? tiles : each) + kFewWorkgroups;
-    return 2.0 * most * Hkv < 2147483647.0;
+    if (2.0 * most * Hkv >= 2147483647.0) return false;
+    const Shape   s = shape(T, B, Hkv, H / Hkv, D, max_new, W * block_tokens);
+    const int64_t threads = ((int64_t)s.few.groups + s.many.groups) * Hkv * 64 * (s.many.groups ? 4 : s.waves);
+    return threads <= atom_launch::kMostThreads && ((int64_t)s.few.merges + s.many.merges) * Hkv * 256 <= atom_launch::kMostThreads;
 }
 
 // How a call of these sizes runs, as its tests ask it: wavefronts of a workgroup of few rows, 32 where those requests' keys may be cut, 64 where

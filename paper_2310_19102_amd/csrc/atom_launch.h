@@ -7,10 +7,12 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <cstdint>
 
 namespace atom_launch {
 
 constexpr int kMaxDevices = 64;
+constexpr int64_t kMostThreads = 0xffffffffLL;     // of a launch, in one dimension: HIP takes no more
 
 inline int current_device()
 {
