@@ -642,7 +642,7 @@ atom_status atom_kv8_append(const void *k_f16, const void *v_f16, int64_t T, int
  *                  more workgroups, evenly over all sequences whatever their lengths, whose partial results meet in a second kernel.
  *                  Contents need no initialisation and are dead after the call.
  * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE (H % Hkv, negative sizes, W = 0 with B > 0, ld), ATOM_ERR_ALIGN,
- * ATOM_ERR_UNSUPPORTED (block_tokens, D, sm_scale negative, above 1e6 or no number, W * block_tokens > 2^30, a cache that
+ * ATOM_ERR_UNSUPPORTED (block_tokens, D, B > 65536, sm_scale negative, above 1e6 or no number, W * block_tokens > 2^30, a cache that
  * atom_kv8_append does not take, T * H >= 2^31, a launch of 2^32 threads or more: as 2^24 single tokens times cache heads would be),
  * ATOM_ERR_WORKSPACE.
  * T = 0, B = 0 or max_new = 0 returns ATOM_OK.

@@ -101,7 +101,7 @@ atom_status kv8_attention(int64_t T, int32_t B, int32_t H, int32_t Hkv, int32_t 
 {
     if (T < 0 || B < 0 || H <= 0 || Hkv <= 0 || H % Hkv || D <= 0 || max_new < 0 || W < 0 || (B > 0 && W == 0)) return ATOM_ERR_SHAPE;
     if ((D != 64 && D != 128) || !kv8_block(block_tokens) || T > 0x7ffffffeLL || W > 0x40000000LL / block_tokens ||
-        B > 0x3fffffff || T * H > 0x7fffffffLL || (int64_t)max_new * (H / Hkv) > 0x7fffffffLL ||
+        B > atom_internal::kMaxAttentionRequests || T * H > 0x7fffffffLL || (int64_t)max_new * (H / Hkv) > 0x7fffffffLL ||
         !atom_internal::attention_kv8_fits(T, B, H, Hkv, D, max_new, W, block_tokens))
         return ATOM_ERR_UNSUPPORTED;
     return ATOM_OK;

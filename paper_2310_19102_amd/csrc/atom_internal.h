@@ -133,6 +133,9 @@ bool       kv8_append_fits(int64_t T, int Hkv, int block_tokens);               
 hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ldk, int64_t ldv, int Hkv, int D,
                              const int32_t *slot, int64_t n_blocks, int block_tokens, void *k_codes, float *k_scale,
                              void *v_codes, float *v_scale, hipStream_t stream);
+// Every workgroup of the attention scans the requests' lengths for its place, so its time grows with their square: 16384 single tokens of 8 cache heads 5.9 ms,
+// 32768 22.8, and 2^24 would hold the GPU for minutes.
+constexpr int kMaxAttentionRequests = 65536;
 struct AttentionKv8 {
     const void *q; int64_t T, ldq;
     int B, H, Hkv, D, max_new;

@@ -22,7 +22,8 @@ def test_append(bs, T, Hkv, want):
 @pytest.mark.parametrize("B,T,max_new,H,Hkv,W,want", [
     (65535, 65535, 1, 256, 256, 1, NULL), (65536, 65536, 1, 256, 256, 1, UNSUPPORTED), (65536, 65536, 1, 256, 256, 4096, UNSUPPORTED),
     (65535, 2 ** 18, 4, 512, 256, 2, NULL), (65536, 2 ** 18, 4, 512, 256, 2, UNSUPPORTED), (2 ** 14 - 1, 2 ** 14, 1, 2 ** 13, 1024, 1, NULL),
-    (2 ** 14, 2 ** 14, 1, 2 ** 13, 1024, 1, UNSUPPORTED)])
+    (2 ** 14, 2 ** 14, 1, 2 ** 13, 1024, 1, UNSUPPORTED),
+    (65536, 70000, 1, 8, 1, 1, NULL), (65537, 70000, 1, 8, 1, 1, UNSUPPORTED)])            # lengths that every workgroup scans
 def test_attention(B, T, max_new, H, Hkv, W, want):
     D = 128
     assert atom.load_library().atom_attention_kv8(None, T, H * D, B, H, Hkv, D, max_new, P, P, P, W, 100, 64, P, P, P, P, ctypes.c_float(0.1), P,
