@@ -419,7 +419,8 @@ static AppendShape append_shape(int64_t T, int Hkv, int block_tokens)
     // (16 cache heads of 64, blocks of 16, 331 tokens 4.4 us, 5.5 the other way; 8 of 128, blocks of 64, a chunk of 512 9.0 and 4.3).
     const bool long_runs = block_tokens >= 64;
     if (long_runs ? T < kManyTokens : T * heads <= 16384) return {0, (T * heads + 3) / 4};
-    // 8 tokens to a workgroup, and 64 from as many on as fill the card so (a workgroup that finds no run's beginning costs more than several runs in one).
+    // 8 tokens to a workgroup, and 64 from as many on as fill the card so (a workgroup that finds no run's beginning costs more than several runs in one).  Single tokens
+    // pay for it, 16 to a wavefront: 32 cache heads of 128, blocks of 64, 256 of them 8.3 us, 257 18.3; 8 heads, blocks of 16, 1024 10.8, 1025 18.0.
     const int slab = T * heads <= 16384 ? 8 : 64;
     return {slab, (T + slab - 1) / slab * heads};
 }

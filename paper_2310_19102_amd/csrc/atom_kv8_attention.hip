@@ -44,7 +44,7 @@ __device__ __forceinline__ float quotient(float sum) { return sum == 0.0f ? 0.0f
 // What all kernels of a call are told.
 struct Args {
     const __half *q; int T; int64_t ldq;
-    int B, H, Hkv, group;                         // group = H / Hkv query heads to a cache head
+    int B, Hkv, group;                            // group = H / Hkv query heads to a cache head
     uint32_t div_mul; int div_shift;              // n / group = n * div_mul >> div_shift for n below 2^31
     int max_new;
     const int32_t *token_start, *seq_len, *table;
@@ -270,8 +270,8 @@ __device__ __forceinline__ float sum_of_chunks(float v)
 //
 // One workgroup of four wavefronts (8 or 16 where a lone one has a whole context) for a tile of 16 or 32 query rows of a (request, cache head) and a piece of its keys;
 // the wavefronts take steps of 32 keys in turn, each with a softmax of its own, and meet in LDS.  Bound by memory where there is enough of it: 64 single tokens over
-// up to 2048 keys of 32 heads of 128 (673 MB) 113 us, 5.9 TB/s; 16 over up to 16000 keys of 8 cache heads, 8 heads to each (329 MB), 57 us, 5.8 TB/s, and the merge 4.9.
-// With little to read by the chain of lengths, block numbers, scales and codes: one token over 1000 keys of 32 heads 6.8 us.
+// up to 2048 keys of 32 heads of 128 (673 MB) 113 us, 5.95 TB/s; 16 over up to 16000 keys of 8 cache heads, 8 heads to each (329 MB), 57.6 us, 5.7 TB/s, and the merge 4.8.
+// With little to read by the chain of lengths, block numbers, scales and codes: one token over 1000 keys of 32 heads 6.9 us.
 //
 //   scores: S^T = K Q^T on 16x16x32 fp16 matrix instructions.  Keys are the rows, so that a lane holds four keys of ONE query row.  Lane (l & 15, c =
 //           l >> 4) has the 16 dimensions from 16 c on of every 64 of key l & 15; the order of the dimensions within a product is free as long as Q has the
@@ -574,7 +574,7 @@ void attention_kv8_rows_kernel(const Args a, const Job few)
 //   loads: codes of the next tile but one are on their way, and their block numbers a tile earlier, while one is computed; two buffers, a barrier a tile.
 //   order: the last tiles of a request, which see the most keys, first.
 //
-// Bound by the issue of both units: two prompts of up to 4096 tokens, 64 heads on 8 cache heads of 128 (292 GFLOP), 318 us, 918 TFLOP/s; of a SIMD's cycles the matrix
+// Bound by the issue of both units: two prompts of up to 4096 tokens, 64 heads on 8 cache heads of 128 (292 GFLOP), 311 to 342 us by card, 854 to 940 TFLOP/s; of a SIMD's cycles the matrix
 // unit has 46 % and the vector unit 61 %, which hold each other up (a matrix instruction keeps the vector unit from starting one for 13 to 16 cycles of its 32).
 
 __device__ __forceinline__ float larger(float a, float b, float c)
@@ -1159,7 +1159,7 @@ hipError_t launch_attention_kv8(const AttentionKv8 &c, hipStream_t stream)
 {
     Args a;
     a.q = (const __half *)c.q; a.T = (int)c.T; a.ldq = c.ldq;
-    a.B = c.B; a.H = c.H; a.Hkv = c.Hkv; a.group = c.H / c.Hkv;
+    a.B = c.B; a.Hkv = c.Hkv; a.group = c.H / c.Hkv;
     const int log = a.group > 1 ? 32 - __builtin_clz((unsigned)(a.group - 1)) : 0;
     a.div_shift = 31 + log;
     a.div_mul = (uint32_t)(((uint64_t)1 << a.div_shift) / (unsigned)a.group + 1);
