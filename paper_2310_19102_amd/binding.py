@@ -561,8 +561,8 @@ def atom_kv8_append(k: torch.Tensor, v: torch.Tensor, k_cache: Tuple[torch.Tenso
                     v_cache: Tuple[torch.Tensor, ...], slot: torch.Tensor):
     """The step's K and V rows ([T, Hkv, D] fp16, each token's heads contiguous, any stride between tokens) quantised into
     the blocks of their caches ``(codes, scale)`` (``atom_kv8_cache``) at ``slot`` [T] (``atom_kv_block_map``; -1: not
-    stored).  A block's scale grows with its contents; older rows are brought to it.  Returns
-    ``(k_cache, v_cache)``, updated in place."""
+    stored).  A block's scale grows with its contents; older rows are brought to it.  A value that is not finite makes
+    its block's scale so for its head, until the block is begun anew.  Returns ``(k_cache, v_cache)``, updated in place."""
     return _run().kv8_append(k, v, k_cache, v_cache, slot)
 
 
@@ -577,7 +577,7 @@ def atom_attention_kv8(q: torch.Tensor, k_cache: Tuple[torch.Tensor, ...], v_cac
                        workspace: Optional[torch.Tensor] = None):
     """Causal attention of a step's queries ``q`` [T, H, D] fp16 over the paged 8-bit cache: request b's tokens are
     ``token_start[b] .. token_start[b + 1]``, the last ones of its ``seq_len[b]`` positions, and the cache holds them
-    already.  ``max_new``: no request has more new tokens (None: unknown; 1 for a decoding step).  Returns [T, H, D] fp16 (``out``
+    already; a query that sees a key of a block whose scale is not finite gives NaN.  ``max_new``: no request has more new tokens (None: unknown; 1 for a decoding step).  Returns [T, H, D] fp16 (``out``
     if given, which may be ``q``; rows behind the last request are left as they were, of a new output without a value).  In a capture that was not begun by torch.cuda.graph a
     ``workspace`` has to be given where ``atom_attention_kv8_workspace_bytes`` is not 0."""
     return _run().attention_kv8(q, k_cache, v_cache, block_table, token_start, seq_len, sm_scale,
