@@ -661,6 +661,109 @@ size_t atom_attention_kv8_workspace_bytes(int64_t T, int32_t B, int32_t H, int32
                                           int32_t max_new, int64_t W, int32_t block_tokens);
 
 /*
+ * Rotary positions, of one or several axes (time, height and width of images and video).  What turns the queries and keys
+ * that atom_kv8_append and atom_attention_kv8 take.  Of a head's D channels the first 2 n_pairs turn in pairs:
+ *   a' = a c - b s,  b' = b c + a s,   (c, s) = table[positions[axis[j], t], j]        for pair j = (a, b) of token t
+ * IEEE fp32, every step rounded once, then fp16: results are bit-exact.  Channels from 2 n_pairs on are copied.  transposed
+ * turns the other way (s with its sign changed): the way back, and the way of a gradient.  A position outside [0, n_pos) gives NaN.
+ */
+typedef struct {
+    int32_t n_pairs;       /* pairs of a head that turn: a multiple of 4, 2 n_pairs <= D                */
+    int32_t interleaved;   /* pair j is 0: channels j and j + n_pairs; 1: channels 2 j and 2 j + 1      */
+    int32_t n_axes;        /* positions of a token, 1 to 4                                              */
+    uint8_t axis[128];     /* of every pair, below n_axes                                               */
+} atom_rotary_desc;
+
+/*
+ * The table: (cos, sin) of p * inv_freq[j], both in 64 bits and rounded once, for p = 0 .. n_pos - 1.
+ *   inv_freq  device double [n_pairs], n_pairs 1 to 128;   table  device float [n_pos, n_pairs, 2], 16-byte aligned
+ * A table of the caller's own is as good (other frequencies beyond some position, a factor on all entries).
+ * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE (n_pairs <= 0, n_pos < 0), ATOM_ERR_UNSUPPORTED (n_pairs > 128, n_pos >= 2^31, n_pos *
+ * n_pairs > 2^32 - 256), ATOM_ERR_ALIGN.  n_pos = 0 returns ATOM_OK.
+ */
+atom_status atom_rotary_table(const double *inv_freq, int32_t n_pairs, int64_t n_pos, float *table, void *stream);
+
+/*
+ * atom_rotary: the heads of T tokens, e.g. all query and key heads of a fused projection's output in one call.
+ *   x_f16      device fp16, token t's heads [heads, D] from t * ldx on; out_f16 likewise with ldo.  16-byte aligned, ld % 8 == 0.
+ *              out may be x itself (ldo = ldx); no other overlap
+ *   D          a multiple of 8, up to 256
+ *   positions  device int32 [n_axes, T], axis a's from a * ldp on (ldp >= T where n_axes > 1)
+ *   table      device float [n_pos, n_pairs, 2], 16-byte aligned
+ * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE (sizes, ld, an axis of a pair >= n_axes, 2 n_pairs > D), ATOM_ERR_ALIGN,
+ * ATOM_ERR_UNSUPPORTED (D, n_pairs % 4, n_axes > 4, n_pos > 2^31 - 1, heads * D >= 2^31, T * heads * D / 8 > 2^32 - 256).
+ * T = 0 returns ATOM_OK.
+ */
+atom_status atom_rotary(const void *x_f16, int64_t T, int64_t ldx, int32_t heads, int32_t D,
+                        const atom_rotary_desc *r, const int32_t *positions, int64_t ldp,
+                        const float *table, int64_t n_pos, int32_t transposed, void *out_f16,
+                        int64_t ldo, void *stream);
+
+/*
+ * atom_rotary_kv8_append: everything between a step's fused projection and atom_attention_kv8 in one launch: the queries turned
+ * into q_out as by atom_rotary, the keys turned and appended to the paged 8-bit cache, the values appended, as by atom_kv8_append
+ * (its definition, arguments and errors).  A turned key goes into the block's scale and codes as it is in fp32: it is not rounded
+ * to fp16 on the way, which atom_rotary followed by atom_kv8_append would do (codes may differ by one then).  A key with a position outside
+ * the table is not finite, and shows as atom_kv8_append says.  Queries of all T tokens are turned, also of those without a slot.
+ * A scale below fp32's normal numbers counts as 0: codes 0.
+ *
+ *   q_f16, H   device fp16 [T, H, D] with ldq, q_out_f16 with ldqo (q itself with ldqo = ldq, or no overlap); H = 0: no queries, q and q_out not read
+ *   D          64 or 128 (the cache's)
+ *   r, positions, ldp, table, n_pos   as atom_rotary
+ *   k_f16 .. v_scale   as atom_kv8_append; k and v are not written
+ * Errors: those of atom_rotary and of atom_kv8_append; ATOM_ERR_UNSUPPORTED also where the launch would have 2^32 threads
+ * or more (128 Hkv + H D / 8 for a token).
+ */
+atom_status atom_rotary_kv8_append(const void *q_f16, int64_t ldq, int32_t H, void *q_out_f16,
+                                   int64_t ldqo, const void *k_f16, const void *v_f16, int64_t T,
+                                   int64_t ldk, int64_t ldv, int32_t Hkv, int32_t D,
+                                   const atom_rotary_desc *r, const int32_t *positions, int64_t ldp,
+                                   const float *table, int64_t n_pos, const int32_t *slot,
+                                   int64_t n_blocks, int32_t block_tokens, void *k_codes,
+                                   float *k_scale, void *v_codes, float *v_scale, void *stream);
+
+/*
+ * Linear layers on the quantised weights with activations that stay in fp16 (the W4A16 setting that the paper compares with in
+ * Section 5.3; a layer of few rows is bound by reading its weights, Section 3, and those are the same):
+ *   xr[m, j] = x[m, idx[j]], or with gamma fp16(RMSNorm(x)[m, idx[j]] * gamma[idx[j]])       (RMSNorm and product in fp32)
+ *   y[m, n]  = fp16( residual[m, n] + sum_g w_scale[n, g] * sum_{k in g} w[n, k] * xr[m, k] )
+ * Codes meet xr exactly in the fp16 matrix cores, sums are fp32, in an order that depends on the sizes alone: results are
+ * deterministic.  Meant for few rows (any number is taken; the 4-bit path is the faster one beyond a few hundred).
+ *
+ *   x_f16        [M, ldx] fp16, ldx >= K, ldx % 8 == 0, 16-byte aligned
+ *   gamma_f16    [K] fp16 in original channel order, or NULL for no norm; eps: RMSNorm epsilon
+ *   reorder_idx  [K] int32, 16-byte aligned, or NULL when x already is in reordered channel order, as in atom_quantize_act
+ *   w_q4 / w_q8 / w_scale   canonical codes and scales of N rows as atom_quantize_weight writes them (4 or 3 bits); 16-, 16- and 2-byte aligned
+ *   residual_f16 [M, ldr] fp16, ldr >= N, or NULL; may be y_f16 itself (ldr = ldy)
+ *   y_f16        [M, ldy] fp16 out, ldy >= N; overlaps no other input
+ *   workspace    device scratch of atom_w4a16_workspace_bytes(M, N, d, 0, gamma != NULL, reorder_idx != NULL) bytes, 256-byte aligned (NULL when
+ *                that is 0).  Contents need no initialisation and are dead after the call.
+ * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE, ATOM_ERR_ALIGN, ATOM_ERR_WORKSPACE, ATOM_ERR_UNSUPPORTED (a descriptor that
+ * atom_w4a4_gemm_packed does not take, a launch of 2^32 threads or more: 512 for every 16 outputs of 64 rows).
+ */
+atom_status atom_w4a16_linear(const void *x_f16, int64_t M, int64_t ldx, const void *gamma_f16, float eps,
+                              const int32_t *reorder_idx, const atom_desc *d, const void *w_q4,
+                              const void *w_q8, const void *w_scale, int64_t N, const void *residual_f16,
+                              int64_t ldr, void *y_f16, int64_t ldy, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
+ * The gated half of a feed-forward block on such weights: both projections, the activation and the product,
+ *   h[m, n] = fp16( (g * sigma(g)) * u ),   g and u the fp32 sums of atom_w4a16_linear with the gate's and the up projection's weights
+ * The gate and the up arrays have N rows each and one descriptor.  Other arguments and errors as atom_w4a16_linear (the workspace:
+ * atom_w4a16_workspace_bytes with gated = 1).
+ */
+atom_status atom_w4a16_swiglu(const void *x_f16, int64_t M, int64_t ldx, const void *gamma_f16, float eps,
+                              const int32_t *reorder_idx, const atom_desc *d, const void *gate_q4,
+                              const void *gate_q8, const void *gate_scale, const void *up_q4,
+                              const void *up_q8, const void *up_scale, int64_t N, void *h_f16,
+                              int64_t ldh, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Scratch the two calls need for these sizes (0 when none, and for sizes and descriptors that they refuse). */
+size_t atom_w4a16_workspace_bytes(int64_t M, int64_t N, const atom_desc *d, int gated, int with_norm,
+                                  int with_index);
+
+/*
  * MX variant of the path.  The paper also runs its recipe with FP4 codes and
  * names the MX formats, whose group scaling new hardware applies by itself and
  * which it expects to remove the group-dequantisation overhead of the fused

@@ -58,6 +58,12 @@ EXPORTS = (
     "atom_kv8_append",
     "atom_attention_kv8",
     "atom_attention_kv8_workspace_bytes",
+    "atom_rotary_table",
+    "atom_rotary",
+    "atom_rotary_kv8_append",
+    "atom_w4a16_linear",
+    "atom_w4a16_swiglu",
+    "atom_w4a16_workspace_bytes",
     "atom_mfma_rate_probe",
     "atom_check_reorder_idx",
     "atom_status_string",
@@ -73,6 +79,11 @@ class AtomError(RuntimeError):
 class _Desc(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("group_size", ctypes.c_int32), ("n_outlier", ctypes.c_int32),
                 ("bits_normal", ctypes.c_int32), ("bits_outlier", ctypes.c_int32)]
+
+
+class _RotaryDesc(ctypes.Structure):
+    _fields_ = [("n_pairs", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("axis", ctypes.c_uint8 * 128)]
 
 
 def library_path() -> str:
@@ -177,6 +188,20 @@ def load_library():
                                      vp, i64, vp, sz, vp]
     L.atom_attention_kv8_workspace_bytes.restype = sz
     L.atom_attention_kv8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i64, i32]
+    L.atom_rotary_table.restype = ctypes.c_int
+    L.atom_rotary_table.argtypes = [vp, i32, i64, vp, vp]
+    rp = ctypes.POINTER(_RotaryDesc)
+    L.atom_rotary.restype = ctypes.c_int
+    L.atom_rotary.argtypes = [vp, i64, i64, i32, i32, rp, vp, i64, vp, i64, i32, vp, i64, vp]
+    L.atom_rotary_kv8_append.restype = ctypes.c_int
+    L.atom_rotary_kv8_append.argtypes = [vp, i64, i32, vp, i64, vp, vp, i64, i64, i64, i32, i32, rp, vp, i64, vp, i64, vp, i64, i32,
+                                         vp, vp, vp, vp, vp]
+    L.atom_w4a16_linear.restype = ctypes.c_int
+    L.atom_w4a16_linear.argtypes = [vp, i64, i64, vp, f32, vp, dp, vp, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+    L.atom_w4a16_swiglu.restype = ctypes.c_int
+    L.atom_w4a16_swiglu.argtypes = [vp, i64, i64, vp, f32, vp, dp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    L.atom_w4a16_workspace_bytes.restype = sz
+    L.atom_w4a16_workspace_bytes.argtypes = [i64, i64, dp, ctypes.c_int, ctypes.c_int, ctypes.c_int]
     L.atom_mfma_rate_probe.restype = ctypes.c_double
     L.atom_mfma_rate_probe.argtypes = [i32, i32, vp, vp, ctypes.POINTER(ctypes.c_int)]
     L.atom_check_reorder_idx.restype = ctypes.c_int
@@ -582,6 +607,74 @@ def atom_attention_kv8(q: torch.Tensor, k_cache: Tuple[torch.Tensor, ...], v_cac
     ``workspace`` has to be given where ``atom_attention_kv8_workspace_bytes`` is not 0."""
     return _run().attention_kv8(q, k_cache, v_cache, block_table, token_start, seq_len, sm_scale,
                                 q.shape[0] if max_new is None else max_new, out, workspace)
+
+
+def atom_rotary_table(inv_freq: torch.Tensor, n_pos: int, out: Optional[torch.Tensor] = None):
+    """``(cos, sin)`` of position times frequency for positions 0 .. ``n_pos`` - 1 (angles in 64 bits): float32
+    [n_pos, n_pairs, 2] from ``inv_freq`` [n_pairs] float64 on the device.  Once per model."""
+    L = load_library()
+    _dev(inv_freq, torch.float64, "inv_freq")
+    if inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be contiguous [n_pairs]")
+    n = inv_freq.numel()
+    if out is None:
+        out = torch.empty((max(0, n_pos), n, 2), dtype=torch.float32, device=inv_freq.device)
+    _dev(out, torch.float32, "out")
+    if tuple(out.shape) != (n_pos, n, 2) or not out.is_contiguous() or out.device != inv_freq.device:
+        raise ValueError("out must be contiguous float32 [n_pos, n_pairs, 2] on the device of inv_freq")
+    with torch.cuda.device(inv_freq.device):
+        st = L.atom_rotary_table(_ptr(inv_freq), n, n_pos, _ptr(out), _stream())
+    if st != 0:
+        raise AtomError(st, "atom_rotary_table")
+    return out
+
+
+def _axis(axis):
+    return axis if axis is None or type(axis) is bytes else bytes(axis)
+
+
+def atom_rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, axis=None, interleaved: bool = False,
+                transposed: bool = False, out: Optional[torch.Tensor] = None):
+    """The heads of ``x`` [T, heads, D] fp16 (each token's heads contiguous, any stride between tokens) turned by their
+    ``positions``: int32 [T], or [axes, T] with the ``axis`` of every pair of channels (bytes or integers, one for each pair of
+    ``table`` [n_pos, n_pairs, 2], see ``atom_rotary_table``).  The first 2 n_pairs channels of a head turn, pair j being channels
+    j and j + n_pairs, or 2j and 2j + 1 with ``interleaved``.  ``transposed`` turns the other way: the way back, and a gradient's.
+    A position outside the table gives NaN.  Returns [T, heads, D] fp16 (``out`` if given, which may be ``x``)."""
+    return _run().rotary(x, positions, table, _axis(axis), interleaved, transposed, out)
+
+
+def atom_rotary_kv8_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cache: Tuple[torch.Tensor, ...],
+                           v_cache: Tuple[torch.Tensor, ...], slot: torch.Tensor, positions: torch.Tensor, table: torch.Tensor,
+                           axis=None, interleaved: bool = False, out: Optional[torch.Tensor] = None):
+    """Everything between a step's fused projection and ``atom_attention_kv8``, one launch: ``q`` [T, H, D] turned (into ``out``,
+    which may be ``q``; None: no queries), ``k`` [T, Hkv, D] turned and appended to ``k_cache``, ``v`` appended to ``v_cache``, at
+    ``slot`` as by ``atom_kv8_append``.  Keys are quantised as they come out of the turn, in fp32.  Positions, table, axes and
+    pairs as in ``atom_rotary``.  Returns ``(q turned, k_cache, v_cache)``, the caches updated in place."""
+    return _run().rotary_kv8_append(q, k, v, k_cache, v_cache, slot, positions, table, _axis(axis), interleaved, out)
+
+
+def atom_w4a16_workspace_bytes(M: int, N: int, K: int, group_size: int = 128, n_outlier: int = 128, gated: bool = False,
+                               norm: bool = True, index: bool = True) -> int:
+    d = _desc(K, group_size, n_outlier)
+    return int(load_library().atom_w4a16_workspace_bytes(M, N, ctypes.byref(d), int(gated), int(norm), int(index)))
+
+
+def atom_w4a16_linear(x: torch.Tensor, gamma: Optional[torch.Tensor], eps: float, reorder_idx: Optional[torch.Tensor],
+                      w_q4: torch.Tensor, w_q8: torch.Tensor, w_scale: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                      group_size: int = 128, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """A linear layer with quantised weights (``atom_quantize_weight``) and activations that stay in fp16: ``x`` [M, K] fp16,
+    behind RMSNorm where ``gamma`` is given, in the order of ``reorder_idx`` (None: x already is in reordered order), plus
+    ``residual`` [M, N] where given (it may be ``out``).  Returns [M, N] fp16.  In a capture that was not begun by
+    torch.cuda.graph a ``workspace`` has to be given where ``atom_w4a16_workspace_bytes`` is not 0."""
+    return _run().w4a16_linear(x, gamma, eps, reorder_idx, w_q4, w_q8, w_scale, residual, group_size, out, workspace)
+
+
+def atom_w4a16_swiglu(x: torch.Tensor, gamma: Optional[torch.Tensor], eps: float, reorder_idx: Optional[torch.Tensor],
+                      gate: Tuple[torch.Tensor, ...], up: Tuple[torch.Tensor, ...], group_size: int = 128,
+                      out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """``silu(x gate^T) * (x up^T)`` on quantised weights, ``gate`` and ``up`` ``(w_q4, w_q8, w_scale)`` of N rows each, sums and
+    activation in fp32; other arguments as in ``atom_w4a16_linear``.  Returns [M, N] fp16."""
+    return _run().w4a16_swiglu(x, gamma, eps, reorder_idx, gate, up, group_size, out, workspace)
 
 
 def _mx_outputs(rows: int, K: int, n_outlier: int, device):

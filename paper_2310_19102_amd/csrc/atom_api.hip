@@ -8,6 +8,7 @@
 
 #include "atom.h"
 #include "atom_internal.h"
+#include "atom_launch.h"
 
 namespace {
 
@@ -756,6 +757,150 @@ atom_status atom_calibrate_reorder(const void *x_f16, int64_t T, int64_t ldx, in
     hipError_t err = atom_internal::launch_calibrate_reorder(x_f16, T, ldx, K, workspace, idx_out,
                                                              static_cast<hipStream_t>(stream));
     return err == hipSuccess ? ATOM_OK : ATOM_ERR_HIP;
+}
+
+}  // extern "C"
+
+// ---- rotary positions
+
+extern "C" {
+
+atom_status atom_rotary_table(const double *inv_freq, int32_t n_pairs, int64_t n_pos, float *table, void *stream)
+{
+    if (n_pairs <= 0 || n_pos < 0) return ATOM_ERR_SHAPE;
+    if (n_pairs > 128 || n_pos > 0x7fffffffLL || n_pos * n_pairs > atom_launch::kMostThreads / 256 * 256) return ATOM_ERR_UNSUPPORTED;
+    if (n_pos == 0) return ATOM_OK;
+    if (!inv_freq || !table) return ATOM_ERR_NULL;
+    if (!aligned(inv_freq, 8) || !aligned(table, 16)) return ATOM_ERR_ALIGN;
+    return atom_internal::launch_rotary_table(inv_freq, n_pairs, n_pos, table, static_cast<hipStream_t>(stream)) == hipSuccess ? ATOM_OK : ATOM_ERR_HIP;
+}
+
+}  // extern "C"
+
+namespace {
+
+// The descriptor, positions and table of a call on T tokens of heads of D channels; `turn` as the kernels take it.
+atom_status check_turn(const atom_rotary_desc *r, int64_t T, int32_t D, const int32_t *positions, int64_t ldp, const float *table, int64_t n_pos,
+                       atom_internal::Turn *turn)
+{
+    if (!r) return ATOM_ERR_NULL;
+    if (r->n_pairs <= 0 || r->n_axes <= 0 || n_pos <= 0 || r->n_pairs > D / 2 || (r->n_axes > 1 && ldp < T)) return ATOM_ERR_SHAPE;
+    if (r->n_pairs % 4 || r->n_pairs > 128 || r->n_axes > 4 || (r->interleaved != 0 && r->interleaved != 1) || n_pos > 0x7fffffffLL)
+        return ATOM_ERR_UNSUPPORTED;
+    *turn = {positions, ldp, table, (uint32_t)n_pos, r->n_pairs, r->n_axes, r->interleaved != 0, {}};
+    for (int32_t j = 0; j < r->n_pairs; ++j) {
+        if (r->axis[j] >= r->n_axes) return ATOM_ERR_SHAPE;
+        turn->axis[j / 16] |= (uint32_t)r->axis[j] << (2 * (j % 16));
+    }
+    return ATOM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+atom_status atom_rotary(const void *x_f16, int64_t T, int64_t ldx, int32_t heads, int32_t D, const atom_rotary_desc *r,
+                        const int32_t *positions, int64_t ldp, const float *table, int64_t n_pos, int32_t transposed,
+                        void *out_f16, int64_t ldo, void *stream)
+{
+    if (T < 0 || heads <= 0 || D <= 0 || ldx < (int64_t)heads * D || ldo < (int64_t)heads * D) return ATOM_ERR_SHAPE;
+    atom_internal::Turn turn;
+    const atom_status st = check_turn(r, T, D, positions, ldp, table, n_pos, &turn);
+    if (st != ATOM_OK) return st;
+    if (D % 8 || D > 256 || (int64_t)heads * D > 0x7fffffffLL || T > atom_launch::kMostThreads / 256 * 256 / ((int64_t)heads * (D / 8)))
+        return ATOM_ERR_UNSUPPORTED;
+    if (T == 0) return ATOM_OK;
+    if (!x_f16 || !positions || !table || !out_f16) return ATOM_ERR_NULL;
+    if (!aligned(x_f16, 16) || !aligned(out_f16, 16) || ldx % 8 || ldo % 8 || !aligned(positions, 4) || !aligned(table, 16)) return ATOM_ERR_ALIGN;
+    return atom_internal::launch_rotary(x_f16, T, ldx, heads, D, turn, transposed != 0, out_f16, ldo, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? ATOM_OK : ATOM_ERR_HIP;
+}
+
+atom_status atom_rotary_kv8_append(const void *q_f16, int64_t ldq, int32_t H, void *q_out_f16, int64_t ldqo, const void *k_f16,
+                                   const void *v_f16, int64_t T, int64_t ldk, int64_t ldv, int32_t Hkv, int32_t D,
+                                   const atom_rotary_desc *r, const int32_t *positions, int64_t ldp, const float *table,
+                                   int64_t n_pos, const int32_t *slot, int64_t n_blocks, int32_t block_tokens, void *k_codes,
+                                   float *k_scale, void *v_codes, float *v_scale, void *stream)
+{
+    if (T < 0 || H < 0 || Hkv <= 0 || D <= 0 || n_blocks <= 0 || ldk < (int64_t)Hkv * D || ldv < (int64_t)Hkv * D ||
+        (H > 0 && (ldq < (int64_t)H * D || ldqo < (int64_t)H * D)))
+        return ATOM_ERR_SHAPE;
+    atom_internal::RotaryKv8 a = {q_f16, ldq, H, q_out_f16, ldqo, k_f16, v_f16, T, ldk, ldv, Hkv, D, {}, slot, n_blocks, block_tokens,
+                                  k_codes, k_scale, v_codes, v_scale};
+    const atom_status st = check_turn(r, T, D, positions, ldp, table, n_pos, &a.turn);
+    if (st != ATOM_OK) return st;
+    if (!kv8_cache(n_blocks, Hkv, D, block_tokens) || T > 0x7ffffffeLL || !atom_internal::rotary_kv8_fits(T, H, Hkv, D, block_tokens))
+        return ATOM_ERR_UNSUPPORTED;
+    if (T == 0) return ATOM_OK;
+    if ((H > 0 && (!q_f16 || !q_out_f16)) || !k_f16 || !v_f16 || !positions || !table || !slot || !k_codes || !k_scale || !v_codes || !v_scale)
+        return ATOM_ERR_NULL;
+    if (!aligned(k_f16, 16) || !aligned(v_f16, 16) || ldk % 8 || ldv % 8 || !aligned(positions, 4) || !aligned(table, 16) || !aligned(slot, 4) ||
+        !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4) ||
+        (H > 0 && (!aligned(q_f16, 16) || !aligned(q_out_f16, 16) || ldq % 8 || ldqo % 8)))
+        return ATOM_ERR_ALIGN;
+    return atom_internal::launch_rotary_kv8_append(a, static_cast<hipStream_t>(stream)) == hipSuccess ? ATOM_OK : ATOM_ERR_HIP;
+}
+
+}  // extern "C"
+
+// ---- linear layers with fp16 activations
+
+namespace {
+
+atom_status w4a16(const void *x, int64_t M, int64_t ldx, const void *gamma, float eps, const int32_t *idx, const atom_desc *d,
+                  const atom_internal::W4 (&w)[2], bool gated, int64_t N, const void *residual, int64_t ldr, void *y, int64_t ldy, void *workspace,
+                  size_t workspace_bytes, void *stream)
+{
+    const atom_status st = check_desc(d);
+    if (st != ATOM_OK) return st;
+    if (M < 0 || N < 0 || ldx < d->K || ldy < N || (residual && ldr < N)) return ATOM_ERR_SHAPE;
+    if (!atom_internal::w4a16_fits(M, N, d->K, d->n_outlier, gated)) return ATOM_ERR_UNSUPPORTED;
+    if (M == 0 || N == 0) return ATOM_OK;
+    if (!x || !y) return ATOM_ERR_NULL;
+    for (int i = 0; i <= (int)gated; ++i)
+        if (!w[i].q4 || !w[i].q8 || !w[i].scale) return ATOM_ERR_NULL;
+    if (!aligned(x, 16) || ldx % 8 || (gamma && !aligned(gamma, 16)) || !aligned(idx, 16) || !aligned(y, 2) || (residual && !aligned(residual, 2)))
+        return ATOM_ERR_ALIGN;
+    for (int i = 0; i <= (int)gated; ++i)
+        if (!aligned(w[i].q4, 16) || !aligned(w[i].q8, 16) || !aligned(w[i].scale, 2)) return ATOM_ERR_ALIGN;
+    const size_t need = atom_internal::w4a16_workspace_bytes(M, N, d->K, d->n_outlier, gated, gamma != nullptr, idx != nullptr);
+    if (need && (!workspace || workspace_bytes < need)) return ATOM_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 256)) return ATOM_ERR_ALIGN;
+    const atom_internal::W4A16 a = {x, M, ldx, gamma, eps, idx, d->K, d->n_outlier, {w[0], w[1]}, N, residual, ldr, y, ldy, workspace};
+    return atom_internal::launch_w4a16(a, static_cast<hipStream_t>(stream)) == hipSuccess ? ATOM_OK : ATOM_ERR_HIP;
+}
+
+atom_internal::W4 weights(const void *q4, const void *q8, const void *scale)
+{
+    return {static_cast<const uint8_t *>(q4), static_cast<const int8_t *>(q8), static_cast<const uint16_t *>(scale)};
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t atom_w4a16_workspace_bytes(int64_t M, int64_t N, const atom_desc *d, int gated, int with_norm, int with_index)
+{
+    if (check_desc(d) != ATOM_OK || M <= 0 || N <= 0 || !atom_internal::w4a16_fits(M, N, d->K, d->n_outlier, gated != 0)) return 0;
+    return atom_internal::w4a16_workspace_bytes(M, N, d->K, d->n_outlier, gated != 0, with_norm != 0, with_index != 0);
+}
+
+atom_status atom_w4a16_linear(const void *x_f16, int64_t M, int64_t ldx, const void *gamma_f16, float eps, const int32_t *reorder_idx,
+                              const atom_desc *d, const void *w_q4, const void *w_q8, const void *w_scale, int64_t N,
+                              const void *residual_f16, int64_t ldr, void *y_f16, int64_t ldy, void *workspace, size_t workspace_bytes,
+                              void *stream)
+{
+    return w4a16(x_f16, M, ldx, gamma_f16, eps, reorder_idx, d, {weights(w_q4, w_q8, w_scale), {}}, false, N, residual_f16, ldr, y_f16, ldy,
+                 workspace, workspace_bytes, stream);
+}
+
+atom_status atom_w4a16_swiglu(const void *x_f16, int64_t M, int64_t ldx, const void *gamma_f16, float eps, const int32_t *reorder_idx,
+                              const atom_desc *d, const void *gate_q4, const void *gate_q8, const void *gate_scale, const void *up_q4,
+                              const void *up_q8, const void *up_scale, int64_t N, void *h_f16, int64_t ldh, void *workspace,
+                              size_t workspace_bytes, void *stream)
+{
+    return w4a16(x_f16, M, ldx, gamma_f16, eps, reorder_idx, d, {weights(gate_q4, gate_q8, gate_scale), weights(up_q4, up_q8, up_scale)}, true, N,
+                 nullptr, 0, h_f16, ldh, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -133,6 +133,40 @@ bool       kv8_append_fits(int64_t T, int Hkv, int block_tokens);               
 hipError_t launch_kv8_append(const void *k, const void *v, int64_t T, int64_t ldk, int64_t ldv, int Hkv, int D,
                              const int32_t *slot, int64_t n_blocks, int block_tokens, void *k_codes, float *k_scale,
                              void *v_codes, float *v_scale, hipStream_t stream);
+// Rotary positions (atom_rotary.hip) and the append of turned keys (atom_rotary_kv8.hip).
+struct Turn {
+    const int32_t *positions; int64_t ldp;      // [axes, T]
+    const float *table; uint32_t n_pos;         // [n_pos, n_pairs] of (cos, sin)
+    int n_pairs, axes; bool interleaved;
+    uint32_t axis[8];                           // of each pair, two bits
+};
+hipError_t launch_rotary_table(const double *freq, int n_pairs, int64_t n_pos, float *table, hipStream_t stream);
+hipError_t launch_rotary(const void *x, int64_t T, int64_t ldx, int heads, int D, const Turn &t, bool transposed, void *out, int64_t ldo,
+                         hipStream_t stream);
+struct RotaryKv8 {
+    const void *q; int64_t ldq; int H; void *q_out; int64_t ldqo;
+    const void *k, *v; int64_t T, ldk, ldv; int Hkv, D;
+    Turn turn;
+    const int32_t *slot; int64_t n_blocks; int block_tokens;
+    void *k_codes; float *k_scale; void *v_codes; float *v_scale;
+};
+bool       rotary_kv8_fits(int64_t T, int H, int Hkv, int D, int block_tokens);   // its grid
+hipError_t launch_rotary_kv8_append(const RotaryKv8 &a, hipStream_t stream);
+// Linear layers with 4-bit weights and fp16 activations (atom_w4a16.hip).
+struct W4 { const uint8_t *q4; const int8_t *q8; const uint16_t *scale; };
+struct W4A16 {
+    const void *x; int64_t M, ldx;
+    const void *gamma; float eps; const int32_t *idx;
+    int K, O;
+    W4 w[2]; int64_t N;                         // w[1]: the up projection of the gated form, or null
+    const void *residual; int64_t ldr;
+    void *y; int64_t ldy;
+    void *workspace;
+};
+size_t     w4a16_workspace_bytes(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index);
+bool       w4a16_fits(int64_t M, int64_t N, int K, int O, bool gated);            // its grids
+hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream);
+
 // Every workgroup of the attention scans the requests' lengths for its place, so its time grows with their square: 16384 single tokens of 8 cache heads 5.9 ms,
 // 32768 22.8, and 2^24 would hold the GPU for minutes.
 constexpr int kMaxAttentionRequests = 65536;

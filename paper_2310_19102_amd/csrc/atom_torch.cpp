@@ -800,7 +800,7 @@ PyObject *kv_block_map(Args a)
 // Rows [T, heads, D] of a step: each token's heads contiguous.  The stride between tokens (of one token: any that the library takes).
 void token_rows(const Tensor &t, const char *name)
 {
-    if (t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2)))
+    if (t.dim() != 3 || (t.numel() > 0 && ((t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2)))))
         value_error(name, "must be [T, heads, D] with contiguous heads");
 }
 int64_t token_stride(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2); }
@@ -893,6 +893,196 @@ PyObject *attention_kv8(Args a)
     return out.give();
 }
 
+// What atom_rotary and atom_rotary_kv8_append share: positions [T] or [axes, T], table [n_pos, n_pairs, 2], the pairs' axes.
+struct Turn {
+    atom_rotary_desc d = {};
+    const Tensor *positions, *table;
+    int64_t ldp = 0;
+    Turn(PyObject *pos, PyObject *tab, PyObject *axis, PyObject *interleaved, int64_t T)
+    {
+        positions = &device(pos, kInt, "positions");
+        table = &contiguous(tab, kFloat, "table");
+        const Tensor &p = *positions;
+        if ((p.dim() != 1 && p.dim() != 2) || p.size(-1) != T || (T > 1 && p.stride(-1) != 1))
+            value_error("positions must be int32 [T] or [axes, T] with a contiguous last dimension");
+        if (table->dim() != 3 || table->size(2) != 2) value_error("table must be float32 [n_pos, n_pairs, 2]");
+        const int64_t axes = p.dim() == 2 ? p.size(0) : 1;
+        d.n_axes = narrow(axes, "axes");
+        d.n_pairs = narrow(table->size(1), "n_pairs");
+        const int truth = PyObject_IsTrue(interleaved);
+        if (truth < 0) throw Raised();
+        d.interleaved = truth;
+        ldp = axes > 1 ? p.stride(0) : T;
+        if (axis == Py_None) {
+            if (axes > 1) value_error("positions of several axes need the axis of every pair");
+            return;
+        }
+        char *at;
+        Py_ssize_t n;
+        if (PyBytes_AsStringAndSize(axis, &at, &n) < 0) throw Raised();
+        if (n != table->size(1)) value_error("axis must have an entry for every pair of the table");
+        for (Py_ssize_t j = 0; j < n && j < (Py_ssize_t)sizeof(d.axis); ++j) d.axis[j] = (uint8_t)at[j];
+    }
+};
+
+// The caller's memory for turned rows like `x`, where given.
+void turned_rows(Out &out, PyObject *o, const Tensor &x)
+{
+    if (o == Py_None) return;
+    device(o, kHalf, "out");
+    out.given(o, "out");
+    token_rows(*out.t, "out");
+    if (out.t->sizes() != x.sizes()) value_error("out must have the shape of the rows that turn");
+}
+
+// a: x, positions, table, axis, interleaved, transposed, out
+PyObject *rotary(Args a)
+{
+    const Tensor &x = device(a[0], kHalf, "x");
+    token_rows(x, "x");
+    const int64_t T = x.size(0), heads = x.size(1), D = x.size(2);
+    const Turn turn(a[1], a[2], a[3], a[4], T);
+    const int back = PyObject_IsTrue(a[5]);
+    if (back < 0) throw Raised();
+    Out out;
+    turned_rows(out, a[6], x);
+    const OnDevice on(x);
+    on.with({turn.positions, turn.table});
+    if (out.t) on.with({out.t});
+    else out.fresh(make({T, heads, D}, kHalf, x));
+    ATOM_CALL(atom_rotary, data(x), T, token_stride(x), narrow(heads, "heads"), narrow(D, "D"), &turn.d, (const int32_t *)data(*turn.positions), turn.ldp,
+              (const float *)data(*turn.table), turn.table->size(0), back, out.data(), token_stride(*out.t));
+    return out.give();
+}
+
+// a: q, k, v, k_cache, v_cache, slot, positions, table, axis, interleaved, out
+PyObject *rotary_kv8_append(Args a)
+{
+    const Tensor &k = device(a[1], kHalf, "k"), &v = device(a[2], kHalf, "v");
+    token_rows(k, "k");
+    token_rows(v, "v");
+    if (v.sizes() != k.sizes()) value_error("k and v shapes disagree");
+    const int64_t T = k.size(0), Hkv = k.size(1), D = k.size(2);
+    const Tensor *q = a[0] == Py_None ? nullptr : &device(a[0], kHalf, "q");
+    if (q) {
+        token_rows(*q, "q");
+        if (q->size(0) != T || q->size(2) != D) value_error("q must be [T, H, D] with the tokens and channels of k");
+    } else if (a[10] != Py_None)
+        value_error("out is the turned queries' memory: there are no queries");
+    const Pages kc(a[3], "k codes", "k scale"), vc(a[4], "v codes", "v scale");
+    const Tensor &slot = vector(a[5], T, "slot");
+    if (vc.codes->sizes() != kc.codes->sizes() || kc.codes->size(1) != Hkv || kc.codes->size(3) != D)
+        value_error("cache and row shapes disagree");
+    const Turn turn(a[6], a[7], a[8], a[9], T);
+    Out out;
+    if (q) turned_rows(out, a[10], *q);
+    const OnDevice on(k);
+    on.with({&v, kc.codes, kc.scale, vc.codes, vc.scale, &slot, turn.positions, turn.table});
+    if (q) {
+        on.with({q});
+        if (out.t) on.with({out.t});
+        else out.fresh(make({T, q->size(1), D}, kHalf, k));
+    }
+    const int64_t ldq = q ? token_stride(*q) : 0, ldqo = q ? token_stride(*out.t) : 0;
+    ATOM_CALL(atom_rotary_kv8_append, q ? data(*q) : nullptr, ldq, q ? narrow(q->size(1), "H") : 0, q ? out.data() : nullptr, ldqo, data(k), data(v), T,
+              token_stride(k), token_stride(v), narrow(Hkv, "Hkv"), narrow(D, "D"), &turn.d, (const int32_t *)data(*turn.positions), turn.ldp,
+              (const float *)data(*turn.table), turn.table->size(0), (const int32_t *)data(slot), kc.codes->size(0),
+              narrow(kc.codes->size(2), "block_tokens"), data(*kc.codes), (float *)data(*kc.scale), data(*vc.codes), (float *)data(*vc.scale));
+    PyObject *turned = q ? out.give() : (Py_INCREF(Py_None), Py_None);
+    PyObject *r = turned ? PyTuple_Pack(3, turned, a[3], a[4]) : nullptr;
+    Py_XDECREF(turned);
+    return r;
+}
+
+// Weight codes and scales of N rows: q4 [N, (K - O) / 2], q8 [N, O], scale [N, K / group size].
+struct Weights {
+    const Tensor &q4, &q8, &scale;
+    Weights(PyObject *a, PyObject *b, PyObject *c)
+        : q4(contiguous(a, kByte, "w_q4")), q8(contiguous(b, kChar, "w_q8")), scale(contiguous(c, kHalf, "w_scale"))
+    {
+        rows_and_columns(q4, "w_q4");
+        rows_and_columns(q8, "w_q8");
+        rows_and_columns(scale, "w_scale");
+    }
+    int64_t N() const { return q8.size(0); }
+    int64_t O() const { return q8.size(1); }
+    int64_t K() const { return 2 * q4.size(1) + O(); }
+    bool agree(int64_t gs) const { return q4.size(0) == N() && scale.size(0) == N() && scale.size(1) == groups(K(), gs); }
+};
+
+const Tensor *optional(PyObject *o, Kind k, const char *name) { return o == Py_None ? nullptr : &device(o, k, name); }
+
+// One vector of a layer's K input channels (gamma, the index), or null.
+const Tensor *channels(PyObject *o, Kind k, int64_t K, const char *name)
+{
+    const Tensor *t = optional(o, k, name);
+    if (t && (t->dim() != 1 || t->size(0) != K || !t->is_contiguous())) value_error(name, "must be contiguous [K]");
+    return t;
+}
+
+// The two calls on rows x [M, K]; up: null for the plain form.  a: group_size, out, workspace
+PyObject *w4a16(const Tensor &x, PyObject *gamma_, PyObject *eps_, PyObject *idx_, const Weights &w, const Weights *up, PyObject *residual_, Args a)
+{
+    matrix(x, "x must be [M, K] with a contiguous last dimension");
+    const int64_t M = x.size(0), K = x.size(1), N = w.N(), gs = whole(a[0]);
+    if (w.K() != K || !w.agree(gs) || (up && (up->K() != K || up->O() != w.O() || up->N() != N || !up->agree(gs))))
+        value_error("weight and activation shapes disagree");
+    const Tensor *gamma = channels(gamma_, kHalf, K, "gamma"), *idx = channels(idx_, kInt, K, "reorder_idx");
+    const Tensor *residual = optional(residual_, kHalf, "residual");
+    if (residual && (residual->dim() != 2 || residual->size(0) != M || residual->size(1) != N || (N > 1 && residual->stride(1) != 1)))
+        value_error("residual must be [M, N] with a contiguous last dimension");
+    const float eps = real(eps_);
+    Out y;
+    if (a[1] != Py_None) {
+        device(a[1], kHalf, "out");
+        y.given(a[1], "out");
+        if (y.t->dim() != 2 || y.t->size(0) != M || y.t->size(1) != N || (N > 1 && y.t->stride(1) != 1))
+            value_error("out must be [M, N] with a contiguous last dimension");
+    }
+    const Tensor *ws = a[2] == Py_None ? nullptr : &tensor(a[2], "workspace");
+    if (ws && (!ws->is_cuda() || ws->device() != x.device() || !ws->is_contiguous()))
+        value_error("workspace must be a contiguous tensor on the device of x");
+    const OnDevice on(x);
+    on.with({&w.q4, &w.q8, &w.scale});
+    if (up) on.with({&up->q4, &up->q8, &up->scale});
+    for (const Tensor *t : {gamma, idx, residual, y.t})
+        if (t) on.with({t});
+    if (!y.t) y.fresh(make({M, N}, kHalf, x));
+    const atom_desc d = desc(K, gs, w.O());
+    const size_t need = atom_w4a16_workspace_bytes(M, N, &d, up != nullptr, gamma != nullptr, idx != nullptr);
+    Tensor own;
+    if (need && (!ws || bytes(*ws) < need)) {
+        own = make({(int64_t)need}, kByte, x);
+        if (!safe_to_capture(own))
+            value_error("workspace of atom_w4a16_workspace_bytes needed: PyTorch's allocator does not know of this capture");
+        ws = &own;
+    }
+    void *g = gamma ? data(*gamma) : nullptr, *wsp = ws ? data(*ws) : nullptr;
+    const int32_t *index = idx ? (const int32_t *)data(*idx) : nullptr;
+    const size_t wsn = ws ? bytes(*ws) : 0;
+    if (up)
+        ATOM_CALL(atom_w4a16_swiglu, data(x), M, ld(x, M, K), g, eps, index, &d, data(w.q4), data(w.q8), data(w.scale), data(up->q4), data(up->q8),
+                  data(up->scale), N, y.data(), ld(*y.t, M, N), wsp, wsn);
+    else
+        ATOM_CALL(atom_w4a16_linear, data(x), M, ld(x, M, K), g, eps, index, &d, data(w.q4), data(w.q8), data(w.scale), N,
+                  residual ? data(*residual) : nullptr, residual ? ld(*residual, M, N) : 0, y.data(), ld(*y.t, M, N), wsp, wsn);
+    return y.give();
+}
+
+// a: x, gamma, eps, reorder_idx, w_q4, w_q8, w_scale, residual, group_size, out, workspace
+PyObject *w4a16_linear(Args a)
+{
+    return w4a16(device(a[0], kHalf, "x"), a[1], a[2], a[3], Weights(a[4], a[5], a[6]), nullptr, a[7], a + 8);
+}
+
+// a: x, gamma, eps, reorder_idx, gate, up, group_size, out, workspace
+PyObject *w4a16_swiglu(Args a)
+{
+    const Three gate(a[4]), up(a[5]);
+    const Weights u(up.item[0], up.item[1], up.item[2]);
+    return w4a16(device(a[0], kHalf, "x"), a[1], a[2], a[3], Weights(gate.item[0], gate.item[1], gate.item[2]), &u, Py_None, a + 6);
+}
+
 PyObject *mx_quantize_act(Args a)
 {
     const Tensor &x = device(a[0], kHalf, "x"), &idx = device(a[3], kInt, "reorder_idx");
@@ -970,6 +1160,7 @@ PyMethodDef methods[] = {
     ENTRY(quantize_act_packed, 9), ENTRY(add_quantize_act_packed, 11), ENTRY(swiglu_quantize_act_packed, 8),
     ENTRY(w4a4_gemm_prepacked, 9), ENTRY(w4a4_gemm_packed, 9), ENTRY(kv_quantize, 4), ENTRY(kv_quantize_pair, 6),
     ENTRY(kv_block_map, 8), ENTRY(kv8_append, 5), ENTRY(attention_kv8, 10),
+    ENTRY(rotary, 7), ENTRY(rotary_kv8_append, 11), ENTRY(w4a16_linear, 11), ENTRY(w4a16_swiglu, 9),
     ENTRY(decode_attention_kv4, 7), ENTRY(decode_attention_kv4_static, 6), ENTRY(mx_quantize_act, 7), ENTRY(mx_gemm, 7),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
