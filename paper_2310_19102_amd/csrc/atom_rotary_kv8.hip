@@ -23,69 +23,93 @@ __device__ __forceinline__ uint32_t codes4(const float *x, float r)
     return pack4(code_of(x[0] * r), code_of(x[1] * r), code_of(x[2] * r), code_of(x[3] * r));
 }
 
-// Run (atom_kv8_append.h) of turned rows: the same members and steps on fp32 values, the maximum as the bits of a float.
+__device__ __forceinline__ uint2 load_once(const __half *p)
+{
+    typedef unsigned u2 __attribute__((ext_vector_type(2)));
+    const u2 v = __builtin_nontemporal_load(reinterpret_cast<const u2 *>(p));
+    return make_uint2(v[0], v[1]);
+}
+
+// A run of rows of K, turned, or of V, for one head after another: Run (atom_kv8_append.h) on fp32 values, the maximum as the bits of a
+// float.  Row r is token `token` + r; a wavefront has ROWS of them in registers (those of a longer run are read twice), with
+// their angles, which all heads share.
 template <int D, int ROWS, bool ONE, bool NEIGHBOURS>
 struct TurnedRun {
     static constexpr int LPR = D / 8, RPL = 64 / LPR, kLoads = ROWS / RPL;
+    Angles ang[kLoads];
+    uint2 raw[kLoads][2];
     float x[kLoads][8];
-    const __half *rows; int64_t ld, token;
-    int8_t *block; float *scale;
-    int o, at, len, g, i;
+    int64_t token; int last;                                // (the last row that there is, of this run or not)
+    int g, i, len, at, o;
     Channels ch;
     uint32_t axes;
-    float s_old;
+    bool turns;
 
-    __device__ __forceinline__ void load(const Turn &t, int row, float *v) const
-    {
-        const int r = min(row, len - 1);
-        const __half *p = rows + (int64_t)r * ld;
-        const uint2 lo = *reinterpret_cast<const uint2 *>(p + ch.lo), hi = *reinterpret_cast<const uint2 *>(p + ch.hi);
-        widen(lo, v);
-        widen(hi, v + 4);
-        if (ch.turned) turn<NEIGHBOURS>(v, angles<ONE>(t, positions<ONE>(t, token + r), i, axes), 1.0f);
-    }
-    static __device__ __forceinline__ uint32_t magnitude(const float *v)
-    {
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) top = max(top, __builtin_bit_cast(uint32_t, v[k]) & 0x7fffffffu);
-        return top;
-    }
-
-    __device__ __forceinline__ uint32_t begin(const Turn &t, const Side &side, int h, int Hkv, int32_t first, int len_, int64_t tok, int shift,
-                                              int row0 = 0)
+    __device__ __forceinline__ void place(const Turn &t, int64_t tok, int T, bool turns_)
     {
         const int lane = threadIdx.x & 63;
         g = lane / LPR;
         i = lane % LPR;
         ch = channels(t, i);
+        turns = turns_ && ch.turned;
         axes = lane_axes(t, i);
-        len = len_;
-        ld = side.ld;
-        token = tok + row0;
-        o = first & ((1 << shift) - 1);
-        at = o + row0;
-        const int64_t head = (int64_t)(first >> shift) * Hkv + h;
-        block = side.codes + (head << shift) * D;
-        scale = side.scale + head;
-        rows = side.x + (int64_t)h * D + token * ld;
+        token = tok;
+        last = (int)((int64_t)T - 1 - tok);
+    }
+    __device__ __forceinline__ int64_t token_of(int row) const { return token + min(row, last); }
+    __device__ __forceinline__ void fetch_angles(const Turn &t, int u)
+    {
+        if (turns) ang[u] = angles<ONE>(t, positions<ONE>(t, token_of(u * RPL + g)), i, axes);
+    }
+    __device__ __forceinline__ void fetch(const Side &side, int h, int u)
+    {
+        const __half *p = side.x + token_of(u * RPL + g) * side.ld + (int64_t)h * D;
+        raw[u][0] = load_once(p + ch.lo);
+        raw[u][1] = load_once(p + ch.hi);
+    }
+    // a row beyond those in registers
+    __device__ __forceinline__ void again(const Turn &t, const Side &side, int h, int row, float *v) const
+    {
+        const int64_t tok = token_of(row);
+        const __half *p = side.x + tok * side.ld + (int64_t)h * D;
+        widen(*reinterpret_cast<const uint2 *>(p + ch.lo), v);
+        widen(*reinterpret_cast<const uint2 *>(p + ch.hi), v + 4);
+        if (turns) turn<NEIGHBOURS>(v, angles<ONE>(t, positions<ONE>(t, tok), i, axes), 1.0f);
+    }
+    __device__ __forceinline__ uint32_t magnitude(int row, const float *v) const
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = max(top, __builtin_bit_cast(uint32_t, v[k]) & 0x7fffffffu);
+        return row < len ? top : 0;
+    }
+
+    // the rows that were fetched as fp32 values
+    __device__ __forceinline__ void take()
+    {
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            if (u * RPL < len) load(t, u * RPL + g, x[u]);
-        s_old = o > 0 ? *scale : 0.0f;
+            if (u * RPL < len) {
+                widen(raw[u][0], x[u]);
+                widen(raw[u][1], x[u] + 4);
+                if (turns) turn<NEIGHBOURS>(x[u], ang[u], 1.0f);
+            }
+    }
+    __device__ __forceinline__ uint32_t largest(const Turn &t, const Side &side, int h)
+    {
         uint32_t top = 0;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            if (u * RPL < len) top = max(top, magnitude(x[u]));
+            if (u * RPL < len) top = max(top, magnitude(u * RPL + g, x[u]));
         for (int row = ROWS; row < len; row += RPL) {
             float v[8];
-            load(t, row + g, v);
-            top = max(top, magnitude(v));
+            again(t, side, h, row + g, v);
+            top = max(top, magnitude(row + g, v));
         }
         return wave_max(top);
     }
 
-    __device__ __forceinline__ void store(int row, const float *v, float r)
+    __device__ __forceinline__ void store(int8_t *block, int row, const float *v, float r)
     {
         if (row >= len) return;
         // (a NaN that came with the table may have anything in its low byte)
@@ -94,8 +118,10 @@ struct TurnedRun {
         *reinterpret_cast<uint32_t *>(block + (at + row) * D + ch.hi) = b;
     }
 
-    __device__ __forceinline__ void end(const Turn &t, uint32_t top, int thread, int threads)
+    // `top` of the whole run, s_old of its block (0 where it begins the block); `thread` of `threads` that have one: the older rows are theirs in turn
+    __device__ __forceinline__ void end(const Turn &t, const Side &side, int h, int64_t head, int shift, float s_old, uint32_t top, int thread, int threads)
     {
+        int8_t *block = side.codes + (head << shift) * D;
         const float s_new = __builtin_bit_cast(float, top) / 127.0f, s = s_new > s_old || s_new != s_new ? s_new : s_old;
         // (a scale below the normal numbers has no reciprocal)
         const float r = s >= 1.17549435e-38f ? 1.0f / s : 0.0f;
@@ -109,59 +135,156 @@ struct TurnedRun {
         }
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            if (u * RPL < len) store(u * RPL + g, x[u], r);
+            if (u * RPL < len) store(block, u * RPL + g, x[u], r);
         for (int row = ROWS; row < len; row += RPL) {
             float v[8];
-            load(t, row + g, v);
-            store(row + g, v, r);
+            again(t, side, h, row + g, v);
+            store(block, row + g, v, r);
         }
-        if (thread == 0) *scale = s;
+        if (thread == 0) side.scale[head] = s;
     }
 };
 
 struct Queries { const __half *x; int64_t ld; __half *out; int64_t ldo; int heads; };
 
-// Eight channels of a query head to a lane.
+constexpr int kQueryHeads = 4;                               // of a lane, in flight together
+
+// Eight channels of a lane, for `count` heads of a token from h0 on.
 template <int D, bool ONE, bool NEIGHBOURS>
-__device__ __forceinline__ void turn_queries(const Queries &q, const Turn &t, int64_t T, int64_t group)
+__device__ __forceinline__ void turn_queries(const Queries &q, const Turn &t, int64_t token, int i, int h0, int count)
 {
-    const int64_t e = group * 256 + threadIdx.x, row = e / (D / 8);
-    const int i = (int)(e % (D / 8));
-    const int64_t token = row / q.heads;
-    if (token >= T) return;
-    const int h = (int)(row - token * q.heads);
     const Channels ch = channels(t, i);
-    const __half *x = q.x + token * q.ld + (int64_t)h * D;
-    __half *out = q.out + token * q.ldo + (int64_t)h * D;
-    const uint2 lo = *reinterpret_cast<const uint2 *>(x + ch.lo), hi = *reinterpret_cast<const uint2 *>(x + ch.hi);
-    float v[8];
-    widen(lo, v);
-    widen(hi, v + 4);
-    if (ch.turned) turn<NEIGHBOURS>(v, angles<ONE>(t, positions<ONE>(t, token), i, lane_axes(t, i)), 1.0f);
-    *reinterpret_cast<uint2 *>(out + ch.lo) = narrow(v);
-    *reinterpret_cast<uint2 *>(out + ch.hi) = narrow(v + 4);
+    Angles r;
+    if (ch.turned) r = angles<ONE>(t, positions<ONE>(t, token), i, lane_axes(t, i));
+    const __half *x = q.x + token * q.ld + (int64_t)h0 * D;
+    __half *out = q.out + token * q.ldo + (int64_t)h0 * D;
+    for (int h = 0; h < count; h += kQueryHeads) {
+        uint2 raw[kQueryHeads][2];
+#pragma unroll
+        for (int u = 0; u < kQueryHeads; ++u) {
+            const int at = min(h + u, count - 1) * D;
+            raw[u][0] = load_once(x + at + ch.lo);
+            raw[u][1] = load_once(x + at + ch.hi);
+        }
+#pragma unroll
+        for (int u = 0; u < kQueryHeads; ++u) {
+            if (h + u >= count) break;
+            float v[8];
+            widen(raw[u][0], v);
+            widen(raw[u][1], v + 4);
+            if (ch.turned) turn<NEIGHBOURS>(v, r, 1.0f);
+            *reinterpret_cast<uint2 *>(out + (h + u) * D + ch.lo) = narrow(v);
+            *reinterpret_cast<uint2 *>(out + (h + u) * D + ch.hi) = narrow(v + 4);
+        }
+    }
 }
 
-// One wavefront for a head (of K or of V) and a token; where a run begins with that token it writes the run, whole.  The first
-// `appends` workgroups do this, four wavefronts each, the others turn queries.
+struct Step {
+    Queries q; Side k, v;
+    Turn turn;
+    const int32_t *slot; int32_t slots;
+    int T, Hkv, shift;
+    int slab, heads;                                         // of a workgroup: tokens, cache heads
+    uint32_t appends;                                        // workgroups that append; the others turn queries
+    int q_heads;                                             // heads of a lane there
+};
+
+template <int D, bool ONE, bool NEIGHBOURS>
+__device__ __forceinline__ void query_group(const Step &p, uint32_t group)
+{
+    constexpr int LPR = D / 8;
+    const int chunks = (p.q.heads + p.q_heads - 1) / p.q_heads;
+    const int64_t row = (int64_t)group * (256 / LPR) + threadIdx.x / LPR, token = row / chunks;
+    if (token >= p.T) return;
+    const int h0 = (int)(row - token * chunks) * p.q_heads;
+    turn_queries<D, ONE, NEIGHBOURS>(p.q, p.turn, token, threadIdx.x % LPR, h0, min(p.q_heads, p.q.heads - h0));
+}
+
+// Few tokens: one wavefront for a head (of K or of V) and a token; where a run begins with that token it writes the run, whole.  Bound by its
+// chain of reads, so the token's position, angles and row are on their way before its slot is known.
 template <int D, bool ONE, bool NEIGHBOURS>
 __global__ __launch_bounds__(256)
-void rotary_kv8_kernel(Queries q, Side k, Side v, int T, int Hkv, Turn turn, const int32_t *__restrict__ slot, int32_t slots, int shift, uint32_t appends)
+void rotary_kv8_kernel(Step p)
 {
-    if (blockIdx.x >= appends) return turn_queries<D, ONE, NEIGHBOURS>(q, turn, T, blockIdx.x - appends);
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = item / (2 * Hkv);
-    const int which = (int)(item - t * (2 * Hkv)), h = which % Hkv;
-    if (t >= T) return;
-    const Window w = window(slot, slots, T, t, 1, 1 << shift);
+    if (blockIdx.x >= p.appends) return query_group<D, ONE, NEIGHBOURS>(p, blockIdx.x - p.appends);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = (int64_t)blockIdx.x * 4 + wave, t = item / (2 * p.Hkv);
+    const int which = (int)(item - t * (2 * p.Hkv));
+    if (t >= p.T) return;
+    const bool is_k = which < p.Hkv;
+    const int h = is_k ? which : which - p.Hkv;
+    const Side side = is_k ? p.k : p.v;
+    TurnedRun<D, 16, ONE, NEIGHBOURS> run;
+    run.place(p.turn, t, p.T, is_k);
+    run.fetch(side, h, 0);
+    run.fetch_angles(p.turn, 0);
+    const Window w = window(p.slot, p.slots, p.T, t, 1, 1 << p.shift);
     if (!w.leaders) return;
     const int32_t first = __builtin_amdgcn_readlane(w.got, 0);
-    const int len = run_length(slot, T, w, t, 0, 1 << shift), lane = threadIdx.x & 63;
-    if (which < Hkv) {
-        TurnedRun<D, 16, ONE, NEIGHBOURS> run;
-        run.end(turn, run.begin(turn, k, h, Hkv, first, len, t, shift), lane, 64);
-    } else {
-        Run<D, 16> run;
-        run.end(run.begin(v, h, Hkv, first, len, t, shift), lane, 64);
+    run.o = run.at = first & ((1 << p.shift) - 1);
+    const int64_t head = (int64_t)(first >> p.shift) * p.Hkv + h;
+    const float s_old = run.o > 0 ? side.scale[head] : 0.0f;
+    run.len = run_length(p.slot, p.T, w, t, 0, 1 << p.shift);
+#pragma unroll
+    for (int u = 1; u < run.kLoads; ++u)
+        if (u * run.RPL < run.len) {
+            run.fetch(side, h, u);
+            run.fetch_angles(p.turn, u);
+        }
+    run.take();
+    run.end(p.turn, side, h, head, p.shift, s_old, run.largest(p.turn, side, h), threadIdx.x & 63, 64);
+}
+
+// Many tokens: a workgroup of four wavefronts for `slab` tokens and some heads of K or of V writes the runs that begin among them, each whole, also past
+// the slab's end.  Up to three runs are written by all four, ROWS rows each; more of them, and runs of ROWS at most, one by each in turn.
+template <int D, int ROWS, bool ONE, bool NEIGHBOURS>
+__global__ __launch_bounds__(256)
+void rotary_kv8_many_kernel(Step p)
+{
+    __shared__ uint32_t s_top[2][4];
+    if (blockIdx.x >= p.appends) return query_group<D, ONE, NEIGHBOURS>(p, blockIdx.x - p.appends);
+    const int chunks = (p.Hkv + p.heads - 1) / p.heads;
+    const int64_t group = blockIdx.x / (2 * chunks), t_first = group * p.slab;
+    const int which = (int)(blockIdx.x - group * (2 * chunks));
+    const bool is_k = which < chunks;
+    const int h0 = (is_k ? which : which - chunks) * p.heads, h1 = min(h0 + p.heads, p.Hkv);
+    const Side side = is_k ? p.k : p.v;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), bs = 1 << p.shift;
+    const Window w = window(p.slot, p.slots, p.T, t_first, p.slab, bs);        // (the same in all four)
+    const bool alone = __builtin_popcountll(w.leaders) > 3 || bs <= ROWS;
+    int turn = 0, sync = 0;                                                  // of the runs; nobody writes maxima before all have read the last but one's
+    for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1, ++turn) {
+        if (alone && (turn & 3) != wave) continue;
+        const int l0 = __builtin_ctzll(leaders), len = run_length(p.slot, p.T, w, t_first, l0, bs);
+        const int row0 = alone ? 0 : wave * ROWS;
+        const int32_t first = __builtin_amdgcn_readlane(w.got, l0);
+        TurnedRun<D, ROWS, ONE, NEIGHBOURS> run;
+        run.place(p.turn, t_first + l0 + row0, p.T, is_k);
+        run.o = first & (bs - 1);
+        run.at = run.o + row0;
+        run.len = alone ? len : min(max(len - row0, 0), ROWS);
+#pragma unroll
+        for (int u = 0; u < run.kLoads; ++u)
+            if (u * run.RPL < run.len) run.fetch(side, h0, u);
+#pragma unroll
+        for (int u = 0; u < run.kLoads; ++u)
+            if (u * run.RPL < run.len) run.fetch_angles(p.turn, u);
+        for (int h = h0; h < h1; ++h) {
+            const int64_t head = (int64_t)(first >> p.shift) * p.Hkv + h;
+            const float s_old = run.o > 0 ? side.scale[head] : 0.0f;
+            run.take();
+#pragma unroll
+            for (int u = 0; u < run.kLoads; ++u)
+                if (u * run.RPL < run.len && h + 1 < h1) run.fetch(side, h + 1, u);
+            uint32_t top = run.largest(p.turn, side, h);
+            if (!alone) {
+                uint32_t *tops = s_top[sync++ & 1];
+                if ((threadIdx.x & 63) == 0) tops[wave] = top;
+                __syncthreads();
+                top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+            }
+            run.end(p.turn, side, h, head, p.shift, s_old, top, alone ? threadIdx.x & 63 : threadIdx.x, alone ? 64 : 256);
+        }
     }
 }
 
@@ -169,25 +292,54 @@ void rotary_kv8_kernel(Queries q, Side k, Side v, int T, int Hkv, Turn turn, con
 
 namespace atom_internal {
 
-static int64_t append_groups(int64_t T, int Hkv) { return (T * 2 * Hkv + 3) / 4; }
-static int64_t query_groups(int64_t T, int H, int D) { return (T * H * (D / 8) + 255) / 256; }
+// How a call runs: tokens to a workgroup (0: a wavefront for each token and head), cache heads to a workgroup, workgroups that append;
+// query heads to a lane, workgroups that turn them.
+struct TurnShape { int slab, heads; int64_t appends; int q_heads; int64_t queries; };
+
+static TurnShape turn_shape(int64_t T, int H, int Hkv, int D, int block_tokens)
+{
+    TurnShape s = {};
+    const int64_t items = T * 2 * Hkv;
+    const bool long_runs = block_tokens >= 64;
+    if (long_runs ? T < 256 : items <= 16384) {
+        s.heads = 1;
+        s.appends = (items + 3) / 4;
+    } else {
+        s.slab = items <= 16384 ? 8 : 64;
+        const int64_t slabs = (T + s.slab - 1) / s.slab;
+        s.heads = 8;
+        while (s.heads > 1 && slabs * 2 * ((Hkv + s.heads - 1) / s.heads) < 1024) s.heads /= 2;
+        s.appends = slabs * 2 * ((Hkv + s.heads - 1) / s.heads);
+    }
+    s.q_heads = 8;
+    const int64_t rows = 256 / (D / 8);
+    while (s.q_heads > 1 && T * ((H + s.q_heads - 1) / s.q_heads) / rows < 1024) s.q_heads /= 2;
+    s.queries = (T * ((H + s.q_heads - 1) / s.q_heads) + rows - 1) / rows;
+    return s;
+}
 
 bool rotary_kv8_fits(int64_t T, int H, int Hkv, int D, int block_tokens)
 {
-    (void)block_tokens;
-    return append_groups(T, Hkv) + query_groups(T, H, D) <= atom_launch::kMostThreads / 256;
+    const TurnShape s = turn_shape(T, H, Hkv, D, block_tokens);
+    return s.appends + s.queries <= atom_launch::kMostThreads / 256;
 }
 
 hipError_t launch_rotary_kv8_append(const RotaryKv8 &a, hipStream_t stream)
 {
-    const Queries q = {(const __half *)a.q, a.ldq, (__half *)a.q_out, a.ldqo, a.H};
-    const Side k = {(const __half *)a.k, a.ldk, (int8_t *)a.k_codes, a.k_scale}, v = {(const __half *)a.v, a.ldv, (int8_t *)a.v_codes, a.v_scale};
-    const int32_t slots = (int32_t)(a.n_blocks * a.block_tokens);
-    const int     shift = __builtin_ctz((unsigned)a.block_tokens);
-    const int64_t appends = append_groups(a.T, a.Hkv), groups = appends + query_groups(a.T, a.H, a.D);
-#define ATOM_TURN(D, ONE, NEIGHBOURS)                                                                                                          \
-    hipLaunchKernelGGL((rotary_kv8_kernel<D, ONE, NEIGHBOURS>), dim3((unsigned)groups), dim3(256), 0, stream, q, k, v, (int)a.T, a.Hkv, a.turn, \
-                       a.slot, slots, shift, (uint32_t)appends)
+    const TurnShape s = turn_shape(a.T, a.H, a.Hkv, a.D, a.block_tokens);
+    const Step p = {{(const __half *)a.q, a.ldq, (__half *)a.q_out, a.ldqo, a.H},
+                    {(const __half *)a.k, a.ldk, (int8_t *)a.k_codes, a.k_scale},
+                    {(const __half *)a.v, a.ldv, (int8_t *)a.v_codes, a.v_scale},
+                    a.turn, a.slot, (int32_t)(a.n_blocks * a.block_tokens), (int)a.T, a.Hkv, __builtin_ctz((unsigned)a.block_tokens),
+                    s.slab, s.heads, (uint32_t)s.appends, s.q_heads};
+    const dim3 grid((unsigned)(s.appends + s.queries));
+#define ATOM_TURN(D, ONE, NEIGHBOURS)                                                                                      \
+    do {                                                                                                                   \
+        auto kern = !s.slab ? &rotary_kv8_kernel<D, ONE, NEIGHBOURS>                                                       \
+                    : a.block_tokens == 128 || a.block_tokens == 32 ? &rotary_kv8_many_kernel<D, 32, ONE, NEIGHBOURS>       \
+                                                                    : &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS>;      \
+        hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, p);                                                           \
+    } while (0)
 #define ATOM_TURN_D(D)                                                \
     do {                                                              \
         if (a.turn.axes == 1) {                                       \
