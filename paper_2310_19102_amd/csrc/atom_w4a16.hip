@@ -2,10 +2,15 @@
 // the gated half of a feed-forward block made of two of them:
 //   y[m, n] = fp16( residual[m, n] + sum_g scale[n, g] * sum_{k in g} code[n, k] * xr[m, k] )
 //   h[m, n] = fp16( silu(gate) * up ),  gate and up two such sums of one xr
-// xr: the activations in reordered order, behind RMSNorm where gamma is given (then rounded to fp16, which the matrix cores take).
+// xr: the activations in reordered order, behind RMSNorm where gamma is given.  The matrix cores take fp16; what the norm gives has more bits,
+// and rounding it would be the largest error of the whole layer (1.4 to 1.8 times that of the output's own rounding), so it goes in as
+// two halves, hi + lo, 22 bits.
 //
 // MFMA 16x16x32 f16: lane l supplies row (l & 15) of its operand and the 8 values of k-chunk (l >> 4); the result has column
-// (l & 15) in lane l and rows 4 (l >> 4) + e in register e.  Activations are the row operand, weights the columns.
+// (l & 15) in lane l and rows 4 (l >> 4) + e in register e.  Activations are the row operand, weights the columns.  Which channels a
+// chunk has is free as long as both operands agree: a lane reads 16 bytes of a weight row, channels 32 c .. 32 c + 31 of a
+// group in its chunk c, and the i-th instruction takes eight of them; activations are laid out so that its four chunks are
+// 64 bytes in a row, with the eight in the order in which the codes come out of their word.
 
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
@@ -41,12 +46,6 @@ __device__ __forceinline__ h8 widen4(uint32_t w)
     const h2 d = __builtin_elementwise_fma(as_h2((v & 0x00f000f0u) | 0x64006400u), sixteenth, high);
     return as_h8(bits(a), bits(b), bits(c), bits(d));
 }
-// The activations that meet them, from eight in a row.
-__device__ __forceinline__ h8 paired(const uint4 &x)
-{
-    return as_h8(__builtin_amdgcn_perm(x.z, x.x, 0x05040100u), __builtin_amdgcn_perm(x.z, x.x, 0x07060302u),
-                 __builtin_amdgcn_perm(x.w, x.y, 0x05040100u), __builtin_amdgcn_perm(x.w, x.y, 0x07060302u));
-}
 // Eight 8-bit codes in a row, likewise: 1024 + (code + 128).
 __device__ __forceinline__ h8 widen8(uint32_t lo, uint32_t hi)
 {
@@ -59,124 +58,290 @@ __device__ __forceinline__ h8 widen8(uint32_t lo, uint32_t hi)
 
 struct Args {
     const __half *x; int64_t ldx, M;
+    const __half *gamma; float eps; const int32_t *idx;
     int K, O;
     W4 w[2]; int64_t N;
     const __half *residual; int64_t ldr;
     __half *y; int64_t ldy;
-    uint32_t row_tiles;
+    const __half *staged; int rows;                          // laid out, `rows` rows of hi and behind them those of lo
+    bool combine;                                            // lo in rows 8 .. 15 of the one tile
+    uint32_t tiles, row_tiles;
 };
 
-// A workgroup has 16 output channels (of gate and of up) and 16 MT rows; its eight wavefronts have a run of groups each, and
-// their sums meet in LDS, added in order.
-template <int MT, bool GATED>
-__global__ __launch_bounds__(kThreads)
-void w4a16_kernel(Args p)
-{
-    constexpr int WM = GATED ? 2 : 1;
-    __shared__ float red[kWaves][WM * MT][4][64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 15, kc = lane >> 4;
-    const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7;
-    const uint32_t tile = blockIdx.x / p.row_tiles;
-    const int64_t n0 = (int64_t)tile * 16, m0 = (int64_t)(blockIdx.x - tile * p.row_tiles) * (16 * MT);
-    const int g_begin = (int)((int64_t)wave * G / kWaves), g_end = (int)((int64_t)(wave + 1) * G / kWaves);
+// ---- the activations as the product takes them
 
-    const int64_t row = min(n0 + col, p.N - 1);               // (columns >= N are computed and never stored, rows >= M likewise)
-    const __half *x[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) x[mt] = p.x + min(m0 + 16 * mt + col, p.M - 1) * p.ldx + kc * 32;
-    f4 acc[WM][MT] = {};
-    for (int g = g_begin; g < g_end; ++g) {
-        f4 part[WM][MT] = {};
-        h8 w[WM][4];
-        float scale[WM];
-        const bool is4 = g < G4;
-#pragma unroll
-        for (int i = 0; i < WM; ++i) {
-            scale[i] = __half2float(__ushort_as_half(p.w[i].scale[row * G + g]));
-            if (is4) {
-                const uint4 q = *reinterpret_cast<const uint4 *>(p.w[i].q4 + row * (K4 >> 1) + g * 64 + kc * 16);
-                w[i][0] = widen4(q.x);
-                w[i][1] = widen4(q.y);
-                w[i][2] = widen4(q.z);
-                w[i][3] = widen4(q.w);
-            } else {
-                const uint4 *q = reinterpret_cast<const uint4 *>(p.w[i].q8 + row * p.O + (g - G4) * 128 + kc * 32);
-                const uint4 a = q[0], b = q[1];
-                w[i][0] = widen8(a.x, a.y);
-                w[i][1] = widen8(a.z, a.w);
-                w[i][2] = widen8(b.x, b.y);
-                w[i][3] = widen8(b.z, b.w);
-            }
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(x[mt] + g * 128 + c * 8);
-                const h8 a = is4 ? paired(v) : as_h8(v.x, v.y, v.z, v.w);
-#pragma unroll
-                for (int i = 0; i < WM; ++i) part[i][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, w[i][c], part[i][mt], 0, 0, 0);
-            }
-#pragma unroll
-        for (int i = 0; i < WM; ++i)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][mt][e] = fmaf(part[i][mt][e], scale[i], acc[i][mt][e]);
-    }
-#pragma unroll
-    for (int i = 0; i < WM; ++i)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) red[wave][i * MT + mt][e][lane] = acc[i][mt][e];
-    __syncthreads();
-    for (int at = tid; at < MT * 256; at += kThreads) {
-        const int l = at & 63, e = (at >> 6) & 3, mt = at >> 8;
-        float sum[WM];
-#pragma unroll
-        for (int i = 0; i < WM; ++i) {
-            sum[i] = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) sum[i] += red[w][i * MT + mt][e][l];
-        }
-        const int64_t m = m0 + 16 * mt + 4 * (l >> 4) + e, n = n0 + (l & 15);
-        if (m >= p.M || n >= p.N) continue;
-        float y = sum[0];
-        if constexpr (GATED) y = y / (1.0f + expf(-y)) * sum[WM - 1];
-        else if (p.residual) y += __half2float(p.residual[m * p.ldr + n]);
-        p.y[m * p.ldy + n] = __float2half_rn(y);
-    }
-}
-
-// The activations as the product takes them: a row to a workgroup.
-__global__ __launch_bounds__(256)
-void w4a16_rows_kernel(const __half *__restrict__ x, int64_t ldx, const __half *__restrict__ gamma, float eps, const int32_t *__restrict__ idx, int K,
-                       __half *__restrict__ out)
+// Row x in reordered order, behind the norm where there is gamma, laid out for the product (lo: null where there is no
+// norm).  nat: K words of LDS (halves without norm, none without an index either); all threads of the workgroup call.
+template <int THREADS>
+__device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict__ x, uint32_t *nat, float *s_sum, __half *hi, __half *lo)
 {
-    __shared__ float s_sum[4];
-    const int tid = threadIdx.x;
-    x += (int64_t)blockIdx.x * ldx;
-    out += (int64_t)blockIdx.x * K;
-    float r = 1.0f;
-    if (gamma) {
+    const int tid = threadIdx.x, blocks = p.K / 8, K4 = p.K - p.O;
+    const uint4 *row = reinterpret_cast<const uint4 *>(x);
+    auto half_of = [](const uint4 &v, int i) -> uint32_t { return ((i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w) >> (16 * (i & 1))) & 0xffffu; };
+    auto value = [](uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); };
+    if (p.gamma) {
         float sum = 0.0f;
-        for (int k = tid; k < K; k += 256) {
-            const float v = __half2float(x[k]);
-            sum += v * v;
+        for (int b = tid; b < blocks; b += THREADS) {
+            const uint4 v = row[b];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(value(half_of(v, i)), value(half_of(v, i)), sum);
         }
 #pragma unroll
         for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
         if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
         __syncthreads();
-        sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
-        r = 1.0f / sqrtf(sum / (float)K + eps);
+        sum = 0.0f;
+        for (int w = 0; w < THREADS / 64; ++w) sum += s_sum[w];
+        const float r = 1.0f / sqrtf(sum / (float)p.K + p.eps);
+        for (int b = tid; b < blocks; b += THREADS) {
+            const uint4 v = row[b], g = reinterpret_cast<const uint4 *>(p.gamma)[b];
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = value(half_of(v, i)) * r * value(half_of(g, i));
+                const __half h = __float2half_rn(y);
+                // (of what is not finite hi says it all: infinity minus infinity would be NaN)
+                const __half l = __hisinf(h) || __hisnan(h) ? __ushort_as_half(0) : __float2half_rn(y - __half2float(h));
+                w[i] = (uint32_t)__half_as_ushort(h) | (uint32_t)__half_as_ushort(l) << 16;
+            }
+            reinterpret_cast<uint4 *>(nat)[2 * b] = make_uint4(w[0], w[1], w[2], w[3]);
+            reinterpret_cast<uint4 *>(nat)[2 * b + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+        __syncthreads();
+    } else if (p.idx) {
+        for (int b = tid; b < blocks; b += THREADS) reinterpret_cast<uint4 *>(nat)[b] = row[b];
+        __syncthreads();
     }
-    for (int k = tid; k < K; k += 256) {
-        const uint32_t at = idx ? min((uint32_t)idx[k], (uint32_t)(K - 1)) : (uint32_t)k;
-        const float v = __half2float(x[at]);
-        out[k] = __float2half_rn(gamma ? v * r * __half2float(gamma[at]) : v);
+    for (int b = tid; b < blocks; b += THREADS) {
+        const int g = b >> 4, k = g * 128 + (b & 3) * 32 + ((b >> 2) & 3) * 8;        // the eight channels of place b
+        uint32_t w[8];
+        if (p.idx) {
+            const int4 i0 = *reinterpret_cast<const int4 *>(p.idx + k), i1 = *reinterpret_cast<const int4 *>(p.idx + k + 4);
+            const int32_t at[8] = {i0.x, i0.y, i0.z, i0.w, i1.x, i1.y, i1.z, i1.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t c = min((uint32_t)at[i], (uint32_t)(p.K - 1));
+                w[i] = p.gamma ? nat[c] : reinterpret_cast<const uint16_t *>(nat)[c];
+            }
+        } else if (p.gamma) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = nat[k + i];
+        } else {
+            const uint4 v = row[k / 8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = half_of(v, i);
+        }
+        if (k < K4) {
+            const uint32_t t1 = w[1], t2 = w[2], t3 = w[3];                           // 0 4 1 5 2 6 3 7
+            w[1] = w[4];
+            w[2] = t1;
+            w[3] = w[5];
+            w[4] = t2;
+            w[5] = w[6];
+            w[6] = t3;
+        }
+        auto pack = [&](uint32_t sel) {
+            return make_uint4(__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel), __builtin_amdgcn_perm(w[5], w[4], sel),
+                              __builtin_amdgcn_perm(w[7], w[6], sel));
+        };
+        *reinterpret_cast<uint4 *>(hi + 8 * b) = pack(0x05040100u);
+        if (lo) *reinterpret_cast<uint4 *>(lo + 8 * b) = pack(0x07060302u);
+    }
+}
+
+__host__ __device__ constexpr size_t natural_bytes(int K, bool norm, bool index) { return norm ? 4 * (size_t)K : index ? 2 * (size_t)K : 0; }
+
+// A row to a workgroup, into the workspace.
+__global__ __launch_bounds__(512)
+void w4a16_rows_kernel(Args p, __half *out)
+{
+    extern __shared__ uint32_t s_nat[];
+    __shared__ float s_sum[8];
+    lay_out<512>(p, p.x + (int64_t)blockIdx.x * p.ldx, s_nat, s_sum, out + (int64_t)blockIdx.x * p.K,
+                 p.gamma ? out + ((int64_t)p.M + blockIdx.x) * p.K : nullptr);
+}
+
+// ---- the product
+
+// A workgroup has 16 NT output channels (of gate and of up) and 16 RT rows; its eight wavefronts share the groups, and their sums
+// meet in LDS, added in order.  A wavefront has a run of INT4 groups and every eighth INT8 group; CH of them are on their way while it
+// works, across the tiles that the workgroup has in turn.
+//   HL: halves of the activations that go in one after the other (2: hi and lo)
+//   KEPT: the activations are laid out in LDS by the workgroup itself (RT = HL = 1), under way with the first weights
+template <int NT, bool GATED, int RT, int HL, int CH, bool KEPT>
+__global__ __launch_bounds__(kThreads, KEPT ? 4 : 2)
+void w4a16_kernel(Args p)
+{
+    constexpr int WM = GATED ? 2 : 1, CT = WM * NT, AT = KEPT ? 1 : RT * HL;
+    static_assert(CT <= 4, "a lane's chunk loads the scales of one tile");
+    extern __shared__ __align__(16) unsigned char s_all[];   // KEPT: the rows, then the sums or what is laid out; else the sums
+    __shared__ float s_part[8];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, kc = lane >> 4;
+    const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, G8 = G - G4;
+    const int begin = (int)((int64_t)wave * G4 / kWaves), n4 = (int)((int64_t)(wave + 1) * G4 / kWaves) - begin;
+    const int n = n4 + (G8 > wave ? (G8 - wave + kWaves - 1) / kWaves : 0);           // elements of this wavefront
+
+    // (rows >= M are computed and never stored, columns >= N likewise)
+    const uint32_t row_tile = blockIdx.x % p.row_tiles, first = blockIdx.x / p.row_tiles, stride = gridDim.x / p.row_tiles;
+    const int64_t m0 = (int64_t)row_tile * (16 * RT);
+    const int rows = p.rows, lds_row = p.K + 8;
+    const __half *act[AT];
+    const __half *s_act = nullptr;
+    if constexpr (KEPT) {
+        const int r = p.combine && col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1);
+        s_act = reinterpret_cast<const __half *>(s_all) + (size_t)r * lds_row + kc * 8;
+    } else {
+#pragma unroll
+        for (int t = 0; t < AT; ++t) {
+            const int64_t m = p.combine ? (col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1))
+                                        : min(m0 + 16 * (t % RT) + col, (int64_t)rows - 1) + (t / RT) * (int64_t)rows;
+            act[t] = p.staged + m * p.K + kc * 8;
+        }
+    }
+    float *red = reinterpret_cast<float *>(s_all + (KEPT ? (size_t)rows * (p.gamma ? 2 : 1) * lds_row * 2 : 0));
+
+    struct Element { uint4 q[CT], q1[CT]; uint16_t scale; uint4 a[AT][4]; };
+    Element ring[CH];
+    // the element that is loaded next
+    uint32_t load_tile = first;
+    int load_i = 0;
+    int64_t row4[CT], row8[CT], row_s;
+    auto rows_of = [&](uint32_t tile) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            const int64_t r = min((int64_t)tile * (16 * NT) + 16 * (t % NT) + col, p.N - 1);
+            row4[t] = r * (K4 >> 1) + kc * 16;
+            row8[t] = r * p.O + kc * 32;
+        }
+        row_s = min((int64_t)tile * (16 * NT) + 16 * ((kc % CT) % NT) + col, p.N - 1) * G;
+    };
+    auto load = [&](Element &e) {
+        if (load_tile >= p.tiles) return;
+        const bool is4 = load_i < n4;
+        const int  g = is4 ? begin + load_i : wave + kWaves * (load_i - n4);          // of the INT4 or of the INT8 groups
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            const W4 &w = p.w[t / NT];
+            const uint8_t *at = is4 ? w.q4 + row4[t] + g * 64 : reinterpret_cast<const uint8_t *>(w.q8) + row8[t] + g * 128;
+            e.q[t] = *reinterpret_cast<const uint4 *>(at);
+            if (!is4) e.q1[t] = *reinterpret_cast<const uint4 *>(at + 16);
+        }
+        const int k = is4 ? g : G4 + g;
+        e.scale = (CT > 1 && (kc % CT) / NT ? p.w[WM - 1] : p.w[0]).scale[row_s + k];
+        if constexpr (!KEPT) {
+#pragma unroll
+            for (int t = 0; t < AT; ++t)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) e.a[t][c] = *reinterpret_cast<const uint4 *>(act[t] + k * 128 + c * 32);
+        }
+        if (++load_i == n) {
+            load_i = 0;
+            load_tile += stride;
+            rows_of(load_tile);
+        }
+    };
+    f4 acc[CT][RT] = {};
+    auto compute = [&](const Element &e, int i) {
+        const bool is4 = i < n4;
+        const int  k = is4 ? begin + i : G4 + wave + kWaves * (i - n4);
+        f4 part[CT][RT] = {};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            h8 w[CT];
+#pragma unroll
+            for (int t = 0; t < CT; ++t) {
+                if (is4) w[t] = widen4(c == 0 ? e.q[t].x : c == 1 ? e.q[t].y : c == 2 ? e.q[t].z : e.q[t].w);
+                else     w[t] = c == 0 ? widen8(e.q[t].x, e.q[t].y) : c == 1 ? widen8(e.q[t].z, e.q[t].w) : c == 2 ? widen8(e.q1[t].x, e.q1[t].y) : widen8(e.q1[t].z, e.q1[t].w);
+            }
+#pragma unroll
+            for (int a = 0; a < AT; ++a) {
+                h8 x;
+                if constexpr (KEPT) x = *reinterpret_cast<const h8 *>(s_act + k * 128 + c * 32);
+                else x = __builtin_bit_cast(h8, e.a[a][c]);
+#pragma unroll
+                for (int t = 0; t < CT; ++t) part[t][a % RT] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w[t], part[t][a % RT], 0, 0, 0);
+            }
+        }
+        const float mine = __half2float(__ushort_as_half(e.scale));
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            const float s = CT == 1 ? mine : __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * (16 * t + col), __builtin_bit_cast(int, mine)));
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[t][r][j] = fmaf(part[t][r][j], s, acc[t][r][j]);
+        }
+    };
+    int buffer = 0;
+    auto finish = [&](uint32_t tile) {
+        float *mine = red + (size_t)buffer * (kWaves * CT * RT * 256);
+        buffer ^= 1;                                         // (nobody writes a buffer before all have read what it held two tiles ago)
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    mine[((wave * CT + t) * RT + r) * 256 + j * 64 + lane] = acc[t][r][j];
+                    acc[t][r][j] = 0.0f;
+                }
+        __syncthreads();
+        for (int at = tid; at < NT * RT * 256; at += kThreads) {
+            const int l = at & 63, j = (at >> 6) & 3, r = (at >> 8) % RT, t = (at >> 8) / RT;
+            const int64_t m = m0 + 16 * r + 4 * (l >> 4) + j, out = (int64_t)tile * (16 * NT) + 16 * t + (l & 15);
+            if (m >= p.M || out >= p.N) continue;
+            float sum[WM];
+#pragma unroll
+            for (int i = 0; i < WM; ++i) {
+                float lo = 0.0f;
+                sum[i] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const float *s = mine + ((w * CT + i * NT + t) * RT + r) * 256 + j * 64 + l;
+                    sum[i] += s[0];
+                    if (p.combine) lo += s[32];
+                }
+                sum[i] += lo;
+            }
+            float y = sum[0];
+            if constexpr (GATED) y = y / (1.0f + expf(-y)) * sum[WM - 1];
+            else if (p.residual) y += __half2float(p.residual[m * p.ldr + out]);
+            p.y[m * p.ldy + out] = __float2half_rn(y);
+        }
+    };
+
+    rows_of(first);
+    if (n > 0) {
+#pragma unroll
+        for (int s = 0; s < CH; ++s) load(ring[s]);
+    }
+    if constexpr (KEPT) {
+        uint32_t *nat = reinterpret_cast<uint32_t *>(red);
+        __half *out = reinterpret_cast<__half *>(s_all);
+        for (int m = 0; m < rows; ++m) {
+            if (m) __syncthreads();
+            lay_out<kThreads>(p, p.x + m * p.ldx, nat, s_part, out + (size_t)m * lds_row, p.gamma ? out + (size_t)(rows + m) * lds_row : nullptr);
+        }
+        __syncthreads();
+    }
+    if (n == 0) {
+        for (uint32_t tile = first; tile < p.tiles; tile += stride) finish(tile);
+        return;
+    }
+    uint32_t tile = first;
+    for (int i = 0;;) {
+#pragma unroll
+        for (int s = 0; s < CH; ++s) {
+            compute(ring[s], i);
+            load(ring[s]);
+            if (++i == n) {
+                i = 0;
+                finish(tile);
+                tile += stride;
+                if (tile >= p.tiles) return;
+            }
+        }
     }
 }
 
@@ -184,13 +349,33 @@ void w4a16_rows_kernel(const __half *__restrict__ x, int64_t ldx, const __half *
 
 namespace atom_internal {
 
-size_t w4a16_workspace_bytes(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index)
+// How a call runs: whether the workgroups lay the activations out themselves, column and row tiles, LDS.
+struct ProductShape { bool kept, combine; int NT, RT; size_t lds; };
+
+static ProductShape product_shape(int64_t M, int64_t N, int K, bool gated, bool norm, bool index)
 {
-    (void)N, (void)O, (void)gated;
-    return norm || index ? (size_t)M * K * 2 : 0;
+    const int WM = gated ? 2 : 1;
+    ProductShape s = {};
+    s.NT = 1;
+    s.RT = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+    s.combine = norm && M <= 8;
+    const size_t sums = (size_t)2 * kWaves * WM * 1024, nat = natural_bytes(K, norm, index), rest = nat > sums ? nat : sums;
+    if (M <= (norm ? 8 : 16)) {
+        s.lds = (size_t)M * (norm ? 2 : 1) * (K + 8) * 2 + rest;
+        s.kept = s.lds <= 80 * 1024;
+    }
+    if (!s.kept) {
+        while (M <= 16 && s.NT * WM < 4 && (N + 32 * s.NT - 1) / (32 * s.NT) >= 192) s.NT *= 2;
+        s.lds = (size_t)2 * kWaves * WM * s.NT * s.RT * 1024;
+    }
+    return s;
 }
 
-static int row_tiles_of(int64_t M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }
+size_t w4a16_workspace_bytes(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index)
+{
+    (void)O;
+    return product_shape(M, N, K, gated, norm, index).kept ? 0 : (size_t)M * K * (norm ? 4 : 2);
+}
 
 bool w4a16_fits(int64_t M, int64_t N, int K, int O, bool gated)
 {
@@ -202,29 +387,57 @@ bool w4a16_fits(int64_t M, int64_t N, int K, int O, bool gated)
 
 hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
 {
-    Args p = {(const __half *)a.x, a.ldx, a.M, a.K, a.O, {a.w[0], a.w[1]}, a.N, (const __half *)a.residual, a.ldr, (__half *)a.y, a.ldy, 1};
-    if (a.gamma || a.idx) {
-        hipLaunchKernelGGL(w4a16_rows_kernel, dim3((unsigned)a.M), dim3(256), 0, stream, p.x, a.ldx, (const __half *)a.gamma, a.eps, a.idx, a.K,
-                           (__half *)a.workspace);
-        p.x = (const __half *)a.workspace;
-        p.ldx = a.K;
+    const bool gated = a.w[1].q4 != nullptr, norm = a.gamma != nullptr;
+    const ProductShape s = product_shape(a.M, a.N, a.K, gated, norm, a.idx != nullptr);
+    Args p = {(const __half *)a.x, a.ldx, a.M, (const __half *)a.gamma, a.eps, a.idx, a.K, a.O, {a.w[0], a.w[1]}, a.N, (const __half *)a.residual, a.ldr,
+              (__half *)a.y, a.ldy, (const __half *)a.workspace, (int)a.M, s.combine, 0, 1};
+    p.tiles = (uint32_t)((a.N + 16 * s.NT - 1) / (16 * s.NT));
+    p.row_tiles = (uint32_t)((a.M + 16 * s.RT - 1) / (16 * s.RT));
+    const uint32_t room = (uint32_t)(2 * atom_launch::compute_units());
+    const uint32_t grid = (p.tiles < room ? p.tiles : room) * p.row_tiles;
+    if (!s.kept) {
+        static atom_launch::LdsOptIn opt;
+        const size_t nat = natural_bytes(a.K, norm, a.idx != nullptr);
+        if (nat > 60 * 1024) {
+            const hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(&w4a16_rows_kernel), nat);
+            if (err != hipSuccess) return err;
+        }
+        hipLaunchKernelGGL(w4a16_rows_kernel, dim3((unsigned)a.M), dim3(512), nat, stream, p, (__half *)a.workspace);
     }
-    const int     MT = row_tiles_of(a.M);
-    p.row_tiles = (uint32_t)((a.M + 16 * MT - 1) / (16 * MT));
-    const int64_t groups = (a.N + 15) / 16 * p.row_tiles;
-    const bool    gated = a.w[1].q4 != nullptr;
-#define ATOM_W4A16(MT, GATED) hipLaunchKernelGGL((w4a16_kernel<MT, GATED>), dim3((unsigned)groups), dim3(kThreads), 0, stream, p)
+#define ATOM_W4A16(...)                                                                        \
+    do {                                                                                       \
+        static atom_launch::LdsOptIn opt;                                                      \
+        auto kern = &w4a16_kernel<__VA_ARGS__>;                                                \
+        if (s.lds > 60 * 1024) {                                                               \
+            const hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(kern), s.lds); \
+            if (err != hipSuccess) return err;                                                 \
+        }                                                                                      \
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), s.lds, stream, p);                \
+        return hipGetLastError();                                                              \
+    } while (0)
+    const bool twice = norm && !s.combine;
+    if (s.kept) {
+        if (gated) ATOM_W4A16(1, true, 1, 1, 3, true);
+        else       ATOM_W4A16(1, false, 1, 1, 4, true);
+    }
+#define ATOM_ROWS(NT, GATED, RT, CH)                                 \
+    do {                                                             \
+        if (twice) ATOM_W4A16(NT, GATED, RT, 2, CH, false);          \
+        else       ATOM_W4A16(NT, GATED, RT, 1, CH, false);          \
+    } while (0)
     if (gated) {
-        if (MT == 1)      ATOM_W4A16(1, true);
-        else if (MT == 2) ATOM_W4A16(2, true);
-        else              ATOM_W4A16(4, true);
-    } else {
-        if (MT == 1)      ATOM_W4A16(1, false);
-        else if (MT == 2) ATOM_W4A16(2, false);
-        else              ATOM_W4A16(4, false);
+        if (s.RT == 4) ATOM_ROWS(1, true, 4, 1);
+        if (s.RT == 2) ATOM_ROWS(1, true, 2, 1);
+        if (s.NT == 2) ATOM_ROWS(2, true, 1, 2);
+        ATOM_ROWS(1, true, 1, 2);
     }
+    if (s.RT == 4) ATOM_ROWS(1, false, 4, 1);
+    if (s.RT == 2) ATOM_ROWS(1, false, 2, 1);
+    if (s.NT == 4) ATOM_ROWS(4, false, 1, 2);
+    if (s.NT == 2) ATOM_ROWS(2, false, 1, 2);
+    ATOM_ROWS(1, false, 1, 2);
+#undef ATOM_ROWS
 #undef ATOM_W4A16
-    return hipGetLastError();
 }
 
 }  // namespace atom_internal

@@ -36,9 +36,9 @@ def activations(x, gamma, eps, idx):
     off = np.zeros_like(x)
     if gamma is not None:
         x = x / np.sqrt((x * x).mean(1, keepdims=True) + eps) * gamma.astype(np.float64)
-        # rounded to fp16 (2^-11 of itself, 2^-25 below the normal numbers); before that the sum of squares in fp32, K additions at most
-        # (half of their error in the root), and five more roundings
-        off = (2.0 ** -11 + (x.shape[1] / 2 + 8) * 2.0 ** -24) * np.abs(x) + 2.0 ** -25
+        # two halves (2^-22 of itself, 2^-25 below the normal numbers); before that the sum of squares in fp32, at most K / 256 + 24 additions
+        # behind one another (half of their error in the root), and five more roundings
+        off = (2.0 ** -22 + (x.shape[1] / 512 + 17) * 2.0 ** -24) * np.abs(x) + 2.0 ** -25
     return (x, off) if idx is None else (x[:, idx], off[:, idx])
 
 

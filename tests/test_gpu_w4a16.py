@@ -124,6 +124,18 @@ def test_rows_keep_to_themselves(M, norm):
     close(torch.where(torch.from_numpy(sure).cuda(), got, 0.0), np.where(sure, want, 0), np.where(sure, tol, np.inf))
 
 
+@pytest.mark.parametrize("M", [2, 20, 60])
+def test_numbers_below_the_normal_ones_count(M):
+    """fp16's smallest numbers times large scales: nothing is flushed on the way."""
+    N, K = 33, 384
+    x, _, idx, (w,), rng = case(M, N, K)
+    x = (rng.integers(-40, 41, (M, K)) * 2.0 ** -24).astype(np.float16)
+    w = (w[0], w[1], np.full_like(w[2], 2048))
+    want, tol = ref.linear(x, None, 0.0, idx, w)
+    assert np.abs(want).mean() > 0.05
+    close(atom.atom_w4a16_linear(gpu(x), None, 0.0, gpu(idx), *gpu(w)), want, tol)
+
+
 def test_gate_far_from_zero():
     """silu of very negative gates is 0 (or below fp16), of very positive ones the gate itself."""
     M, N, K = 2, 32, 256
