@@ -26,6 +26,7 @@ using atom_internal::W4;
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float    f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
@@ -65,15 +66,42 @@ struct Args {
     __half *y; int64_t ldy;
     const __half *staged; int rows;                          // laid out, `rows` rows of hi and behind them those of lo
     bool combine;                                            // lo in rows 8 .. 15 of the one tile
-    uint32_t tiles, row_tiles;
+    uint32_t tiles;
+    // the kernel of many rows: tiles of 32 rows in a block, halves of the activations, parts of K and their sums
+    int wide, halves, parts; uint32_t row_blocks; float *sums;
 };
 
 // ---- the activations as the product takes them
 
-// Row x in reordered order, behind the norm where there is gamma, laid out for the product (lo: null where there is no
-// norm).  nat: K words of LDS (halves without norm, none without an index either); all threads of the workgroup call.
+// Where the eight channels from k on lie in a row that is laid out for the kernel of few rows, in blocks of eight.  Of an INT4 group chunk c of
+// the instructions has channels 32 c .. 32 c + 31, eight an instruction; of 64 INT8 channels 16 c .. 16 c + 15.
+__device__ __forceinline__ int row_place(int k, int K4)
+{
+    const int g = k >> 7, j = (k >> 3) & 15;
+    return 16 * g + (k < K4 ? 4 * (j & 3) + (j >> 2) : (j & 8) + 4 * (j & 1) + ((j >> 1) & 3));
+}
+
+// What a thread reads of a row first, so that it is on its way before anything waits.
+struct Front { uint4 x, gamma; int4 i0, i1; };
+
 template <int THREADS>
-__device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict__ x, uint32_t *nat, float *s_sum, __half *hi, __half *lo)
+__device__ __forceinline__ Front front_of(const Args &p, const __half *__restrict__ x)
+{
+    Front f = {};
+    const int b = min((int)threadIdx.x, p.K / 8 - 1);
+    f.x = reinterpret_cast<const uint4 *>(x)[b];
+    if (p.gamma) f.gamma = reinterpret_cast<const uint4 *>(p.gamma)[b];
+    if (p.idx) {
+        f.i0 = reinterpret_cast<const int4 *>(p.idx)[2 * b];
+        f.i1 = reinterpret_cast<const int4 *>(p.idx)[2 * b + 1];
+    }
+    return f;
+}
+
+// Row x in reordered order, behind the norm where there is gamma, laid out for the product: eight channels from k on go to
+// place(k), hi and lo apart (lo only behind a norm).  nat: LDS of natural_bytes(); all threads of the workgroup call.
+template <int THREADS, class Place>
+__device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict__ x, const Front &f, uint32_t *nat, float *s_sum, Place place)
 {
     const int tid = threadIdx.x, blocks = p.K / 8, K4 = p.K - p.O;
     const uint4 *row = reinterpret_cast<const uint4 *>(x);
@@ -82,7 +110,7 @@ __device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict_
     if (p.gamma) {
         float sum = 0.0f;
         for (int b = tid; b < blocks; b += THREADS) {
-            const uint4 v = row[b];
+            const uint4 v = b == tid ? f.x : row[b];
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = fmaf(value(half_of(v, i)), value(half_of(v, i)), sum);
         }
@@ -94,7 +122,7 @@ __device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict_
         for (int w = 0; w < THREADS / 64; ++w) sum += s_sum[w];
         const float r = 1.0f / sqrtf(sum / (float)p.K + p.eps);
         for (int b = tid; b < blocks; b += THREADS) {
-            const uint4 v = row[b], g = reinterpret_cast<const uint4 *>(p.gamma)[b];
+            const uint4 v = b == tid ? f.x : row[b], g = b == tid ? f.gamma : reinterpret_cast<const uint4 *>(p.gamma)[b];
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -109,14 +137,13 @@ __device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict_
         }
         __syncthreads();
     } else if (p.idx) {
-        for (int b = tid; b < blocks; b += THREADS) reinterpret_cast<uint4 *>(nat)[b] = row[b];
+        for (int b = tid; b < blocks; b += THREADS) reinterpret_cast<uint4 *>(nat)[b] = b == tid ? f.x : row[b];
         __syncthreads();
     }
     for (int b = tid; b < blocks; b += THREADS) {
-        const int g = b >> 4, k = g * 128 + (b & 3) * 32 + ((b >> 2) & 3) * 8;        // the eight channels of place b
         uint32_t w[8];
         if (p.idx) {
-            const int4 i0 = *reinterpret_cast<const int4 *>(p.idx + k), i1 = *reinterpret_cast<const int4 *>(p.idx + k + 4);
+            const int4 i0 = b == tid ? f.i0 : reinterpret_cast<const int4 *>(p.idx)[2 * b], i1 = b == tid ? f.i1 : reinterpret_cast<const int4 *>(p.idx)[2 * b + 1];
             const int32_t at[8] = {i0.x, i0.y, i0.z, i0.w, i1.x, i1.y, i1.z, i1.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -124,172 +151,181 @@ __device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict_
                 w[i] = p.gamma ? nat[c] : reinterpret_cast<const uint16_t *>(nat)[c];
             }
         } else if (p.gamma) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = nat[k + i];
+            const uint4 u = reinterpret_cast<const uint4 *>(nat)[2 * b], v = reinterpret_cast<const uint4 *>(nat)[2 * b + 1];
+            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w, w[4] = v.x, w[5] = v.y, w[6] = v.z, w[7] = v.w;
         } else {
-            const uint4 v = row[k / 8];
+            const uint4 v = b == tid ? f.x : row[b];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = half_of(v, i);
         }
-        if (k < K4) {
+        if (8 * b < K4) {
             const uint32_t t1 = w[1], t2 = w[2], t3 = w[3];                           // 0 4 1 5 2 6 3 7
-            w[1] = w[4];
-            w[2] = t1;
-            w[3] = w[5];
-            w[4] = t2;
-            w[5] = w[6];
-            w[6] = t3;
+            w[1] = w[4], w[2] = t1, w[3] = w[5], w[4] = t2, w[5] = w[6], w[6] = t3;
         }
         auto pack = [&](uint32_t sel) {
             return make_uint4(__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel), __builtin_amdgcn_perm(w[5], w[4], sel),
                               __builtin_amdgcn_perm(w[7], w[6], sel));
         };
-        *reinterpret_cast<uint4 *>(hi + 8 * b) = pack(0x05040100u);
-        if (lo) *reinterpret_cast<uint4 *>(lo + 8 * b) = pack(0x07060302u);
+        place(8 * b, 0, pack(0x05040100u));
+        if (p.gamma) place(8 * b, 1, pack(0x07060302u));
     }
 }
 
 __host__ __device__ constexpr size_t natural_bytes(int K, bool norm, bool index) { return norm ? 4 * (size_t)K : index ? 2 * (size_t)K : 0; }
 
-// A row to a workgroup, into the workspace.
+// A row to a workgroup, into the workspace: rows of hi and behind them those of lo, or (WIDE) the tiles of the kernel of many rows.
+template <bool WIDE>
 __global__ __launch_bounds__(512)
-void w4a16_rows_kernel(Args p, __half *out)
+void w4a16_rows_kernel(Args p, uint4 *out)
 {
     extern __shared__ uint32_t s_nat[];
     __shared__ float s_sum[8];
-    lay_out<512>(p, p.x + (int64_t)blockIdx.x * p.ldx, s_nat, s_sum, out + (int64_t)blockIdx.x * p.K,
-                 p.gamma ? out + ((int64_t)p.M + blockIdx.x) * p.K : nullptr);
+    const int64_t m = blockIdx.x;
+    const int K4 = p.K - p.O, G4 = K4 >> 7, U = (p.K + p.O) >> 7;
+    const __half *x = p.x + m * p.ldx;
+    lay_out<512>(p, x, front_of<512>(p, x), s_nat, s_sum, [&](int k, int half, const uint4 &v) {
+        if constexpr (!WIDE) out[(m + half * p.M) * (p.K / 8) + row_place(k, K4)] = v;
+        else {
+            const bool is4 = k < K4;
+            const int  j = k - K4, u = is4 ? k >> 7 : G4 + (j >> 6), i = is4 ? (k >> 3) & 7 : (j >> 3) & 3, c = is4 ? (k >> 6) & 1 : (j >> 5) & 1;
+            const int64_t block = m / (32 * p.wide), t = m / 32 % p.wide;
+            out[((((block * U + u) * p.halves + half) * p.wide + t) * 8 + i) * 64 + c * 32 + m % 32] = v;
+        }
+    });
 }
 
 // ---- the product
 
-// A workgroup has 16 NT output channels (of gate and of up) and 16 RT rows; its eight wavefronts share the groups, and their sums
-// meet in LDS, added in order.  A wavefront has a run of INT4 groups and every eighth INT8 group; CH of them are on their way while it
-// works, across the tiles that the workgroup has in turn.
+#define ATOM_INLINE __attribute__((always_inline))      // of lambdas that registers go through: one that is called in many places is not inlined by itself
+
+__device__ __forceinline__ float gated(float gate, float up) { return gate / (1.0f + expf(-gate)) * up; }
+
+template <bool GATED>
+__device__ __forceinline__ void store(const Args &p, int64_t m, int64_t n, float y, float up)
+{
+    if constexpr (GATED) y = gated(y, up);
+    else if (p.residual) y += __half2float(p.residual[m * p.ldr + n]);
+    p.y[m * p.ldy + n] = __float2half_rn(y);
+}
+
+// Up to 16 rows.  A workgroup has 16 NT output channels (of gate and of up); its eight wavefronts share the K channels in runs of units, and their
+// sums meet in LDS, added in order.  A unit is 64 bytes of every weight row: an INT4 group, or half of an INT8 group.  CH units of a
+// wavefront are on their way while it works, across the tiles that the workgroup has in turn; every unit takes the same loads, also those
+// behind the last (one address for all lanes then), so that none is waited for before its turn.
 //   HL: halves of the activations that go in one after the other (2: hi and lo)
-//   KEPT: the activations are laid out in LDS by the workgroup itself (RT = HL = 1), under way with the first weights
-template <int NT, bool GATED, int RT, int HL, int CH, bool KEPT>
+//   KEPT: the activations are laid out in LDS by the workgroup itself (HL = 1), under way with the first weights
+template <int NT, bool GATED, int HL, int CH, bool KEPT>
 __global__ __launch_bounds__(kThreads, KEPT ? 4 : 2)
 void w4a16_kernel(Args p)
 {
-    constexpr int WM = GATED ? 2 : 1, CT = WM * NT, AT = KEPT ? 1 : RT * HL;
+    constexpr int WM = GATED ? 2 : 1, CT = WM * NT, AT = HL;
     static_assert(CT <= 4, "a lane's chunk loads the scales of one tile");
     extern __shared__ __align__(16) unsigned char s_all[];   // KEPT: the rows, then the sums or what is laid out; else the sums
     __shared__ float s_part[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, kc = lane >> 4;
-    const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, G8 = G - G4;
-    const int begin = (int)((int64_t)wave * G4 / kWaves), n4 = (int)((int64_t)(wave + 1) * G4 / kWaves) - begin;
-    const int n = n4 + (G8 > wave ? (G8 - wave + kWaves - 1) / kWaves : 0);           // elements of this wavefront
+    const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, U = 2 * G - G4;
+    const int begin = wave * U / kWaves, end = (wave + 1) * U / kWaves;
+    const int rows = p.rows, lds_row = p.K + 8;
+
+    Front front;
+    if constexpr (KEPT) front = front_of<kThreads>(p, p.x);
 
     // (rows >= M are computed and never stored, columns >= N likewise)
-    const uint32_t row_tile = blockIdx.x % p.row_tiles, first = blockIdx.x / p.row_tiles, stride = gridDim.x / p.row_tiles;
-    const int64_t m0 = (int64_t)row_tile * (16 * RT);
-    const int rows = p.rows, lds_row = p.K + 8;
-    const __half *act[AT];
-    const __half *s_act = nullptr;
-    if constexpr (KEPT) {
-        const int r = p.combine && col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1);
-        s_act = reinterpret_cast<const __half *>(s_all) + (size_t)r * lds_row + kc * 8;
-    } else {
-#pragma unroll
-        for (int t = 0; t < AT; ++t) {
-            const int64_t m = p.combine ? (col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1))
-                                        : min(m0 + 16 * (t % RT) + col, (int64_t)rows - 1) + (t / RT) * (int64_t)rows;
-            act[t] = p.staged + m * p.K + kc * 8;
-        }
-    }
+    const int r = p.combine && col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1);
+    const __half *act = KEPT ? reinterpret_cast<const __half *>(s_all) + (size_t)r * lds_row + kc * 8 : p.staged + (int64_t)r * p.K + kc * 8;
+    const int64_t to_lo = (int64_t)rows * p.K;
     float *red = reinterpret_cast<float *>(s_all + (KEPT ? (size_t)rows * (p.gamma ? 2 : 1) * lds_row * 2 : 0));
 
-    struct Element { uint4 q[CT], q1[CT]; uint16_t scale; uint4 a[AT][4]; };
-    Element ring[CH];
-    // the element that is loaded next
-    uint32_t load_tile = first;
-    int load_i = 0;
-    int64_t row4[CT], row8[CT], row_s;
-    auto rows_of = [&](uint32_t tile) {
+    struct Unit { uint4 q[CT]; uint16_t scale; uint4 a[KEPT ? 1 : AT][4]; };
+    Unit ring[CH];
+    uint32_t load_tile = blockIdx.x;                         // of the unit that is loaded next
+    int load_u = begin;
+    uint32_t at4[CT], at8[CT], at_s;                         // bytes from the arrays' beginnings (below 4 GiB: host)
+    auto rows_of = [&](uint32_t tile) ATOM_INLINE {
+        const bool live = tile < p.tiles;
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            const int64_t r = min((int64_t)tile * (16 * NT) + 16 * (t % NT) + col, p.N - 1);
-            row4[t] = r * (K4 >> 1) + kc * 16;
-            row8[t] = r * p.O + kc * 32;
+            const uint32_t row = (uint32_t)min((int64_t)tile * (16 * NT) + 16 * (t % NT) + col, p.N - 1);
+            at4[t] = live ? row * (uint32_t)(K4 >> 1) + kc * 16 : 0;
+            at8[t] = live ? row * (uint32_t)p.O + kc * 16 : 0;
         }
-        row_s = min((int64_t)tile * (16 * NT) + 16 * ((kc % CT) % NT) + col, p.N - 1) * G;
+        at_s = live ? (uint32_t)min((int64_t)tile * (16 * NT) + 16 * ((kc % CT) % NT) + col, p.N - 1) * (uint32_t)(2 * G) : 0;
     };
-    auto load = [&](Element &e) {
-        if (load_tile >= p.tiles) return;
-        const bool is4 = load_i < n4;
-        const int  g = is4 ? begin + load_i : wave + kWaves * (load_i - n4);          // of the INT4 or of the INT8 groups
+    const uint8_t *my_scale = reinterpret_cast<const uint8_t *>(CT > 1 && (kc % CT) / NT ? p.w[WM - 1].scale : p.w[0].scale);
+    auto load = [&](Unit &e) ATOM_INLINE {
+        const bool is4 = load_u < G4;
+        const int  v = load_u - G4, k = is4 ? load_u * 128 : K4 + v * 64;
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
             const W4 &w = p.w[t / NT];
-            const uint8_t *at = is4 ? w.q4 + row4[t] + g * 64 : reinterpret_cast<const uint8_t *>(w.q8) + row8[t] + g * 128;
-            e.q[t] = *reinterpret_cast<const uint4 *>(at);
-            if (!is4) e.q1[t] = *reinterpret_cast<const uint4 *>(at + 16);
+            const uint8_t *base = is4 ? w.q4 + load_u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64;
+            e.q[t] = *reinterpret_cast<const uint4 *>(base + (is4 ? at4[t] : at8[t]));
         }
-        const int k = is4 ? g : G4 + g;
-        e.scale = (CT > 1 && (kc % CT) / NT ? p.w[WM - 1] : p.w[0]).scale[row_s + k];
+        e.scale = *reinterpret_cast<const uint16_t *>(my_scale + at_s + 2 * (k >> 7));
         if constexpr (!KEPT) {
 #pragma unroll
-            for (int t = 0; t < AT; ++t)
+            for (int a = 0; a < AT; ++a)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) e.a[t][c] = *reinterpret_cast<const uint4 *>(act[t] + k * 128 + c * 32);
+                for (int c = 0; c < 4; ++c)
+                    e.a[a][c] = *reinterpret_cast<const uint4 *>(act + a * to_lo + k + (is4 ? c : c & 1) * 32);
         }
-        if (++load_i == n) {
-            load_i = 0;
-            load_tile += stride;
+        if (++load_u == end) {
+            load_u = begin;
+            load_tile += gridDim.x;
             rows_of(load_tile);
         }
     };
-    f4 acc[CT][RT] = {};
-    auto compute = [&](const Element &e, int i) {
-        const bool is4 = i < n4;
-        const int  k = is4 ? begin + i : G4 + wave + kWaves * (i - n4);
-        f4 part[CT][RT] = {};
+    f4 acc[CT] = {};
+    auto compute = [&](const Unit &e, int u) ATOM_INLINE {
+        f4 part[CT] = {};
+        auto activations = [&](int a, int k, int c) ATOM_INLINE {
+            if constexpr (KEPT) return *reinterpret_cast<const h8 *>(act + k + c * 32);
+            else return __builtin_bit_cast(h8, e.a[a][c]);
+        };
+        if (u < G4) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            h8 w[CT];
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int t = 0; t < CT; ++t) {
-                if (is4) w[t] = widen4(c == 0 ? e.q[t].x : c == 1 ? e.q[t].y : c == 2 ? e.q[t].z : e.q[t].w);
-                else     w[t] = c == 0 ? widen8(e.q[t].x, e.q[t].y) : c == 1 ? widen8(e.q[t].z, e.q[t].w) : c == 2 ? widen8(e.q1[t].x, e.q1[t].y) : widen8(e.q1[t].z, e.q1[t].w);
-            }
+                for (int t = 0; t < CT; ++t) {
+                    const h8 w = widen4(c == 0 ? e.q[t].x : c == 1 ? e.q[t].y : c == 2 ? e.q[t].z : e.q[t].w);
 #pragma unroll
-            for (int a = 0; a < AT; ++a) {
-                h8 x;
-                if constexpr (KEPT) x = *reinterpret_cast<const h8 *>(s_act + k * 128 + c * 32);
-                else x = __builtin_bit_cast(h8, e.a[a][c]);
+                    for (int a = 0; a < AT; ++a) part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(activations(a, u * 128, c), w, part[t], 0, 0, 0);
+                }
+        } else {
 #pragma unroll
-                for (int t = 0; t < CT; ++t) part[t][a % RT] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w[t], part[t][a % RT], 0, 0, 0);
-            }
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int t = 0; t < CT; ++t) {
+                    const h8 w = c == 0 ? widen8(e.q[t].x, e.q[t].y) : widen8(e.q[t].z, e.q[t].w);
+#pragma unroll
+                    for (int a = 0; a < AT; ++a)
+                        part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(activations(a, K4 + (u - G4) * 64, c), w, part[t], 0, 0, 0);
+                }
         }
         const float mine = __half2float(__ushort_as_half(e.scale));
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
             const float s = CT == 1 ? mine : __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * (16 * t + col), __builtin_bit_cast(int, mine)));
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[t][r][j] = fmaf(part[t][r][j], s, acc[t][r][j]);
+            for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(part[t][j], s, acc[t][j]);
         }
     };
     int buffer = 0;
-    auto finish = [&](uint32_t tile) {
-        float *mine = red + (size_t)buffer * (kWaves * CT * RT * 256);
+    auto finish = [&](uint32_t tile) ATOM_INLINE {
+        float *mine = red + (size_t)buffer * (kWaves * CT * 256);
         buffer ^= 1;                                         // (nobody writes a buffer before all have read what it held two tiles ago)
 #pragma unroll
         for (int t = 0; t < CT; ++t)
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    mine[((wave * CT + t) * RT + r) * 256 + j * 64 + lane] = acc[t][r][j];
-                    acc[t][r][j] = 0.0f;
-                }
+            for (int j = 0; j < 4; ++j) {
+                mine[(wave * CT + t) * 256 + j * 64 + lane] = acc[t][j];
+                acc[t][j] = 0.0f;
+            }
         __syncthreads();
-        for (int at = tid; at < NT * RT * 256; at += kThreads) {
-            const int l = at & 63, j = (at >> 6) & 3, r = (at >> 8) % RT, t = (at >> 8) / RT;
-            const int64_t m = m0 + 16 * r + 4 * (l >> 4) + j, out = (int64_t)tile * (16 * NT) + 16 * t + (l & 15);
+        for (int at = tid; at < NT * 256; at += kThreads) {
+            const int l = at & 63, j = (at >> 6) & 3, t = at >> 8;
+            const int64_t m = 4 * (l >> 4) + j, out = (int64_t)tile * (16 * NT) + 16 * t + (l & 15);
             if (m >= p.M || out >= p.N) continue;
             float sum[WM];
 #pragma unroll
@@ -298,21 +334,18 @@ void w4a16_kernel(Args p)
                 sum[i] = 0.0f;
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) {
-                    const float *s = mine + ((w * CT + i * NT + t) * RT + r) * 256 + j * 64 + l;
+                    const float *s = mine + (w * CT + i * NT + t) * 256 + j * 64 + l;
                     sum[i] += s[0];
                     if (p.combine) lo += s[32];
                 }
                 sum[i] += lo;
             }
-            float y = sum[0];
-            if constexpr (GATED) y = y / (1.0f + expf(-y)) * sum[WM - 1];
-            else if (p.residual) y += __half2float(p.residual[m * p.ldr + out]);
-            p.y[m * p.ldy + out] = __float2half_rn(y);
+            store<GATED>(p, m, out, sum[0], sum[WM - 1]);
         }
     };
 
-    rows_of(first);
-    if (n > 0) {
+    rows_of(load_tile);
+    if (begin < end) {
 #pragma unroll
         for (int s = 0; s < CH; ++s) load(ring[s]);
     }
@@ -320,44 +353,231 @@ void w4a16_kernel(Args p)
         uint32_t *nat = reinterpret_cast<uint32_t *>(red);
         __half *out = reinterpret_cast<__half *>(s_all);
         for (int m = 0; m < rows; ++m) {
-            if (m) __syncthreads();
-            lay_out<kThreads>(p, p.x + m * p.ldx, nat, s_part, out + (size_t)m * lds_row, p.gamma ? out + (size_t)(rows + m) * lds_row : nullptr);
+            if (m) {
+                __syncthreads();
+                front.x = front_of<kThreads>(p, p.x + m * p.ldx).x;
+            }
+            lay_out<kThreads>(p, p.x + m * p.ldx, front, nat, s_part,
+                              [&](int k, int half, const uint4 &v) { *reinterpret_cast<uint4 *>(out + (size_t)(m + half * rows) * lds_row + 8 * row_place(k, K4)) = v; });
         }
         __syncthreads();
     }
-    if (n == 0) {
-        for (uint32_t tile = first; tile < p.tiles; tile += stride) finish(tile);
+    uint32_t tile = blockIdx.x;
+    if (begin == end) {
+        for (; tile < p.tiles; tile += gridDim.x) finish(tile);
         return;
     }
-    uint32_t tile = first;
-    for (int i = 0;;) {
+    for (int u = begin;;) {
 #pragma unroll
         for (int s = 0; s < CH; ++s) {
-            compute(ring[s], i);
+            compute(ring[s], u);
             load(ring[s]);
-            if (++i == n) {
-                i = 0;
+            if (++u == end) {
+                u = begin;
                 finish(tile);
-                tile += stride;
+                tile += gridDim.x;
                 if (tile >= p.tiles) return;
             }
         }
     }
 }
 
+typedef float f16 __attribute__((ext_vector_type(16)));
+
+// More than 16 rows: MFMA 32x32x16, whose operands bring twice the products for their bytes (lane l: row or column l & 31, the eight values
+// of k-chunk l >> 5; register r of the result: row 8 (r / 4) + 4 (l >> 5) + r % 4).  A workgroup has 32 RT rows; each of its four wavefronts
+// has two tiles of 32 weight rows (gate and up, or two of the one) for itself, and all of them share the activations, which come a
+// unit at a time through LDS.  `parts` workgroups share a tile's units where the tiles alone do not fill the card; their sums meet in the workspace.
+template <bool GATED, int RT, int HL, int CH>
+__global__ __launch_bounds__(256, 1)
+void w4a16_wide_kernel(Args p)
+{
+    constexpr int kChunks = RT * HL * 2;                     // 16-byte pieces of a unit's activations a thread brings
+    __shared__ __align__(16) u4 s_act[2][RT * HL * 8 * 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, kc = lane >> 5;
+    const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, U = 2 * G - G4;
+    const uint32_t block = blockIdx.x % p.row_blocks, rest = blockIdx.x / p.row_blocks, part = rest % (uint32_t)p.parts, tile = rest / (uint32_t)p.parts;
+    const int begin = (int)((int64_t)part * U / p.parts), end = (int)((int64_t)(part + 1) * U / p.parts);
+
+    // weight rows of this lane (columns >= N are computed and never stored)
+    int64_t n[2];
+    uint32_t at4[2], at8[2], at_s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        n[t] = GATED ? ((int64_t)tile * 4 + wave) * 32 + col : (((int64_t)tile * 4 + wave) * 2 + t) * 32 + col;
+        const uint32_t row = (uint32_t)min(n[t], p.N - 1);
+        at4[t] = row * (uint32_t)(K4 >> 1) + kc * 32;
+        at8[t] = row * (uint32_t)p.O + kc * 32;
+        at_s[t] = row * (uint32_t)(2 * G);
+    }
+    struct Unit { uint4 q[2][2]; uint16_t scale[2]; };
+    Unit ring[CH];
+    int load_u = begin;
+    auto load = [&](Unit &e) ATOM_INLINE {
+        const int  u = min(load_u, end - 1), v = u - G4;
+        const bool is4 = u < G4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const W4 &w = p.w[GATED ? t : 0];
+            const uint8_t *at = (is4 ? w.q4 + u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64) + (is4 ? at4[t] : at8[t]);
+            e.q[t][0] = *reinterpret_cast<const uint4 *>(at);
+            e.q[t][1] = *reinterpret_cast<const uint4 *>(at + 16);
+            e.scale[t] = *reinterpret_cast<const uint16_t *>(reinterpret_cast<const uint8_t *>(w.scale) + at_s[t] + 2 * (is4 ? u : G4 + (v >> 1)));
+        }
+        ++load_u;
+    };
+    const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + (int64_t)block * U * (RT * HL * 512) + tid;
+    u4 next[kChunks];
+    auto fetch = [&](int u) ATOM_INLINE {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) next[c] = acts[(int64_t)min(u, end - 1) * (RT * HL * 512) + c * 256];
+    };
+    auto keep = [&](int u) ATOM_INLINE {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) s_act[(u - begin) & 1][c * 256 + tid] = next[c];
+    };
+
+    f16 acc[2][RT] = {};
+    auto compute = [&](const Unit &e, int u) ATOM_INLINE {
+        const u4 *a = s_act[(u - begin) & 1] + lane;
+        f16 sum[2][RT] = {};
+        auto word = [&](int t, int i) { const uint4 &q = e.q[t][i >> 2]; return (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w; };
+        auto products = [&](int i, const h8 (&w)[2]) ATOM_INLINE {
+#pragma unroll
+            for (int h = 0; h < HL; ++h)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const h8 x = __builtin_bit_cast(h8, a[((h * RT + r) * 8 + i) * 64]);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) sum[t][r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, w[t], sum[t][r], 0, 0, 0);
+                }
+        };
+        if (u < G4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const h8 w[2] = {widen4(word(0, i)), widen4(word(1, i))};
+                products(i, w);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const h8 w[2] = {widen8(word(0, 2 * i), word(0, 2 * i + 1)), widen8(word(1, 2 * i), word(1, 2 * i + 1))};
+                products(i, w);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const float s = __half2float(__ushort_as_half(e.scale[t]));
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[t][r][j] = fmaf(sum[t][r][j], s, acc[t][r][j]);
+        }
+    };
+
+    fetch(begin);
+#pragma unroll
+    for (int s = 0; s < CH; ++s) load(ring[s]);
+    keep(begin);
+    fetch(begin + 1);
+    __syncthreads();
+    for (int u = begin; u < end; u += CH)
+#pragma unroll
+        for (int s = 0; s < CH; ++s) {
+            if (u + s >= end) break;                         // (the same for all)
+            keep(u + s + 1);
+            fetch(u + s + 2);
+            compute(ring[s], u + s);
+            load(ring[s]);
+            __syncthreads();                                 // (all have read this unit's activations, the next one's are there)
+        }
+
+    const int64_t m0 = (int64_t)block * (32 * RT) + 4 * kc;
+    auto row_of = [&](int r, int j) ATOM_INLINE { return m0 + 32 * r + 8 * (j >> 2) + (j & 3); };
+    if (p.parts > 1) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            if (n[t] < p.N)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (row_of(r, j) < p.M) p.sums[(((int64_t)part * (GATED ? 2 : 1) + (GATED ? t : 0)) * p.M + row_of(r, j)) * p.N + n[t]] = acc[t][r][j];
+        return;
+    }
+    if constexpr (GATED) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (row_of(r, j) < p.M && n[0] < p.N) p.y[row_of(r, j) * p.ldy + n[0]] = __float2half_rn(gated(acc[0][r][j], acc[1][r][j]));
+    } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if (p.residual)                                  // (all of them on their way at once)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    uint16_t res[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) res[j] = reinterpret_cast<const uint16_t *>(p.residual)[min(row_of(r, j), p.M - 1) * p.ldr + min(n[t], p.N - 1)];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[t][r][j] += __half2float(__ushort_as_half(res[j]));
+                }
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (row_of(r, j) < p.M && n[t] < p.N) p.y[row_of(r, j) * p.ldy + n[t]] = __float2half_rn(acc[t][r][j]);
+        }
+    }
+}
+
+// The parts' sums, in their order.
+template <bool GATED>
+__global__ __launch_bounds__(256)
+void w4a16_join_kernel(Args p)
+{
+    const int64_t outputs = p.M * p.N, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= outputs) return;
+    float y = 0.0f, up = 0.0f;
+    for (int s = 0; s < p.parts; ++s) {
+        y += p.sums[s * (GATED ? 2 : 1) * outputs + e];
+        if constexpr (GATED) up += p.sums[(2 * s + 1) * outputs + e];
+    }
+    const int64_t m = e / p.N;
+    store<GATED>(p, m, e - m * p.N, y, up);
+}
+
 }  // namespace
 
 namespace atom_internal {
 
-// How a call runs: whether the workgroups lay the activations out themselves, column and row tiles, LDS.
-struct ProductShape { bool kept, combine; int NT, RT; size_t lds; };
+// How a call runs.  Up to 16 rows: whether the workgroups lay the activations out themselves, tiles of 16 channels, LDS.  More: tiles of
+// 32 rows in a block, parts of K.
+struct ProductShape { bool kept, combine; int NT; size_t lds; int wide, parts; };
 
-static ProductShape product_shape(int64_t M, int64_t N, int K, bool gated, bool norm, bool index)
+static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index)
 {
     const int WM = gated ? 2 : 1;
     ProductShape s = {};
+    if (M > 16) {
+        s.wide = M <= 32 ? 1 : 2;
+        const int U = (K + O) / 128;
+        const int64_t tiles = (N + (gated ? 127 : 255)) / (gated ? 128 : 256) * ((M + 32 * s.wide - 1) / (32 * s.wide)), cus = 256;
+        // rounds of workgroups, each as long as its units; a join costs about two units and what it moves
+        double best = 1e30;
+        for (int parts = 1; parts <= 16 && parts * 4 <= U; ++parts) {
+            const double cost = (double)((tiles * parts + cus - 1) / cus) * ((U + parts - 1) / parts + 3) + (parts > 1 ? 4 + (double)parts * M * N * WM * 8 / 5e6 : 0);
+            if (cost < best) {
+                best = cost;
+                s.parts = parts;
+            }
+        }
+        if (!s.parts) s.parts = 1;
+        return s;
+    }
     s.NT = 1;
-    s.RT = M <= 16 ? 1 : M <= 32 ? 2 : 4;
     s.combine = norm && M <= 8;
     const size_t sums = (size_t)2 * kWaves * WM * 1024, nat = natural_bytes(K, norm, index), rest = nat > sums ? nat : sums;
     if (M <= (norm ? 8 : 16)) {
@@ -365,79 +585,118 @@ static ProductShape product_shape(int64_t M, int64_t N, int K, bool gated, bool 
         s.kept = s.lds <= 80 * 1024;
     }
     if (!s.kept) {
-        while (M <= 16 && s.NT * WM < 4 && (N + 32 * s.NT - 1) / (32 * s.NT) >= 192) s.NT *= 2;
-        s.lds = (size_t)2 * kWaves * WM * s.NT * s.RT * 1024;
+        while (s.NT * WM < 4 && (N + 32 * s.NT - 1) / (32 * s.NT) >= 192) s.NT *= 2;
+        s.lds = (size_t)2 * kWaves * WM * s.NT * 1024;
     }
     return s;
 }
 
+static size_t laid_out_bytes(const ProductShape &s, int64_t M, int K, int O, bool norm)
+{
+    if (s.kept) return 0;
+    if (!s.wide) return (size_t)M * K * (norm ? 4 : 2);
+    return (size_t)((M + 32 * s.wide - 1) / (32 * s.wide)) * ((K + O) / 128) * s.wide * (norm ? 2 : 1) * 8192;
+}
+
 size_t w4a16_workspace_bytes(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index)
 {
-    (void)O;
-    return product_shape(M, N, K, gated, norm, index).kept ? 0 : (size_t)M * K * (norm ? 4 : 2);
+    const ProductShape s = product_shape(M, N, K, O, gated, norm, index);
+    return laid_out_bytes(s, M, K, O, norm) + (s.parts > 1 ? (size_t)s.parts * M * N * (gated ? 8 : 4) : 0);
 }
 
 bool w4a16_fits(int64_t M, int64_t N, int K, int O, bool gated)
 {
-    (void)K, (void)O, (void)gated;
+    (void)gated;
     if (M == 0 || N == 0) return true;
-    const int64_t rows = (M + 63) / 64, tiles = (N + 15) / 16, most = atom_launch::kMostThreads / kThreads;
-    return rows <= most && tiles <= most / rows && M <= most;
+    const int64_t G = K / 128, widest = (K - O) / 2 > O ? (K - O) / 2 : O;
+    if (N > 0xffffffffLL / (widest > 2 * G ? widest : 2 * G)) return false;           // 32-bit offsets
+    // workgroups: a row each, tiles of outputs (of 128 at least where there are many rows) and rows, 256 outputs of a join each
+    const int64_t most = atom_launch::kMostThreads / kThreads;
+    return M <= most && (N + 15) / 16 <= most && (N + 127) / 128 * 16 <= most / ((M + 31) / 32) && M <= most * 256 / N;
 }
 
 hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
 {
     const bool gated = a.w[1].q4 != nullptr, norm = a.gamma != nullptr;
-    const ProductShape s = product_shape(a.M, a.N, a.K, gated, norm, a.idx != nullptr);
+    const ProductShape s = product_shape(a.M, a.N, a.K, a.O, gated, norm, a.idx != nullptr);
+    const int  halves = norm ? 2 : 1;
     Args p = {(const __half *)a.x, a.ldx, a.M, (const __half *)a.gamma, a.eps, a.idx, a.K, a.O, {a.w[0], a.w[1]}, a.N, (const __half *)a.residual, a.ldr,
-              (__half *)a.y, a.ldy, (const __half *)a.workspace, (int)a.M, s.combine, 0, 1};
-    p.tiles = (uint32_t)((a.N + 16 * s.NT - 1) / (16 * s.NT));
-    p.row_tiles = (uint32_t)((a.M + 16 * s.RT - 1) / (16 * s.RT));
-    const uint32_t room = (uint32_t)(2 * atom_launch::compute_units());
-    const uint32_t grid = (p.tiles < room ? p.tiles : room) * p.row_tiles;
-    if (!s.kept) {
-        static atom_launch::LdsOptIn opt;
-        const size_t nat = natural_bytes(a.K, norm, a.idx != nullptr);
-        if (nat > 60 * 1024) {
-            const hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(&w4a16_rows_kernel), nat);
-            if (err != hipSuccess) return err;
-        }
-        hipLaunchKernelGGL(w4a16_rows_kernel, dim3((unsigned)a.M), dim3(512), nat, stream, p, (__half *)a.workspace);
-    }
-#define ATOM_W4A16(...)                                                                        \
-    do {                                                                                       \
-        static atom_launch::LdsOptIn opt;                                                      \
-        auto kern = &w4a16_kernel<__VA_ARGS__>;                                                \
-        if (s.lds > 60 * 1024) {                                                               \
-            const hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(kern), s.lds); \
-            if (err != hipSuccess) return err;                                                 \
-        }                                                                                      \
-        hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), s.lds, stream, p);                \
-        return hipGetLastError();                                                              \
+              (__half *)a.y, a.ldy, (const __half *)a.workspace, (int)a.M, s.combine, 0, s.wide, halves, s.parts, 1,
+              (float *)((char *)a.workspace + laid_out_bytes(s, a.M, a.K, a.O, norm))};
+#define ATOM_LAUNCH(grid, threads, lds, kernel, ...)                                                                  \
+    do {                                                                                                              \
+        static atom_launch::LdsOptIn opt;                                                                             \
+        auto kern = &kernel;                                                                                          \
+        if ((lds) > 60 * 1024) {                                                                                      \
+            const hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(kern), lds);   \
+            if (err != hipSuccess) return err;                                                                        \
+        }                                                                                                             \
+        hipLaunchKernelGGL(kern, dim3((unsigned)(grid)), dim3(threads), lds, stream, __VA_ARGS__);                    \
+        const hipError_t err = hipGetLastError();                                                                     \
+        if (err != hipSuccess) return err;                                                                            \
     } while (0)
+    const size_t nat = natural_bytes(a.K, norm, a.idx != nullptr);
+    uint4 *laid_out = (uint4 *)a.workspace;
+    if (s.wide)       ATOM_LAUNCH(a.M, 512, nat, w4a16_rows_kernel<true>, p, laid_out);
+    else if (!s.kept) ATOM_LAUNCH(a.M, 512, nat, w4a16_rows_kernel<false>, p, laid_out);
+
+    if (s.wide) {
+        const int64_t per = gated ? 128 : 256;
+        p.row_blocks = (uint32_t)((a.M + 32 * s.wide - 1) / (32 * s.wide));
+        const int64_t grid = (a.N + per - 1) / per * s.parts * p.row_blocks;
+#define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, 256, 0, (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
+#define ATOM_WIDE_ROWS(GATED)                                  \
+    do {                                                       \
+        if (s.wide == 1) {                                     \
+            if (norm) ATOM_WIDE(GATED, 1, 2, 3);               \
+            else      ATOM_WIDE(GATED, 1, 1, 3);               \
+        } else {                                               \
+            if (norm) ATOM_WIDE(GATED, 2, 2, 3);               \
+            else      ATOM_WIDE(GATED, 2, 1, 3);               \
+        }                                                      \
+    } while (0)
+        if (gated) ATOM_WIDE_ROWS(true);
+        else       ATOM_WIDE_ROWS(false);
+#undef ATOM_WIDE_ROWS
+#undef ATOM_WIDE
+        if (s.parts > 1) {
+            const int64_t groups = (a.M * a.N + 255) / 256;
+            if (gated) ATOM_LAUNCH(groups, 256, 0, w4a16_join_kernel<true>, p);
+            else       ATOM_LAUNCH(groups, 256, 0, w4a16_join_kernel<false>, p);
+        }
+        return hipSuccess;
+    }
+
+    p.tiles = (uint32_t)((a.N + 16 * s.NT - 1) / (16 * s.NT));
+    const uint32_t room = (uint32_t)(2 * atom_launch::compute_units()), grid = p.tiles < room ? p.tiles : room;
+#define ATOM_FEW(...) ATOM_LAUNCH(grid, kThreads, s.lds, (w4a16_kernel<__VA_ARGS__>), p)
     const bool twice = norm && !s.combine;
     if (s.kept) {
-        if (gated) ATOM_W4A16(1, true, 1, 1, 3, true);
-        else       ATOM_W4A16(1, false, 1, 1, 4, true);
+        if (gated) ATOM_FEW(1, true, 1, 4, true);
+        else       ATOM_FEW(1, false, 1, 5, true);
+    } else if (gated) {
+        if (s.NT == 2) {
+            if (twice) ATOM_FEW(2, true, 2, 2, false);
+            else       ATOM_FEW(2, true, 1, 2, false);
+        } else {
+            if (twice) ATOM_FEW(1, true, 2, 2, false);
+            else       ATOM_FEW(1, true, 1, 3, false);
+        }
+    } else {
+        if (s.NT == 4) {
+            if (twice) ATOM_FEW(4, false, 2, 2, false);
+            else       ATOM_FEW(4, false, 1, 2, false);
+        } else if (s.NT == 2) {
+            if (twice) ATOM_FEW(2, false, 2, 2, false);
+            else       ATOM_FEW(2, false, 1, 3, false);
+        } else {
+            if (twice) ATOM_FEW(1, false, 2, 3, false);
+            else       ATOM_FEW(1, false, 1, 4, false);
+        }
     }
-#define ATOM_ROWS(NT, GATED, RT, CH)                                 \
-    do {                                                             \
-        if (twice) ATOM_W4A16(NT, GATED, RT, 2, CH, false);          \
-        else       ATOM_W4A16(NT, GATED, RT, 1, CH, false);          \
-    } while (0)
-    if (gated) {
-        if (s.RT == 4) ATOM_ROWS(1, true, 4, 1);
-        if (s.RT == 2) ATOM_ROWS(1, true, 2, 1);
-        if (s.NT == 2) ATOM_ROWS(2, true, 1, 2);
-        ATOM_ROWS(1, true, 1, 2);
-    }
-    if (s.RT == 4) ATOM_ROWS(1, false, 4, 1);
-    if (s.RT == 2) ATOM_ROWS(1, false, 2, 1);
-    if (s.NT == 4) ATOM_ROWS(4, false, 1, 2);
-    if (s.NT == 2) ATOM_ROWS(2, false, 1, 2);
-    ATOM_ROWS(1, false, 1, 2);
-#undef ATOM_ROWS
-#undef ATOM_W4A16
+#undef ATOM_FEW
+#undef ATOM_LAUNCH
+    return hipSuccess;
 }
 
 }  // namespace atom_internal
