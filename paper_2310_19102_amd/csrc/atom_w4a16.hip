@@ -198,6 +198,10 @@ void w4a16_rows_kernel(Args p, uint4 *out)
 
 #define ATOM_INLINE __attribute__((always_inline))      // of lambdas that registers go through: one that is called in many places is not inlined by itself
 
+// Between the loads before a loop and the loop, which goes on loading: without it the compiler, which orders the first ones as it likes, has the
+// loop wait for all loads under way in every turn, not in the first alone.
+__device__ __forceinline__ void all_loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 __device__ __forceinline__ float gated(float gate, float up) { return gate / (1.0f + expf(-gate)) * up; }
 
 template <bool GATED>
@@ -311,6 +315,23 @@ void w4a16_kernel(Args p)
             for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(part[t][j], s, acc[t][j]);
         }
     };
+    constexpr int kOut = (NT * 256 + kThreads - 1) / kThreads;         // outputs of a thread
+    auto output = [&](uint32_t tile, int i, int64_t &m, int64_t &out) ATOM_INLINE {
+        const int at = tid + i * kThreads, l = at & 63;
+        m = 4 * (l >> 4) + ((at >> 6) & 3);
+        out = (int64_t)tile * (16 * NT) + 16 * (at >> 8) + (l & 15);
+        return at < NT * 256 && m < p.M && out < p.N;
+    };
+    uint16_t residual[kOut];
+    auto fetch_residual = [&](uint32_t tile) ATOM_INLINE {               // (at a tile's beginning: at its end all loads under way would be waited for)
+        if constexpr (!GATED) {
+            int64_t m, out;
+            if (p.residual)
+#pragma unroll
+                for (int i = 0; i < kOut; ++i)
+                    if (output(tile, i, m, out)) residual[i] = reinterpret_cast<const uint16_t *>(p.residual)[m * p.ldr + out];
+        }
+    };
     int buffer = 0;
     auto finish = [&](uint32_t tile) ATOM_INLINE {
         float *mine = red + (size_t)buffer * (kWaves * CT * 256);
@@ -323,28 +344,34 @@ void w4a16_kernel(Args p)
                 acc[t][j] = 0.0f;
             }
         __syncthreads();
-        for (int at = tid; at < NT * 256; at += kThreads) {
-            const int l = at & 63, j = (at >> 6) & 3, t = at >> 8;
-            const int64_t m = 4 * (l >> 4) + j, out = (int64_t)tile * (16 * NT) + 16 * t + (l & 15);
-            if (m >= p.M || out >= p.N) continue;
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) {
+            int64_t m, out;
+            if (!output(tile, i, m, out)) continue;
+            const int at = tid + i * kThreads;
             float sum[WM];
 #pragma unroll
-            for (int i = 0; i < WM; ++i) {
+            for (int x = 0; x < WM; ++x) {
                 float lo = 0.0f;
-                sum[i] = 0.0f;
+                sum[x] = 0.0f;
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) {
-                    const float *s = mine + (w * CT + i * NT + t) * 256 + j * 64 + l;
-                    sum[i] += s[0];
+                    const float *s = mine + (w * CT + x * NT) * 256 + at;
+                    sum[x] += s[0];
                     if (p.combine) lo += s[32];
                 }
-                sum[i] += lo;
+                sum[x] += lo;
             }
-            store<GATED>(p, m, out, sum[0], sum[WM - 1]);
+            float y = sum[0];
+            if constexpr (GATED) y = gated(y, sum[WM - 1]);
+            else if (p.residual) y += __half2float(__ushort_as_half(residual[i]));
+            p.y[m * p.ldy + out] = __float2half_rn(y);
         }
     };
 
     rows_of(load_tile);
+    uint32_t tile = blockIdx.x;
+    fetch_residual(tile);
     if (begin < end) {
 #pragma unroll
         for (int s = 0; s < CH; ++s) load(ring[s]);
@@ -362,133 +389,122 @@ void w4a16_kernel(Args p)
         }
         __syncthreads();
     }
-    uint32_t tile = blockIdx.x;
     if (begin == end) {
-        for (; tile < p.tiles; tile += gridDim.x) finish(tile);
+        for (; tile < p.tiles; tile += gridDim.x) {
+            finish(tile);
+            fetch_residual(min(tile + gridDim.x, p.tiles - 1));
+        }
         return;
     }
-    for (int u = begin;;) {
+    all_loads_done();
+    const uint32_t turns = (p.tiles - tile + gridDim.x - 1) / gridDim.x * (uint32_t)(end - begin);
+    int u = begin;
+    for (uint32_t turn = 0; turn < turns; turn += CH)        // (with no way out inside: the compiler would wait at its head for what had been asked for by then)
 #pragma unroll
         for (int s = 0; s < CH; ++s) {
-            compute(ring[s], u);
+            if (turn + s < turns) compute(ring[s], u);
             load(ring[s]);
             if (++u == end) {
                 u = begin;
-                finish(tile);
+                if (turn + s < turns) finish(tile);
                 tile += gridDim.x;
-                if (tile >= p.tiles) return;
+                fetch_residual(min(tile, p.tiles - 1));
             }
         }
-    }
 }
 
 typedef float f16 __attribute__((ext_vector_type(16)));
 
 // More than 16 rows: MFMA 32x32x16, whose operands bring twice the products for their bytes (lane l: row or column l & 31, the eight values
-// of k-chunk l >> 5; register r of the result: row 8 (r / 4) + 4 (l >> 5) + r % 4).  A workgroup has 32 RT rows; each of its four wavefronts
-// has two tiles of 32 weight rows (gate and up, or two of the one) for itself, and all of them share the activations, which come a
-// unit at a time through LDS.  `parts` workgroups share a tile's units where the tiles alone do not fill the card; their sums meet in the workspace.
+// of k-chunk l >> 5; register r of the result: row 8 (r / 4) + 4 (l >> 5) + r % 4).  A workgroup has 32 RT rows; each of its eight wavefronts
+// has a tile of 32 weight rows for itself (four of the gate and the same four of the up projection), and all of them share the activations, which
+// come a unit at a time through LDS.  `parts` workgroups share a tile's units where the tiles alone do not fill the card; their sums meet
+// in the workspace.
 template <bool GATED, int RT, int HL, int CH>
-__global__ __launch_bounds__(256, 1)
+__global__ __launch_bounds__(kThreads, 2)
 void w4a16_wide_kernel(Args p)
 {
-    constexpr int kChunks = RT * HL * 2;                     // 16-byte pieces of a unit's activations a thread brings
-    __shared__ __align__(16) u4 s_act[2][RT * HL * 8 * 64];
+    constexpr int kOps = RT * HL;                            // row operands of an instruction's k-chunk; 16-byte pieces of a unit that a thread brings
+    constexpr int kTiles = GATED ? kWaves / 2 : kWaves;
+    __shared__ __align__(16) u4 s_act[2][kOps * 8 * 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, kc = lane >> 5;
     const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, U = 2 * G - G4;
     const uint32_t block = blockIdx.x % p.row_blocks, rest = blockIdx.x / p.row_blocks, part = rest % (uint32_t)p.parts, tile = rest / (uint32_t)p.parts;
     const int begin = (int)((int64_t)part * U / p.parts), end = (int)((int64_t)(part + 1) * U / p.parts);
 
-    // weight rows of this lane (columns >= N are computed and never stored)
-    int64_t n[2];
-    uint32_t at4[2], at8[2], at_s[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        n[t] = GATED ? ((int64_t)tile * 4 + wave) * 32 + col : (((int64_t)tile * 4 + wave) * 2 + t) * 32 + col;
-        const uint32_t row = (uint32_t)min(n[t], p.N - 1);
-        at4[t] = row * (uint32_t)(K4 >> 1) + kc * 32;
-        at8[t] = row * (uint32_t)p.O + kc * 32;
-        at_s[t] = row * (uint32_t)(2 * G);
-    }
-    struct Unit { uint4 q[2][2]; uint16_t scale[2]; };
+    // the weight row of this lane (columns >= N are computed and never stored)
+    const int matrix = GATED ? wave / kTiles : 0;
+    const W4  w = p.w[matrix];
+    const int64_t n = ((int64_t)tile * kTiles + wave % kTiles) * 32 + col;
+    const uint32_t row = (uint32_t)min(n, p.N - 1), at4 = row * (uint32_t)(K4 >> 1) + kc * 32, at8 = row * (uint32_t)p.O + kc * 32, at_s = row * (uint32_t)(2 * G);
+    // (a load is waited for with all before it, so a unit's weights and activations come the same way ahead)
+    struct Unit { u4 q[2], a[kOps]; uint16_t scale; };
     Unit ring[CH];
+    const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + (int64_t)block * U * (kOps * 512) + tid;
     int load_u = begin;
     auto load = [&](Unit &e) ATOM_INLINE {
         const int  u = min(load_u, end - 1), v = u - G4;
-        const bool is4 = u < G4;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const W4 &w = p.w[GATED ? t : 0];
-            const uint8_t *at = (is4 ? w.q4 + u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64) + (is4 ? at4[t] : at8[t]);
-            e.q[t][0] = *reinterpret_cast<const uint4 *>(at);
-            e.q[t][1] = *reinterpret_cast<const uint4 *>(at + 16);
-            e.scale[t] = *reinterpret_cast<const uint16_t *>(reinterpret_cast<const uint8_t *>(w.scale) + at_s[t] + 2 * (is4 ? u : G4 + (v >> 1)));
-        }
+        for (int c = 0; c < kOps; ++c) e.a[c] = acts[(int64_t)u * (kOps * 512) + c * 512];
+        const bool is4 = u < G4;
+        const uint8_t *at = (is4 ? w.q4 + u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64) + (is4 ? at4 : at8);
+        e.q[0] = *reinterpret_cast<const u4 *>(at);
+        e.q[1] = *reinterpret_cast<const u4 *>(at + 16);
+        e.scale = *reinterpret_cast<const uint16_t *>(reinterpret_cast<const uint8_t *>(w.scale) + at_s + 2 * (is4 ? u : G4 + (v >> 1)));
         ++load_u;
     };
-    const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + (int64_t)block * U * (RT * HL * 512) + tid;
-    u4 next[kChunks];
-    auto fetch = [&](int u) ATOM_INLINE {
+    auto keep = [&](const Unit &e, int u) ATOM_INLINE {
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) next[c] = acts[(int64_t)min(u, end - 1) * (RT * HL * 512) + c * 256];
-    };
-    auto keep = [&](int u) ATOM_INLINE {
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) s_act[(u - begin) & 1][c * 256 + tid] = next[c];
+        for (int c = 0; c < kOps; ++c) s_act[(u - begin) & 1][c * 512 + tid] = e.a[c];
     };
 
-    f16 acc[2][RT] = {};
+    f16 acc[RT] = {};
     auto compute = [&](const Unit &e, int u) ATOM_INLINE {
         const u4 *a = s_act[(u - begin) & 1] + lane;
-        f16 sum[2][RT] = {};
-        auto word = [&](int t, int i) { const uint4 &q = e.q[t][i >> 2]; return (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w; };
-        auto products = [&](int i, const h8 (&w)[2]) ATOM_INLINE {
+        f16 sum[RT] = {};
+        h8 x[2][kOps];                                       // the next k-chunk's operands come while this one's are in use
+        auto operands = [&](int i) ATOM_INLINE {
 #pragma unroll
-            for (int h = 0; h < HL; ++h)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    const h8 x = __builtin_bit_cast(h8, a[((h * RT + r) * 8 + i) * 64]);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) sum[t][r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, w[t], sum[t][r], 0, 0, 0);
-                }
+            for (int o = 0; o < kOps; ++o) x[i & 1][o] = __builtin_bit_cast(h8, a[(o * 8 + i) * 64]);
         };
+        auto products = [&](int i, h8 y) ATOM_INLINE {
+#pragma unroll
+            for (int o = 0; o < kOps; ++o) sum[o % RT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i & 1][o], y, sum[o % RT], 0, 0, 0);
+        };
+        operands(0);
         if (u < G4) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const h8 w[2] = {widen4(word(0, i)), widen4(word(1, i))};
-                products(i, w);
+                if (i < 7) operands(i + 1);
+                __builtin_amdgcn_sched_barrier(0);           // (or the reads move to where they are used)
+                products(i, widen4(e.q[i >> 2][i & 3]));
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const h8 w[2] = {widen8(word(0, 2 * i), word(0, 2 * i + 1)), widen8(word(1, 2 * i), word(1, 2 * i + 1))};
-                products(i, w);
+                if (i < 3) operands(i + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                products(i, widen8(e.q[i >> 1][2 * (i & 1)], e.q[i >> 1][2 * (i & 1) + 1]));
             }
         }
+        const float s = __half2float(__ushort_as_half(e.scale));
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const float s = __half2float(__ushort_as_half(e.scale[t]));
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) acc[t][r][j] = fmaf(sum[t][r][j], s, acc[t][r][j]);
-        }
+            for (int j = 0; j < 16; ++j) acc[r][j] = fmaf(sum[r][j], s, acc[r][j]);
     };
 
-    fetch(begin);
 #pragma unroll
     for (int s = 0; s < CH; ++s) load(ring[s]);
-    keep(begin);
-    fetch(begin + 1);
+    all_loads_done();
+    keep(ring[0], begin);
     __syncthreads();
     for (int u = begin; u < end; u += CH)
 #pragma unroll
-        for (int s = 0; s < CH; ++s) {
-            if (u + s >= end) break;                         // (the same for all)
-            keep(u + s + 1);
-            fetch(u + s + 2);
-            compute(ring[s], u + s);
+        for (int s = 0; s < CH; ++s) {                       // (no way out of the loop here: the compiler would wait at its head for what had been asked for by then)
+            keep(ring[(s + 1) % CH], u + s + 1);
+            if (u + s < end) compute(ring[s], u + s);
             load(ring[s]);
             __syncthreads();                                 // (all have read this unit's activations, the next one's are there)
         }
@@ -496,40 +512,43 @@ void w4a16_wide_kernel(Args p)
     const int64_t m0 = (int64_t)block * (32 * RT) + 4 * kc;
     auto row_of = [&](int r, int j) ATOM_INLINE { return m0 + 32 * r + 8 * (j >> 2) + (j & 3); };
     if (p.parts > 1) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-            if (n[t] < p.N)
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (row_of(r, j) < p.M) p.sums[(((int64_t)part * (GATED ? 2 : 1) + (GATED ? t : 0)) * p.M + row_of(r, j)) * p.N + n[t]] = acc[t][r][j];
-        return;
-    }
-    if constexpr (GATED) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (row_of(r, j) < p.M && n[0] < p.N) p.y[row_of(r, j) * p.ldy + n[0]] = __float2half_rn(gated(acc[0][r][j], acc[1][r][j]));
-    } else {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if (p.residual)                                  // (all of them on their way at once)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    uint16_t res[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) res[j] = reinterpret_cast<const uint16_t *>(p.residual)[min(row_of(r, j), p.M - 1) * p.ldr + min(n[t], p.N - 1)];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[t][r][j] += __half2float(__ushort_as_half(res[j]));
-                }
+        if (n < p.N)
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (row_of(r, j) < p.M && n[t] < p.N) p.y[row_of(r, j) * p.ldy + n[t]] = __float2half_rn(acc[t][r][j]);
-        }
+                    if (row_of(r, j) < p.M) p.sums[(((int64_t)part * (GATED ? 2 : 1) + matrix) * p.M + row_of(r, j)) * p.N + n] = acc[r][j];
+        return;
+    }
+    if constexpr (GATED) {
+        float *s_up = reinterpret_cast<float *>(s_act) + (wave % kTiles) * (RT * 1024) + lane;
+        if (matrix)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s_up[(16 * r + j) * 64] = acc[r][j];
+        __syncthreads();
+        if (matrix) return;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (row_of(r, j) < p.M && n < p.N) p.y[row_of(r, j) * p.ldy + n] = __float2half_rn(gated(acc[r][j], s_up[(16 * r + j) * 64]));
+    } else {
+        if (p.residual)                                      // (all of them on their way at once)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                uint16_t res[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) res[j] = reinterpret_cast<const uint16_t *>(p.residual)[min(row_of(r, j), p.M - 1) * p.ldr + min(n, p.N - 1)];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[r][j] += __half2float(__ushort_as_half(res[j]));
+            }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (row_of(r, j) < p.M && n < p.N) p.y[row_of(r, j) * p.ldy + n] = __float2half_rn(acc[r][j]);
     }
 }
 
@@ -644,15 +663,15 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
         const int64_t per = gated ? 128 : 256;
         p.row_blocks = (uint32_t)((a.M + 32 * s.wide - 1) / (32 * s.wide));
         const int64_t grid = (a.N + per - 1) / per * s.parts * p.row_blocks;
-#define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, 256, 0, (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
+#define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, kThreads, 0, (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
 #define ATOM_WIDE_ROWS(GATED)                                  \
     do {                                                       \
         if (s.wide == 1) {                                     \
-            if (norm) ATOM_WIDE(GATED, 1, 2, 3);               \
-            else      ATOM_WIDE(GATED, 1, 1, 3);               \
+            if (norm) ATOM_WIDE(GATED, 1, 2, 4);               \
+            else      ATOM_WIDE(GATED, 1, 1, 4);               \
         } else {                                               \
-            if (norm) ATOM_WIDE(GATED, 2, 2, 3);               \
-            else      ATOM_WIDE(GATED, 2, 1, 3);               \
+            if (norm) ATOM_WIDE(GATED, 2, 2, 4);               \
+            else      ATOM_WIDE(GATED, 2, 1, 4);               \
         }                                                      \
     } while (0)
         if (gated) ATOM_WIDE_ROWS(true);
