@@ -28,7 +28,7 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float    f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kWaves = 8, kThreads = 64 * kWaves, kWide = 256;
 
 __device__ __forceinline__ h2 as_h2(uint32_t v) { return __builtin_bit_cast(h2, v); }
 __device__ __forceinline__ uint32_t bits(h2 v) { return __builtin_bit_cast(uint32_t, v); }
@@ -38,13 +38,12 @@ __device__ __forceinline__ h8 as_h8(uint32_t a, uint32_t b, uint32_t c, uint32_t
 // exponent of 1024 it is 1024 + that, or 16 times it where it lies four bits higher.
 __device__ __forceinline__ h8 widen4(uint32_t w)
 {
-    w ^= 0x88888888u;
     const uint32_t v = w >> 8;
     const h2 low = {(_Float16)-1032.0f, (_Float16)-1032.0f}, high = {(_Float16)-72.0f, (_Float16)-72.0f}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
-    const h2 a = as_h2((w & 0x000f000fu) | 0x64006400u) + low;
-    const h2 b = __builtin_elementwise_fma(as_h2((w & 0x00f000f0u) | 0x64006400u), sixteenth, high);
-    const h2 c = as_h2((v & 0x000f000fu) | 0x64006400u) + low;
-    const h2 d = __builtin_elementwise_fma(as_h2((v & 0x00f000f0u) | 0x64006400u), sixteenth, high);
+    const h2 a = as_h2((w & 0x000f000fu) ^ 0x64086408u) + low;
+    const h2 b = __builtin_elementwise_fma(as_h2((w & 0x00f000f0u) ^ 0x64806480u), sixteenth, high);
+    const h2 c = as_h2((v & 0x000f000fu) ^ 0x64086408u) + low;
+    const h2 d = __builtin_elementwise_fma(as_h2((v & 0x00f000f0u) ^ 0x64806480u), sixteenth, high);
     return as_h8(bits(a), bits(b), bits(c), bits(d));
 }
 // Eight 8-bit codes in a row, likewise: 1024 + (code + 128).
@@ -173,7 +172,8 @@ __device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict_
 
 __host__ __device__ constexpr size_t natural_bytes(int K, bool norm, bool index) { return norm ? 4 * (size_t)K : index ? 2 * (size_t)K : 0; }
 
-// A row to a workgroup, into the workspace: rows of hi and behind them those of lo, or (WIDE) the tiles of the kernel of many rows.
+// A row to a workgroup, into the workspace, in the order in which the product's loads take it (64 lanes of 16 bytes in a row): for every unit
+// and half the operands of its instructions, of a tile of 16 rows, or (WIDE) of tiles of 32.
 template <bool WIDE>
 __global__ __launch_bounds__(512)
 void w4a16_rows_kernel(Args p, uint4 *out)
@@ -184,10 +184,14 @@ void w4a16_rows_kernel(Args p, uint4 *out)
     const int K4 = p.K - p.O, G4 = K4 >> 7, U = (p.K + p.O) >> 7;
     const __half *x = p.x + m * p.ldx;
     lay_out<512>(p, x, front_of<512>(p, x), s_nat, s_sum, [&](int k, int half, const uint4 &v) {
-        if constexpr (!WIDE) out[(m + half * p.M) * (p.K / 8) + row_place(k, K4)] = v;
-        else {
-            const bool is4 = k < K4;
-            const int  j = k - K4, u = is4 ? k >> 7 : G4 + (j >> 6), i = is4 ? (k >> 3) & 7 : (j >> 3) & 3, c = is4 ? (k >> 6) & 1 : (j >> 5) & 1;
+        const bool is4 = k < K4;
+        const int  j = k - K4, u = is4 ? k >> 7 : G4 + (j >> 6);
+        if constexpr (!WIDE) {
+            const int place = row_place(k, K4) & (is4 ? 15 : 7);                          // (instruction, chunk)
+            const int tile = p.combine ? 0 : half, row = (int)m + (p.combine && half ? 8 : 0);
+            out[((((int64_t)u * p.halves + tile) * 4 + (place >> 2)) * 4 + (place & 3)) * 16 + row] = v;
+        } else {
+            const int i = is4 ? (k >> 3) & 7 : (j >> 3) & 3, c = is4 ? (k >> 6) & 1 : (j >> 5) & 1;
             const int64_t block = m / (32 * p.wide), t = m / 32 % p.wide;
             out[((((block * U + u) * p.halves + half) * p.wide + t) * 8 + i) * 64 + c * 32 + m % 32] = v;
         }
@@ -224,7 +228,7 @@ void w4a16_kernel(Args p)
 {
     constexpr int WM = GATED ? 2 : 1, CT = WM * NT, AT = HL;
     static_assert(CT <= 4, "a lane's chunk loads the scales of one tile");
-    extern __shared__ __align__(16) unsigned char s_all[];   // KEPT: the rows, then the sums or what is laid out; else the sums
+    extern __shared__ __align__(16) unsigned char s_all[];   // KEPT: the rows; the weights' way to the operands; the sums (before: what is laid out)
     __shared__ float s_part[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, kc = lane >> 4;
@@ -237,11 +241,15 @@ void w4a16_kernel(Args p)
 
     // (rows >= M are computed and never stored, columns >= N likewise)
     const int r = p.combine && col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1);
-    const __half *act = KEPT ? reinterpret_cast<const __half *>(s_all) + (size_t)r * lds_row + kc * 8 : p.staged + (int64_t)r * p.K + kc * 8;
-    const int64_t to_lo = (int64_t)rows * p.K;
-    float *red = reinterpret_cast<float *>(s_all + (KEPT ? (size_t)rows * (p.gamma ? 2 : 1) * lds_row * 2 : 0));
+    const __half *s_act = reinterpret_cast<const __half *>(s_all) + (size_t)r * lds_row + kc * 8;
+    const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + lane;
+    unsigned char *s_mine = s_all + (KEPT ? (size_t)rows * (p.gamma ? 2 : 1) * lds_row * 2 : 0);
+    u4 *s_turn = reinterpret_cast<u4 *>(s_mine) + wave * (CT * 64);     // this wavefront's own
+    float *red = reinterpret_cast<float *>(s_mine + kWaves * CT * 1024);
 
-    struct Unit { uint4 q[CT]; uint16_t scale; uint4 a[KEPT ? 1 : AT][4]; };
+    // A load brings 64 bytes of 16 rows, four lanes a row: lanes that go to one line apart, or one load after the other, hold up the cache until the line
+    // is there.  The operands want a row in one lane of each 16, so the pieces go through LDS.
+    struct Unit { u4 q[CT], a[KEPT ? 1 : 4 * AT]; uint16_t scale; };
     Unit ring[CH];
     uint32_t load_tile = blockIdx.x;                         // of the unit that is loaded next
     int load_u = begin;
@@ -250,13 +258,14 @@ void w4a16_kernel(Args p)
         const bool live = tile < p.tiles;
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            const uint32_t row = (uint32_t)min((int64_t)tile * (16 * NT) + 16 * (t % NT) + col, p.N - 1);
-            at4[t] = live ? row * (uint32_t)(K4 >> 1) + kc * 16 : 0;
-            at8[t] = live ? row * (uint32_t)p.O + kc * 16 : 0;
+            const uint32_t row = (uint32_t)min((int64_t)tile * (16 * NT) + 16 * (t % NT) + (lane >> 2), p.N - 1);
+            at4[t] = live ? row * (uint32_t)(K4 >> 1) + (lane & 3) * 16 : 0;
+            at8[t] = live ? row * (uint32_t)p.O + (lane & 3) * 16 : 0;
         }
-        at_s = live ? (uint32_t)min((int64_t)tile * (16 * NT) + 16 * ((kc % CT) % NT) + col, p.N - 1) * (uint32_t)(2 * G) : 0;
+        // (lane 16 t + c: the scale of row c of tile t; the others go where lane 0 does)
+        at_s = live ? (uint32_t)min((int64_t)tile * (16 * NT) + (kc < CT ? 16 * (kc % NT) + col : 0), p.N - 1) * (uint32_t)(2 * G) : 0;
     };
-    const uint8_t *my_scale = reinterpret_cast<const uint8_t *>(CT > 1 && (kc % CT) / NT ? p.w[WM - 1].scale : p.w[0].scale);
+    const uint8_t *my_scale = reinterpret_cast<const uint8_t *>(kc < CT && kc >= NT ? p.w[WM - 1].scale : p.w[0].scale);
     auto load = [&](Unit &e) ATOM_INLINE {
         const bool is4 = load_u < G4;
         const int  v = load_u - G4, k = is4 ? load_u * 128 : K4 + v * 64;
@@ -264,15 +273,15 @@ void w4a16_kernel(Args p)
         for (int t = 0; t < CT; ++t) {
             const W4 &w = p.w[t / NT];
             const uint8_t *base = is4 ? w.q4 + load_u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64;
-            e.q[t] = *reinterpret_cast<const uint4 *>(base + (is4 ? at4[t] : at8[t]));
+            const uint32_t a4 = at4[t], a8 = at8[t];
+            e.q[t] = *reinterpret_cast<const u4 *>(base + (is4 ? a4 : a8));
         }
         e.scale = *reinterpret_cast<const uint16_t *>(my_scale + at_s + 2 * (k >> 7));
         if constexpr (!KEPT) {
 #pragma unroll
             for (int a = 0; a < AT; ++a)
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    e.a[a][c] = *reinterpret_cast<const uint4 *>(act + a * to_lo + k + (is4 ? c : c & 1) * 32);
+                for (int c = 0; c < 4; ++c) e.a[4 * a + c] = acts[((int64_t)load_u * AT + a) * 256 + c * 64];
         }
         if (++load_u == end) {
             load_u = begin;
@@ -284,15 +293,21 @@ void w4a16_kernel(Args p)
     auto compute = [&](const Unit &e, int u) ATOM_INLINE {
         f4 part[CT] = {};
         auto activations = [&](int a, int k, int c) ATOM_INLINE {
-            if constexpr (KEPT) return *reinterpret_cast<const h8 *>(act + k + c * 32);
-            else return __builtin_bit_cast(h8, e.a[a][c]);
+            if constexpr (KEPT) return *reinterpret_cast<const h8 *>(s_act + k + c * 32);
+            else return __builtin_bit_cast(h8, e.a[4 * a + c]);
         };
+        // piece p of row r lies at 4 r + (p ^ (r / 4 & 3)): the 16 lanes of a chunk read all banks
+        u4 q[CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) s_turn[t * 64 + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = e.q[t];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) q[t] = s_turn[t * 64 + 4 * col + ((kc ^ (col >> 2)) & 3)];
         if (u < G4) {
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int t = 0; t < CT; ++t) {
-                    const h8 w = widen4(c == 0 ? e.q[t].x : c == 1 ? e.q[t].y : c == 2 ? e.q[t].z : e.q[t].w);
+                    const h8 w = widen4(q[t][c]);
 #pragma unroll
                     for (int a = 0; a < AT; ++a) part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(activations(a, u * 128, c), w, part[t], 0, 0, 0);
                 }
@@ -301,7 +316,7 @@ void w4a16_kernel(Args p)
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int t = 0; t < CT; ++t) {
-                    const h8 w = c == 0 ? widen8(e.q[t].x, e.q[t].y) : widen8(e.q[t].z, e.q[t].w);
+                    const h8 w = widen8(q[t][2 * c], q[t][2 * c + 1]);
 #pragma unroll
                     for (int a = 0; a < AT; ++a)
                         part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(activations(a, K4 + (u - G4) * 64, c), w, part[t], 0, 0, 0);
@@ -310,7 +325,7 @@ void w4a16_kernel(Args p)
         const float mine = __half2float(__ushort_as_half(e.scale));
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            const float s = CT == 1 ? mine : __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * (16 * t + col), __builtin_bit_cast(int, mine)));
+            const float s = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * (16 * t + col), __builtin_bit_cast(int, mine)));
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(part[t][j], s, acc[t][j]);
         }
@@ -377,7 +392,7 @@ void w4a16_kernel(Args p)
         for (int s = 0; s < CH; ++s) load(ring[s]);
     }
     if constexpr (KEPT) {
-        uint32_t *nat = reinterpret_cast<uint32_t *>(red);
+        uint32_t *nat = reinterpret_cast<uint32_t *>(s_mine);
         __half *out = reinterpret_cast<__half *>(s_all);
         for (int m = 0; m < rows; ++m) {
             if (m) {
@@ -416,83 +431,131 @@ void w4a16_kernel(Args p)
 typedef float f16 __attribute__((ext_vector_type(16)));
 
 // More than 16 rows: MFMA 32x32x16, whose operands bring twice the products for their bytes (lane l: row or column l & 31, the eight values
-// of k-chunk l >> 5; register r of the result: row 8 (r / 4) + 4 (l >> 5) + r % 4).  A workgroup has 32 RT rows; each of its eight wavefronts
-// has a tile of 32 weight rows for itself (four of the gate and the same four of the up projection), and all of them share the activations, which
+// of k-chunk l >> 5; register r of the result: row 8 (r / 4) + 4 (l >> 5) + r % 4).  A workgroup has 32 RT rows; each of its four wavefronts
+// has two tiles of 32 weight rows for itself (the same of gate and up, or two of the one), and all of them share the activations, which
 // come a unit at a time through LDS.  `parts` workgroups share a tile's units where the tiles alone do not fill the card; their sums meet
 // in the workspace.
 template <bool GATED, int RT, int HL, int CH>
-__global__ __launch_bounds__(kThreads, 2)
+__global__ __launch_bounds__(kWide, 1)
 void w4a16_wide_kernel(Args p)
 {
-    constexpr int kOps = RT * HL;                            // row operands of an instruction's k-chunk; 16-byte pieces of a unit that a thread brings
-    constexpr int kTiles = GATED ? kWaves / 2 : kWaves;
-    __shared__ __align__(16) u4 s_act[2][kOps * 8 * 64];
+    constexpr int kOps = RT * HL;                            // row operands of an instruction's k-chunk
+    constexpr int kPieces = kOps * 512 / kWide;              // 16-byte pieces of a unit's activations that a thread brings
+    extern __shared__ __align__(16) unsigned char s_all[];
+    u4 (*s_act)[kOps * 512] = reinterpret_cast<u4 (*)[kOps * 512]>(s_all);                     // [2], and behind them
+    u4 (*s_turn)[kWide / 64][256] = reinterpret_cast<u4 (*)[kWide / 64][256]>(s_act + 2);      // [2]: the weights' way to the operands
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, kc = lane >> 5;
     const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, U = 2 * G - G4;
     const uint32_t block = blockIdx.x % p.row_blocks, rest = blockIdx.x / p.row_blocks, part = rest % (uint32_t)p.parts, tile = rest / (uint32_t)p.parts;
     const int begin = (int)((int64_t)part * U / p.parts), end = (int)((int64_t)(part + 1) * U / p.parts);
 
-    // the weight row of this lane (columns >= N are computed and never stored)
-    const int matrix = GATED ? wave / kTiles : 0;
-    const W4  w = p.w[matrix];
-    const int64_t n = ((int64_t)tile * kTiles + wave % kTiles) * 32 + col;
-    const uint32_t row = (uint32_t)min(n, p.N - 1), at4 = row * (uint32_t)(K4 >> 1) + kc * 32, at8 = row * (uint32_t)p.O + kc * 32, at_s = row * (uint32_t)(2 * G);
+    // output channels of this lane (>= N: computed and never stored); the weight rows that it loads, 64 bytes of 16 rows at a time, four lanes
+    // a row (lanes that go to one line apart, or one load after the other, hold up the cache until the line is there)
+    int64_t n[2];
+    uint32_t at4[2][2], at8[2][2], at_s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int64_t n0 = ((int64_t)tile * (kWide / 64) + wave) * (GATED ? 32 : 64) + (GATED ? 0 : 32 * t);
+        n[t] = n0 + col;
+        at_s[t] = (uint32_t)min(n0 + (kc ? 0 : col), p.N - 1) * (uint32_t)(2 * G);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t row = (uint32_t)min(n0 + 16 * i + (lane >> 2), p.N - 1);
+            at4[t][i] = row * (uint32_t)(K4 >> 1) + (lane & 3) * 16;
+            at8[t][i] = row * (uint32_t)p.O + (lane & 3) * 16;
+        }
+    }
     // (a load is waited for with all before it, so a unit's weights and activations come the same way ahead)
-    struct Unit { u4 q[2], a[kOps]; uint16_t scale; };
+    struct Unit { u4 q[2][2], a[kPieces]; uint16_t scale[2]; };
     Unit ring[CH];
     const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + (int64_t)block * U * (kOps * 512) + tid;
     int load_u = begin;
     auto load = [&](Unit &e) ATOM_INLINE {
         const int  u = min(load_u, end - 1), v = u - G4;
-#pragma unroll
-        for (int c = 0; c < kOps; ++c) e.a[c] = acts[(int64_t)u * (kOps * 512) + c * 512];
         const bool is4 = u < G4;
-        const uint8_t *at = (is4 ? w.q4 + u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64) + (is4 ? at4 : at8);
-        e.q[0] = *reinterpret_cast<const u4 *>(at);
-        e.q[1] = *reinterpret_cast<const u4 *>(at + 16);
-        e.scale = *reinterpret_cast<const uint16_t *>(reinterpret_cast<const uint8_t *>(w.scale) + at_s + 2 * (is4 ? u : G4 + (v >> 1)));
+#pragma unroll
+        for (int c = 0; c < kPieces; ++c) e.a[c] = acts[(int64_t)u * (kOps * 512) + c * kWide];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const W4 &w = p.w[GATED ? t : 0];
+            const uint8_t *base = is4 ? w.q4 + u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t a4 = at4[t][i], a8 = at8[t][i];
+                e.q[t][i] = *reinterpret_cast<const u4 *>(base + (is4 ? a4 : a8));
+            }
+            e.scale[t] = *reinterpret_cast<const uint16_t *>(reinterpret_cast<const uint8_t *>(w.scale) + at_s[t] + 2 * (is4 ? u : G4 + (v >> 1)));
+        }
         ++load_u;
     };
     auto keep = [&](const Unit &e, int u) ATOM_INLINE {
 #pragma unroll
-        for (int c = 0; c < kOps; ++c) s_act[(u - begin) & 1][c * 512 + tid] = e.a[c];
+        for (int c = 0; c < kPieces; ++c) s_act[(u - begin) & 1][c * kWide + tid] = e.a[c];
+        // piece p of row r lies at 4 r + (p ^ (r / 4 & 3)): the lanes of a chunk read all banks
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s_turn[(u - begin) & 1][wave][128 * t + 64 * i + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = e.q[t][i];
     };
 
-    f16 acc[RT] = {};
+    f16 acc[2][RT] = {};
     auto compute = [&](const Unit &e, int u) ATOM_INLINE {
         const u4 *a = s_act[(u - begin) & 1] + lane;
-        f16 sum[RT] = {};
-        h8 x[2][kOps];                                       // the next k-chunk's operands come while this one's are in use
+        u4 q[2][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) q[t][i] = s_turn[(u - begin) & 1][wave][128 * t + 4 * col + (((2 * kc + i) ^ (col >> 2)) & 3)];
+        f16 sum[2][RT] = {};
+        h8 x[2][kOps], y[2][2];                              // the next k-chunk's operands come and are widened between this one's products
         auto operands = [&](int i) ATOM_INLINE {
 #pragma unroll
             for (int o = 0; o < kOps; ++o) x[i & 1][o] = __builtin_bit_cast(h8, a[(o * 8 + i) * 64]);
         };
-        auto products = [&](int i, h8 y) ATOM_INLINE {
+        auto widened = [&](int i, bool is4) ATOM_INLINE {
 #pragma unroll
-            for (int o = 0; o < kOps; ++o) sum[o % RT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i & 1][o], y, sum[o % RT], 0, 0, 0);
+            for (int t = 0; t < 2; ++t)
+                y[i & 1][t] = is4 ? widen4(q[t][i >> 2][i & 3]) : widen8(q[t][i >> 1 & 1][2 * (i & 1)], q[t][i >> 1 & 1][2 * (i & 1) + 1]);
         };
-        operands(0);
-        if (u < G4) {
+        auto products = [&](int i) ATOM_INLINE {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (i < 7) operands(i + 1);
-                __builtin_amdgcn_sched_barrier(0);           // (or the reads move to where they are used)
-                products(i, widen4(e.q[i >> 2][i & 3]));
-            }
-        } else {
+            for (int o = 0; o < kOps; ++o)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (i < 3) operands(i + 1);
+                for (int t = 0; t < 2; ++t) sum[t][o % RT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i & 1][o], y[i & 1][t], sum[t][o % RT], 0, 0, 0);
+        };
+        auto chunks = [&](int count, bool is4) ATOM_INLINE {
+            operands(0);
+            widened(0, is4);
+#pragma unroll
+            for (int i = 0; i < count; ++i) {
+                if (i + 1 < count) {
+                    operands(i + 1);
+                    widened(i + 1, is4);
+                }
+                products(i);
+                // reads first, then a product and its share of the widening in turn: a wavefront's next product waits for the matrix unit, and
+                // everything behind it in the program with it
+                __builtin_amdgcn_sched_group_barrier(0x100, kOps, 0);
+#pragma unroll
+                for (int k = 0; k < 2 * kOps; ++k) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, (20 + 2 * kOps - 1) / (2 * kOps), 0);
+                }
                 __builtin_amdgcn_sched_barrier(0);
-                products(i, widen8(e.q[i >> 1][2 * (i & 1)], e.q[i >> 1][2 * (i & 1) + 1]));
             }
+        };
+        if (u < G4) chunks(8, true);
+        else        chunks(4, false);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            float s = __half2float(__ushort_as_half(e.scale[t]));
+            s = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * col, __builtin_bit_cast(int, s)));
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[t][r][j] = fmaf(sum[t][r][j], s, acc[t][r][j]);
         }
-        const float s = __half2float(__ushort_as_half(e.scale));
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[r][j] = fmaf(sum[r][j], s, acc[r][j]);
     };
 
 #pragma unroll
@@ -512,43 +575,40 @@ void w4a16_wide_kernel(Args p)
     const int64_t m0 = (int64_t)block * (32 * RT) + 4 * kc;
     auto row_of = [&](int r, int j) ATOM_INLINE { return m0 + 32 * r + 8 * (j >> 2) + (j & 3); };
     if (p.parts > 1) {
-        if (n < p.N)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            if (n[t] < p.N)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (row_of(r, j) < p.M) p.sums[(((int64_t)part * (GATED ? 2 : 1) + (GATED ? t : 0)) * p.M + row_of(r, j)) * p.N + n[t]] = acc[t][r][j];
+        return;
+    }
+    if constexpr (GATED) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (row_of(r, j) < p.M && n[0] < p.N) p.y[row_of(r, j) * p.ldy + n[0]] = __float2half_rn(gated(acc[0][r][j], acc[1][r][j]));
+    } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if (p.residual)                                  // (all of them on their way at once)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    uint16_t res[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) res[j] = reinterpret_cast<const uint16_t *>(p.residual)[min(row_of(r, j), p.M - 1) * p.ldr + min(n[t], p.N - 1)];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[t][r][j] += __half2float(__ushort_as_half(res[j]));
+                }
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (row_of(r, j) < p.M) p.sums[(((int64_t)part * (GATED ? 2 : 1) + matrix) * p.M + row_of(r, j)) * p.N + n] = acc[r][j];
-        return;
-    }
-    if constexpr (GATED) {
-        float *s_up = reinterpret_cast<float *>(s_act) + (wave % kTiles) * (RT * 1024) + lane;
-        if (matrix)
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s_up[(16 * r + j) * 64] = acc[r][j];
-        __syncthreads();
-        if (matrix) return;
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (row_of(r, j) < p.M && n < p.N) p.y[row_of(r, j) * p.ldy + n] = __float2half_rn(gated(acc[r][j], s_up[(16 * r + j) * 64]));
-    } else {
-        if (p.residual)                                      // (all of them on their way at once)
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                uint16_t res[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) res[j] = reinterpret_cast<const uint16_t *>(p.residual)[min(row_of(r, j), p.M - 1) * p.ldr + min(n, p.N - 1)];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) acc[r][j] += __half2float(__ushort_as_half(res[j]));
-            }
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (row_of(r, j) < p.M && n < p.N) p.y[row_of(r, j) * p.ldy + n] = __float2half_rn(acc[r][j]);
+                    if (row_of(r, j) < p.M && n[t] < p.N) p.y[row_of(r, j) * p.ldy + n[t]] = __float2half_rn(acc[t][r][j]);
+        }
     }
 }
 
@@ -598,14 +658,14 @@ static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated
     }
     s.NT = 1;
     s.combine = norm && M <= 8;
-    const size_t sums = (size_t)2 * kWaves * WM * 1024, nat = natural_bytes(K, norm, index), rest = nat > sums ? nat : sums;
+    const size_t sums = (size_t)3 * kWaves * WM * 1024, nat = natural_bytes(K, norm, index), rest = nat > sums ? nat : sums;
     if (M <= (norm ? 8 : 16)) {
         s.lds = (size_t)M * (norm ? 2 : 1) * (K + 8) * 2 + rest;
         s.kept = s.lds <= 80 * 1024;
     }
     if (!s.kept) {
         while (s.NT * WM < 4 && (N + 32 * s.NT - 1) / (32 * s.NT) >= 192) s.NT *= 2;
-        s.lds = (size_t)2 * kWaves * WM * s.NT * 1024;
+        s.lds = (size_t)3 * kWaves * WM * s.NT * 1024;
     }
     return s;
 }
@@ -613,7 +673,7 @@ static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated
 static size_t laid_out_bytes(const ProductShape &s, int64_t M, int K, int O, bool norm)
 {
     if (s.kept) return 0;
-    if (!s.wide) return (size_t)M * K * (norm ? 4 : 2);
+    if (!s.wide) return (size_t)((K + O) / 128) * (norm && !s.combine ? 2 : 1) * 4096;
     return (size_t)((M + 32 * s.wide - 1) / (32 * s.wide)) * ((K + O) / 128) * s.wide * (norm ? 2 : 1) * 8192;
 }
 
@@ -638,7 +698,7 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
 {
     const bool gated = a.w[1].q4 != nullptr, norm = a.gamma != nullptr;
     const ProductShape s = product_shape(a.M, a.N, a.K, a.O, gated, norm, a.idx != nullptr);
-    const int  halves = norm ? 2 : 1;
+    const int  halves = norm && !s.combine ? 2 : 1;           // that go in one after the other
     Args p = {(const __half *)a.x, a.ldx, a.M, (const __half *)a.gamma, a.eps, a.idx, a.K, a.O, {a.w[0], a.w[1]}, a.N, (const __half *)a.residual, a.ldr,
               (__half *)a.y, a.ldy, (const __half *)a.workspace, (int)a.M, s.combine, 0, s.wide, halves, s.parts, 1,
               (float *)((char *)a.workspace + laid_out_bytes(s, a.M, a.K, a.O, norm))};
@@ -663,15 +723,15 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
         const int64_t per = gated ? 128 : 256;
         p.row_blocks = (uint32_t)((a.M + 32 * s.wide - 1) / (32 * s.wide));
         const int64_t grid = (a.N + per - 1) / per * s.parts * p.row_blocks;
-#define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, kThreads, 0, (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
+#define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, kWide, (size_t)2 * ((RT) * (HL) * 8192 + kWide * 64), (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
 #define ATOM_WIDE_ROWS(GATED)                                  \
     do {                                                       \
         if (s.wide == 1) {                                     \
-            if (norm) ATOM_WIDE(GATED, 1, 2, 4);               \
+            if (norm) ATOM_WIDE(GATED, 1, 2, 3);               \
             else      ATOM_WIDE(GATED, 1, 1, 4);               \
         } else {                                               \
-            if (norm) ATOM_WIDE(GATED, 2, 2, 4);               \
-            else      ATOM_WIDE(GATED, 2, 1, 4);               \
+            if (norm) ATOM_WIDE(GATED, 2, 2, 2);               \
+            else      ATOM_WIDE(GATED, 2, 1, 3);               \
         }                                                      \
     } while (0)
         if (gated) ATOM_WIDE_ROWS(true);
