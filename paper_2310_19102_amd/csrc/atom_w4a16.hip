@@ -28,7 +28,8 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float    f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves, kWide = 256;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kScales = 64;                                   // of a weight row, in LDS at once
 
 __device__ __forceinline__ h2 as_h2(uint32_t v) { return __builtin_bit_cast(h2, v); }
 __device__ __forceinline__ uint32_t bits(h2 v) { return __builtin_bit_cast(uint32_t, v); }
@@ -351,6 +352,11 @@ void w4a16_kernel(Args p)
     auto finish = [&](uint32_t tile) ATOM_INLINE {
         float *mine = red + (size_t)buffer * (kWaves * CT * 256);
         buffer ^= 1;                                         // (nobody writes a buffer before all have read what it held two tiles ago)
+        if (p.combine)                                       // rows 8 .. 15 to rows 0 .. 7
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[t][j] += __shfl_xor(acc[t][j], 32, 64);
 #pragma unroll
         for (int t = 0; t < CT; ++t)
 #pragma unroll
@@ -367,15 +373,9 @@ void w4a16_kernel(Args p)
             float sum[WM];
 #pragma unroll
             for (int x = 0; x < WM; ++x) {
-                float lo = 0.0f;
                 sum[x] = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
-                    const float *s = mine + (w * CT + x * NT) * 256 + at;
-                    sum[x] += s[0];
-                    if (p.combine) lo += s[32];
-                }
-                sum[x] += lo;
+                for (int w = 0; w < kWaves; ++w) sum[x] += mine[(w * CT + x * NT) * 256 + at];
             }
             float y = sum[0];
             if constexpr (GATED) y = gated(y, sum[WM - 1]);
@@ -431,184 +431,166 @@ void w4a16_kernel(Args p)
 typedef float f16 __attribute__((ext_vector_type(16)));
 
 // More than 16 rows: MFMA 32x32x16, whose operands bring twice the products for their bytes (lane l: row or column l & 31, the eight values
-// of k-chunk l >> 5; register r of the result: row 8 (r / 4) + 4 (l >> 5) + r % 4).  A workgroup has 32 RT rows; each of its four wavefronts
-// has two tiles of 32 weight rows for itself (the same of gate and up, or two of the one), and all of them share the activations, which
-// come a unit at a time through LDS.  `parts` workgroups share a tile's units where the tiles alone do not fill the card; their sums meet
-// in the workspace.
+// of k-chunk l >> 5; register r of the result: row 8 (r / 4) + 4 (l >> 5) + r % 4).  A workgroup has 32 RT rows and eight tiles of 32 weight
+// rows (of a gated call four of the gate and the same four of the up projection in turn).  Each wavefront has
+// one of them for all rows.  Activations and weights come a unit at a time through LDS, a tile by each wavefront.  `parts` workgroups share a tile's units where the tiles alone do not fill the card; their
+// sums meet in the workspace.  What the L2 delivers to all compute units together (about 8 TB/s) is the tightest bound beside memory, so
+// scales come 64 of a row at a time (by themselves, 2 bytes bring a line each: as much as the weights), and rows behind M are not fetched.
 template <bool GATED, int RT, int HL, int CH>
-__global__ __launch_bounds__(kWide, 1)
+__global__ __launch_bounds__(kThreads, 2)
 void w4a16_wide_kernel(Args p)
 {
-    constexpr int kOps = RT * HL;                            // row operands of an instruction's k-chunk
-    constexpr int kPieces = kOps * 512 / kWide;              // 16-byte pieces of a unit's activations that a thread brings
+    constexpr int kOps = RT * HL;                            // 16-byte pieces of a unit's activations that a thread brings
     extern __shared__ __align__(16) unsigned char s_all[];
     u4 (*s_act)[kOps * 512] = reinterpret_cast<u4 (*)[kOps * 512]>(s_all);                     // [2], and behind them
-    u4 (*s_turn)[kWide / 64][256] = reinterpret_cast<u4 (*)[kWide / 64][256]>(s_act + 2);      // [2]: the weights' way to the operands
+    u4 (*s_turn)[kWaves][128] = reinterpret_cast<u4 (*)[kWaves][128]>(s_act + 2);              // [2]: the weights' way to the operands
+    uint16_t (*s_scale)[kScales + 2] = reinterpret_cast<uint16_t (*)[kScales + 2]>(s_turn + 2);    // [256]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, kc = lane >> 5;
     const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, U = 2 * G - G4;
     const uint32_t block = blockIdx.x % p.row_blocks, rest = blockIdx.x / p.row_blocks, part = rest % (uint32_t)p.parts, tile = rest / (uint32_t)p.parts;
     const int begin = (int)((int64_t)part * U / p.parts), end = (int)((int64_t)(part + 1) * U / p.parts);
 
-    // output channels of this lane (>= N: computed and never stored); the weight rows that it loads, 64 bytes of 16 rows at a time, four lanes
-    // a row (lanes that go to one line apart, or one load after the other, hold up the cache until the line is there)
-    int64_t n[2];
-    uint32_t at4[2][2], at8[2][2], at_s[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int64_t n0 = ((int64_t)tile * (kWide / 64) + wave) * (GATED ? 32 : 64) + (GATED ? 0 : 32 * t);
-        n[t] = n0 + col;
-        at_s[t] = (uint32_t)min(n0 + (kc ? 0 : col), p.N - 1) * (uint32_t)(2 * G);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t row = (uint32_t)min(n0 + 16 * i + (lane >> 2), p.N - 1);
-            at4[t][i] = row * (uint32_t)(K4 >> 1) + (lane & 3) * 16;
-            at8[t][i] = row * (uint32_t)p.O + (lane & 3) * 16;
-        }
-    }
+    // The first weight row of a tile; its matrix.  (Columns >= N are computed and never stored.)
+    auto rows_of = [&](int t) ATOM_INLINE { return GATED ? ((int64_t)tile * (kWaves / 2) + t / 2) * 32 : ((int64_t)tile * kWaves + t) * 32; };
+    auto matrix_of = [&](int t) ATOM_INLINE { return GATED ? t & 1 : 0; };
+    // This wavefront brings tile `wave`, 64 bytes of 16 rows at a time, four lanes a row (lanes that go to one line apart, or one load after the
+    // other, hold up the cache until the line is there).
+    const W4 w = p.w[matrix_of(wave)];
+    const uint32_t row0 = (uint32_t)min(rows_of(wave) + (lane >> 2), p.N - 1), row1 = (uint32_t)min(rows_of(wave) + 16 + (lane >> 2), p.N - 1);
+    const uint32_t at4_0 = row0 * (uint32_t)(K4 >> 1) + (lane & 3) * 16, at4_1 = row1 * (uint32_t)(K4 >> 1) + (lane & 3) * 16;
+    const uint32_t at8_0 = row0 * (uint32_t)p.O + (lane & 3) * 16, at8_1 = row1 * (uint32_t)p.O + (lane & 3) * 16;
     // (a load is waited for with all before it, so a unit's weights and activations come the same way ahead)
-    struct Unit { u4 q[2][2], a[kPieces]; uint16_t scale[2]; };
+    struct Unit { u4 q[2], a[kOps]; };
     Unit ring[CH];
-    const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + (int64_t)block * U * (kOps * 512) + tid;
+    const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + (int64_t)block * U * (kOps * 512);
+    int piece[RT];                                           // (lanes of rows >= M take the last row's)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) piece[r] = (tid & ~31) + min(tid & 31, max((int)(p.M - ((int64_t)block * RT + r) * 32) - 1, 0));
     int load_u = begin;
     auto load = [&](Unit &e) ATOM_INLINE {
         const int  u = min(load_u, end - 1), v = u - G4;
         const bool is4 = u < G4;
+        const u4 *from = acts + (int64_t)u * (kOps * 512);
 #pragma unroll
-        for (int c = 0; c < kPieces; ++c) e.a[c] = acts[(int64_t)u * (kOps * 512) + c * kWide];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const W4 &w = p.w[GATED ? t : 0];
-            const uint8_t *base = is4 ? w.q4 + u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t a4 = at4[t][i], a8 = at8[t][i];
-                e.q[t][i] = *reinterpret_cast<const u4 *>(base + (is4 ? a4 : a8));
-            }
-            e.scale[t] = *reinterpret_cast<const uint16_t *>(reinterpret_cast<const uint8_t *>(w.scale) + at_s[t] + 2 * (is4 ? u : G4 + (v >> 1)));
-        }
+        for (int c = 0; c < kOps; ++c) e.a[c] = from[c * 512 + piece[c % RT]];
+        const uint8_t *base = is4 ? w.q4 + u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64;
+        e.q[0] = *reinterpret_cast<const u4 *>(base + (is4 ? at4_0 : at8_0));
+        e.q[1] = *reinterpret_cast<const u4 *>(base + (is4 ? at4_1 : at8_1));
         ++load_u;
     };
     auto keep = [&](const Unit &e, int u) ATOM_INLINE {
 #pragma unroll
-        for (int c = 0; c < kPieces; ++c) s_act[(u - begin) & 1][c * kWide + tid] = e.a[c];
+        for (int c = 0; c < kOps; ++c) s_act[(u - begin) & 1][c * 512 + tid] = e.a[c];
         // piece p of row r lies at 4 r + (p ^ (r / 4 & 3)): the lanes of a chunk read all banks
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) s_turn[(u - begin) & 1][wave][128 * t + 64 * i + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = e.q[t][i];
+        for (int i = 0; i < 2; ++i) s_turn[(u - begin) & 1][wave][64 * i + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = e.q[i];
     };
 
-    f16 acc[2][RT] = {};
+    // the scales of kScales groups from that of unit u on
+    int scale0 = 0, scale_end = begin;
+    auto fetch_scales = [&](int u) ATOM_INLINE {
+        scale0 = u < G4 ? u : G4 + ((u - G4) >> 1);
+        const int count = min(kScales, G - scale0);
+        scale_end = scale0 + count < G ? scale0 + count : U; // (units beyond G4 are halves of groups: the last groups are there as a whole or not at all)
+        if (scale_end > G4 && scale_end < U) scale_end = G4 + 2 * (scale_end - G4);
+        for (int e = tid; e < 256 * count; e += kThreads) {
+            const int row = e / count, k = e - row * count;
+            s_scale[row][k] = p.w[matrix_of(row >> 5)].scale[min(rows_of(row >> 5) + (row & 31), p.N - 1) * G + scale0 + k];
+        }
+    };
+    f16 acc[RT] = {};
     auto compute = [&](const Unit &e, int u) ATOM_INLINE {
         const u4 *a = s_act[(u - begin) & 1] + lane;
-        u4 q[2][2];
+        u4 q[2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) q[t][i] = s_turn[(u - begin) & 1][wave][128 * t + 4 * col + (((2 * kc + i) ^ (col >> 2)) & 3)];
-        f16 sum[2][RT] = {};
-        h8 x[2][kOps], y[2][2];                              // the next k-chunk's operands come and are widened between this one's products
+        for (int i = 0; i < 2; ++i) q[i] = s_turn[(u - begin) & 1][wave][4 * col + (((2 * kc + i) ^ (col >> 2)) & 3)];
+        f16 sum[RT] = {};
+        h8 x[2][kOps];                                       // the next k-chunk's operands come while this one's are in use
         auto operands = [&](int i) ATOM_INLINE {
 #pragma unroll
-            for (int o = 0; o < kOps; ++o) x[i & 1][o] = __builtin_bit_cast(h8, a[(o * 8 + i) * 64]);
-        };
-        auto widened = [&](int i, bool is4) ATOM_INLINE {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-                y[i & 1][t] = is4 ? widen4(q[t][i >> 2][i & 3]) : widen8(q[t][i >> 1 & 1][2 * (i & 1)], q[t][i >> 1 & 1][2 * (i & 1) + 1]);
-        };
-        auto products = [&](int i) ATOM_INLINE {
-#pragma unroll
-            for (int o = 0; o < kOps; ++o)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) sum[t][o % RT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i & 1][o], y[i & 1][t], sum[t][o % RT], 0, 0, 0);
+            for (int o = 0; o < kOps; ++o) x[i & 1][o] = __builtin_bit_cast(h8, a[o * 512 + i * 64]);
         };
         auto chunks = [&](int count, bool is4) ATOM_INLINE {
             operands(0);
-            widened(0, is4);
 #pragma unroll
             for (int i = 0; i < count; ++i) {
-                if (i + 1 < count) {
-                    operands(i + 1);
-                    widened(i + 1, is4);
-                }
-                products(i);
-                // reads first, then a product and its share of the widening in turn: a wavefront's next product waits for the matrix unit, and
-                // everything behind it in the program with it
-                __builtin_amdgcn_sched_group_barrier(0x100, kOps, 0);
+                if (i + 1 < count) operands(i + 1);
+                __builtin_amdgcn_sched_barrier(0);           // (or the reads move to where they are used)
+                const h8 y = is4 ? widen4(q[i >> 2][i & 3]) : widen8(q[i >> 1 & 1][2 * (i & 1)], q[i >> 1 & 1][2 * (i & 1) + 1]);
 #pragma unroll
-                for (int k = 0; k < 2 * kOps; ++k) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, (20 + 2 * kOps - 1) / (2 * kOps), 0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                for (int o = 0; o < kOps; ++o) sum[o % RT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i & 1][o], y, sum[o % RT], 0, 0, 0);
             }
         };
         if (u < G4) chunks(8, true);
         else        chunks(4, false);
+        const float s = __half2float(__ushort_as_half(s_scale[32 * wave + col][(u < G4 ? u : G4 + ((u - G4) >> 1)) - scale0]));
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            float s = __half2float(__ushort_as_half(e.scale[t]));
-            s = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * col, __builtin_bit_cast(int, s)));
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) acc[t][r][j] = fmaf(sum[t][r][j], s, acc[t][r][j]);
-        }
+            for (int j = 0; j < 16; ++j) acc[r][j] = fmaf(sum[r][j], s, acc[r][j]);
     };
 
 #pragma unroll
     for (int s = 0; s < CH; ++s) load(ring[s]);
     all_loads_done();
+    fetch_scales(begin);
     keep(ring[0], begin);
     __syncthreads();
-    for (int u = begin; u < end; u += CH)
+    for (int u = begin; u < end; u += CH) {
+        if (u + CH > scale_end && scale_end < end) {         // (every wavefront is past its last use)
+            fetch_scales(u);
+            __syncthreads();
+        }
 #pragma unroll
         for (int s = 0; s < CH; ++s) {                       // (no way out of the loop here: the compiler would wait at its head for what had been asked for by then)
             keep(ring[(s + 1) % CH], u + s + 1);
             if (u + s < end) compute(ring[s], u + s);
             load(ring[s]);
-            __syncthreads();                                 // (all have read this unit's activations, the next one's are there)
+            __syncthreads();                                 // (all have read this unit, the next one is there)
         }
+    }
 
-    const int64_t m0 = (int64_t)block * (32 * RT) + 4 * kc;
+    const int64_t n = rows_of(wave) + col, m0 = (int64_t)block * (32 * RT) + 4 * kc;
     auto row_of = [&](int r, int j) ATOM_INLINE { return m0 + 32 * r + 8 * (j >> 2) + (j & 3); };
     if (p.parts > 1) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-            if (n[t] < p.N)
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (row_of(r, j) < p.M) p.sums[(((int64_t)part * (GATED ? 2 : 1) + (GATED ? t : 0)) * p.M + row_of(r, j)) * p.N + n[t]] = acc[t][r][j];
-        return;
-    }
-    if constexpr (GATED) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (row_of(r, j) < p.M && n[0] < p.N) p.y[row_of(r, j) * p.ldy + n[0]] = __float2half_rn(gated(acc[0][r][j], acc[1][r][j]));
-    } else {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if (p.residual)                                  // (all of them on their way at once)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    uint16_t res[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) res[j] = reinterpret_cast<const uint16_t *>(p.residual)[min(row_of(r, j), p.M - 1) * p.ldr + min(n[t], p.N - 1)];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[t][r][j] += __half2float(__ushort_as_half(res[j]));
-                }
+        if (n < p.N)
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (row_of(r, j) < p.M && n[t] < p.N) p.y[row_of(r, j) * p.ldy + n[t]] = __float2half_rn(acc[t][r][j]);
-        }
+                    if (row_of(r, j) < p.M) p.sums[(((int64_t)part * (GATED ? 2 : 1) + matrix_of(wave)) * p.M + row_of(r, j)) * p.N + n] = acc[r][j];
+        return;
+    }
+    if constexpr (GATED) {                                   // the wavefront after a gate's has the up projection
+        float *s_up = reinterpret_cast<float *>(s_all) + (wave >> 1) * (RT * 1024) + lane;
+        if (wave & 1)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s_up[(16 * r + j) * 64] = acc[r][j];
+        __syncthreads();
+        if (wave & 1) return;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (row_of(r, j) < p.M && n < p.N) p.y[row_of(r, j) * p.ldy + n] = __float2half_rn(gated(acc[r][j], s_up[(16 * r + j) * 64]));
+    } else {
+        if (p.residual)                                      // (all of them on their way at once)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                uint16_t res[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) res[j] = reinterpret_cast<const uint16_t *>(p.residual)[min(row_of(r, j), p.M - 1) * p.ldr + min(n, p.N - 1)];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[r][j] += __half2float(__ushort_as_half(res[j]));
+            }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (row_of(r, j) < p.M && n < p.N) p.y[row_of(r, j) * p.ldy + n] = __float2half_rn(acc[r][j]);
     }
 }
 
@@ -723,15 +705,15 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
         const int64_t per = gated ? 128 : 256;
         p.row_blocks = (uint32_t)((a.M + 32 * s.wide - 1) / (32 * s.wide));
         const int64_t grid = (a.N + per - 1) / per * s.parts * p.row_blocks;
-#define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, kWide, (size_t)2 * ((RT) * (HL) * 8192 + kWide * 64), (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
+#define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, kThreads, (size_t)2 * ((RT) * (HL) * 8192 + kWaves * 2048) + 256 * (kScales + 2) * 2, (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
 #define ATOM_WIDE_ROWS(GATED)                                  \
     do {                                                       \
         if (s.wide == 1) {                                     \
-            if (norm) ATOM_WIDE(GATED, 1, 2, 3);               \
+            if (norm) ATOM_WIDE(GATED, 1, 2, 4);               \
             else      ATOM_WIDE(GATED, 1, 1, 4);               \
         } else {                                               \
-            if (norm) ATOM_WIDE(GATED, 2, 2, 2);               \
-            else      ATOM_WIDE(GATED, 2, 1, 3);               \
+            if (norm) ATOM_WIDE(GATED, 2, 2, 4);               \
+            else      ATOM_WIDE(GATED, 2, 1, 4);               \
         }                                                      \
     } while (0)
         if (gated) ATOM_WIDE_ROWS(true);
