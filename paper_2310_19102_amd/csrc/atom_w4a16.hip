@@ -81,6 +81,44 @@ __device__ __forceinline__ int row_place(int k, int K4)
     return 16 * g + (k < K4 ? 4 * (j & 3) + (j >> 2) : (j & 8) + 4 * (j & 1) + ((j >> 1) & 3));
 }
 
+__device__ __forceinline__ uint32_t half_of(const uint4 &v, int i) { return ((i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w) >> (16 * (i & 1))) & 0xffffu; }
+__device__ __forceinline__ float value_of(uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); }
+
+// A normed value as hi (the low half) and lo.  (Of what is not finite hi says it all: infinity minus infinity would be NaN.)
+__device__ __forceinline__ uint32_t halves_of(float y)
+{
+    const __half h = __float2half_rn(y), l = __hisinf(h) || __hisnan(h) ? __ushort_as_half(0) : __float2half_rn(y - __half2float(h));
+    return (uint32_t)__half_as_ushort(h) | (uint32_t)__half_as_ushort(l) << 16;
+}
+
+// The eight halves in the low or the high parts of w, in the order in which the codes come out of their word (INT4), or as they are.
+__device__ __forceinline__ void in_order(uint32_t (&w)[8], bool is4)
+{
+    if (!is4) return;
+    const uint32_t t1 = w[1], t2 = w[2], t3 = w[3];          // 0 4 1 5 2 6 3 7
+    w[1] = w[4], w[2] = t1, w[3] = w[5], w[4] = t2, w[5] = w[6], w[6] = t3;
+}
+template <bool HIGH>
+__device__ __forceinline__ uint4 packed(const uint32_t (&w)[8])
+{
+    constexpr uint32_t sel = HIGH ? 0x07060302u : 0x05040100u;
+    return make_uint4(__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel), __builtin_amdgcn_perm(w[5], w[4], sel),
+                      __builtin_amdgcn_perm(w[7], w[6], sel));
+}
+
+template <int THREADS>
+__device__ __forceinline__ float sum_over_threads(float sum, float *s_sum)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) sum += s_sum[w];
+    return sum;
+}
+
 // What a thread reads of a row first, so that it is on its way before anything waits.
 struct Front { uint4 x, gamma; int4 i0, i1; };
 
@@ -105,33 +143,20 @@ __device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict_
 {
     const int tid = threadIdx.x, blocks = p.K / 8, K4 = p.K - p.O;
     const uint4 *row = reinterpret_cast<const uint4 *>(x);
-    auto half_of = [](const uint4 &v, int i) -> uint32_t { return ((i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w) >> (16 * (i & 1))) & 0xffffu; };
-    auto value = [](uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); };
     if (p.gamma) {
         float sum = 0.0f;
         for (int b = tid; b < blocks; b += THREADS) {
             const uint4 v = b == tid ? f.x : row[b];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(value(half_of(v, i)), value(half_of(v, i)), sum);
+            for (int i = 0; i < 8; ++i) sum = fmaf(value_of(half_of(v, i)), value_of(half_of(v, i)), sum);
         }
-#pragma unroll
-        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
-        if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
-        __syncthreads();
-        sum = 0.0f;
-        for (int w = 0; w < THREADS / 64; ++w) sum += s_sum[w];
+        sum = sum_over_threads<THREADS>(sum, s_sum);
         const float r = 1.0f / sqrtf(sum / (float)p.K + p.eps);
         for (int b = tid; b < blocks; b += THREADS) {
             const uint4 v = b == tid ? f.x : row[b], g = b == tid ? f.gamma : reinterpret_cast<const uint4 *>(p.gamma)[b];
             uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float y = value(half_of(v, i)) * r * value(half_of(g, i));
-                const __half h = __float2half_rn(y);
-                // (of what is not finite hi says it all: infinity minus infinity would be NaN)
-                const __half l = __hisinf(h) || __hisnan(h) ? __ushort_as_half(0) : __float2half_rn(y - __half2float(h));
-                w[i] = (uint32_t)__half_as_ushort(h) | (uint32_t)__half_as_ushort(l) << 16;
-            }
+            for (int i = 0; i < 8; ++i) w[i] = halves_of(value_of(half_of(v, i)) * r * value_of(half_of(g, i)));
             reinterpret_cast<uint4 *>(nat)[2 * b] = make_uint4(w[0], w[1], w[2], w[3]);
             reinterpret_cast<uint4 *>(nat)[2 * b + 1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
@@ -158,45 +183,76 @@ __device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict_
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = half_of(v, i);
         }
-        if (8 * b < K4) {
-            const uint32_t t1 = w[1], t2 = w[2], t3 = w[3];                           // 0 4 1 5 2 6 3 7
-            w[1] = w[4], w[2] = t1, w[3] = w[5], w[4] = t2, w[5] = w[6], w[6] = t3;
-        }
-        auto pack = [&](uint32_t sel) {
-            return make_uint4(__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel), __builtin_amdgcn_perm(w[5], w[4], sel),
-                              __builtin_amdgcn_perm(w[7], w[6], sel));
-        };
-        place(8 * b, 0, pack(0x05040100u));
-        if (p.gamma) place(8 * b, 1, pack(0x07060302u));
+        in_order(w, 8 * b < K4);
+        place(8 * b, 0, packed<false>(w));
+        if (p.gamma) place(8 * b, 1, packed<true>(w));
     }
 }
 
 __host__ __device__ constexpr size_t natural_bytes(int K, bool norm, bool index) { return norm ? 4 * (size_t)K : index ? 2 * (size_t)K : 0; }
 
-// A row to a workgroup, into the workspace, in the order in which the product's loads take it (64 lanes of 16 bytes in a row): for every unit
-// and half the operands of its instructions, of a tile of 16 rows, or (WIDE) of tiles of 32.
+// Rows into the workspace, in the order in which the product's loads take them (64 lanes of 16 bytes in a row): for every unit and half the operands
+// of its instructions, of a tile of 16 rows, or (WIDE) of tiles of 32.
+template <bool WIDE>
+__device__ __forceinline__ void put(const Args &p, uint4 *out, int64_t m, int k, int half, const uint4 &v)
+{
+    const int  K4 = p.K - p.O, G4 = K4 >> 7, U = (p.K + p.O) >> 7, j = k - K4;
+    const bool is4 = k < K4;
+    const int  u = is4 ? k >> 7 : G4 + (j >> 6);
+    if constexpr (!WIDE) {
+        const int place = row_place(k, K4) & (is4 ? 15 : 7);                              // (instruction, chunk)
+        const int tile = p.combine ? 0 : half, row = (int)m + (p.combine && half ? 8 : 0);
+        out[((((int64_t)u * p.halves + tile) * 4 + (place >> 2)) * 4 + (place & 3)) * 16 + row] = v;
+    } else {
+        const int i = is4 ? (k >> 3) & 7 : (j >> 3) & 3, c = is4 ? (k >> 6) & 1 : (j >> 5) & 1;
+        const int64_t block = m / (32 * p.wide), t = m / 32 % p.wide;
+        out[((((block * U + u) * p.halves + half) * p.wide + t) * 8 + i) * 64 + c * 32 + m % 32] = v;
+    }
+}
+
+// With an index: a row to a workgroup, gathered in LDS (from memory 2 bytes at a time it takes longer: eight rows of 4096 channels behind the norm 5.6 us
+// against 4.1).  Bound by its chain of reads, barriers and launch; a thread for eight channels up to 8192 of them.
+template <bool WIDE, int THREADS>
+__global__ __launch_bounds__(THREADS)
+void w4a16_gather_kernel(Args p, uint4 *out)
+{
+    extern __shared__ uint32_t s_nat[];
+    __shared__ float s_sum[THREADS / 64];
+    const int64_t m = blockIdx.x;
+    const __half *x = p.x + m * p.ldx;
+    lay_out<THREADS>(p, x, front_of<THREADS>(p, x), s_nat, s_sum, [&](int k, int half, const uint4 &v) { put<WIDE>(p, out, m, k, half, v); });
+}
+
+constexpr int kRowChannels = 4096;                            // of a row, of a workgroup
+
+// Without: 4096 channels of a row to a workgroup, each of which adds up the whole row.
 template <bool WIDE>
 __global__ __launch_bounds__(512)
 void w4a16_rows_kernel(Args p, uint4 *out)
 {
-    extern __shared__ uint32_t s_nat[];
     __shared__ float s_sum[8];
+    const int tid = threadIdx.x, blocks = p.K / 8, b = (int)blockIdx.y * (kRowChannels / 8) + tid, k = 8 * min(b, blocks - 1);
     const int64_t m = blockIdx.x;
-    const int K4 = p.K - p.O, G4 = K4 >> 7, U = (p.K + p.O) >> 7;
     const __half *x = p.x + m * p.ldx;
-    lay_out<512>(p, x, front_of<512>(p, x), s_nat, s_sum, [&](int k, int half, const uint4 &v) {
-        const bool is4 = k < K4;
-        const int  j = k - K4, u = is4 ? k >> 7 : G4 + (j >> 6);
-        if constexpr (!WIDE) {
-            const int place = row_place(k, K4) & (is4 ? 15 : 7);                          // (instruction, chunk)
-            const int tile = p.combine ? 0 : half, row = (int)m + (p.combine && half ? 8 : 0);
-            out[((((int64_t)u * p.halves + tile) * 4 + (place >> 2)) * 4 + (place & 3)) * 16 + row] = v;
-        } else {
-            const int i = is4 ? (k >> 3) & 7 : (j >> 3) & 3, c = is4 ? (k >> 6) & 1 : (j >> 5) & 1;
-            const int64_t block = m / (32 * p.wide), t = m / 32 % p.wide;
-            out[((((block * U + u) * p.halves + half) * p.wide + t) * 8 + i) * 64 + c * 32 + m % 32] = v;
+    const uint4 v = *reinterpret_cast<const uint4 *>(x + k), g = p.gamma ? *reinterpret_cast<const uint4 *>(p.gamma + k) : v;
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = half_of(v, i);
+    if (p.gamma) {
+        float sum = 0.0f;
+        for (int j = tid; j < blocks; j += 512) {
+            const uint4 y = reinterpret_cast<const uint4 *>(x)[j];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(value_of(half_of(y, i)), value_of(half_of(y, i)), sum);
         }
-    });
+        const float r = 1.0f / sqrtf(sum_over_threads<512>(sum, s_sum) / (float)p.K + p.eps);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = halves_of(value_of(w[i]) * r * value_of(half_of(g, i)));
+    }
+    if (b >= blocks) return;
+    in_order(w, k < p.K - p.O);
+    put<WIDE>(p, out, m, k, 0, packed<false>(w));
+    if (p.gamma) put<WIDE>(p, out, m, k, 1, packed<true>(w));
 }
 
 // ---- the product
@@ -487,17 +543,16 @@ void w4a16_wide_kernel(Args p)
         for (int i = 0; i < 2; ++i) s_turn[(u - begin) & 1][wave][64 * i + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = e.q[i];
     };
 
-    // the scales of kScales groups from that of unit u on
+    // the scales of kScales groups from that of unit u on, each wavefront those of its own rows
+    uint16_t *my_scales = s_scale[32 * wave];
     int scale0 = 0, scale_end = begin;
     auto fetch_scales = [&](int u) ATOM_INLINE {
         scale0 = u < G4 ? u : G4 + ((u - G4) >> 1);
         const int count = min(kScales, G - scale0);
-        scale_end = scale0 + count < G ? scale0 + count : U; // (units beyond G4 are halves of groups: the last groups are there as a whole or not at all)
-        if (scale_end > G4 && scale_end < U) scale_end = G4 + 2 * (scale_end - G4);
-        for (int e = tid; e < 256 * count; e += kThreads) {
-            const int row = e / count, k = e - row * count;
-            s_scale[row][k] = p.w[matrix_of(row >> 5)].scale[min(rows_of(row >> 5) + (row & 31), p.N - 1) * G + scale0 + k];
-        }
+        scale_end = scale0 + count <= G4 ? scale0 + count : G4 + 2 * (scale0 + count - G4);
+        const uint16_t *from = w.scale + scale0 + min(lane, count - 1);
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r) my_scales[r * (kScales + 2) + lane] = from[min(rows_of(wave) + r, p.N - 1) * G];
     };
     f16 acc[RT] = {};
     auto compute = [&](const Unit &e, int u) ATOM_INLINE {
@@ -524,7 +579,7 @@ void w4a16_wide_kernel(Args p)
         };
         if (u < G4) chunks(8, true);
         else        chunks(4, false);
-        const float s = __half2float(__ushort_as_half(s_scale[32 * wave + col][(u < G4 ? u : G4 + ((u - G4) >> 1)) - scale0]));
+        const float s = __half2float(__ushort_as_half(my_scales[col * (kScales + 2) + (u < G4 ? u : G4 + ((u - G4) >> 1)) - scale0]));
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -538,10 +593,7 @@ void w4a16_wide_kernel(Args p)
     keep(ring[0], begin);
     __syncthreads();
     for (int u = begin; u < end; u += CH) {
-        if (u + CH > scale_end && scale_end < end) {         // (every wavefront is past its last use)
-            fetch_scales(u);
-            __syncthreads();
-        }
+        if (u + CH > scale_end && scale_end < end) fetch_scales(u);
 #pragma unroll
         for (int s = 0; s < CH; ++s) {                       // (no way out of the loop here: the compiler would wait at its head for what had been asked for by then)
             keep(ring[(s + 1) % CH], u + s + 1);
@@ -672,7 +724,7 @@ bool w4a16_fits(int64_t M, int64_t N, int K, int O, bool gated)
     const int64_t G = K / 128, widest = (K - O) / 2 > O ? (K - O) / 2 : O;
     if (N > 0xffffffffLL / (widest > 2 * G ? widest : 2 * G)) return false;           // 32-bit offsets
     // workgroups: a row each, tiles of outputs (of 128 at least where there are many rows) and rows, 256 outputs of a join each
-    const int64_t most = atom_launch::kMostThreads / kThreads;
+    const int64_t most = atom_launch::kMostThreads / 1024;
     return M <= most && (N + 15) / 16 <= most && (N + 127) / 128 * 16 <= most / ((M + 31) / 32) && M <= most * 256 / N;
 }
 
@@ -692,19 +744,27 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
             const hipError_t err = atom_launch::ensure_dynamic_lds(opt, reinterpret_cast<const void *>(kern), lds);   \
             if (err != hipSuccess) return err;                                                                        \
         }                                                                                                             \
-        hipLaunchKernelGGL(kern, dim3((unsigned)(grid)), dim3(threads), lds, stream, __VA_ARGS__);                    \
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(threads), lds, stream, __VA_ARGS__);                                \
         const hipError_t err = hipGetLastError();                                                                     \
         if (err != hipSuccess) return err;                                                                            \
     } while (0)
-    const size_t nat = natural_bytes(a.K, norm, a.idx != nullptr);
     uint4 *laid_out = (uint4 *)a.workspace;
-    if (s.wide)       ATOM_LAUNCH(a.M, 512, nat, w4a16_rows_kernel<true>, p, laid_out);
-    else if (!s.kept) ATOM_LAUNCH(a.M, 512, nat, w4a16_rows_kernel<false>, p, laid_out);
+#define ATOM_ROWS(WIDE)                                                                                                               \
+    do {                                                                                                                              \
+        const size_t nat = natural_bytes(a.K, norm, true);                                                                            \
+        const dim3 split((unsigned)a.M, (unsigned)((a.K + kRowChannels - 1) / kRowChannels));                                         \
+        if (!a.idx)             ATOM_LAUNCH(split, 512, 0, w4a16_rows_kernel<WIDE>, p, laid_out);                                     \
+        else if (a.K <= 4096)   ATOM_LAUNCH((unsigned)a.M, 512, nat, (w4a16_gather_kernel<WIDE, 512>), p, laid_out);                  \
+        else                    ATOM_LAUNCH((unsigned)a.M, 1024, nat, (w4a16_gather_kernel<WIDE, 1024>), p, laid_out);                \
+    } while (0)
+    if (s.wide)       ATOM_ROWS(true);
+    else if (!s.kept) ATOM_ROWS(false);
+#undef ATOM_ROWS
 
     if (s.wide) {
         const int64_t per = gated ? 128 : 256;
         p.row_blocks = (uint32_t)((a.M + 32 * s.wide - 1) / (32 * s.wide));
-        const int64_t grid = (a.N + per - 1) / per * s.parts * p.row_blocks;
+        const unsigned grid = (unsigned)((a.N + per - 1) / per * s.parts * p.row_blocks);
 #define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, kThreads, (size_t)2 * ((RT) * (HL) * 8192 + kWaves * 2048) + 256 * (kScales + 2) * 2, (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
 #define ATOM_WIDE_ROWS(GATED)                                  \
     do {                                                       \
@@ -712,8 +772,8 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
             if (norm) ATOM_WIDE(GATED, 1, 2, 4);               \
             else      ATOM_WIDE(GATED, 1, 1, 4);               \
         } else {                                               \
-            if (norm) ATOM_WIDE(GATED, 2, 2, 4);               \
-            else      ATOM_WIDE(GATED, 2, 1, 4);               \
+            if (norm) ATOM_WIDE(GATED, 2, 2, 3);               \
+            else      ATOM_WIDE(GATED, 2, 1, 3);               \
         }                                                      \
     } while (0)
         if (gated) ATOM_WIDE_ROWS(true);
@@ -721,7 +781,7 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
 #undef ATOM_WIDE_ROWS
 #undef ATOM_WIDE
         if (s.parts > 1) {
-            const int64_t groups = (a.M * a.N + 255) / 256;
+            const unsigned groups = (unsigned)((a.M * a.N + 255) / 256);
             if (gated) ATOM_LAUNCH(groups, 256, 0, w4a16_join_kernel<true>, p);
             else       ATOM_LAUNCH(groups, 256, 0, w4a16_join_kernel<false>, p);
         }
