@@ -273,13 +273,13 @@ __device__ __forceinline__ void store(const Args &p, int64_t m, int64_t n, float
     p.y[m * p.ldy + n] = __float2half_rn(y);
 }
 
-// Up to 16 rows.  A workgroup has 16 NT output channels (of gate and of up); its eight wavefronts share the K channels in runs of units, and their
-// sums meet in LDS, added in order.  A unit is 64 bytes of every weight row: an INT4 group, or half of an INT8 group.  CH units of a
-// wavefront are on their way while it works, across the tiles that the workgroup has in turn; every unit takes the same loads, also those
-// behind the last (one address for all lanes then), so that none is waited for before its turn.
+// Up to 16 rows.  A workgroup has 16 NT output channels (of gate and of up); its eight wavefronts share the K channels in runs of INT4 groups and
+// every eighth half of an INT8 group each (64 bytes of every weight row either way: a unit), and their sums meet in LDS, added in order.  A wavefront's
+// next unit is on its way while it works, across the tiles that the workgroup has in turn (behind the last, one address for all lanes).  With a tile or
+// two for a workgroup the time is latencies, among them the code's own way to the wavefronts: two to five units under way in unrolled code were slower.
 //   HL: halves of the activations that go in one after the other (2: hi and lo)
 //   KEPT: the activations are laid out in LDS by the workgroup itself (HL = 1), under way with the first weights
-template <int NT, bool GATED, int HL, int CH, bool KEPT>
+template <int NT, bool GATED, int HL, bool KEPT>
 __global__ __launch_bounds__(kThreads, KEPT ? 4 : 2)
 void w4a16_kernel(Args p)
 {
@@ -289,8 +289,8 @@ void w4a16_kernel(Args p)
     __shared__ float s_part[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, kc = lane >> 4;
-    const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, U = 2 * G - G4;
-    const int begin = wave * U / kWaves, end = (wave + 1) * U / kWaves;
+    const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, V = 2 * (G - G4);
+    const int begin = wave * G4 / kWaves, n = (wave + 1) * G4 / kWaves - begin;           // INT4 units of this wavefront
     const int rows = p.rows, lds_row = p.K + 8;
 
     Front front;
@@ -306,86 +306,113 @@ void w4a16_kernel(Args p)
 
     // A load brings 64 bytes of 16 rows, four lanes a row: lanes that go to one line apart, or one load after the other, hold up the cache until the line
     // is there.  The operands want a row in one lane of each 16, so the pieces go through LDS.
-    struct Unit { u4 q[CT], a[KEPT ? 1 : 4 * AT]; uint16_t scale; };
-    Unit ring[CH];
+    struct { u4 q[CT], a[KEPT ? 1 : 4 * AT]; uint16_t scale; } e;    // (lane 16 t + c: the scale of row c of tile t)
+    struct { u4 q[CT], a[KEPT ? 1 : 2 * AT]; uint16_t scale; } half;                // of an INT8 group
     uint32_t load_tile = blockIdx.x;                         // of the unit that is loaded next
-    int load_u = begin;
-    uint32_t at4[CT], at8[CT], at_s;                         // bytes from the arrays' beginnings (below 4 GiB: host)
+    int load_i = 0;
+    uint32_t at4[CT], at_scale;                              // (bytes from the arrays' beginnings are below 4 GiB: host)
+    const uint16_t *scale_of = kc < CT && kc >= NT ? p.w[WM - 1].scale : p.w[0].scale;
     auto rows_of = [&](uint32_t tile) ATOM_INLINE {
         const bool live = tile < p.tiles;
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            const uint32_t row = (uint32_t)min((int64_t)tile * (16 * NT) + 16 * (t % NT) + (lane >> 2), p.N - 1);
-            at4[t] = live ? row * (uint32_t)(K4 >> 1) + (lane & 3) * 16 : 0;
-            at8[t] = live ? row * (uint32_t)p.O + (lane & 3) * 16 : 0;
+            const uint32_t r = (uint32_t)min((int64_t)tile * (16 * NT) + 16 * (t % NT) + (lane >> 2), p.N - 1);
+            at4[t] = live ? r * (uint32_t)(K4 >> 1) + (lane & 3) * 16 : 0;
         }
-        // (lane 16 t + c: the scale of row c of tile t; the others go where lane 0 does)
-        at_s = live ? (uint32_t)min((int64_t)tile * (16 * NT) + (kc < CT ? 16 * (kc % NT) + col : 0), p.N - 1) * (uint32_t)(2 * G) : 0;
+        const uint32_t r = (uint32_t)min((int64_t)tile * (16 * NT) + (kc < CT ? 16 * (kc % NT) + col : 0), p.N - 1);
+        at_scale = live ? r * (uint32_t)G : 0;
     };
-    const uint8_t *my_scale = reinterpret_cast<const uint8_t *>(kc < CT && kc >= NT ? p.w[WM - 1].scale : p.w[0].scale);
-    auto load = [&](Unit &e) ATOM_INLINE {
-        const bool is4 = load_u < G4;
-        const int  v = load_u - G4, k = is4 ? load_u * 128 : K4 + v * 64;
+    auto load = [&]() ATOM_INLINE {
+        const bool live = load_i < n;
+        const int  u = begin + (live ? load_i : 0);
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            const W4 &w = p.w[t / NT];
-            const uint8_t *base = is4 ? w.q4 + load_u * 64 : reinterpret_cast<const uint8_t *>(w.q8) + v * 64;
-            const uint32_t a4 = at4[t], a8 = at8[t];
-            e.q[t] = *reinterpret_cast<const u4 *>(base + (is4 ? a4 : a8));
+            const uint32_t at = live ? at4[t] : 0;
+            e.q[t] = *reinterpret_cast<const u4 *>(p.w[t / NT].q4 + u * 64 + at);
         }
-        e.scale = *reinterpret_cast<const uint16_t *>(my_scale + at_s + 2 * (k >> 7));
+        e.scale = scale_of[u + (live ? at_scale : 0)];
         if constexpr (!KEPT) {
 #pragma unroll
             for (int a = 0; a < AT; ++a)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) e.a[4 * a + c] = acts[((int64_t)load_u * AT + a) * 256 + c * 64];
+                for (int c = 0; c < 4; ++c) e.a[4 * a + c] = acts[((int64_t)u * AT + a) * 256 + c * 64];
         }
-        if (++load_u == end) {
-            load_u = begin;
+        if (++load_i >= n) {
+            load_i = 0;
             load_tile += gridDim.x;
             rows_of(load_tile);
         }
     };
-    f4 acc[CT] = {};
-    auto compute = [&](const Unit &e, int u) ATOM_INLINE {
-        f4 part[CT] = {};
-        auto activations = [&](int a, int k, int c) ATOM_INLINE {
-            if constexpr (KEPT) return *reinterpret_cast<const h8 *>(s_act + k + c * 32);
-            else return __builtin_bit_cast(h8, e.a[4 * a + c]);
-        };
-        // piece p of row r lies at 4 r + (p ^ (r / 4 & 3)): the 16 lanes of a chunk read all banks
-        u4 q[CT];
-#pragma unroll
-        for (int t = 0; t < CT; ++t) s_turn[t * 64 + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = e.q[t];
-#pragma unroll
-        for (int t = 0; t < CT; ++t) q[t] = s_turn[t * 64 + 4 * col + ((kc ^ (col >> 2)) & 3)];
-        if (u < G4) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int t = 0; t < CT; ++t) {
-                    const h8 w = widen4(q[t][c]);
-#pragma unroll
-                    for (int a = 0; a < AT; ++a) part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(activations(a, u * 128, c), w, part[t], 0, 0, 0);
-                }
-        } else {
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int t = 0; t < CT; ++t) {
-                    const h8 w = widen8(q[t][2 * c], q[t][2 * c + 1]);
-#pragma unroll
-                    for (int a = 0; a < AT; ++a)
-                        part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(activations(a, K4 + (u - G4) * 64, c), w, part[t], 0, 0, 0);
-                }
-        }
-        const float mine = __half2float(__ushort_as_half(e.scale));
+    auto load_half = [&](uint32_t tile, int v) ATOM_INLINE {
+        const bool live = tile < p.tiles && v < V;
+        const int  i = live ? v : 0;
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            const float s = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * (16 * t + col), __builtin_bit_cast(int, mine)));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(part[t][j], s, acc[t][j]);
+            const uint32_t r = (uint32_t)min((int64_t)tile * (16 * NT) + 16 * (t % NT) + (lane >> 2), p.N - 1), at = live ? r * (uint32_t)p.O + (lane & 3) * 16 : 0;
+            half.q[t] = *reinterpret_cast<const u4 *>(reinterpret_cast<const uint8_t *>(p.w[t / NT].q8) + i * 64 + at);
         }
+        const uint32_t r = (uint32_t)min((int64_t)tile * (16 * NT) + (kc < CT ? 16 * (kc % NT) + col : 0), p.N - 1), at = live ? r * (uint32_t)G : 0;
+        half.scale = scale_of[at + G4 + (i >> 1)];
+        if constexpr (!KEPT) {
+#pragma unroll
+            for (int a = 0; a < AT; ++a)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) half.a[2 * a + c] = acts[((int64_t)(G4 + i) * AT + a) * 256 + c * 64];
+        }
+    };
+    f4 acc[CT] = {};
+    // piece p of row r lies at 4 r + (p ^ (r / 4 & 3)): the 16 lanes of a chunk read all banks
+    u4 *turn_to = s_turn + (lane & ~3) + ((lane ^ (lane >> 4)) & 3), *turn_from = s_turn + 4 * col + ((kc ^ (col >> 2)) & 3);
+    auto operands = [&](const u4 (&from)[CT], u4 (&q)[CT]) ATOM_INLINE {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) turn_to[t * 64] = from[t];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) q[t] = turn_from[t * 64];
+    };
+    auto add = [&](int t, const f4 &part, uint32_t scale) ATOM_INLINE {
+        const float s = __half2float(__ushort_as_half((unsigned short)scale));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(part[j], s, acc[t][j]);
+    };
+    auto compute = [&](int u) ATOM_INLINE {
+        f4 part[CT] = {};
+        u4 q[CT];
+        operands(e.q, q);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int t = 0; t < CT; ++t) {
+                const h8 w = widen4(q[t][c]);
+#pragma unroll
+                for (int a = 0; a < AT; ++a) {
+                    h8 x;
+                    if constexpr (KEPT) x = *reinterpret_cast<const h8 *>(s_act + u * 128 + c * 32);
+                    else x = __builtin_bit_cast(h8, e.a[4 * a + c]);
+                    part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, part[t], 0, 0, 0);
+                }
+            }
+#pragma unroll
+        for (int t = 0; t < CT; ++t) add(t, part[t], (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * t + col), (int)e.scale));
+    };
+    auto compute_half = [&](int v) ATOM_INLINE {
+        f4 part[CT] = {};
+        u4 q[CT];
+        operands(half.q, q);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int t = 0; t < CT; ++t) {
+                const h8 w = widen8(q[t][2 * c], q[t][2 * c + 1]);
+#pragma unroll
+                for (int a = 0; a < AT; ++a) {
+                    h8 x;
+                    if constexpr (KEPT) x = *reinterpret_cast<const h8 *>(s_act + K4 + v * 64 + c * 32);
+                    else x = __builtin_bit_cast(h8, half.a[2 * a + c]);
+                    part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, part[t], 0, 0, 0);
+                }
+            }
+#pragma unroll
+        for (int t = 0; t < CT; ++t) add(t, part[t], (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * t + col), (int)half.scale));
     };
     constexpr int kOut = (NT * 256 + kThreads - 1) / kThreads;         // outputs of a thread
     auto output = [&](uint32_t tile, int i, int64_t &m, int64_t &out) ATOM_INLINE {
@@ -440,13 +467,11 @@ void w4a16_kernel(Args p)
         }
     };
 
-    rows_of(load_tile);
     uint32_t tile = blockIdx.x;
+    rows_of(tile);
     fetch_residual(tile);
-    if (begin < end) {
-#pragma unroll
-        for (int s = 0; s < CH; ++s) load(ring[s]);
-    }
+    load();
+    load_half(tile, wave);
     if constexpr (KEPT) {
         uint32_t *nat = reinterpret_cast<uint32_t *>(s_mine);
         __half *out = reinterpret_cast<__half *>(s_all);
@@ -460,28 +485,21 @@ void w4a16_kernel(Args p)
         }
         __syncthreads();
     }
-    if (begin == end) {
-        for (; tile < p.tiles; tile += gridDim.x) {
-            finish(tile);
-            fetch_residual(min(tile + gridDim.x, p.tiles - 1));
-        }
-        return;
-    }
     all_loads_done();
-    const uint32_t turns = (p.tiles - tile + gridDim.x - 1) / gridDim.x * (uint32_t)(end - begin);
-    int u = begin;
-    for (uint32_t turn = 0; turn < turns; turn += CH)        // (with no way out inside: the compiler would wait at its head for what had been asked for by then)
-#pragma unroll
-        for (int s = 0; s < CH; ++s) {
-            if (turn + s < turns) compute(ring[s], u);
-            load(ring[s]);
-            if (++u == end) {
-                u = begin;
-                if (turn + s < turns) finish(tile);
-                tile += gridDim.x;
-                fetch_residual(min(tile, p.tiles - 1));
-            }
+    for (; tile < p.tiles; tile += gridDim.x) {
+        for (int i = 0; i < n; ++i) {
+            compute(begin + i);
+            load();
         }
+        if (wave < V) compute_half(wave);
+        for (int v = wave + kWaves; v < V; v += kWaves) {     // (more than 512 outlier channels)
+            load_half(tile, v);
+            compute_half(v);
+        }
+        load_half(tile + gridDim.x, wave);
+        finish(tile);
+        fetch_residual(min(tile + gridDim.x, p.tiles - 1));
+    }
 }
 
 typedef float f16 __attribute__((ext_vector_type(16)));
@@ -793,26 +811,26 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
 #define ATOM_FEW(...) ATOM_LAUNCH(grid, kThreads, s.lds, (w4a16_kernel<__VA_ARGS__>), p)
     const bool twice = norm && !s.combine;
     if (s.kept) {
-        if (gated) ATOM_FEW(1, true, 1, 4, true);
-        else       ATOM_FEW(1, false, 1, 5, true);
+        if (gated) ATOM_FEW(1, true, 1, true);
+        else       ATOM_FEW(1, false, 1, true);
     } else if (gated) {
         if (s.NT == 2) {
-            if (twice) ATOM_FEW(2, true, 2, 2, false);
-            else       ATOM_FEW(2, true, 1, 2, false);
+            if (twice) ATOM_FEW(2, true, 2, false);
+            else       ATOM_FEW(2, true, 1, false);
         } else {
-            if (twice) ATOM_FEW(1, true, 2, 2, false);
-            else       ATOM_FEW(1, true, 1, 3, false);
+            if (twice) ATOM_FEW(1, true, 2, false);
+            else       ATOM_FEW(1, true, 1, false);
         }
     } else {
         if (s.NT == 4) {
-            if (twice) ATOM_FEW(4, false, 2, 2, false);
-            else       ATOM_FEW(4, false, 1, 2, false);
+            if (twice) ATOM_FEW(4, false, 2, false);
+            else       ATOM_FEW(4, false, 1, false);
         } else if (s.NT == 2) {
-            if (twice) ATOM_FEW(2, false, 2, 2, false);
-            else       ATOM_FEW(2, false, 1, 3, false);
+            if (twice) ATOM_FEW(2, false, 2, false);
+            else       ATOM_FEW(2, false, 1, false);
         } else {
-            if (twice) ATOM_FEW(1, false, 2, 3, false);
-            else       ATOM_FEW(1, false, 1, 4, false);
+            if (twice) ATOM_FEW(1, false, 2, false);
+            else       ATOM_FEW(1, false, 1, false);
         }
     }
 #undef ATOM_FEW
