@@ -23,17 +23,18 @@ __device__ __forceinline__ uint32_t codes4(const float *x, float r)
     return pack4(code_of(x[0] * r), code_of(x[1] * r), code_of(x[2] * r), code_of(x[3] * r));
 }
 
-__device__ __forceinline__ uint2 load_once(const __half *p)
+template <bool ONCE>
+__device__ __forceinline__ uint2 load4(const __half *p)
 {
     typedef unsigned u2 __attribute__((ext_vector_type(2)));
-    const u2 v = __builtin_nontemporal_load(reinterpret_cast<const u2 *>(p));
-    return make_uint2(v[0], v[1]);
+    if constexpr (ONCE) return __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u2 *>(p)));
+    else return *reinterpret_cast<const uint2 *>(p);
 }
 
 // A run of rows of K, turned, or of V, for one head after another: Run (atom_kv8_append.h) on fp32 values, the maximum as the bits of a
 // float.  Row r is token `token` + r; a wavefront has ROWS of them in registers (those of a longer run are read twice), with
-// their angles, which all heads share.
-template <int D, int ROWS, bool ONE, bool NEIGHBOURS>
+// their angles, which all heads share.  ONCE: what is read is not kept in the caches.
+template <int D, int ROWS, bool ONE, bool NEIGHBOURS, bool ONCE>
 struct TurnedRun {
     static constexpr int LPR = D / 8, RPL = 64 / LPR, kLoads = ROWS / RPL;
     Angles ang[kLoads];
@@ -64,8 +65,8 @@ struct TurnedRun {
     __device__ __forceinline__ void fetch(const Side &side, int h, int u)
     {
         const __half *p = side.x + token_of(u * RPL + g) * side.ld + (int64_t)h * D;
-        raw[u][0] = load_once(p + ch.lo);
-        raw[u][1] = load_once(p + ch.hi);
+        raw[u][0] = load4<ONCE>(p + ch.lo);
+        raw[u][1] = load4<ONCE>(p + ch.hi);
     }
     // a row beyond those in registers
     __device__ __forceinline__ void again(const Turn &t, const Side &side, int h, int row, float *v) const
@@ -147,7 +148,8 @@ struct TurnedRun {
 
 struct Queries { const __half *x; int64_t ld; __half *out; int64_t ldo; int heads; };
 
-constexpr int kQueryHeads = 4;                               // of a lane, in flight together
+constexpr int kQueryHeads = 4;                               // of a lane, in flight together; through the caches (where the step comes from the projection before it:
+                                                             // 1116 tokens, 64 heads on 8, 15.8 us; past the caches 19.2, and up to 5 % less where nothing is cached)
 
 // Eight channels of a lane, for `count` heads of a token from h0 on.
 template <int D, bool ONE, bool NEIGHBOURS>
@@ -163,8 +165,8 @@ __device__ __forceinline__ void turn_queries(const Queries &q, const Turn &t, in
 #pragma unroll
         for (int u = 0; u < kQueryHeads; ++u) {
             const int at = min(h + u, count - 1) * D;
-            raw[u][0] = load_once(x + at + ch.lo);
-            raw[u][1] = load_once(x + at + ch.hi);
+            raw[u][0] = load4<false>(x + at + ch.lo);
+            raw[u][1] = load4<false>(x + at + ch.hi);
         }
 #pragma unroll
         for (int u = 0; u < kQueryHeads; ++u) {
@@ -214,7 +216,7 @@ void rotary_kv8_kernel(Step p)
     const bool is_k = which < p.Hkv;
     const int h = is_k ? which : which - p.Hkv;
     const Side side = is_k ? p.k : p.v;
-    TurnedRun<D, 16, ONE, NEIGHBOURS> run;
+    TurnedRun<D, 16, ONE, NEIGHBOURS, false> run;
     run.place(p.turn, t, p.T, is_k);
     run.fetch(side, h, 0);
     run.fetch_angles(p.turn, 0);
@@ -237,7 +239,7 @@ void rotary_kv8_kernel(Step p)
 
 // Many tokens: a workgroup of four wavefronts for `slab` tokens and some heads of K or of V writes the runs that begin among them, each whole, also past
 // the slab's end.  Up to three runs are written by all four, ROWS rows each; more of them, and runs of ROWS at most, one by each in turn.
-template <int D, int ROWS, bool ONE, bool NEIGHBOURS>
+template <int D, int ROWS, bool ONE, bool NEIGHBOURS, bool ONCE>
 __global__ __launch_bounds__(256)
 void rotary_kv8_many_kernel(Step p)
 {
@@ -258,7 +260,7 @@ void rotary_kv8_many_kernel(Step p)
         const int l0 = __builtin_ctzll(leaders), len = run_length(p.slot, p.T, w, t_first, l0, bs);
         const int row0 = alone ? 0 : wave * ROWS;
         const int32_t first = __builtin_amdgcn_readlane(w.got, l0);
-        TurnedRun<D, ROWS, ONE, NEIGHBOURS> run;
+        TurnedRun<D, ROWS, ONE, NEIGHBOURS, ONCE> run;
         run.place(p.turn, t_first + l0 + row0, p.T, is_k);
         run.o = first & (bs - 1);
         run.at = run.o + row0;
@@ -296,6 +298,10 @@ namespace atom_internal {
 // query heads to a lane, workgroups that turn them.
 struct TurnShape { int slab, heads; int64_t appends; int q_heads; int64_t queries; };
 
+//
+// A wavefront for each token and head is the shorter chain (64 tokens, 32 heads: 7.6 us); with many tokens most of them would find that their run begins
+// elsewhere.  Short blocks: 32 tokens a workgroup, so that a wavefront has a run and not two in turn (343 tokens of 32 heads, blocks of 16: 15.7 us
+// against 18.3 with 64).  Heads are shared out while there are fewer than 1024 workgroups.
 static TurnShape turn_shape(int64_t T, int H, int Hkv, int D, int block_tokens)
 {
     TurnShape s = {};
@@ -305,7 +311,7 @@ static TurnShape turn_shape(int64_t T, int H, int Hkv, int D, int block_tokens)
         s.heads = 1;
         s.appends = (items + 3) / 4;
     } else {
-        s.slab = items <= 16384 ? 8 : 64;
+        s.slab = items <= 16384 ? 8 : long_runs ? 64 : 32;
         const int64_t slabs = (T + s.slab - 1) / s.slab;
         s.heads = 8;
         while (s.heads > 1 && slabs * 2 * ((Hkv + s.heads - 1) / s.heads) < 1024) s.heads /= 2;
@@ -313,7 +319,7 @@ static TurnShape turn_shape(int64_t T, int H, int Hkv, int D, int block_tokens)
     }
     s.q_heads = 8;
     const int64_t rows = 256 / (D / 8);
-    while (s.q_heads > 1 && T * ((H + s.q_heads - 1) / s.q_heads) / rows < 1024) s.q_heads /= 2;
+    while (s.q_heads > 1 && T * ((H + s.q_heads - 1) / s.q_heads) / rows < 512) s.q_heads /= 2;
     s.queries = (T * ((H + s.q_heads - 1) / s.q_heads) + rows - 1) / rows;
     return s;
 }
@@ -336,8 +342,10 @@ hipError_t launch_rotary_kv8_append(const RotaryKv8 &a, hipStream_t stream)
 #define ATOM_TURN(D, ONE, NEIGHBOURS)                                                                                      \
     do {                                                                                                                   \
         auto kern = !s.slab ? &rotary_kv8_kernel<D, ONE, NEIGHBOURS>                                                       \
-                    : a.block_tokens == 128 || a.block_tokens == 32 ? &rotary_kv8_many_kernel<D, 32, ONE, NEIGHBOURS>       \
-                                                                    : &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS>;      \
+                    : a.block_tokens == 128 ? &rotary_kv8_many_kernel<D, 32, ONE, NEIGHBOURS, true>                        \
+                    : a.block_tokens == 64  ? &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS, true>                        \
+                    : a.block_tokens == 32  ? &rotary_kv8_many_kernel<D, 32, ONE, NEIGHBOURS, false>                       \
+                                            : &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS, false>;                      \
         hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, p);                                                           \
     } while (0)
 #define ATOM_TURN_D(D)                                                \
