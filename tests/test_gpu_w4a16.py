@@ -205,3 +205,59 @@ def test_on_a_stream_of_the_callers():
         y = atom.atom_w4a16_linear(*args)
     stream.synchronize()
     assert torch.equal(y, want)
+
+
+def device_weights(N, K, O, g):
+    r = lambda lo, hi, n, t: torch.randint(lo, hi, (N, n), generator=g, device="cuda", dtype=t)         # noqa: E731
+    scale = (0.01 * (1 + 0.2 * torch.rand((N, K // 128), generator=g, device="cuda"))).to(torch.float16)
+    return r(0, 256, (K - O) // 2, torch.uint8), r(-128, 128, O, torch.int8), scale
+
+
+@pytest.mark.parametrize("M,gated,norm", [(20, False, True), (40, True, False), (33, True, True), (64, False, False)])
+def test_many_outputs_whole_rows_of_scales_in_turn(M, gated, norm):
+    """So many outputs that no workgroup shares its K channels: 80 groups of scales, which come 64 at a time.  Every hundredth output
+    and the last ones against 64 bits."""
+    K, O, N = 10240, 256, 25607 if gated else 51195
+    g = torch.Generator(device="cuda").manual_seed(M)
+    w = [device_weights(N, K, O, g) for _ in range(2 if gated else 1)]
+    x, gamma, idx, _, _ = case(M, 1, K, O)
+    x, gamma = x * np.float16(0.125 if gated else 1), gamma if norm else None
+    some = np.unique(np.concatenate([np.arange(0, N, 101), np.arange(N - 140, N)]))
+    few = [tuple(t[torch.from_numpy(some).cuda()].cpu().numpy() for t in m) for m in w]
+    args = (gpu(x), gpu(gamma), 1e-5, gpu(idx))
+    if gated:
+        want, tol = ref.swiglu(x, gamma, 1e-5, idx, *few)
+        got = atom.atom_w4a16_swiglu(*args, *w)
+    else:
+        want, tol = ref.linear(x, gamma, 1e-5, idx, *few)
+        got = atom.atom_w4a16_linear(*args, *w[0])
+    fits = np.abs(want) < 60000
+    got = torch.where(torch.from_numpy(fits).cuda(), got[:, torch.from_numpy(some).cuda()], 0.0)
+    close(got, np.where(fits, want, 0), np.where(fits, tol, np.inf))
+
+
+@pytest.mark.parametrize("M", [1, 3, 8, 9, 16, 24, 50])
+@pytest.mark.parametrize("K,O", [(1280, 1152), (2048, 640), (9088, 128), (4224, 4096)])
+def test_many_outliers_and_few_groups(M, K, O):
+    N = 50
+    x, gamma, idx, (w, u), _ = case(M, N, K, O, 2)
+    w, u = ((q4, q8, (s * np.float16(0.125)).astype(np.float16)) for q4, q8, s in (w, u))
+    want, tol = ref.linear(x, gamma, 1e-5, idx, w)
+    close(atom.atom_w4a16_linear(gpu(x), gpu(gamma), 1e-5, gpu(idx), *gpu(w)), want, tol)
+    x = x * np.float16(0.125)
+    want, tol = ref.swiglu(x, None, 1e-5, idx, w, u)
+    fits = np.abs(want) < 60000
+    got = atom.atom_w4a16_swiglu(gpu(x), None, 1e-5, gpu(idx), gpu(w), gpu(u))
+    close(torch.where(torch.from_numpy(fits).cuda(), got, 0.0), np.where(fits, want, 0), np.where(fits, tol, np.inf))
+
+
+@pytest.mark.parametrize("M", [1, 12, 20])
+def test_a_normed_value_beyond_fp16_counts_as_infinite(M):
+    N, K = 20, 512
+    x, gamma, idx, (w,), _ = case(M, N, K)
+    x[:] = 0
+    x[:, 5], gamma[5] = 100, 60000                            # sqrt(512) * 60000
+    y = atom.atom_w4a16_linear(gpu(x), gpu(gamma), 0.0, gpu(idx), *gpu(w)).cpu().numpy()
+    code = ref.codes_of(w[0], w[1])[:, list(idx).index(5)]
+    want = np.where(code == 0, np.nan, np.where(code > 0, np.inf, -np.inf)).astype(np.float16)
+    assert np.array_equal(y, np.broadcast_to(want, y.shape), equal_nan=True)
