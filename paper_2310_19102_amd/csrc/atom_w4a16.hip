@@ -67,8 +67,9 @@ struct Args {
     const __half *staged; int rows;                          // laid out, `rows` rows of hi and behind them those of lo
     bool combine;                                            // lo in rows 8 .. 15 of the one tile
     uint32_t tiles;
-    // the kernel of many rows: tiles of 32 rows in a block, halves of the activations, parts of K and their sums
-    int wide, halves, parts; uint32_t row_blocks; float *sums;
+    int parts, span; float *sums;                            // parts of K, INT4 groups of one (few rows), their sums
+    // the kernel of many rows: tiles of 32 rows in a block, halves of the activations
+    int wide, halves; uint32_t row_blocks;
 };
 
 // ---- the activations as the product takes them
@@ -290,7 +291,9 @@ void w4a16_kernel(Args p)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, kc = lane >> 4;
     const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, V = 2 * (G - G4);
-    const int begin = wave * G4 / kWaves, n = (wave + 1) * G4 / kWaves - begin;           // INT4 units of this wavefront
+    const int part = (int)blockIdx.y, from = part * p.span, share = min(G4 - from, p.span);
+    const int begin = from + wave * share / kWaves, n = from + (wave + 1) * share / kWaves - begin;       // INT4 units of this wavefront
+    const int first_half = wave + part * kWaves;
     const int rows = p.rows, lds_row = p.K + 8;
 
     Front front;
@@ -425,7 +428,7 @@ void w4a16_kernel(Args p)
     auto fetch_residual = [&](uint32_t tile) ATOM_INLINE {               // (at a tile's beginning: at its end all loads under way would be waited for)
         if constexpr (!GATED) {
             int64_t m, out;
-            if (p.residual)
+            if (p.residual && p.parts == 1)
 #pragma unroll
                 for (int i = 0; i < kOut; ++i)
                     if (output(tile, i, m, out)) residual[i] = reinterpret_cast<const uint16_t *>(p.residual)[m * p.ldr + out];
@@ -461,6 +464,11 @@ void w4a16_kernel(Args p)
                 for (int w = 0; w < kWaves; ++w) sum[x] += mine[(w * CT + x * NT) * 256 + at];
             }
             float y = sum[0];
+            if (p.parts > 1) {
+#pragma unroll
+                for (int x = 0; x < WM; ++x) p.sums[((int64_t)(part * WM + x) * p.M + m) * p.N + out] = sum[x];
+                continue;
+            }
             if constexpr (GATED) y = gated(y, sum[WM - 1]);
             else if (p.residual) y += __half2float(__ushort_as_half(residual[i]));
             p.y[m * p.ldy + out] = __float2half_rn(y);
@@ -471,7 +479,7 @@ void w4a16_kernel(Args p)
     rows_of(tile);
     fetch_residual(tile);
     load();
-    load_half(tile, wave);
+    load_half(tile, first_half);
     if constexpr (KEPT) {
         uint32_t *nat = reinterpret_cast<uint32_t *>(s_mine);
         __half *out = reinterpret_cast<__half *>(s_all);
@@ -491,12 +499,12 @@ void w4a16_kernel(Args p)
             compute(begin + i);
             load();
         }
-        if (wave < V) compute_half(wave);
-        for (int v = wave + kWaves; v < V; v += kWaves) {     // (more than 512 outlier channels)
+        if (first_half < V) compute_half(first_half);
+        for (int v = first_half + kWaves * p.parts; v < V; v += kWaves * p.parts) {       // (more than 512 outlier channels)
             load_half(tile, v);
             compute_half(v);
         }
-        load_half(tile + gridDim.x, wave);
+        load_half(tile + gridDim.x, first_half);
         finish(tile);
         fetch_residual(min(tile + gridDim.x, p.tiles - 1));
     }
@@ -686,7 +694,12 @@ namespace atom_internal {
 
 // How a call runs.  Up to 16 rows: whether the workgroups lay the activations out themselves, tiles of 16 channels, LDS.  More: tiles of
 // 32 rows in a block, parts of K.
-struct ProductShape { bool kept, combine; int NT; size_t lds; int wide, parts; };
+struct ProductShape { bool kept, combine; int NT; size_t lds; int wide, parts, span; };
+
+// Few outputs of many channels: INT4 groups of a part of K at least, and as many parts as leave a workgroup a CU.  A wavefront takes about half a
+// microsecond for a unit and a join 2.5: 64 outputs of 24576 channels 19.6 us whole and 12.6 in parts, 2048 of them 23.0 and 20.4, of 8192 channels
+// 6.5 and 7.0; 4096 outputs of 24576 in two parts (two workgroups a CU) 26.9 instead of 24.2.
+constexpr int kPartGroups = 32, kPartWorkgroups = 256;
 
 static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index)
 {
@@ -718,6 +731,17 @@ static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated
     if (!s.kept) {
         while (s.NT * WM < 4 && (N + 32 * s.NT - 1) / (32 * s.NT) >= 192) s.NT *= 2;
         s.lds = (size_t)3 * kWaves * WM * s.NT * 1024;
+    }
+    const int64_t tiles = (N + 16 * s.NT - 1) / (16 * s.NT);
+    const int     G4 = (K - O) / 128;
+    s.parts = 1;
+    s.span = G4;
+    const int64_t most = kPartWorkgroups / tiles;
+    int wanted = G4 / kPartGroups;
+    if (wanted > most) wanted = (int)most;
+    if (wanted > 1) {
+        s.span = (G4 + wanted - 1) / wanted;
+        s.parts = (G4 + s.span - 1) / s.span;
     }
     return s;
 }
@@ -752,8 +776,8 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
     const ProductShape s = product_shape(a.M, a.N, a.K, a.O, gated, norm, a.idx != nullptr);
     const int  halves = norm && !s.combine ? 2 : 1;           // that go in one after the other
     Args p = {(const __half *)a.x, a.ldx, a.M, (const __half *)a.gamma, a.eps, a.idx, a.K, a.O, {a.w[0], a.w[1]}, a.N, (const __half *)a.residual, a.ldr,
-              (__half *)a.y, a.ldy, (const __half *)a.workspace, (int)a.M, s.combine, 0, s.wide, halves, s.parts, 1,
-              (float *)((char *)a.workspace + laid_out_bytes(s, a.M, a.K, a.O, norm))};
+              (__half *)a.y, a.ldy, (const __half *)a.workspace, (int)a.M, s.combine, 0, s.parts, s.span,
+              (float *)((char *)a.workspace + laid_out_bytes(s, a.M, a.K, a.O, norm)), s.wide, halves, 1};
 #define ATOM_LAUNCH(grid, threads, lds, kernel, ...)                                                                  \
     do {                                                                                                              \
         static atom_launch::LdsOptIn opt;                                                                             \
@@ -798,42 +822,42 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
         else       ATOM_WIDE_ROWS(false);
 #undef ATOM_WIDE_ROWS
 #undef ATOM_WIDE
-        if (s.parts > 1) {
-            const unsigned groups = (unsigned)((a.M * a.N + 255) / 256);
-            if (gated) ATOM_LAUNCH(groups, 256, 0, w4a16_join_kernel<true>, p);
-            else       ATOM_LAUNCH(groups, 256, 0, w4a16_join_kernel<false>, p);
-        }
-        return hipSuccess;
-    }
-
-    p.tiles = (uint32_t)((a.N + 16 * s.NT - 1) / (16 * s.NT));
-    const uint32_t room = (uint32_t)(2 * atom_launch::compute_units()), grid = p.tiles < room ? p.tiles : room;
-#define ATOM_FEW(...) ATOM_LAUNCH(grid, kThreads, s.lds, (w4a16_kernel<__VA_ARGS__>), p)
-    const bool twice = norm && !s.combine;
-    if (s.kept) {
-        if (gated) ATOM_FEW(1, true, 1, true);
-        else       ATOM_FEW(1, false, 1, true);
-    } else if (gated) {
-        if (s.NT == 2) {
-            if (twice) ATOM_FEW(2, true, 2, false);
-            else       ATOM_FEW(2, true, 1, false);
-        } else {
-            if (twice) ATOM_FEW(1, true, 2, false);
-            else       ATOM_FEW(1, true, 1, false);
-        }
     } else {
-        if (s.NT == 4) {
-            if (twice) ATOM_FEW(4, false, 2, false);
-            else       ATOM_FEW(4, false, 1, false);
-        } else if (s.NT == 2) {
-            if (twice) ATOM_FEW(2, false, 2, false);
-            else       ATOM_FEW(2, false, 1, false);
+        p.tiles = (uint32_t)((a.N + 16 * s.NT - 1) / (16 * s.NT));
+        const uint32_t room = (uint32_t)(2 * atom_launch::compute_units()), groups = p.tiles < room ? p.tiles : room;
+        const dim3 grid(groups, s.parts);
+#define ATOM_FEW(...) ATOM_LAUNCH(grid, kThreads, s.lds, (w4a16_kernel<__VA_ARGS__>), p)
+        const bool twice = norm && !s.combine;
+        if (s.kept) {
+            if (gated) ATOM_FEW(1, true, 1, true);
+            else       ATOM_FEW(1, false, 1, true);
+        } else if (gated) {
+            if (s.NT == 2) {
+                if (twice) ATOM_FEW(2, true, 2, false);
+                else       ATOM_FEW(2, true, 1, false);
+            } else {
+                if (twice) ATOM_FEW(1, true, 2, false);
+                else       ATOM_FEW(1, true, 1, false);
+            }
         } else {
-            if (twice) ATOM_FEW(1, false, 2, false);
-            else       ATOM_FEW(1, false, 1, false);
+            if (s.NT == 4) {
+                if (twice) ATOM_FEW(4, false, 2, false);
+                else       ATOM_FEW(4, false, 1, false);
+            } else if (s.NT == 2) {
+                if (twice) ATOM_FEW(2, false, 2, false);
+                else       ATOM_FEW(2, false, 1, false);
+            } else {
+                if (twice) ATOM_FEW(1, false, 2, false);
+                else       ATOM_FEW(1, false, 1, false);
+            }
         }
-    }
 #undef ATOM_FEW
+    }
+    if (s.parts > 1) {
+        const unsigned groups = (unsigned)((a.M * a.N + 255) / 256);
+        if (gated) ATOM_LAUNCH(groups, 256, 0, w4a16_join_kernel<true>, p);
+        else       ATOM_LAUNCH(groups, 256, 0, w4a16_join_kernel<false>, p);
+    }
 #undef ATOM_LAUNCH
     return hipSuccess;
 }
