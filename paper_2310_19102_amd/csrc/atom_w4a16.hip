@@ -202,8 +202,8 @@ __device__ __forceinline__ void put(const Args &p, uint4 *out, int64_t m, int k,
     const int  u = is4 ? k >> 7 : G4 + (j >> 6);
     if constexpr (!WIDE) {
         const int place = row_place(k, K4) & (is4 ? 15 : 7);                              // (instruction, chunk)
-        const int tile = p.combine ? 0 : half, row = (int)m + (p.combine && half ? 8 : 0);
-        out[((((int64_t)u * p.halves + tile) * 4 + (place >> 2)) * 4 + (place & 3)) * 16 + row] = v;
+        const int tile = p.combine ? 0 : half, row = (int)m + (p.combine && half ? p.rows : 0);
+        out[(((int64_t)u * p.halves + tile) * 16 + place) * (p.combine ? 2 * p.rows : p.rows) + row] = v;
     } else {
         const int i = is4 ? (k >> 3) & 7 : (j >> 3) & 3, c = is4 ? (k >> 6) & 1 : (j >> 5) & 1;
         const int64_t block = m / (32 * p.wide), t = m / 32 % p.wide;
@@ -292,7 +292,7 @@ void w4a16_kernel(Args p)
     const int col = lane & 15, kc = lane >> 4;
     const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, V = 2 * (G - G4);
     const int part = (int)blockIdx.y, from = part * p.span, share = min(G4 - from, p.span);
-    const int begin = from + wave * share / kWaves, n = from + (wave + 1) * share / kWaves - begin;       // INT4 units of this wavefront
+    const int begin = from + wave, n = (share - wave + kWaves - 1) / kWaves;       // INT4 units of this wavefront
     const int first_half = wave + part * kWaves;
     const int rows = p.rows, lds_row = p.K + 8;
 
@@ -302,7 +302,8 @@ void w4a16_kernel(Args p)
     // (rows >= M are computed and never stored, columns >= N likewise)
     const int r = p.combine && col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1);
     const __half *s_act = reinterpret_cast<const __half *>(s_all) + (size_t)r * lds_row + kc * 8;
-    const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + lane;
+    const int laid_rows = p.combine ? 2 * rows : rows;          // rows that are laid out; lanes of others read the last
+    const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + kc * laid_rows + r;
     unsigned char *s_mine = s_all + (KEPT ? (size_t)rows * (p.gamma ? 2 : 1) * lds_row * 2 : 0);
     u4 *s_turn = reinterpret_cast<u4 *>(s_mine) + wave * (CT * 64);     // this wavefront's own
     float *red = reinterpret_cast<float *>(s_mine + kWaves * CT * 1024);
@@ -327,7 +328,7 @@ void w4a16_kernel(Args p)
     };
     auto load = [&]() ATOM_INLINE {
         const bool live = load_i < n;
-        const int  u = begin + (live ? load_i : 0);
+        const int  u = live ? begin + load_i * kWaves : 0;
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
             const uint32_t at = live ? at4[t] : 0;
@@ -338,7 +339,7 @@ void w4a16_kernel(Args p)
 #pragma unroll
             for (int a = 0; a < AT; ++a)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) e.a[4 * a + c] = acts[((int64_t)u * AT + a) * 256 + c * 64];
+                for (int c = 0; c < 4; ++c) e.a[4 * a + c] = acts[((u * AT + a) * 16 + c * 4) * laid_rows];
         }
         if (++load_i >= n) {
             load_i = 0;
@@ -360,7 +361,7 @@ void w4a16_kernel(Args p)
 #pragma unroll
             for (int a = 0; a < AT; ++a)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) half.a[2 * a + c] = acts[((int64_t)(G4 + i) * AT + a) * 256 + c * 64];
+                for (int c = 0; c < 2; ++c) half.a[2 * a + c] = acts[(((G4 + i) * AT + a) * 16 + c * 4) * laid_rows];
         }
     };
     f4 acc[CT] = {};
@@ -496,7 +497,7 @@ void w4a16_kernel(Args p)
     all_loads_done();
     for (; tile < p.tiles; tile += gridDim.x) {
         for (int i = 0; i < n; ++i) {
-            compute(begin + i);
+            compute(begin + i * kWaves);
             load();
         }
         if (first_half < V) compute_half(first_half);
@@ -749,7 +750,7 @@ static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated
 static size_t laid_out_bytes(const ProductShape &s, int64_t M, int K, int O, bool norm)
 {
     if (s.kept) return 0;
-    if (!s.wide) return (size_t)((K + O) / 128) * (norm && !s.combine ? 2 : 1) * 4096;
+    if (!s.wide) return (size_t)((K + O) / 128) * (norm ? 2 : 1) * M * 256;
     return (size_t)((M + 32 * s.wide - 1) / (32 * s.wide)) * ((K + O) / 128) * s.wide * (norm ? 2 : 1) * 8192;
 }
 
