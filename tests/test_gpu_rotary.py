@@ -152,3 +152,16 @@ def test_captured_and_replayed_on_another_stream():
         got = atom.atom_rotary(xd, pd, td, axis)
     stream.synchronize()
     assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("T,heads,D,R,axes", [
+    (1500, 5, 128, 128, 1), (903, 9, 80, 32, 3), (2049, 8, 64, 64, 2), (77, 71, 128, 64, 1), (7001, 29, 128, 128, 1), (6601, 30, 128, 96, 3)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_bits_of_many_heads_and_tokens(T, heads, D, R, axes, interleaved):
+    """Four heads to a lane, the last lane's fewer; the largest past the caches."""
+    x, pos, tab, axis = case(T, heads, D, R, axes, interleaved, seed=1)
+    want = ref.turned(x, pos, tab, axis, interleaved, interleaved)
+    xd, pd, td = gpu(x, pos, tab)
+    same(atom.atom_rotary(xd, pd, td, axis, interleaved, interleaved), want)
+    atom.atom_rotary(xd, pd, td, axis, interleaved, interleaved, out=xd)
+    same(xd, want)

@@ -170,3 +170,38 @@ def test_captured_with_new_lengths_on_every_replay():
         graph.replay()
         torch.cuda.synchronize()
         check(t, (out, *caches, None))
+
+
+@pytest.mark.parametrize("bs", [16, 32, 64, 128])
+@pytest.mark.parametrize("axes,interleaved,padding", [(1, False, 0), (3, True, 100)])
+def test_bits_of_many_tokens_and_several_heads_to_a_workgroup(bs, axes, interleaved, padding):
+    s = step([(0, 2100), (37, 1000), (9, 1), (501, 1111), (0, 2)], 4, 16, 64, bs, 32, axes, padding=padding)
+    s["slot"][1500:1500 + bs] = -1                            # a hole of a block's length
+    if bs > 16:
+        s["slot"][1500 // bs * bs:1500 // bs * bs + bs] = -1  # (and what began the block before it)
+    check(s, run(s, interleaved), interleaved)
+
+
+@pytest.mark.parametrize("new", [[3, 1], [200, 150]])
+def test_cache_offsets_past_32_bits(new):
+    """Blocks at both ends of a cache of 4.6 GB a side, as in a small one."""
+    H, Hkv, D, bs, n = 4, 4, 128, 64, 140000
+    s = step([(70, new[0]), (0, new[1])], H, Hkv, D, bs)
+    small = run(s)
+    check(s, small)
+    blocks = s["k"][0].shape[0]
+    far = torch.arange(n - blocks, n, device="cuda")
+    far[:2] = torch.tensor([0, 70000])
+    caches = []
+    for side in "kv":
+        codes, scale = torch.zeros((n, Hkv, bs, D), dtype=torch.int8, device="cuda"), torch.zeros((n, Hkv), device="cuda")
+        codes[far], scale[far] = torch.from_numpy(s[side][0]).cuda(), torch.from_numpy(s[side][1]).cuda()
+        caches.append((codes, scale))
+    slot = torch.from_numpy(s["slot"]).cuda()
+    slot = (far[slot // bs] * bs + slot % bs).to(torch.int32)
+    qkv = torch.from_numpy(s["qkv"]).cuda()
+    q, kc, vc = atom.atom_rotary_kv8_append(qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:], *caches, slot, *(torch.from_numpy(s[x]).cuda() for x in ("pos", "tab")))
+    assert torch.equal(q, small[0])
+    for got, want in ((kc, small[1]), (vc, small[2])):
+        assert torch.equal(got[0][far], want[0]) and torch.equal(got[1][far], want[1])
+        assert int(torch.count_nonzero(got[1])) == int(torch.count_nonzero(want[1]))
