@@ -712,7 +712,7 @@ atom_status atom_rotary(const void *x_f16, int64_t T, int64_t ldx, int32_t heads
  *   r, positions, ldp, table, n_pos   as atom_rotary
  *   k_f16 .. v_scale   as atom_kv8_append; k and v are not written
  * Errors: those of atom_rotary and of atom_kv8_append; ATOM_ERR_UNSUPPORTED also where the launch would have 2^32 threads
- * or more (128 Hkv + H D / 8 for a token).
+ * or more (from about 1000 tokens on 16 ceil(Hkv / 8) + ceil(H / 8) D / 8 for a token).
  */
 atom_status atom_rotary_kv8_append(const void *q_f16, int64_t ldq, int32_t H, void *q_out_f16,
                                    int64_t ldqo, const void *k_f16, const void *v_f16, int64_t T,
@@ -725,21 +725,24 @@ atom_status atom_rotary_kv8_append(const void *q_f16, int64_t ldq, int32_t H, vo
 /*
  * Linear layers on the quantised weights with activations that stay in fp16 (the W4A16 setting that the paper compares with in
  * Section 5.3; a layer of few rows is bound by reading its weights, Section 3, and those are the same):
- *   xr[m, j] = x[m, idx[j]], or with gamma fp16(RMSNorm(x)[m, idx[j]] * gamma[idx[j]])       (RMSNorm and product in fp32)
+ *   xr[m, j] = x[m, idx[j]], or with gamma RMSNorm(x)[m, idx[j]] * gamma[idx[j]]             (RMSNorm and product in fp32)
  *   y[m, n]  = fp16( residual[m, n] + sum_g w_scale[n, g] * sum_{k in g} w[n, k] * xr[m, k] )
- * Codes meet xr exactly in the fp16 matrix cores, sums are fp32, in an order that depends on the sizes alone: results are
- * deterministic.  Meant for few rows (any number is taken; the 4-bit path is the faster one beyond a few hundred).
+ * Codes meet xr exactly in the fp16 matrix cores, where a normed xr goes in as the sum of two halves (22 bits; what is beyond
+ * fp16's range counts as infinite).  Sums are fp32, in an order that depends on the sizes alone: results are deterministic.
+ * Meant for few rows (any number within the limits is taken; the 4-bit path is the faster one beyond a few hundred).
  *
  *   x_f16        [M, ldx] fp16, ldx >= K, ldx % 8 == 0, 16-byte aligned
  *   gamma_f16    [K] fp16 in original channel order, or NULL for no norm; eps: RMSNorm epsilon
- *   reorder_idx  [K] int32, 16-byte aligned, or NULL when x already is in reordered channel order, as in atom_quantize_act
+ *   reorder_idx  [K] int32, 16-byte aligned, or NULL when x already is in reordered channel order, as in atom_quantize_act (an entry
+ *                outside [0, K) counts as K - 1)
  *   w_q4 / w_q8 / w_scale   canonical codes and scales of N rows as atom_quantize_weight writes them (4 or 3 bits); 16-, 16- and 2-byte aligned
  *   residual_f16 [M, ldr] fp16, ldr >= N, or NULL; may be y_f16 itself (ldr = ldy)
  *   y_f16        [M, ldy] fp16 out, ldy >= N; overlaps no other input
  *   workspace    device scratch of atom_w4a16_workspace_bytes(M, N, d, 0, gamma != NULL, reorder_idx != NULL) bytes, 256-byte aligned (NULL when
  *                that is 0).  Contents need no initialisation and are dead after the call.
  * Errors: ATOM_ERR_NULL, ATOM_ERR_SHAPE, ATOM_ERR_ALIGN, ATOM_ERR_WORKSPACE, ATOM_ERR_UNSUPPORTED (a descriptor that
- * atom_w4a4_gemm_packed does not take, a launch of 2^32 threads or more: 512 for every 16 outputs of 64 rows).
+ * atom_w4a4_gemm_packed does not take, one of the weights' arrays of 4 GiB or more, launches of 2^32 threads: more than 2^22 - 1
+ * rows, 2^18 - 1 blocks of 32 rows and 128 outputs, or 2^30 - 256 results).  M = 0 or N = 0 returns ATOM_OK.
  */
 atom_status atom_w4a16_linear(const void *x_f16, int64_t M, int64_t ldx, const void *gamma_f16, float eps,
                               const int32_t *reorder_idx, const atom_desc *d, const void *w_q4,

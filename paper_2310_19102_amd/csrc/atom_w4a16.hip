@@ -278,9 +278,12 @@ __device__ __forceinline__ void store(const Args &p, int64_t m, int64_t n, float
 // every eighth half of an INT8 group each (64 bytes of every weight row either way: a unit), and their sums meet in LDS, added in order.  A wavefront's
 // next unit is on its way while it works, across the tiles that the workgroup has in turn (behind the last, one address for all lanes).  With a tile or
 // two for a workgroup the time is latencies, among them the code's own way to the wavefronts: two to five units under way in unrolled code were slower.
+// One row: 4096 x 4096 5.0 us, gated 11008 of 4096 12.4 (3.9 TB/s of weights from the last-level cache), 8192 x 24576 33 (3.0, from memory); eight rows
+// behind the norm, 12288 of 4096, 13.9.
 //   HL: halves of the activations that go in one after the other (2: hi and lo)
+//   COMBINE: up to eight rows, hi in rows 0 .. 7 and lo in rows 8 .. 15 of the one tile (HL = 1)
 //   KEPT: the activations are laid out in LDS by the workgroup itself (HL = 1), under way with the first weights
-template <int NT, bool GATED, int HL, bool KEPT>
+template <int NT, bool GATED, int HL, bool COMBINE, bool KEPT>
 __global__ __launch_bounds__(kThreads, KEPT ? 4 : 2)
 void w4a16_kernel(Args p)
 {
@@ -300,9 +303,9 @@ void w4a16_kernel(Args p)
     if constexpr (KEPT) front = front_of<kThreads>(p, p.x);
 
     // (rows >= M are computed and never stored, columns >= N likewise)
-    const int r = p.combine && col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1);
+    const int r = COMBINE && col >= 8 ? rows + min(col - 8, rows - 1) : min(col, rows - 1);
     const __half *s_act = reinterpret_cast<const __half *>(s_all) + (size_t)r * lds_row + kc * 8;
-    const int laid_rows = p.combine ? 2 * rows : rows;          // rows that are laid out; lanes of others read the last
+    const int laid_rows = COMBINE ? 2 * rows : rows;          // rows that are laid out; lanes of others read the last
     const u4 *acts = reinterpret_cast<const u4 *>(p.staged) + kc * laid_rows + r;
     unsigned char *s_mine = s_all + (KEPT ? (size_t)rows * (p.gamma ? 2 : 1) * lds_row * 2 : 0);
     u4 *s_turn = reinterpret_cast<u4 *>(s_mine) + wave * (CT * 64);     // this wavefront's own
@@ -418,12 +421,13 @@ void w4a16_kernel(Args p)
 #pragma unroll
         for (int t = 0; t < CT; ++t) add(t, part[t], (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * t + col), (int)half.scale));
     };
-    constexpr int kOut = (NT * 256 + kThreads - 1) / kThreads;         // outputs of a thread
+        constexpr int kLanes = COMBINE ? 32 : 64;                // that have rows: half of them where lo is added to hi
+    constexpr int kTile = 4 * kLanes, kOut = (NT * kTile + kThreads - 1) / kThreads;       // outputs of a tile, of a thread
     auto output = [&](uint32_t tile, int i, int64_t &m, int64_t &out) ATOM_INLINE {
-        const int at = tid + i * kThreads, l = at & 63;
-        m = 4 * (l >> 4) + ((at >> 6) & 3);
-        out = (int64_t)tile * (16 * NT) + 16 * (at >> 8) + (l & 15);
-        return at < NT * 256 && m < p.M && out < p.N;
+        const int at = tid + i * kThreads, l = at % kLanes;
+        m = 4 * (l >> 4) + (at / kLanes & 3);
+        out = (int64_t)tile * (16 * NT) + 16 * (at / kTile) + (l & 15);
+        return at < NT * kTile && m < p.M && out < p.N;
     };
     uint16_t residual[kOut];
     auto fetch_residual = [&](uint32_t tile) ATOM_INLINE {               // (at a tile's beginning: at its end all loads under way would be waited for)
@@ -437,9 +441,9 @@ void w4a16_kernel(Args p)
     };
     int buffer = 0;
     auto finish = [&](uint32_t tile) ATOM_INLINE {
-        float *mine = red + (size_t)buffer * (kWaves * CT * 256);
+        float *mine = red + buffer * (kWaves * CT * kTile);
         buffer ^= 1;                                         // (nobody writes a buffer before all have read what it held two tiles ago)
-        if (p.combine)                                       // rows 8 .. 15 to rows 0 .. 7
+        if constexpr (COMBINE)                               // rows 8 .. 15 to rows 0 .. 7
 #pragma unroll
             for (int t = 0; t < CT; ++t)
 #pragma unroll
@@ -448,7 +452,7 @@ void w4a16_kernel(Args p)
         for (int t = 0; t < CT; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                mine[(wave * CT + t) * 256 + j * 64 + lane] = acc[t][j];
+                if (lane < kLanes) mine[(wave * CT + t) * kTile + j * kLanes + lane] = acc[t][j];
                 acc[t][j] = 0.0f;
             }
         __syncthreads();
@@ -462,7 +466,7 @@ void w4a16_kernel(Args p)
             for (int x = 0; x < WM; ++x) {
                 sum[x] = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) sum[x] += mine[(w * CT + x * NT) * 256 + at];
+                for (int w = 0; w < kWaves; ++w) sum[x] += mine[(w * CT + x * NT) * kTile + at];
             }
             float y = sum[0];
             if (p.parts > 1) {
@@ -515,10 +519,12 @@ typedef float f16 __attribute__((ext_vector_type(16)));
 
 // More than 16 rows: MFMA 32x32x16, whose operands bring twice the products for their bytes (lane l: row or column l & 31, the eight values
 // of k-chunk l >> 5; register r of the result: row 8 (r / 4) + 4 (l >> 5) + r % 4).  A workgroup has 32 RT rows and eight tiles of 32 weight
-// rows (of a gated call four of the gate and the same four of the up projection in turn).  Each wavefront has
-// one of them for all rows.  Activations and weights come a unit at a time through LDS, a tile by each wavefront.  `parts` workgroups share a tile's units where the tiles alone do not fill the card; their
-// sums meet in the workspace.  What the L2 delivers to all compute units together (about 8 TB/s) is the tightest bound beside memory, so
-// scales come 64 of a row at a time (by themselves, 2 bytes bring a line each: as much as the weights), and rows behind M are not fetched.
+// rows (of a gated call four of the gate and the same four of the up projection in turn).  Each wavefront has one of them for all rows.  Activations
+// and weights come a unit at a time through LDS, a tile by each wavefront.  `parts` workgroups share a tile's units where the tiles alone do not
+// fill the card; their sums meet in the workspace.  What the L2 delivers to all compute units together (about 8 TB/s) is the tightest bound beside
+// memory, so scales come 64 of a row at a time (by themselves, 2 bytes bring a line each: as much as the weights), and rows behind M are not fetched.
+// 33 rows, 8192 outputs of 28672 channels: 49 us of the call's 52 (2.4 TB/s of weights; a second tile of 32 rows for one); 64 rows, gated 28672 of 8192
+// behind the norm: 131 of 140, at 825 TFLOP/s with both halves of the activations.
 template <bool GATED, int RT, int HL, int CH>
 __global__ __launch_bounds__(kThreads, 2)
 void w4a16_wide_kernel(Args p)
@@ -697,10 +703,18 @@ namespace atom_internal {
 // 32 rows in a block, parts of K.
 struct ProductShape { bool kept, combine; int NT; size_t lds; int wide, parts, span; };
 
-// Few outputs of many channels: INT4 groups of a part of K at least, and as many parts as leave a workgroup a CU.  A wavefront takes about half a
-// microsecond for a unit and a join 2.5: 64 outputs of 24576 channels 19.6 us whole and 12.6 in parts, 2048 of them 23.0 and 20.4, of 8192 channels
-// 6.5 and 7.0; 4096 outputs of 24576 in two parts (two workgroups a CU) 26.9 instead of 24.2.
+// Up to 16 rows, few outputs of many channels: INT4 groups of a part of K at least, and as many parts as leave a workgroup a CU.  A wavefront takes 0.3 to
+// 0.5 us for a unit and a join 2.5: one row, 64 outputs of 24576 channels 17.0 us whole and 12.0 in parts, 2048 of them 19.8 and 17.0; of 8192 channels
+// 6.5 and (parts of 16) 7.2; 4096 outputs of 24576 in two parts (two workgroups a CU) 26.9 instead of 24.2.
 constexpr int kPartGroups = 32, kPartWorkgroups = 256;
+
+// LDS of a workgroup where two of them share a CU, and where one has it (less what the kernel has beside).  Rows that the workgroups lay out themselves
+// cost no launch: gated 11008 of 4096 channels, one row, 12.4 us and 20.8 with a launch for it; two rows 13.2 and 9.4 to 8.3 for 64 outputs; where one
+// workgroup has a CU only a single row pays, and only without a second round (64 outputs of 24576 channels 10.8 and 12.0, 8192 of them 42.9 and 33.2).
+constexpr size_t kTwoGroupsLds = 80 * 1024 - 64, kOneGroupLds = 150 * 1024;
+
+// The weights' way to the operands and the wavefronts' sums, twice.
+static size_t sums_bytes(const ProductShape &s, int WM) { return (size_t)kWaves * WM * s.NT * (s.combine ? 2048 : 3072); }
 
 static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index)
 {
@@ -724,14 +738,25 @@ static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated
     }
     s.NT = 1;
     s.combine = norm && M <= 8;
-    const size_t sums = (size_t)3 * kWaves * WM * 1024, nat = natural_bytes(K, norm, index), rest = nat > sums ? nat : sums;
+    const size_t sums = sums_bytes(s, WM), nat = natural_bytes(K, norm, index), rest = nat > sums ? nat : sums;
     if (M <= (norm ? 8 : 16)) {
         s.lds = (size_t)M * (norm ? 2 : 1) * (K + 8) * 2 + rest;
-        s.kept = s.lds <= 80 * 1024;
+        s.kept = s.lds <= kTwoGroupsLds || (M == 1 && s.lds <= kOneGroupLds && (N + 15) / 16 <= kPartWorkgroups);
     }
     if (!s.kept) {
-        while (s.NT * WM < 4 && (N + 32 * s.NT - 1) / (32 * s.NT) >= 192) s.NT *= 2;
-        s.lds = (size_t)3 * kWaves * WM * s.NT * 1024;
+        // Rounds of workgroups, a CU each, times what they read for a unit: 1 KB of weights for 16 rows of them, and the activations, which the L2 gives four
+        // times as fast.  (16 rows, 20000 outputs of 24576 channels: NT = 1 111 us, 2 101, 4 117; 6000 of them 34, 25, 28; 28672 152, 133, 123; four rows
+        // and 12288 outputs 50, 56, 56.)
+        const double rows = norm ? 2 * M : M;
+        double best = 1e30;
+        for (int NT = 1; NT * WM <= 4; NT *= 2) {
+            const double cost = (double)(((N + 16 * NT - 1) / (16 * NT) + kPartWorkgroups - 1) / kPartWorkgroups) * (NT * WM + rows / 16);
+            if (cost < best) {
+                best = cost;
+                s.NT = NT;
+            }
+        }
+        s.lds = sums_bytes(s, WM);
     }
     const int64_t tiles = (N + 16 * s.NT - 1) / (16 * s.NT);
     const int     G4 = (K - O) / 128;
@@ -828,30 +853,26 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
         const uint32_t room = (uint32_t)(2 * atom_launch::compute_units()), groups = p.tiles < room ? p.tiles : room;
         const dim3 grid(groups, s.parts);
 #define ATOM_FEW(...) ATOM_LAUNCH(grid, kThreads, s.lds, (w4a16_kernel<__VA_ARGS__>), p)
-        const bool twice = norm && !s.combine;
+#define ATOM_FEW_ROWS(NT, GATED)                                          \
+        do {                                                              \
+            if (!norm)          ATOM_FEW(NT, GATED, 1, false, false);     \
+            else if (s.combine) ATOM_FEW(NT, GATED, 1, true, false);      \
+            else                ATOM_FEW(NT, GATED, 2, false, false);     \
+        } while (0)
         if (s.kept) {
-            if (gated) ATOM_FEW(1, true, 1, true);
-            else       ATOM_FEW(1, false, 1, true);
+            if (gated && norm) ATOM_FEW(1, true, 1, true, true);
+            else if (gated)    ATOM_FEW(1, true, 1, false, true);
+            else if (norm)     ATOM_FEW(1, false, 1, true, true);
+            else               ATOM_FEW(1, false, 1, false, true);
         } else if (gated) {
-            if (s.NT == 2) {
-                if (twice) ATOM_FEW(2, true, 2, false);
-                else       ATOM_FEW(2, true, 1, false);
-            } else {
-                if (twice) ATOM_FEW(1, true, 2, false);
-                else       ATOM_FEW(1, true, 1, false);
-            }
+            if (s.NT == 2) ATOM_FEW_ROWS(2, true);
+            else           ATOM_FEW_ROWS(1, true);
         } else {
-            if (s.NT == 4) {
-                if (twice) ATOM_FEW(4, false, 2, false);
-                else       ATOM_FEW(4, false, 1, false);
-            } else if (s.NT == 2) {
-                if (twice) ATOM_FEW(2, false, 2, false);
-                else       ATOM_FEW(2, false, 1, false);
-            } else {
-                if (twice) ATOM_FEW(1, false, 2, false);
-                else       ATOM_FEW(1, false, 1, false);
-            }
+            if (s.NT == 4)      ATOM_FEW_ROWS(4, false);
+            else if (s.NT == 2) ATOM_FEW_ROWS(2, false);
+            else                ATOM_FEW_ROWS(1, false);
         }
+#undef ATOM_FEW_ROWS
 #undef ATOM_FEW
     }
     if (s.parts > 1) {
