@@ -523,12 +523,14 @@ typedef float f16 __attribute__((ext_vector_type(16)));
 // and weights come a unit at a time through LDS, a tile by each wavefront.  `parts` workgroups share a tile's units where the tiles alone do not
 // fill the card; their sums meet in the workspace.  What the L2 delivers to all compute units together (about 8 TB/s) is the tightest bound beside
 // memory, so scales come 64 of a row at a time (by themselves, 2 bytes bring a line each: as much as the weights), and rows behind M are not fetched.
-// 33 rows, 8192 outputs of 28672 channels: 49 us of the call's 52 (2.4 TB/s of weights; a second tile of 32 rows for one); 64 rows, gated 28672 of 8192
-// behind the norm: 131 of 140, at 825 TFLOP/s with both halves of the activations.
-template <bool GATED, int RT, int HL, int CH>
+// 33 rows, 8192 outputs of 28672 channels: 46 us of the call's 51 (2.6 TB/s of weights; a second tile of 32 rows for one); 64 rows, gated 28672 of 8192
+// behind the norm: 130 of 138, at 920 TFLOP/s with both halves of the activations.  One or two units under way and short code: with three or four, and scales
+// eight rows at a time, 20 rows and 4000 outputs of 8192 channels took 25.2 us, now 20.7.
+template <bool GATED, int RT, int HL>
 __global__ __launch_bounds__(kThreads, 2)
 void w4a16_wide_kernel(Args p)
 {
+    constexpr int CH = HL == 1 ? 2 : 1;                      // units under way
     constexpr int kOps = RT * HL;                            // 16-byte pieces of a unit's activations that a thread brings
     extern __shared__ __align__(16) unsigned char s_all[];
     u4 (*s_act)[kOps * 512] = reinterpret_cast<u4 (*)[kOps * 512]>(s_all);                     // [2], and behind them
@@ -584,11 +586,11 @@ void w4a16_wide_kernel(Args p)
         const int count = min(kScales, G - scale0);
         scale_end = scale0 + count <= G4 ? scale0 + count : G4 + 2 * (scale0 + count - G4);
         const uint16_t *from = w.scale + scale0 + min(lane, count - 1);
-#pragma unroll 8
+#pragma unroll 16
         for (int r = 0; r < 32; ++r) my_scales[r * (kScales + 2) + lane] = from[min(rows_of(wave) + r, p.N - 1) * G];
     };
     f16 acc[RT] = {};
-    auto compute = [&](const Unit &e, int u) ATOM_INLINE {
+    auto compute = [&](int u) ATOM_INLINE {
         const u4 *a = s_act[(u - begin) & 1] + lane;
         u4 q[2];
 #pragma unroll
@@ -619,19 +621,21 @@ void w4a16_wide_kernel(Args p)
             for (int j = 0; j < 16; ++j) acc[r][j] = fmaf(sum[r][j], s, acc[r][j]);
     };
 
+    Unit first;
+    load(first);
 #pragma unroll
     for (int s = 0; s < CH; ++s) load(ring[s]);
     all_loads_done();
     fetch_scales(begin);
-    keep(ring[0], begin);
+    keep(first, begin);
     __syncthreads();
     for (int u = begin; u < end; u += CH) {
         if (u + CH > scale_end && scale_end < end) fetch_scales(u);
 #pragma unroll
         for (int s = 0; s < CH; ++s) {                       // (no way out of the loop here: the compiler would wait at its head for what had been asked for by then)
-            keep(ring[(s + 1) % CH], u + s + 1);
-            if (u + s < end) compute(ring[s], u + s);
+            keep(ring[s], u + s + 1);
             load(ring[s]);
+            if (u + s < end) compute(u + s);
             __syncthreads();                                 // (all have read this unit, the next one is there)
         }
     }
@@ -724,9 +728,10 @@ static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated
         s.wide = M <= 32 ? 1 : 2;
         const int U = (K + O) / 128;
         const int64_t tiles = (N + (gated ? 127 : 255)) / (gated ? 128 : 256) * ((M + 32 * s.wide - 1) / (32 * s.wide)), cus = 256;
-        // rounds of workgroups, each as long as its units; a join costs about two units and what it moves
+        // Rounds of workgroups, each as long as its units; a join costs about two units and what it moves.  More than 16 parts only of six units and more (64
+        // outputs, 50 rows: of 24576 channels 30.7 us in 16 parts and 28.1 in 32, of 8192 18.8 in 16 and 19.0 in 32; of 2048 15.0 in 4 and 14.3 in 8).
         double best = 1e30;
-        for (int parts = 1; parts <= 16 && parts * 4 <= U; ++parts) {
+        for (int parts = 1; parts <= 32 && parts * (parts > 16 ? 6 : 2) <= U; ++parts) {
             const double cost = (double)((tiles * parts + cus - 1) / cus) * ((U + parts - 1) / parts + 3) + (parts > 1 ? 4 + (double)parts * M * N * WM * 8 / 5e6 : 0);
             if (cost < best) {
                 best = cost;
@@ -833,15 +838,15 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
         const int64_t per = gated ? 128 : 256;
         p.row_blocks = (uint32_t)((a.M + 32 * s.wide - 1) / (32 * s.wide));
         const unsigned grid = (unsigned)((a.N + per - 1) / per * s.parts * p.row_blocks);
-#define ATOM_WIDE(GATED, RT, HL, CH) ATOM_LAUNCH(grid, kThreads, (size_t)2 * ((RT) * (HL) * 8192 + kWaves * 2048) + 256 * (kScales + 2) * 2, (w4a16_wide_kernel<GATED, RT, HL, CH>), p)
+#define ATOM_WIDE(GATED, RT, HL) ATOM_LAUNCH(grid, kThreads, (size_t)2 * ((RT) * (HL) * 8192 + kWaves * 2048) + 256 * (kScales + 2) * 2, (w4a16_wide_kernel<GATED, RT, HL>), p)
 #define ATOM_WIDE_ROWS(GATED)                                  \
     do {                                                       \
         if (s.wide == 1) {                                     \
-            if (norm) ATOM_WIDE(GATED, 1, 2, 4);               \
-            else      ATOM_WIDE(GATED, 1, 1, 4);               \
+            if (norm) ATOM_WIDE(GATED, 1, 2);                  \
+            else      ATOM_WIDE(GATED, 1, 1);                  \
         } else {                                               \
-            if (norm) ATOM_WIDE(GATED, 2, 2, 3);               \
-            else      ATOM_WIDE(GATED, 2, 1, 3);               \
+            if (norm) ATOM_WIDE(GATED, 2, 2);                  \
+            else      ATOM_WIDE(GATED, 2, 1);                  \
         }                                                      \
     } while (0)
         if (gated) ATOM_WIDE_ROWS(true);
