@@ -64,18 +64,30 @@ struct Side { const __half *x; int64_t ld; int8_t *codes; float *scale; };
 // A wavefront's window of 64 slots: which of the first `slab` tokens begin a run (a run: tokens whose slots follow one another inside one block).
 struct Window { int32_t got; bool valid; uint64_t leaders; };
 
-__device__ __forceinline__ Window window(const int32_t *__restrict__ slot, int32_t slots, int T, int64_t t_first, int slab, int bs)
+// What it reads: a lane's slot and the one before the first.
+struct Slots { int32_t got, before; };
+
+__device__ __forceinline__ Slots slots_from(const int32_t *__restrict__ slot, int T, int64_t t_first)
+{
+    return {slot[min(t_first + (threadIdx.x & 63), (int64_t)T - 1)], slot[max(t_first - 1, (int64_t)0)]};
+}
+
+__device__ __forceinline__ Window window(const Slots &s, int32_t slots, int T, int64_t t_first, int slab, int bs)
 {
     const int lane = threadIdx.x & 63;
     Window w;
-    w.got = slot[min(t_first + lane, (int64_t)T - 1)];
-    const int32_t before = slot[max(t_first - 1, (int64_t)0)];
+    w.got = s.got;
     w.valid = t_first + lane < T && w.got >= 0 && w.got < slots;
     int32_t prev = __shfl_up(w.got, 1, 64);
-    if (lane == 0) prev = t_first > 0 ? before : -2;
+    if (lane == 0) prev = t_first > 0 ? s.before : -2;
     const bool follows = prev >= 0 && prev < slots && w.got == prev + 1 && (w.got & (bs - 1)) != 0;
     w.leaders = __ballot(w.valid && !follows && lane < slab);
     return w;
+}
+
+__device__ __forceinline__ Window window(const int32_t *__restrict__ slot, int32_t slots, int T, int64_t t_first, int slab, int bs)
+{
+    return window(slots_from(slot, T, t_first), slots, T, t_first, slab, bs);
 }
 
 // The run that token t_first + l0 begins: from its slots at hand, and from those beyond them if it goes on there.

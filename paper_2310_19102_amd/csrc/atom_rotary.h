@@ -54,19 +54,23 @@ __device__ __forceinline__ Positions positions(const Turn &t, int64_t token)
     return at;
 }
 
-// cos and sin of pairs 4i .. 4i + 3; of a position outside the table NaN.  axes: lane_axes()
+// cos and sin of pairs 4i .. 4i + 3 (of pairs 0 .. 3 in a lane whose channels do not turn: loads without a branch around them); of a position outside the
+// table NaN, by bits, as a choice between the loaded and NaN becomes a branch with single loads in it.  axes: lane_axes()
 template <bool ONE>
 __device__ __forceinline__ Angles angles(const Turn &t, const Positions &at, int i, uint32_t axes)
 {
     Angles r;
-    const float nan = __builtin_nanf("");
+    if (4 * i >= t.n_pairs) i = 0;
+    auto marked = [](float c, bool inside) __attribute__((always_inline)) {
+        return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, c) | (inside ? 0u : 0x7fc00000u));
+    };
     if constexpr (ONE) {
         const bool inside = (uint32_t)at.p[0] < t.n_pos;
         const float4 *row = reinterpret_cast<const float4 *>(t.table + (int64_t)(inside ? at.p[0] : 0) * (2 * t.n_pairs) + 8 * i);
         const float4 u = row[0], v = row[1];
         r = {{u.x, u.z, v.x, v.z}, {u.y, u.w, v.y, v.w}};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) r.c[k] = inside ? r.c[k] : nan;
+        for (int k = 0; k < 4; ++k) r.c[k] = marked(r.c[k], inside);
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -74,7 +78,7 @@ __device__ __forceinline__ Angles angles(const Turn &t, const Positions &at, int
             const int32_t p = a == 0 ? at.p[0] : a == 1 ? at.p[1] : a == 2 ? at.p[2] : at.p[3];
             const bool inside = (uint32_t)p < t.n_pos;
             const float2 u = *reinterpret_cast<const float2 *>(t.table + (int64_t)(inside ? p : 0) * (2 * t.n_pairs) + 8 * i + 2 * k);
-            r.c[k] = inside ? u.x : nan;
+            r.c[k] = marked(u.x, inside);
             r.s[k] = u.y;
         }
     }

@@ -37,15 +37,14 @@ __device__ __forceinline__ uint2 load4(const __half *p)
 template <bool ONE, bool NEIGHBOURS, int HEADS, bool ONCE>
 __global__ __launch_bounds__(256)
 void rotary_kernel(const __half *x, int64_t ldx, uint32_t heads, uint32_t D, Turn t, float sign, __half *out, int64_t ldo,
-                   uint32_t chunks, uint64_t lanes)
+                   uint32_t chunks, uint32_t lanes)
 {
-    const uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t e = blockIdx.x * 256 + threadIdx.x;
     if (e >= lanes) return;
-    const uint32_t per = D / 8, row = (uint32_t)(e / per), i = (uint32_t)(e - (uint64_t)row * per);
+    const uint32_t per = D / 8, row = e / per, i = e - row * per;
     const uint32_t token = row / chunks, h0 = (row - token * chunks) * HEADS;
     const Channels at = channels(t, (int)i);
-    Angles r;
-    if (at.turned) r = angles<ONE>(t, positions<ONE>(t, token), (int)i, lane_axes(t, (int)i));
+    const Positions where = positions<ONE>(t, token);        // (first, so that the table's row is asked for while the heads come)
     x += (int64_t)token * ldx;
     out += (int64_t)token * ldo;
     uint2 lo[HEADS], hi[HEADS];
@@ -55,6 +54,7 @@ void rotary_kernel(const __half *x, int64_t ldx, uint32_t heads, uint32_t D, Tur
         lo[u] = load4<ONCE>(x + h * D + at.lo);
         hi[u] = load4<ONCE>(x + h * D + at.hi);
     }
+    const Angles r = angles<ONE>(t, where, (int)i, lane_axes(t, (int)i));
 #pragma unroll
     for (int u = 0; u < HEADS; ++u) {
         if (h0 + u >= heads) break;
@@ -91,7 +91,7 @@ hipError_t launch_rotary(const void *x, int64_t T, int64_t ldx, int heads, int D
         const uint32_t chunks = (uint32_t)((heads + HEADS - 1) / HEADS);                                                              \
         const uint64_t lanes = (uint64_t)T * chunks * (D / 8);                                                                        \
         hipLaunchKernelGGL((rotary_kernel<ONE, NEIGHBOURS, HEADS, ONCE>), dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, stream, (const __half *)x, ldx, \
-                           (uint32_t)heads, (uint32_t)D, t, transposed ? -1.0f : 1.0f, (__half *)out, ldo, chunks, lanes);           \
+                           (uint32_t)heads, (uint32_t)D, t, transposed ? -1.0f : 1.0f, (__half *)out, ldo, chunks, (uint32_t)lanes);           \
     } while (0)
 #define ATOM_ROTARY_SIZE(ONE, NEIGHBOURS)                                    \
     do {                                                                     \

@@ -44,7 +44,7 @@ struct TurnedRun {
     int g, i, len, at, o;
     Channels ch;
     uint32_t axes;
-    bool turns;
+    bool keys, turns;                                       // rows of K; channels of this lane that turn
 
     __device__ __forceinline__ void place(const Turn &t, int64_t tok, int T, bool turns_)
     {
@@ -52,15 +52,26 @@ struct TurnedRun {
         g = lane / LPR;
         i = lane % LPR;
         ch = channels(t, i);
+        keys = turns_;
         turns = turns_ && ch.turned;
         axes = lane_axes(t, i);
         token = tok;
         last = (int)((int64_t)T - 1 - tok);
     }
     __device__ __forceinline__ int64_t token_of(int row) const { return token + min(row, last); }
-    __device__ __forceinline__ void fetch_angles(const Turn &t, int u)
+    // near: the positions of 64 tokens, of which this run's first is `first`, a lane each
+    __device__ __forceinline__ void fetch_angles(const Turn &t, const Positions &near, int first, int u)
     {
-        if (turns) ang[u] = angles<ONE>(t, positions<ONE>(t, token_of(u * RPL + g)), i, axes);
+        if (!keys) return;
+        const int row = u * RPL + g;
+        Positions at;
+        if (first + (u + 1) * RPL <= 64) {
+            at.p[0] = __shfl(near.p[0], first + row, 64);
+            if constexpr (!ONE)
+#pragma unroll
+                for (int a = 1; a < 4; ++a) at.p[a] = __shfl(near.p[a], first + row, 64);
+        } else at = positions<ONE>(t, token_of(row));
+        ang[u] = angles<ONE>(t, at, i, axes);
     }
     __device__ __forceinline__ void fetch(const Side &side, int h, int u)
     {
@@ -156,18 +167,22 @@ template <int D, bool ONE, bool NEIGHBOURS>
 __device__ __forceinline__ void turn_queries(const Queries &q, const Turn &t, int64_t token, int i, int h0, int count)
 {
     const Channels ch = channels(t, i);
-    Angles r;
-    if (ch.turned) r = angles<ONE>(t, positions<ONE>(t, token), i, lane_axes(t, i));
+    const Positions where = positions<ONE>(t, token);        // (first, so that the table's row is asked for while the heads come)
     const __half *x = q.x + token * q.ld + (int64_t)h0 * D;
     __half *out = q.out + token * q.ldo + (int64_t)h0 * D;
-    for (int h = 0; h < count; h += kQueryHeads) {
-        uint2 raw[kQueryHeads][2];
+    uint2 raw[kQueryHeads][2];
+    auto fetch = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kQueryHeads; ++u) {
             const int at = min(h + u, count - 1) * D;
             raw[u][0] = load4<false>(x + at + ch.lo);
             raw[u][1] = load4<false>(x + at + ch.hi);
         }
+    };
+    fetch(0);
+    const Angles r = angles<ONE>(t, where, i, lane_axes(t, i));
+    for (int h = 0; h < count; h += kQueryHeads) {
+        if (h) fetch(h);
 #pragma unroll
         for (int u = 0; u < kQueryHeads; ++u) {
             if (h + u >= count) break;
@@ -196,8 +211,8 @@ __device__ __forceinline__ void query_group(const Step &p, uint32_t group)
 {
     constexpr int LPR = D / 8;
     const int chunks = (p.q.heads + p.q_heads - 1) / p.q_heads;
-    const int64_t row = (int64_t)group * (256 / LPR) + threadIdx.x / LPR, token = row / chunks;
-    if (token >= p.T) return;
+    const uint32_t row = group * (256 / LPR) + threadIdx.x / LPR, token = row / (uint32_t)chunks;      // (2^24 workgroups at most)
+    if (token >= (uint32_t)p.T) return;
     const int h0 = (int)(row - token * chunks) * p.q_heads;
     turn_queries<D, ONE, NEIGHBOURS>(p.q, p.turn, token, threadIdx.x % LPR, h0, min(p.q_heads, p.q.heads - h0));
 }
@@ -210,17 +225,21 @@ void rotary_kv8_kernel(Step p)
 {
     if (blockIdx.x >= p.appends) return query_group<D, ONE, NEIGHBOURS>(p, blockIdx.x - p.appends);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t item = (int64_t)blockIdx.x * 4 + wave, t = item / (2 * p.Hkv);
-    const int which = (int)(item - t * (2 * p.Hkv));
+    const uint32_t item = blockIdx.x * 4 + wave, token = item / (uint32_t)(2 * p.Hkv);
+    const int which = (int)(item - token * (2 * p.Hkv));
+    const int64_t t = token;
     if (t >= p.T) return;
     const bool is_k = which < p.Hkv;
     const int h = is_k ? which : which - p.Hkv;
     const Side side = is_k ? p.k : p.v;
     TurnedRun<D, 16, ONE, NEIGHBOURS, false> run;
+    // (what the rest waits for in turn comes first: slots, positions, then the row, then the angles)
+    const Slots slots = slots_from(p.slot, p.T, t);
+    const Positions near = positions<ONE>(p.turn, min(t + (threadIdx.x & 63), (int64_t)p.T - 1));
     run.place(p.turn, t, p.T, is_k);
     run.fetch(side, h, 0);
-    run.fetch_angles(p.turn, 0);
-    const Window w = window(p.slot, p.slots, p.T, t, 1, 1 << p.shift);
+    run.fetch_angles(p.turn, near, 0, 0);
+    const Window w = window(slots, p.slots, p.T, t, 1, 1 << p.shift);
     if (!w.leaders) return;
     const int32_t first = __builtin_amdgcn_readlane(w.got, 0);
     run.o = run.at = first & ((1 << p.shift) - 1);
@@ -231,7 +250,7 @@ void rotary_kv8_kernel(Step p)
     for (int u = 1; u < run.kLoads; ++u)
         if (u * run.RPL < run.len) {
             run.fetch(side, h, u);
-            run.fetch_angles(p.turn, u);
+            run.fetch_angles(p.turn, near, 0, u);
         }
     run.take();
     run.end(p.turn, side, h, head, p.shift, s_old, run.largest(p.turn, side, h), threadIdx.x & 63, 64);
@@ -252,7 +271,9 @@ void rotary_kv8_many_kernel(Step p)
     const int h0 = (is_k ? which : which - chunks) * p.heads, h1 = min(h0 + p.heads, p.Hkv);
     const Side side = is_k ? p.k : p.v;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), bs = 1 << p.shift;
-    const Window w = window(p.slot, p.slots, p.T, t_first, p.slab, bs);        // (the same in all four)
+    const Slots slots = slots_from(p.slot, p.T, t_first);
+    const Positions near = positions<ONE>(p.turn, min(t_first + (threadIdx.x & 63), (int64_t)p.T - 1));
+    const Window w = window(slots, p.slots, p.T, t_first, p.slab, bs);         // (the same in all four)
     const bool alone = __builtin_popcountll(w.leaders) > 3 || bs <= ROWS;
     int turn = 0, sync = 0;                                                  // of the runs; nobody writes maxima before all have read the last but one's
     for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1, ++turn) {
@@ -270,7 +291,7 @@ void rotary_kv8_many_kernel(Step p)
             if (u * run.RPL < run.len) run.fetch(side, h0, u);
 #pragma unroll
         for (int u = 0; u < run.kLoads; ++u)
-            if (u * run.RPL < run.len) run.fetch_angles(p.turn, u);
+            if (u * run.RPL < run.len) run.fetch_angles(p.turn, near, l0 + row0, u);
         for (int h = h0; h < h1; ++h) {
             const int64_t head = (int64_t)(first >> p.shift) * p.Hkv + h;
             const float s_old = run.o > 0 ? side.scale[head] : 0.0f;
