@@ -33,8 +33,8 @@ __device__ __forceinline__ uint2 load4(const __half *p)
 
 // A run of rows of K, turned, or of V, for one head after another: Run (atom_kv8_append.h) on fp32 values, the maximum as the bits of a
 // float.  Row r is token `token` + r; a wavefront has ROWS of them in registers (those of a longer run are read twice), with
-// their angles, which all heads share.  ONCE: what is read is not kept in the caches.
-template <int D, int ROWS, bool ONE, bool NEIGHBOURS, bool ONCE>
+// their angles, which all heads share.  ONCE: what is read is not kept in the caches.  LONGER: there may be runs of more than ROWS.
+template <int D, int ROWS, bool ONE, bool NEIGHBOURS, bool ONCE, bool LONGER>
 struct TurnedRun {
     static constexpr int LPR = D / 8, RPL = 64 / LPR, kLoads = ROWS / RPL;
     Angles ang[kLoads];
@@ -113,7 +113,7 @@ struct TurnedRun {
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) top = max(top, magnitude(u * RPL + g, x[u]));
-        for (int row = ROWS; row < len; row += RPL) {
+        for (int row = ROWS; LONGER && row < len; row += RPL) {
             float v[8];
             again(t, side, h, row + g, v);
             top = max(top, magnitude(row + g, v));
@@ -148,7 +148,7 @@ struct TurnedRun {
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) store(block, u * RPL + g, x[u], r);
-        for (int row = ROWS; row < len; row += RPL) {
+        for (int row = ROWS; LONGER && row < len; row += RPL) {
             float v[8];
             again(t, side, h, row + g, v);
             store(block, row + g, v, r);
@@ -232,7 +232,7 @@ void rotary_kv8_kernel(Step p)
     const bool is_k = which < p.Hkv;
     const int h = is_k ? which : which - p.Hkv;
     const Side side = is_k ? p.k : p.v;
-    TurnedRun<D, 16, ONE, NEIGHBOURS, false> run;
+    TurnedRun<D, 16, ONE, NEIGHBOURS, false, true> run;
     // (what the rest waits for in turn comes first: slots, positions, then the row, then the angles)
     const Slots slots = slots_from(p.slot, p.T, t);
     const Positions near = positions<ONE>(p.turn, min(t + (threadIdx.x & 63), (int64_t)p.T - 1));
@@ -257,8 +257,11 @@ void rotary_kv8_kernel(Step p)
 }
 
 // Many tokens: a workgroup of four wavefronts for `slab` tokens and some heads of K or of V writes the runs that begin among them, each whole, also past
-// the slab's end.  Up to three runs are written by all four, ROWS rows each; more of them, and runs of ROWS at most, one by each in turn.
-template <int D, int ROWS, bool ONE, bool NEIGHBOURS, bool ONCE>
+// the slab's end.  Up to three runs are written by all four, ROWS rows each; more of them, and runs of blocks of ROWS at most (LONG: of more), one by each in turn.
+// ROWS is 16: 32 rows of 128 channels with their angles are all registers of a SIMD's lane, and one workgroup a CU (15000 tokens of 32 heads, blocks of 32, 396 us
+// for 153; blocks of 128 231 for 102).  Past the caches where blocks are longer and heads of 128 (2381 tokens of 32 heads, blocks of 64, 56.5 us and 60.8 through
+// them; heads of 64 33.3 and 30.4).
+template <int D, int ROWS, bool ONE, bool NEIGHBOURS, bool LONG>
 __global__ __launch_bounds__(256)
 void rotary_kv8_many_kernel(Step p)
 {
@@ -274,14 +277,14 @@ void rotary_kv8_many_kernel(Step p)
     const Slots slots = slots_from(p.slot, p.T, t_first);
     const Positions near = positions<ONE>(p.turn, min(t_first + (threadIdx.x & 63), (int64_t)p.T - 1));
     const Window w = window(slots, p.slots, p.T, t_first, p.slab, bs);         // (the same in all four)
-    const bool alone = __builtin_popcountll(w.leaders) > 3 || bs <= ROWS;
+    const bool alone = !LONG || __builtin_popcountll(w.leaders) > 3;
     int turn = 0, sync = 0;                                                  // of the runs; nobody writes maxima before all have read the last but one's
     for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1, ++turn) {
         if (alone && (turn & 3) != wave) continue;
         const int l0 = __builtin_ctzll(leaders), len = run_length(p.slot, p.T, w, t_first, l0, bs);
         const int row0 = alone ? 0 : wave * ROWS;
         const int32_t first = __builtin_amdgcn_readlane(w.got, l0);
-        TurnedRun<D, ROWS, ONE, NEIGHBOURS, ONCE> run;
+        TurnedRun<D, ROWS, ONE, NEIGHBOURS, LONG && D == 128, LONG> run;
         run.place(p.turn, t_first + l0 + row0, p.T, is_k);
         run.o = first & (bs - 1);
         run.at = run.o + row0;
@@ -363,10 +366,8 @@ hipError_t launch_rotary_kv8_append(const RotaryKv8 &a, hipStream_t stream)
 #define ATOM_TURN(D, ONE, NEIGHBOURS)                                                                                      \
     do {                                                                                                                   \
         auto kern = !s.slab ? &rotary_kv8_kernel<D, ONE, NEIGHBOURS>                                                       \
-                    : a.block_tokens == 128 ? &rotary_kv8_many_kernel<D, 32, ONE, NEIGHBOURS, true>                        \
-                    : a.block_tokens == 64  ? &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS, true>                        \
-                    : a.block_tokens == 32  ? &rotary_kv8_many_kernel<D, 32, ONE, NEIGHBOURS, false>                       \
-                                            : &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS, false>;                      \
+                    : a.block_tokens == 16 ? &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS, false>                        \
+                                           : &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS, true>;                        \
         hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, p);                                                           \
     } while (0)
 #define ATOM_TURN_D(D)                                                \
