@@ -160,7 +160,7 @@ struct TurnedRun {
 struct Queries { const __half *x; int64_t ld; __half *out; int64_t ldo; int heads; };
 
 constexpr int kQueryHeads = 4;                               // of a lane, in flight together; through the caches (where the step comes from the projection before it:
-                                                             // 1116 tokens, 64 heads on 8, 15.8 us; past the caches 19.2, and up to 5 % less where nothing is cached)
+                                                             // 1116 tokens, 64 heads on 8, 13.9 us; past the caches 15.6, and up to 5 % less where nothing is cached)
 
 // Eight channels of a lane, for `count` heads of a token from h0 on.
 template <int D, bool ONE, bool NEIGHBOURS>
@@ -206,12 +206,12 @@ struct Step {
     int q_heads;                                             // heads of a lane there
 };
 
-template <int D, bool ONE, bool NEIGHBOURS>
+template <int D, int THREADS, bool ONE, bool NEIGHBOURS>
 __device__ __forceinline__ void query_group(const Step &p, uint32_t group)
 {
     constexpr int LPR = D / 8;
     const int chunks = (p.q.heads + p.q_heads - 1) / p.q_heads;
-    const uint32_t row = group * (256 / LPR) + threadIdx.x / LPR, token = row / (uint32_t)chunks;      // (2^24 workgroups at most)
+    const uint32_t row = group * (THREADS / LPR) + threadIdx.x / LPR, token = row / (uint32_t)chunks;      // (2^24 workgroups at most)
     if (token >= (uint32_t)p.T) return;
     const int h0 = (int)(row - token * chunks) * p.q_heads;
     turn_queries<D, ONE, NEIGHBOURS>(p.q, p.turn, token, threadIdx.x % LPR, h0, min(p.q_heads, p.q.heads - h0));
@@ -223,7 +223,7 @@ template <int D, bool ONE, bool NEIGHBOURS>
 __global__ __launch_bounds__(256)
 void rotary_kv8_kernel(Step p)
 {
-    if (blockIdx.x >= p.appends) return query_group<D, ONE, NEIGHBOURS>(p, blockIdx.x - p.appends);
+    if (blockIdx.x >= p.appends) return query_group<D, 256, ONE, NEIGHBOURS>(p, blockIdx.x - p.appends);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t item = blockIdx.x * 4 + wave, token = item / (uint32_t)(2 * p.Hkv);
     const int which = (int)(item - token * (2 * p.Hkv));
@@ -256,17 +256,17 @@ void rotary_kv8_kernel(Step p)
     run.end(p.turn, side, h, head, p.shift, s_old, run.largest(p.turn, side, h), threadIdx.x & 63, 64);
 }
 
-// Many tokens: a workgroup of four wavefronts for `slab` tokens and some heads of K or of V writes the runs that begin among them, each whole, also past
-// the slab's end.  Up to three runs are written by all four, ROWS rows each; more of them, and runs of blocks of ROWS at most (LONG: of more), one by each in turn.
-// ROWS is 16: 32 rows of 128 channels with their angles are all registers of a SIMD's lane, and one workgroup a CU (15000 tokens of 32 heads, blocks of 32, 396 us
-// for 153; blocks of 128 231 for 102).  Past the caches where blocks are longer and heads of 128 (2381 tokens of 32 heads, blocks of 64, 56.5 us and 60.8 through
-// them; heads of 64 33.3 and 30.4).
-template <int D, int ROWS, bool ONE, bool NEIGHBOURS, bool LONG>
-__global__ __launch_bounds__(256)
+// Many tokens: a workgroup of four wavefronts (eight for blocks of 128) for `slab` tokens and some heads of K or of V writes the runs that begin among them, each whole, also past
+// the slab's end.  Up to three runs are written by all of them, ROWS rows each; more of them, and runs of blocks of ROWS at most (LONG: of more), one by each in turn.
+// ROWS is 16: 32 rows of 128 channels with their angles are all registers of a SIMD's lane, and one workgroup a CU (15000 tokens of 32 heads, blocks of
+// 32, 396 us for 153; blocks of 128, four wavefronts of 32 rows, 231 for 175).  Past the caches where blocks are longer and heads of 128 (2381 tokens of 32
+// heads, blocks of 64, 56.5 us and 60.8 through them; heads of 64 33.3 and 30.4).  10240 tokens of 32 heads and as many query heads, blocks of 64: 86.4 us.
+template <int D, int ROWS, int WAVES, bool ONE, bool NEIGHBOURS, bool LONG>
+__global__ __launch_bounds__(64 * WAVES)
 void rotary_kv8_many_kernel(Step p)
 {
-    __shared__ uint32_t s_top[2][4];
-    if (blockIdx.x >= p.appends) return query_group<D, ONE, NEIGHBOURS>(p, blockIdx.x - p.appends);
+    __shared__ uint32_t s_top[2][WAVES];
+    if (blockIdx.x >= p.appends) return query_group<D, 64 * WAVES, ONE, NEIGHBOURS>(p, blockIdx.x - p.appends);
     const int chunks = (p.Hkv + p.heads - 1) / p.heads;
     const int64_t group = blockIdx.x / (2 * chunks), t_first = group * p.slab;
     const int which = (int)(blockIdx.x - group * (2 * chunks));
@@ -276,11 +276,11 @@ void rotary_kv8_many_kernel(Step p)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), bs = 1 << p.shift;
     const Slots slots = slots_from(p.slot, p.T, t_first);
     const Positions near = positions<ONE>(p.turn, min(t_first + (threadIdx.x & 63), (int64_t)p.T - 1));
-    const Window w = window(slots, p.slots, p.T, t_first, p.slab, bs);         // (the same in all four)
+    const Window w = window(slots, p.slots, p.T, t_first, p.slab, bs);         // (the same in all of them)
     const bool alone = !LONG || __builtin_popcountll(w.leaders) > 3;
     int turn = 0, sync = 0;                                                  // of the runs; nobody writes maxima before all have read the last but one's
     for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1, ++turn) {
-        if (alone && (turn & 3) != wave) continue;
+        if (alone && (turn & (WAVES - 1)) != wave) continue;
         const int l0 = __builtin_ctzll(leaders), len = run_length(p.slot, p.T, w, t_first, l0, bs);
         const int row0 = alone ? 0 : wave * ROWS;
         const int32_t first = __builtin_amdgcn_readlane(w.got, l0);
@@ -308,8 +308,10 @@ void rotary_kv8_many_kernel(Step p)
                 if ((threadIdx.x & 63) == 0) tops[wave] = top;
                 __syncthreads();
                 top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+#pragma unroll
+                for (int v = 4; v < WAVES; ++v) top = max(top, tops[v]);
             }
-            run.end(p.turn, side, h, head, p.shift, s_old, top, alone ? threadIdx.x & 63 : threadIdx.x, alone ? 64 : 256);
+            run.end(p.turn, side, h, head, p.shift, s_old, top, alone ? threadIdx.x & 63 : threadIdx.x, alone ? 64 : 64 * WAVES);
         }
     }
 }
@@ -320,29 +322,31 @@ namespace atom_internal {
 
 // How a call runs: tokens to a workgroup (0: a wavefront for each token and head), cache heads to a workgroup, workgroups that append;
 // query heads to a lane, workgroups that turn them.
-struct TurnShape { int slab, heads; int64_t appends; int q_heads; int64_t queries; };
+struct TurnShape { int slab, heads; int64_t appends; int q_heads; int64_t queries; int threads; };
 
 //
-// A wavefront for each token and head is the shorter chain (64 tokens, 32 heads: 7.6 us); with many tokens most of them would find that their run begins
+// A wavefront for each token and head is the shorter chain (64 tokens, 32 heads: 4.2 us); with many tokens most of them would find that their run begins
 // elsewhere.  Short blocks: 32 tokens a workgroup, so that a wavefront has a run and not two in turn (343 tokens of 32 heads, blocks of 16: 15.7 us
 // against 18.3 with 64).  Heads are shared out while there are fewer than 1024 workgroups.
 static TurnShape turn_shape(int64_t T, int H, int Hkv, int D, int block_tokens)
 {
     TurnShape s = {};
+    s.threads = 256;
     const int64_t items = T * 2 * Hkv;
     const bool long_runs = block_tokens >= 64;
     if (long_runs ? T < 256 : items <= 16384) {
         s.heads = 1;
         s.appends = (items + 3) / 4;
     } else {
-        s.slab = items <= 16384 ? 8 : long_runs ? 64 : 32;
+        if (block_tokens == 128) s.threads = 512;
+        s.slab = items <= 16384 ? 8 : long_runs && items > 131072 ? 64 : 32;
         const int64_t slabs = (T + s.slab - 1) / s.slab;
         s.heads = 8;
         while (s.heads > 1 && slabs * 2 * ((Hkv + s.heads - 1) / s.heads) < 1024) s.heads /= 2;
         s.appends = slabs * 2 * ((Hkv + s.heads - 1) / s.heads);
     }
     s.q_heads = 8;
-    const int64_t rows = 256 / (D / 8);
+    const int64_t rows = s.threads / (D / 8);
     while (s.q_heads > 1 && T * ((H + s.q_heads - 1) / s.q_heads) / rows < 512) s.q_heads /= 2;
     s.queries = (T * ((H + s.q_heads - 1) / s.q_heads) + rows - 1) / rows;
     return s;
@@ -351,7 +355,7 @@ static TurnShape turn_shape(int64_t T, int H, int Hkv, int D, int block_tokens)
 bool rotary_kv8_fits(int64_t T, int H, int Hkv, int D, int block_tokens)
 {
     const TurnShape s = turn_shape(T, H, Hkv, D, block_tokens);
-    return s.appends + s.queries <= atom_launch::kMostThreads / 256;
+    return s.appends + s.queries <= atom_launch::kMostThreads / s.threads;
 }
 
 hipError_t launch_rotary_kv8_append(const RotaryKv8 &a, hipStream_t stream)
@@ -366,9 +370,10 @@ hipError_t launch_rotary_kv8_append(const RotaryKv8 &a, hipStream_t stream)
 #define ATOM_TURN(D, ONE, NEIGHBOURS)                                                                                      \
     do {                                                                                                                   \
         auto kern = !s.slab ? &rotary_kv8_kernel<D, ONE, NEIGHBOURS>                                                       \
-                    : a.block_tokens == 16 ? &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS, false>                        \
-                                           : &rotary_kv8_many_kernel<D, 16, ONE, NEIGHBOURS, true>;                        \
-        hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, p);                                                           \
+                    : a.block_tokens == 16  ? &rotary_kv8_many_kernel<D, 16, 4, ONE, NEIGHBOURS, false>                    \
+                    : a.block_tokens == 128 ? &rotary_kv8_many_kernel<D, 16, 8, ONE, NEIGHBOURS, true>                     \
+                                            : &rotary_kv8_many_kernel<D, 16, 4, ONE, NEIGHBOURS, true>;                    \
+        hipLaunchKernelGGL(kern, grid, dim3(s.threads), 0, stream, p);                                                          \
     } while (0)
 #define ATOM_TURN_D(D)                                                \
     do {                                                              \
