@@ -325,16 +325,18 @@ namespace atom_internal {
 struct TurnShape { int slab, heads; int64_t appends; int q_heads; int64_t queries; int threads; };
 
 //
-// A wavefront for each token and head is the shorter chain (64 tokens, 32 heads: 4.2 us); with many tokens most of them would find that their run begins
-// elsewhere.  Short blocks: 32 tokens a workgroup, so that a wavefront has a run and not two in turn (343 tokens of 32 heads, blocks of 16: 15.7 us
-// against 18.3 with 64).  Heads are shared out while there are fewer than 1024 workgroups.
+// A wavefront for each token and head is the shorter chain for single tokens (64 of 32 heads 4.2 us, 160 6.5 and 11.1 by workgroups), and slow where one
+// has a long run to itself (a prompt of 200 tokens, blocks of 64, 19.0 us and 6.5); with many tokens most of them would find that their run begins elsewhere.
+// The host knows neither, so: up to 128 tokens where blocks are long.  Tokens to a workgroup: eight while there are few, so that a wavefront has a run or
+// two in turn, then 32 (300 single tokens of 32 heads, blocks of 64: 64 34.0 us, 32 21.1; a step with chunks of 200 26.1 and 23.2), 64 with many (32 as
+// good).  Heads are shared out while there are fewer than 1024 workgroups.
 static TurnShape turn_shape(int64_t T, int H, int Hkv, int D, int block_tokens)
 {
     TurnShape s = {};
     s.threads = 256;
     const int64_t items = T * 2 * Hkv;
     const bool long_runs = block_tokens >= 64;
-    if (long_runs ? T < 256 : items <= 16384) {
+    if (long_runs ? T < 128 : items <= 16384) {
         s.heads = 1;
         s.appends = (items + 3) / 4;
     } else {
