@@ -206,8 +206,9 @@ __device__ __forceinline__ void put(const Args &p, uint4 *out, int64_t m, int k,
         out[(((int64_t)u * p.halves + tile) * 16 + place) * (p.combine ? 2 * p.rows : p.rows) + row] = v;
     } else {
         const int i = is4 ? (k >> 3) & 7 : (j >> 3) & 3, c = is4 ? (k >> 6) & 1 : (j >> 5) & 1;
-        const int64_t block = m / (32 * p.wide), t = m / 32 % p.wide;
-        out[((((block * U + u) * p.halves + half) * p.wide + t) * 8 + i) * 64 + c * 32 + m % 32] = v;
+        const int s = p.wide - 1;                             // (wide is 1 or 2)
+        const int64_t block = m >> (5 + s), t = m >> 5 & s;
+        out[((((block * U + u) * p.halves + half) * p.wide + t) * 8 + i) * 64 + c * 32 + (m & 31)] = v;
     }
 }
 
@@ -540,7 +541,7 @@ void w4a16_wide_kernel(Args p)
     const int col = lane & 31, kc = lane >> 5;
     const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, U = 2 * G - G4;
     const uint32_t block = blockIdx.x % p.row_blocks, rest = blockIdx.x / p.row_blocks, part = rest % (uint32_t)p.parts, tile = rest / (uint32_t)p.parts;
-    const int begin = (int)((int64_t)part * U / p.parts), end = (int)((int64_t)(part + 1) * U / p.parts);
+    const int begin = (int)(part * (uint32_t)U / (uint32_t)p.parts), end = (int)((part + 1) * (uint32_t)U / (uint32_t)p.parts);
 
     // The first weight row of a tile; its matrix.  (Columns >= N are computed and never stored.)
     auto rows_of = [&](int t) ATOM_INLINE { return GATED ? ((int64_t)tile * (kWaves / 2) + t / 2) * 32 : ((int64_t)tile * kWaves + t) * 32; };
@@ -688,15 +689,15 @@ template <bool GATED>
 __global__ __launch_bounds__(256)
 void w4a16_join_kernel(Args p)
 {
-    const int64_t outputs = p.M * p.N, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t e = blockIdx.x * 256 + threadIdx.x, m = e / (uint32_t)p.N;              // (fewer than 2^30: host)
+    const int64_t outputs = p.M * p.N;
     if (e >= outputs) return;
     float y = 0.0f, up = 0.0f;
     for (int s = 0; s < p.parts; ++s) {
         y += p.sums[s * (GATED ? 2 : 1) * outputs + e];
         if constexpr (GATED) up += p.sums[(2 * s + 1) * outputs + e];
     }
-    const int64_t m = e / p.N;
-    store<GATED>(p, m, e - m * p.N, y, up);
+    store<GATED>(p, m, e - m * (uint32_t)p.N, y, up);
 }
 
 }  // namespace
