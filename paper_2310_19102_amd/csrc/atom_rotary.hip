@@ -80,7 +80,7 @@ hipError_t launch_rotary_table(const double *freq, int n_pairs, int64_t n_pos, f
 
 // Values from which a lane takes four heads and their angles once (a step of 64 tokens of 40 heads of 128: 3.2 us with one, 3.55 with four; 200 tokens 4.2
 // and 3.75; 1600 20.8 and 9.3), and from which the heads come past the caches (3200 such tokens: 14.8 us through them, 16.8 past them; 6400 29.3 and
-// 27.4; 4999 tokens of 72 heads with three axes 37.4 and 33.3: 5.6 TB/s, what is read and written bounds it).
+// 27.4; 4999 tokens of 72 heads with three axes 37.4 and 33.3, and 31.4 with the positions asked for first: 5.9 TB/s, what is read and written bounds it).
 constexpr int64_t kFourHeads = 1 << 19, kReadOnce = (int64_t)24 << 20;
 
 hipError_t launch_rotary(const void *x, int64_t T, int64_t ldx, int heads, int D, const Turn &t, bool transposed, void *out, int64_t ldo,
