@@ -61,8 +61,8 @@ __device__ __forceinline__ uint32_t recode4(uint32_t w, float ratio)
 // What a call writes to and from, of K or of V.
 struct Side { const __half *x; int64_t ld; int8_t *codes; float *scale; };
 
-// A wavefront's window of 64 slots: which of the first `slab` tokens begin a run (a run: tokens whose slots follow one another inside one block).
-struct Window { int32_t got; bool valid; uint64_t leaders; };
+// A wavefront's window of 64 slots: which of the first `slab` tokens begin a run (a run: tokens whose slots follow one another inside one block), which of all go on with one.
+struct Window { int32_t got; bool valid; uint64_t leaders, followers; };
 
 // What it reads: a lane's slot and the one before the first.
 struct Slots { int32_t got, before; };
@@ -82,6 +82,7 @@ __device__ __forceinline__ Window window(const Slots &s, int32_t slots, int T, i
     if (lane == 0) prev = t_first > 0 ? s.before : -2;
     const bool follows = prev >= 0 && prev < slots && w.got == prev + 1 && (w.got & (bs - 1)) != 0;
     w.leaders = __ballot(w.valid && !follows && lane < slab);
+    w.followers = __ballot(w.valid && follows);
     return w;
 }
 

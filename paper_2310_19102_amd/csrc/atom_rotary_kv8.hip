@@ -31,6 +31,23 @@ __device__ __forceinline__ uint2 load4(const __half *p)
     else return *reinterpret_cast<const uint2 *>(p);
 }
 
+// A run's scale from its maximum (the bits of a float) and that of the block's older rows (0: none), its reciprocal, and what older codes are brought to it with.
+struct Scale { float s, r, ratio; bool grown; };
+
+__device__ __forceinline__ Scale scale_of(uint32_t top, float s_old)
+{
+    const float s_new = __builtin_bit_cast(float, top) / 127.0f, s = s_new > s_old || s_new != s_new ? s_new : s_old;
+    // (a scale below the normal numbers has no reciprocal)
+    return {s, s >= 1.17549435e-38f ? 1.0f / s : 0.0f, s_old / s, s > s_old && s_old > 0.0f};
+}
+
+__device__ __forceinline__ void recode16(int8_t *at, float ratio)
+{
+    uint4 w = *reinterpret_cast<const uint4 *>(at);
+    w = make_uint4(recode4(w.x, ratio), recode4(w.y, ratio), recode4(w.z, ratio), recode4(w.w, ratio));
+    *reinterpret_cast<uint4 *>(at) = w;
+}
+
 // A run of rows of K, turned, or of V, for one head after another: Run (atom_kv8_append.h) on fp32 values, the maximum as the bits of a
 // float.  Row r is token `token` + r; a wavefront has ROWS of them in registers (those of a longer run are read twice), with
 // their angles, which all heads share.  ONCE: what is read is not kept in the caches.  LONGER: there may be runs of more than ROWS.
@@ -134,17 +151,10 @@ struct TurnedRun {
     __device__ __forceinline__ void end(const Turn &t, const Side &side, int h, int64_t head, int shift, float s_old, uint32_t top, int thread, int threads)
     {
         int8_t *block = side.codes + (head << shift) * D;
-        const float s_new = __builtin_bit_cast(float, top) / 127.0f, s = s_new > s_old || s_new != s_new ? s_new : s_old;
-        // (a scale below the normal numbers has no reciprocal)
-        const float r = s >= 1.17549435e-38f ? 1.0f / s : 0.0f;
-        if (s > s_old && s_old > 0.0f) {
-            const float ratio = s_old / s;
-            for (int b = 16 * thread; b < o * D; b += 16 * threads) {
-                uint4 w = *reinterpret_cast<const uint4 *>(block + b);
-                w = make_uint4(recode4(w.x, ratio), recode4(w.y, ratio), recode4(w.z, ratio), recode4(w.w, ratio));
-                *reinterpret_cast<uint4 *>(block + b) = w;
-            }
-        }
+        const Scale scale = scale_of(top, s_old);
+        const float r = scale.r;
+        if (scale.grown)
+            for (int b = 16 * thread; b < o * D; b += 16 * threads) recode16(block + b, scale.ratio);
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) store(block, u * RPL + g, x[u], r);
@@ -153,9 +163,61 @@ struct TurnedRun {
             again(t, side, h, row + g, v);
             store(block, row + g, v, r);
         }
-        if (thread == 0) side.scale[head] = s;
+        if (thread == 0) side.scale[head] = scale.s;
     }
 };
+
+// Runs of one row each, a row to D / 8 lanes: those of tokens t_first + l that begin one, l from `group` on in steps of `groups`, for heads h0 .. h1 - 1 of K (keys) or
+// of V.  (Taken by a wavefront each, 300 tokens of 32 heads were 21.0 us, now 7.0, 1000 60 and 14.8.)
+template <int D, bool ONE, bool NEIGHBOURS>
+__device__ __forceinline__ void append_singles(const Turn &t, const Side &side, bool keys, const Window &w, const Positions &near, int64_t t_first, int slab,
+                                               int Hkv, int shift, int h0, int h1, int group, int groups)
+{
+    constexpr int LPR = D / 8;
+    const int i = threadIdx.x % LPR;
+    const Channels ch = channels(t, i);
+    const uint32_t axes = lane_axes(t, i);
+    for (int l0 = 0; l0 < slab; l0 += groups) {
+        const int l = min(l0 + group, 63);
+        const int32_t slot = __shfl(w.got, l, 64);
+        Positions at;
+        at.p[0] = __shfl(near.p[0], l, 64);
+        if constexpr (!ONE)
+#pragma unroll
+            for (int a = 1; a < 4; ++a) at.p[a] = __shfl(near.p[a], l, 64);
+        if (l0 + group >= slab || !(w.leaders >> l & 1)) continue;
+        const __half *row = side.x + (t_first + l) * side.ld;
+        uint2 lo = load4<false>(row + h0 * D + ch.lo), hi = load4<false>(row + h0 * D + ch.hi);
+        Angles r;
+        if (keys) r = angles<ONE>(t, at, i, axes);
+        const int o = slot & ((1 << shift) - 1);
+        for (int h = h0; h < h1; ++h) {
+            const int64_t head = (int64_t)(slot >> shift) * Hkv + h;
+            const float s_old = o > 0 ? side.scale[head] : 0.0f;
+            float x[8];
+            widen(lo, x);
+            widen(hi, x + 4);
+            if (h + 1 < h1) {
+                lo = load4<false>(row + (h + 1) * D + ch.lo);
+                hi = load4<false>(row + (h + 1) * D + ch.hi);
+            }
+            if (keys && ch.turned) turn<NEIGHBOURS>(x, r, 1.0f);
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = max(top, __builtin_bit_cast(uint32_t, x[k]) & 0x7fffffffu);
+#pragma unroll
+            for (int step = 1; step < LPR; step *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, step, 64));
+            const Scale s = scale_of(top, s_old);
+            int8_t *block = side.codes + (head << shift) * D;
+            if (s.grown)
+                for (int b = 16 * i; b < o * D; b += 16 * LPR) recode16(block + b, s.ratio);
+            const uint32_t a = s.r > 0.0f ? codes4(x, s.r) : 0, b = s.r > 0.0f ? codes4(x + 4, s.r) : 0;
+            *reinterpret_cast<uint32_t *>(block + o * D + ch.lo) = a;
+            *reinterpret_cast<uint32_t *>(block + o * D + ch.hi) = b;
+            if (i == 0) side.scale[head] = s.s;
+        }
+    }
+}
 
 struct Queries { const __half *x; int64_t ld; __half *out; int64_t ldo; int heads; };
 
@@ -232,7 +294,7 @@ void rotary_kv8_kernel(Step p)
     const bool is_k = which < p.Hkv;
     const int h = is_k ? which : which - p.Hkv;
     const Side side = is_k ? p.k : p.v;
-    TurnedRun<D, 16, ONE, NEIGHBOURS, false, true> run;
+    TurnedRun<D, 16, ONE, NEIGHBOURS, false, false> run;
     // (what the rest waits for in turn comes first: slots, positions, then the row, then the angles)
     const Slots slots = slots_from(p.slot, p.T, t);
     const Positions near = positions<ONE>(p.turn, min(t + (threadIdx.x & 63), (int64_t)p.T - 1));
@@ -277,6 +339,12 @@ void rotary_kv8_many_kernel(Step p)
     const Slots slots = slots_from(p.slot, p.T, t_first);
     const Positions near = positions<ONE>(p.turn, min(t_first + (threadIdx.x & 63), (int64_t)p.T - 1));
     const Window w = window(slots, p.slots, p.T, t_first, p.slab, bs);         // (the same in all of them)
+    if (p.slab < 64 && !(w.followers & (((uint64_t)2 << p.slab) - 2))) {       // single tokens (or none)
+        constexpr int RPL = 512 / D;
+        append_singles<D, ONE, NEIGHBOURS>(p.turn, side, is_k, w, near, t_first, p.slab, p.Hkv, p.shift, h0, h1,
+                                           wave * RPL + (int)(threadIdx.x & 63) / (D / 8), WAVES * RPL);
+        return;
+    }
     const bool alone = !LONG || __builtin_popcountll(w.leaders) > 3;
     int turn = 0, sync = 0;                                                  // of the runs; nobody writes maxima before all have read the last but one's
     for (uint64_t leaders = w.leaders; leaders; leaders &= leaders - 1, ++turn) {
@@ -325,23 +393,23 @@ namespace atom_internal {
 struct TurnShape { int slab, heads; int64_t appends; int q_heads; int64_t queries; int threads; };
 
 //
-// A wavefront for each token and head is the shorter chain for single tokens (64 of 32 heads 4.2 us, 160 6.5 and 11.1 by workgroups), and slow where one
-// has a long run to itself (a prompt of 200 tokens, blocks of 64, 19.0 us and 6.5); with many tokens most of them would find that their run begins elsewhere.
-// The host knows neither, so: up to 128 tokens where blocks are long.  Tokens to a workgroup: eight while there are few, so that a wavefront has a run or
-// two in turn, then 32 (300 single tokens of 32 heads, blocks of 64: 64 34.0 us, 32 21.1; a step with chunks of 200 26.1 and 23.2), 64 with many (32 as
-// good).  Heads are shared out while there are fewer than 1024 workgroups.
+// A wavefront for each token and head is the shorter chain for a few single tokens (20 of 32 heads 3.6 us and 3.7 by workgroups, 100 5.5 and 5.0), and slow
+// where one has a long run to itself (a prompt of 60 tokens, blocks of 64, 15.0 and 5.2).  Tokens to a workgroup: eight while there are few, then 32
+// (300 tokens of 32 heads in runs of one, each by a wavefront, blocks of 64: 64 of them 34.0 us, 32 21.1; a step with chunks of 200 26.1 and 23.2), 64 with many.
+// Heads are shared out while there are fewer than 1024 workgroups.
+constexpr int kFewTokens = 16;                               // (so no run is longer than the rows that a wavefront keeps)
+
 static TurnShape turn_shape(int64_t T, int H, int Hkv, int D, int block_tokens)
 {
     TurnShape s = {};
     s.threads = 256;
     const int64_t items = T * 2 * Hkv;
-    const bool long_runs = block_tokens >= 64;
-    if (long_runs ? T < 128 : items <= 16384) {
+    if (T < kFewTokens) {
         s.heads = 1;
         s.appends = (items + 3) / 4;
     } else {
         if (block_tokens == 128) s.threads = 512;
-        s.slab = items <= 16384 ? 8 : long_runs && items > 131072 ? 64 : 32;
+        s.slab = items <= 16384 ? 8 : block_tokens >= 64 && items > 131072 ? 64 : 32;
         const int64_t slabs = (T + s.slab - 1) / s.slab;
         s.heads = 8;
         while (s.heads > 1 && slabs * 2 * ((Hkv + s.heads - 1) / s.heads) < 1024) s.heads /= 2;

@@ -205,3 +205,35 @@ def test_cache_offsets_past_32_bits(new):
     for got, want in ((kc, small[1]), (vc, small[2])):
         assert torch.equal(got[0][far], want[0]) and torch.equal(got[1][far], want[1])
         assert int(torch.count_nonzero(got[1])) == int(torch.count_nonzero(want[1]))
+
+
+@pytest.mark.parametrize("D,bs,axes,interleaved", [(128, 64, 1, False), (64, 16, 2, True), (128, 128, 3, False), (64, 32, 1, False)])
+@pytest.mark.parametrize("Hkv,n", [(3, 40), (16, 700)])
+def test_single_tokens_of_many_requests(D, bs, axes, interleaved, Hkv, n):
+    """Every kind of row in a batch of single tokens: zeros, large ones, scales that grow under older rows, tokens without a slot; then what is not
+    finite and positions outside the table, which stay in their block and head."""
+    s = step([(i * 7 % 50, 1) for i in range(n)], 2 * Hkv, Hkv, D, bs, D // 2, axes, padding=9, missing=range(3, n, 11))
+    H = 2 * Hkv
+    s["qkv"][5, H:] = 0
+    s["qkv"][6, H:] *= 300
+    s["k"][1][:] *= 0.25
+    check(s, run(s, interleaved), interleaved)
+    s["slot"][[2, 9]] = [s["slot"][9], s["slot"][2]]          # blocks in another order
+    k = s["qkv"][:, H:H + Hkv]
+    k[7, 1, 3], k[8, 0, D - 1] = np.nan, np.inf
+    (s["pos"] if axes == 1 else s["pos"][0])[12] = -5
+    _, kc, vc, _ = run(s, interleaved)
+    with np.errstate(invalid="ignore"):
+        want = ref.turned(s["qkv"][:, :H + Hkv], s["pos"], s["tab"], s["axis"], interleaved)[:, H:]
+        codes, scale = kv8.append(np.where(np.isfinite(want), want, 0), *s["k"], s["slot"])
+    spoilt = np.zeros(scale.shape, bool)
+    for t in (7, 8, 12):
+        spoilt[s["slot"][t] // bs] = ~np.isfinite(want[t]).all(1)
+    assert spoilt.sum() == 2 + Hkv
+    got = kc[1].cpu().numpy()
+    assert np.array_equal(~np.isfinite(got), spoilt) and np.array_equal(got[~spoilt], scale[~spoilt])
+    assert np.array_equal(kc[0].cpu().numpy()[~spoilt], codes[~spoilt])
+    for t in (7, 8, 12):
+        block, o = divmod(int(s["slot"][t]), bs)
+        assert (kc[0].cpu().numpy()[block, spoilt[block], o] == 0).all()
+    assert np.isfinite(vc[1].cpu().numpy()).all()
