@@ -719,7 +719,7 @@ constexpr int kPartGroups = 32, kPartWorkgroups = 256;
 constexpr size_t kTwoGroupsLds = 80 * 1024 - 64, kOneGroupLds = 150 * 1024;
 
 // The weights' way to the operands and the wavefronts' sums, twice.
-static size_t sums_bytes(const ProductShape &s, int WM) { return (size_t)kWaves * WM * s.NT * (s.combine ? 2048 : 3072); }
+static size_t sums_bytes(const ProductShape &s, int WM) { return (size_t)kWaves * WM * s.NT * 1024 * (s.combine ? 2 : 3); }
 
 static ProductShape product_shape(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index)
 {
