@@ -727,8 +727,8 @@ atom_status atom_rotary_kv8_append(const void *q_f16, int64_t ldq, int32_t H, vo
  * Section 5.3; a layer of few rows is bound by reading its weights, Section 3, and those are the same):
  *   xr[m, j] = x[m, idx[j]], or with gamma RMSNorm(x)[m, idx[j]] * gamma[idx[j]]             (RMSNorm and product in fp32)
  *   y[m, n]  = fp16( residual[m, n] + sum_g w_scale[n, g] * sum_{k in g} w[n, k] * xr[m, k] )
- * Codes meet xr exactly in the fp16 matrix cores, where a normed xr goes in as the sum of two halves (22 bits; what is beyond
- * fp16's range counts as infinite).  Sums are fp32, in an order that depends on the sizes alone: results are deterministic.
+ * Codes meet xr exactly in the fp16 matrix cores, where a normed xr goes in as the sum of two halves (off by 2^-22 of itself, or by 2^-38
+ * of the row's largest where that is more; what is beyond fp16's range counts as infinite).  Sums are fp32, in an order that depends on the sizes alone: results are deterministic.
  * Meant for few rows (any number within the limits is taken; the 4-bit path is the faster one beyond a few hundred).
  *
  *   x_f16        [M, ldx] fp16, ldx >= K, ldx % 8 == 0, 16-byte aligned

@@ -664,8 +664,8 @@ def atom_w4a16_linear(x: torch.Tensor, gamma: Optional[torch.Tensor], eps: float
                       group_size: int = 128, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """A linear layer with quantised weights (``atom_quantize_weight``) and activations that stay in fp16: ``x`` [M, K] fp16,
     behind RMSNorm where ``gamma`` is given, in the order of ``reorder_idx`` (None: x already is in reordered order), plus
-    ``residual`` [M, N] where given (it may be ``out``).  Behind the norm a value keeps 22 bits (two halves).  Returns [M, N]
-    fp16.  In a capture that was not begun by torch.cuda.graph a ``workspace`` has to be given where
+    ``residual`` [M, N] where given (it may be ``out``).  Behind the norm a value is off by 2^-22 of itself (two halves), or by 2^-38 of
+    the row's largest where that is more; beyond fp16's range it counts as infinite.  Returns [M, N] fp16.  In a capture that was not begun by torch.cuda.graph a ``workspace`` has to be given where
     ``atom_w4a16_workspace_bytes`` is not 0."""
     return _run().w4a16_linear(x, gamma, eps, reorder_idx, w_q4, w_q8, w_scale, residual, group_size, out, workspace)
 

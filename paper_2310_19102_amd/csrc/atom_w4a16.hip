@@ -4,7 +4,9 @@
 //   h[m, n] = fp16( silu(gate) * up ),  gate and up two such sums of one xr
 // xr: the activations in reordered order, behind RMSNorm where gamma is given.  The matrix cores take fp16; what the norm gives has more bits,
 // and rounding it would be the largest error of the whole layer (1.4 to 1.8 times that of the output's own rounding), so it goes in as
-// two halves, hi + lo, 22 bits.
+// two halves, hi + lo, 22 bits.  A half's last step is 2^-24, so a row of small values (a small gamma, a row below eps) is brought to 2^14 by a power of two
+// first, which is taken back from its fp32 sums: what lo loses is 2^-22 of the value, or 2^-38 of the row's largest where that is more.  (Without it 2^-25 was lost
+// whatever the value: with a gamma of 2e-5 up to nine times all other errors.  It costs 0.1 to 0.4 us of the launch that lays out the rows.)
 //
 // MFMA 16x16x32 f16: lane l supplies row (l & 15) of its operand and the 8 values of k-chunk (l >> 4); the result has column
 // (l & 15) in lane l and rows 4 (l >> 4) + e in register e.  Activations are the row operand, weights the columns.  Which channels a
@@ -65,6 +67,7 @@ struct Args {
     const __half *residual; int64_t ldr;
     __half *y; int64_t ldy;
     const __half *staged; int rows;                          // laid out, `rows` rows of hi and behind them those of lo
+    float *back;                                             // behind a norm: what takes a row's power of two back
     bool combine;                                            // lo in rows 8 .. 15 of the one tile
     uint32_t tiles;
     int parts, span; float *sums;                            // parts of K, INT4 groups of one (few rows), their sums
@@ -107,17 +110,55 @@ __device__ __forceinline__ uint4 packed(const uint32_t (&w)[8])
                       __builtin_amdgcn_perm(w[7], w[6], sel));
 }
 
+// A row behind the norm: the sum of its squares, the largest magnitude of x times gamma; what a thread found of them.
+struct Norm {
+    float sum = 0.0f, top = 0.0f;
+    __device__ __forceinline__ void add(const uint4 &x, const uint4 &gamma)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = value_of(half_of(x, i));
+            sum = fmaf(v, v, sum);
+            top = fmaxf(top, fabsf(v * value_of(half_of(gamma, i))));
+        }
+    }
+};
+
+// The reciprocal root of the mean square, times the power of two that the row goes in with (1, or what brings its largest value to 2^14 or just below 2^15);
+// what takes that back.
+struct Factors { float r, back; };
+
 template <int THREADS>
-__device__ __forceinline__ float sum_over_threads(float sum, float *s_sum)
+__device__ __forceinline__ Factors factors_of(Norm n, int K, float eps, float2 *s_norm)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
-    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+    uint32_t top = __builtin_bit_cast(uint32_t, n.top);       // (in the order of the values, as none is below zero)
+    // to lane 15 of each row of 16, then to lane 63 (lanes that have nobody to take from take 0)
+#define ATOM_FROM(v, ctrl, rows) __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, rows, 0xF, false)
+#define ATOM_STEP(ctrl, rows)                                              \
+    n.sum += __builtin_bit_cast(float, ATOM_FROM(n.sum, ctrl, rows));      \
+    top = max(top, (uint32_t)ATOM_FROM(top, ctrl, rows))
+    ATOM_STEP(0x111, 0xF);
+    ATOM_STEP(0x112, 0xF);
+    ATOM_STEP(0x114, 0xF);
+    ATOM_STEP(0x118, 0xF);
+    ATOM_STEP(0x142, 0xA);
+    ATOM_STEP(0x143, 0xC);
+#undef ATOM_STEP
+#undef ATOM_FROM
+    if ((threadIdx.x & 63) == 63) s_norm[threadIdx.x >> 6] = make_float2(n.sum, __builtin_bit_cast(float, top));
     __syncthreads();
-    sum = 0.0f;
+    n.sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) sum += s_sum[w];
-    return sum;
+    for (int w = 0; w < THREADS / 64; ++w) {
+        n.sum += s_norm[w].x;
+        top = max(top, __builtin_bit_cast(uint32_t, s_norm[w].y));
+    }
+    const float r = 1.0f / sqrtf(n.sum / (float)K + eps);
+    // (What is not finite has the largest exponent, a row of zeros the smallest: both go in as they are.  A product of two halves is 2^-48 at least, so top * r is a normal
+    // number whatever eps.)
+    const int exponent = (int)(__builtin_bit_cast(uint32_t, __builtin_bit_cast(float, top) * r) >> 23 & 0xffu);
+    const int e = exponent ? min(max(127 + 14 - exponent, 0), 126) : 0;
+    return {r * __builtin_bit_cast(float, (127 + e) << 23), __builtin_bit_cast(float, (127 - e) << 23)};
 }
 
 // What a thread reads of a row first, so that it is on its way before anything waits.
@@ -138,26 +179,24 @@ __device__ __forceinline__ Front front_of(const Args &p, const __half *__restric
 }
 
 // Row x in reordered order, behind the norm where there is gamma, laid out for the product: eight channels from k on go to
-// place(k), hi and lo apart (lo only behind a norm).  nat: LDS of natural_bytes(); all threads of the workgroup call.
+// place(k), hi and lo apart (lo only behind a norm).  nat: LDS of natural_bytes(); all threads of the workgroup call.  Gives what takes the row's power of two back.
 template <int THREADS, class Place>
-__device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict__ x, const Front &f, uint32_t *nat, float *s_sum, Place place)
+__device__ __forceinline__ float lay_out(const Args &p, const __half *__restrict__ x, const Front &f, uint32_t *nat, float2 *s_norm, Place place)
 {
     const int tid = threadIdx.x, blocks = p.K / 8, K4 = p.K - p.O;
     const uint4 *row = reinterpret_cast<const uint4 *>(x);
+    float back = 1.0f;
     if (p.gamma) {
-        float sum = 0.0f;
+        const uint4 *gamma = reinterpret_cast<const uint4 *>(p.gamma);
+        Norm norm;
+        for (int b = tid; b < blocks; b += THREADS) norm.add(b == tid ? f.x : row[b], b == tid ? f.gamma : gamma[b]);
+        const Factors by = factors_of<THREADS>(norm, p.K, p.eps, s_norm);
+        back = by.back;
         for (int b = tid; b < blocks; b += THREADS) {
-            const uint4 v = b == tid ? f.x : row[b];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(value_of(half_of(v, i)), value_of(half_of(v, i)), sum);
-        }
-        sum = sum_over_threads<THREADS>(sum, s_sum);
-        const float r = 1.0f / sqrtf(sum / (float)p.K + p.eps);
-        for (int b = tid; b < blocks; b += THREADS) {
-            const uint4 v = b == tid ? f.x : row[b], g = b == tid ? f.gamma : reinterpret_cast<const uint4 *>(p.gamma)[b];
+            const uint4 v = b == tid ? f.x : row[b], g = b == tid ? f.gamma : gamma[b];
             uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = halves_of(value_of(half_of(v, i)) * r * value_of(half_of(g, i)));
+            for (int i = 0; i < 8; ++i) w[i] = halves_of(value_of(half_of(v, i)) * value_of(half_of(g, i)) * by.r);
             reinterpret_cast<uint4 *>(nat)[2 * b] = make_uint4(w[0], w[1], w[2], w[3]);
             reinterpret_cast<uint4 *>(nat)[2 * b + 1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
@@ -188,6 +227,7 @@ __device__ __forceinline__ void lay_out(const Args &p, const __half *__restrict_
         place(8 * b, 0, packed<false>(w));
         if (p.gamma) place(8 * b, 1, packed<true>(w));
     }
+    return back;
 }
 
 __host__ __device__ constexpr size_t natural_bytes(int K, bool norm, bool index) { return norm ? 4 * (size_t)K : index ? 2 * (size_t)K : 0; }
@@ -219,10 +259,11 @@ __global__ __launch_bounds__(THREADS)
 void w4a16_gather_kernel(Args p, uint4 *out)
 {
     extern __shared__ uint32_t s_nat[];
-    __shared__ float s_sum[THREADS / 64];
+    __shared__ float2 s_norm[THREADS / 64];
     const int64_t m = blockIdx.x;
     const __half *x = p.x + m * p.ldx;
-    lay_out<THREADS>(p, x, front_of<THREADS>(p, x), s_nat, s_sum, [&](int k, int half, const uint4 &v) { put<WIDE>(p, out, m, k, half, v); });
+    const float back = lay_out<THREADS>(p, x, front_of<THREADS>(p, x), s_nat, s_norm, [&](int k, int half, const uint4 &v) { put<WIDE>(p, out, m, k, half, v); });
+    if (p.gamma && threadIdx.x == 0) p.back[m] = back;
 }
 
 constexpr int kRowChannels = 4096;                            // of a row, of a workgroup
@@ -232,7 +273,7 @@ template <bool WIDE>
 __global__ __launch_bounds__(512)
 void w4a16_rows_kernel(Args p, uint4 *out)
 {
-    __shared__ float s_sum[8];
+    __shared__ float2 s_norm[8];
     const int tid = threadIdx.x, blocks = p.K / 8, b = (int)blockIdx.y * (kRowChannels / 8) + tid, k = 8 * min(b, blocks - 1);
     const int64_t m = blockIdx.x;
     const __half *x = p.x + m * p.ldx;
@@ -241,15 +282,12 @@ void w4a16_rows_kernel(Args p, uint4 *out)
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = half_of(v, i);
     if (p.gamma) {
-        float sum = 0.0f;
-        for (int j = tid; j < blocks; j += 512) {
-            const uint4 y = reinterpret_cast<const uint4 *>(x)[j];
+        Norm norm;
+        for (int j = tid; j < blocks; j += 512) norm.add(reinterpret_cast<const uint4 *>(x)[j], reinterpret_cast<const uint4 *>(p.gamma)[j]);
+        const Factors by = factors_of<512>(norm, p.K, p.eps, s_norm);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(value_of(half_of(y, i)), value_of(half_of(y, i)), sum);
-        }
-        const float r = 1.0f / sqrtf(sum_over_threads<512>(sum, s_sum) / (float)p.K + p.eps);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = halves_of(value_of(w[i]) * r * value_of(half_of(g, i)));
+        for (int i = 0; i < 8; ++i) w[i] = halves_of(value_of(w[i]) * value_of(half_of(g, i)) * by.r);
+        if (blockIdx.y == 0 && tid == 0) p.back[m] = by.back;
     }
     if (b >= blocks) return;
     in_order(w, k < p.K - p.O);
@@ -291,7 +329,7 @@ void w4a16_kernel(Args p)
     constexpr int WM = GATED ? 2 : 1, CT = WM * NT, AT = HL;
     static_assert(CT <= 4, "a lane's chunk loads the scales of one tile");
     extern __shared__ __align__(16) unsigned char s_all[];   // KEPT: the rows; the weights' way to the operands; the sums (before: what is laid out)
-    __shared__ float s_part[8];
+    __shared__ float2 s_norm[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, kc = lane >> 4;
     const int K4 = p.K - p.O, G = p.K >> 7, G4 = K4 >> 7, V = 2 * (G - G4);
@@ -422,7 +460,7 @@ void w4a16_kernel(Args p)
 #pragma unroll
         for (int t = 0; t < CT; ++t) add(t, part[t], (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * t + col), (int)half.scale));
     };
-        constexpr int kLanes = COMBINE ? 32 : 64;                // that have rows: half of them where lo is added to hi
+    constexpr int kLanes = COMBINE ? 32 : 64;                // that have rows: half of them where lo is added to hi
     constexpr int kTile = 4 * kLanes, kOut = (NT * kTile + kThreads - 1) / kThreads;       // outputs of a tile, of a thread
     auto output = [&](uint32_t tile, int i, int64_t &m, int64_t &out) ATOM_INLINE {
         const int at = tid + i * kThreads, l = at % kLanes;
@@ -430,6 +468,9 @@ void w4a16_kernel(Args p)
         out = (int64_t)tile * (16 * NT) + 16 * (at / kTile) + (l & 15);
         return at < NT * kTile && m < p.M && out < p.N;
     };
+    const int my_row = min(4 * (tid % kLanes >> 4) + (tid / kLanes & 3), rows - 1);       // of all outputs of this thread
+    float back = 1.0f;
+    if constexpr (!KEPT && (COMBINE || HL == 2)) back = p.back[my_row];
     uint16_t residual[kOut];
     auto fetch_residual = [&](uint32_t tile) ATOM_INLINE {               // (at a tile's beginning: at its end all loads under way would be waited for)
         if constexpr (!GATED) {
@@ -468,6 +509,7 @@ void w4a16_kernel(Args p)
                 sum[x] = 0.0f;
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) sum[x] += mine[(w * CT + x * NT) * kTile + at];
+                if constexpr (COMBINE || HL == 2) sum[x] *= back;
             }
             float y = sum[0];
             if (p.parts > 1) {
@@ -494,8 +536,9 @@ void w4a16_kernel(Args p)
                 __syncthreads();
                 front.x = front_of<kThreads>(p, p.x + m * p.ldx).x;
             }
-            lay_out<kThreads>(p, p.x + m * p.ldx, front, nat, s_part,
-                              [&](int k, int half, const uint4 &v) { *reinterpret_cast<uint4 *>(out + (size_t)(m + half * rows) * lds_row + 8 * row_place(k, K4)) = v; });
+            const float by = lay_out<kThreads>(p, p.x + m * p.ldx, front, nat, s_norm,
+                                               [&](int k, int half, const uint4 &v) { *reinterpret_cast<uint4 *>(out + (size_t)(m + half * rows) * lds_row + 8 * row_place(k, K4)) = v; });
+            if (COMBINE && m == my_row) back = by;
         }
         __syncthreads();
     }
@@ -643,6 +686,15 @@ void w4a16_wide_kernel(Args p)
 
     const int64_t n = rows_of(wave) + col, m0 = (int64_t)block * (32 * RT) + 4 * kc;
     auto row_of = [&](int r, int j) ATOM_INLINE { return m0 + 32 * r + 8 * (j >> 2) + (j & 3); };
+    if constexpr (HL == 2)                                   // behind a norm (of rows >= M there is room for it)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f4 back = *reinterpret_cast<const f4 *>(p.back + row_of(r, 4 * q));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[r][4 * q + j] *= back[j];
+            }
     if (p.parts > 1) {
         if (n < p.N)
 #pragma unroll
@@ -785,10 +837,14 @@ static size_t laid_out_bytes(const ProductShape &s, int64_t M, int K, int O, boo
     return (size_t)((M + 32 * s.wide - 1) / (32 * s.wide)) * ((K + O) / 128) * s.wide * (norm ? 2 : 1) * 8192;
 }
 
+// What takes the rows' powers of two back, of whole blocks of 64 rows.
+static size_t back_bytes(const ProductShape &s, int64_t M, bool norm) { return norm && !s.kept ? (size_t)((M + 63) / 64) * 256 : 0; }
+
+// The rows, what takes their powers of two back, the parts' sums.
 size_t w4a16_workspace_bytes(int64_t M, int64_t N, int K, int O, bool gated, bool norm, bool index)
 {
     const ProductShape s = product_shape(M, N, K, O, gated, norm, index);
-    return laid_out_bytes(s, M, K, O, norm) + (s.parts > 1 ? (size_t)s.parts * M * N * (gated ? 8 : 4) : 0);
+    return laid_out_bytes(s, M, K, O, norm) + back_bytes(s, M, norm) + (s.parts > 1 ? (size_t)s.parts * M * N * (gated ? 8 : 4) : 0);
 }
 
 bool w4a16_fits(int64_t M, int64_t N, int K, int O, bool gated)
@@ -807,9 +863,10 @@ hipError_t launch_w4a16(const W4A16 &a, hipStream_t stream)
     const bool gated = a.w[1].q4 != nullptr, norm = a.gamma != nullptr;
     const ProductShape s = product_shape(a.M, a.N, a.K, a.O, gated, norm, a.idx != nullptr);
     const int  halves = norm && !s.combine ? 2 : 1;           // that go in one after the other
+    char *back = (char *)a.workspace + laid_out_bytes(s, a.M, a.K, a.O, norm);
     Args p = {(const __half *)a.x, a.ldx, a.M, (const __half *)a.gamma, a.eps, a.idx, a.K, a.O, {a.w[0], a.w[1]}, a.N, (const __half *)a.residual, a.ldr,
-              (__half *)a.y, a.ldy, (const __half *)a.workspace, (int)a.M, s.combine, 0, s.parts, s.span,
-              (float *)((char *)a.workspace + laid_out_bytes(s, a.M, a.K, a.O, norm)), s.wide, halves, 1};
+              (__half *)a.y, a.ldy, (const __half *)a.workspace, (int)a.M, (float *)back, s.combine, 0, s.parts, s.span,
+              (float *)(back + back_bytes(s, a.M, norm)), s.wide, halves, 1};
 #define ATOM_LAUNCH(grid, threads, lds, kernel, ...)                                                                  \
     do {                                                                                                              \
         static atom_launch::LdsOptIn opt;                                                                             \
