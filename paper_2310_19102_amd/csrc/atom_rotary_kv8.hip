@@ -41,11 +41,9 @@ __device__ __forceinline__ Scale scale_of(uint32_t top, float s_old)
     return {s, s >= 1.17549435e-38f ? 1.0f / s : 0.0f, s_old / s, s > s_old && s_old > 0.0f};
 }
 
-__device__ __forceinline__ void recode16(int8_t *at, float ratio)
+__device__ __forceinline__ uint4 recode16(const uint4 &w, float ratio)
 {
-    uint4 w = *reinterpret_cast<const uint4 *>(at);
-    w = make_uint4(recode4(w.x, ratio), recode4(w.y, ratio), recode4(w.z, ratio), recode4(w.w, ratio));
-    *reinterpret_cast<uint4 *>(at) = w;
+    return make_uint4(recode4(w.x, ratio), recode4(w.y, ratio), recode4(w.z, ratio), recode4(w.w, ratio));
 }
 
 // A run of rows of K, turned, or of V, for one head after another: Run (atom_kv8_append.h) on fp32 values, the maximum as the bits of a
@@ -154,7 +152,8 @@ struct TurnedRun {
         const Scale scale = scale_of(top, s_old);
         const float r = scale.r;
         if (scale.grown)
-            for (int b = 16 * thread; b < o * D; b += 16 * threads) recode16(block + b, scale.ratio);
+            for (int b = 16 * thread; b < o * D; b += 16 * threads)
+                *reinterpret_cast<uint4 *>(block + b) = recode16(*reinterpret_cast<const uint4 *>(block + b), scale.ratio);
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
             if (u * RPL < len) store(block, u * RPL + g, x[u], r);
@@ -166,6 +165,21 @@ struct TurnedRun {
         if (thread == 0) side.scale[head] = scale.s;
     }
 };
+
+// The first `bytes` of a block's codes on a grown scale, by a wavefront: eight pieces of a lane are on their way before the first is written (behind the last piece: that
+// one again; loads under a condition each are slower).
+__device__ __forceinline__ void recode_block(int8_t *block, int bytes, float ratio)
+{
+    constexpr int DEEP = 8;
+    for (int b = 16 * (int)(threadIdx.x & 63); b < bytes; b += 1024 * DEEP) {
+        uint4 w[DEEP];
+#pragma unroll
+        for (int u = 0; u < DEEP; ++u) w[u] = *reinterpret_cast<const uint4 *>(block + min(b + 1024 * u, bytes - 16));
+#pragma unroll
+        for (int u = 0; u < DEEP; ++u)
+            if (b + 1024 * u < bytes) *reinterpret_cast<uint4 *>(block + b + 1024 * u) = recode16(w[u], ratio);
+    }
+}
 
 // Runs of one row each, a row to D / 8 lanes: those of tokens t_first + l that begin one, l from `group` on in steps of `groups`, for heads h0 .. h1 - 1 of K (keys) or
 // of V.  (Taken by a wavefront each, 300 tokens of 32 heads were 21.0 us, now 7.0, 1000 60 and 14.8.)
@@ -185,36 +199,49 @@ __device__ __forceinline__ void append_singles(const Turn &t, const Side &side, 
         if constexpr (!ONE)
 #pragma unroll
             for (int a = 1; a < 4; ++a) at.p[a] = __shfl(near.p[a], l, 64);
-        if (l0 + group >= slab || !(w.leaders >> l & 1)) continue;
+        const bool mine = l0 + group < slab && (w.leaders >> l & 1);
+        if (!__ballot(mine)) continue;
         const __half *row = side.x + (t_first + l) * side.ld;
-        uint2 lo = load4<false>(row + h0 * D + ch.lo), hi = load4<false>(row + h0 * D + ch.hi);
+        uint2 lo, hi;
         Angles r;
-        if (keys) r = angles<ONE>(t, at, i, axes);
+        if (mine) {
+            lo = load4<false>(row + h0 * D + ch.lo);
+            hi = load4<false>(row + h0 * D + ch.hi);
+            if (keys) r = angles<ONE>(t, at, i, axes);
+        }
         const int o = slot & ((1 << shift) - 1);
         for (int h = h0; h < h1; ++h) {
-            const int64_t head = (int64_t)(slot >> shift) * Hkv + h;
-            const float s_old = o > 0 ? side.scale[head] : 0.0f;
-            float x[8];
-            widen(lo, x);
-            widen(hi, x + 4);
-            if (h + 1 < h1) {
-                lo = load4<false>(row + (h + 1) * D + ch.lo);
-                hi = load4<false>(row + (h + 1) * D + ch.hi);
+            const uint32_t head = (uint32_t)(slot >> shift) * Hkv + h;         // (fewer than 2^31: host)
+            Scale s = {};
+            if (mine) {
+                const float s_old = o > 0 ? side.scale[head] : 0.0f;
+                float x[8];
+                widen(lo, x);
+                widen(hi, x + 4);
+                if (h + 1 < h1) {
+                    lo = load4<false>(row + (h + 1) * D + ch.lo);
+                    hi = load4<false>(row + (h + 1) * D + ch.hi);
+                }
+                if (keys && ch.turned) turn<NEIGHBOURS>(x, r, 1.0f);
+                uint32_t top = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = max(top, __builtin_bit_cast(uint32_t, x[k]) & 0x7fffffffu);
+#pragma unroll
+                for (int step = 1; step < LPR; step *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, step, 64));
+                s = scale_of(top, s_old);
+                int8_t *block = side.codes + ((int64_t)head << shift) * D;
+                const uint32_t a = s.r > 0.0f ? codes4(x, s.r) : 0, b = s.r > 0.0f ? codes4(x + 4, s.r) : 0;
+                *reinterpret_cast<uint32_t *>(block + o * D + ch.lo) = a;
+                *reinterpret_cast<uint32_t *>(block + o * D + ch.hi) = b;
+                if (i == 0) side.scale[head] = s.s;
             }
-            if (keys && ch.turned) turn<NEIGHBOURS>(x, r, 1.0f);
-            uint32_t top = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) top = max(top, __builtin_bit_cast(uint32_t, x[k]) & 0x7fffffffu);
-#pragma unroll
-            for (int step = 1; step < LPR; step *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, step, 64));
-            const Scale s = scale_of(top, s_old);
-            int8_t *block = side.codes + (head << shift) * D;
-            if (s.grown)
-                for (int b = 16 * i; b < o * D; b += 16 * LPR) recode16(block + b, s.ratio);
-            const uint32_t a = s.r > 0.0f ? codes4(x, s.r) : 0, b = s.r > 0.0f ? codes4(x + 4, s.r) : 0;
-            *reinterpret_cast<uint32_t *>(block + o * D + ch.lo) = a;
-            *reinterpret_cast<uint32_t *>(block + o * D + ch.hi) = b;
-            if (i == 0) side.scale[head] = s.s;
+            // Older rows by the whole wavefront, as their arithmetic takes as long for a row's own lanes as for all.  (Steps of 64 tokens of 32 heads behind one another, where
+            // some scales grow with every step, at rows 24 to 63 of blocks of 64: 6.6 us, by a row's own lanes 14.7; 4.4 where none grows.)
+            for (uint64_t grown = __ballot(mine && s.grown && i == 0); grown; grown &= grown - 1) {
+                const int from = __builtin_ctzll(grown);
+                recode_block(side.codes + ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)head, from) << shift) * D, __builtin_amdgcn_readlane(o, from) * D,
+                             __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, s.ratio), from)));
+            }
         }
     }
 }
