@@ -81,6 +81,8 @@ hipError_t launch_rotary_table(const double *freq, int n_pairs, int64_t n_pos, f
 // Values from which a lane takes four heads and their angles once (a step of 64 tokens of 40 heads of 128: 3.2 us with one, 3.55 with four; 200 tokens 4.2
 // and 3.75; 1600 20.8 and 9.3), and from which the heads come past the caches (3200 such tokens: 14.8 us through them, 16.8 past them; 6400 29.3 and
 // 27.4; 4999 tokens of 72 heads with three axes 37.4 and 33.3, and 31.4 with the positions asked for first: 5.9 TB/s, what is read and written bounds it).
+// Of two heads a lane takes both, and one where there is no other: a place without a head reads the last one once more (300000 tokens of one head 32.9 us, with four places
+// 44.6; 120000 of two 22.9 and 28.0; of three 25.1 with four places and 25.7 with two).
 constexpr int64_t kFourHeads = 1 << 19, kReadOnce = (int64_t)24 << 20;
 
 hipError_t launch_rotary(const void *x, int64_t T, int64_t ldx, int heads, int D, const Turn &t, bool transposed, void *out, int64_t ldo,
@@ -93,11 +95,13 @@ hipError_t launch_rotary(const void *x, int64_t T, int64_t ldx, int heads, int D
         hipLaunchKernelGGL((rotary_kernel<ONE, NEIGHBOURS, HEADS, ONCE>), dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, stream, (const __half *)x, ldx, \
                            (uint32_t)heads, (uint32_t)D, t, transposed ? -1.0f : 1.0f, (__half *)out, ldo, chunks, (uint32_t)lanes);           \
     } while (0)
-#define ATOM_ROTARY_SIZE(ONE, NEIGHBOURS)                                    \
-    do {                                                                     \
-        if (work < kFourHeads)     ATOM_ROTARY(ONE, NEIGHBOURS, 1, false);   \
-        else if (work < kReadOnce) ATOM_ROTARY(ONE, NEIGHBOURS, 4, false);   \
-        else                       ATOM_ROTARY(ONE, NEIGHBOURS, 4, true);    \
+#define ATOM_ROTARY_SIZE(ONE, NEIGHBOURS)                                                  \
+    do {                                                                                   \
+        if (work < kFourHeads || heads == 1)     ATOM_ROTARY(ONE, NEIGHBOURS, 1, false);   \
+        else if (heads == 2 && work < kReadOnce) ATOM_ROTARY(ONE, NEIGHBOURS, 2, false);   \
+        else if (heads == 2)                     ATOM_ROTARY(ONE, NEIGHBOURS, 2, true);    \
+        else if (work < kReadOnce)               ATOM_ROTARY(ONE, NEIGHBOURS, 4, false);   \
+        else                                     ATOM_ROTARY(ONE, NEIGHBOURS, 4, true);    \
     } while (0)
     const int64_t work = T * heads * D;
     if (t.axes == 1) {
