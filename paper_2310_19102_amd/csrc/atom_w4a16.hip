@@ -303,6 +303,15 @@ void w4a16_rows_kernel(Args p, uint4 *out)
 // loop wait for all loads under way in every turn, not in the first alone.
 __device__ __forceinline__ void all_loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
+// Between LDS writes of a wavefront's lanes and reads of other lanes of it: the LDS takes a wavefront's operations in their order, so no instruction is needed, but the
+// compiler must not change that order.
+__device__ __forceinline__ void lanes_see_lds()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 __device__ __forceinline__ float gated(float gate, float up) { return gate / (1.0f + expf(-gate)) * up; }
 
 template <bool GATED>
@@ -410,8 +419,10 @@ void w4a16_kernel(Args p)
     // piece p of row r lies at 4 r + (p ^ (r / 4 & 3)): the 16 lanes of a chunk read all banks
     u4 *turn_to = s_turn + (lane & ~3) + ((lane ^ (lane >> 4)) & 3), *turn_from = s_turn + 4 * col + ((kc ^ (col >> 2)) & 3);
     auto operands = [&](const u4 (&from)[CT], u4 (&q)[CT]) ATOM_INLINE {
+        lanes_see_lds();                                     // (what was read there is read)
 #pragma unroll
         for (int t = 0; t < CT; ++t) turn_to[t * 64] = from[t];
+        lanes_see_lds();
 #pragma unroll
         for (int t = 0; t < CT; ++t) q[t] = turn_from[t * 64];
     };
@@ -630,8 +641,10 @@ void w4a16_wide_kernel(Args p)
         const int count = min(kScales, G - scale0);
         scale_end = scale0 + count <= G4 ? scale0 + count : G4 + 2 * (scale0 + count - G4);
         const uint16_t *from = w.scale + scale0 + min(lane, count - 1);
+        lanes_see_lds();                                     // (what was read there is read)
 #pragma unroll 16
         for (int r = 0; r < 32; ++r) my_scales[r * (kScales + 2) + lane] = from[min(rows_of(wave) + r, p.N - 1) * G];
+        lanes_see_lds();
     };
     f16 acc[RT] = {};
     auto compute = [&](int u) ATOM_INLINE {
