@@ -113,16 +113,22 @@ __device__ __forceinline__ uint4 packed(const uint32_t (&w)[8])
 // A row behind the norm: the sum of its squares, the largest magnitude of x times gamma; what a thread found of them.
 struct Norm {
     float sum = 0.0f, top = 0.0f;
-    __device__ __forceinline__ void add(const uint4 &x, const uint4 &gamma)
+    __device__ __forceinline__ void add(const uint4 &x, const float (&xg)[8])
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float v = value_of(half_of(x, i));
-            sum = fmaf(v, v, sum);
-            top = fmaxf(top, fabsf(v * value_of(half_of(gamma, i))));
+            sum = fmaf(value_of(half_of(x, i)), value_of(half_of(x, i)), sum);
+            top = fmaxf(top, fabsf(xg[i]));
         }
     }
 };
+
+// x times gamma, exact.
+__device__ __forceinline__ void products(float (&xg)[8], const uint4 &x, const uint4 &gamma)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) xg[i] = value_of(half_of(x, i)) * value_of(half_of(gamma, i));
+}
 
 // The reciprocal root of the mean square, times the power of two that the row goes in with (1, or what brings its largest value to 2^14 or just below 2^15);
 // what takes that back.
@@ -189,14 +195,21 @@ __device__ __forceinline__ float lay_out(const Args &p, const __half *__restrict
     if (p.gamma) {
         const uint4 *gamma = reinterpret_cast<const uint4 *>(p.gamma);
         Norm norm;
-        for (int b = tid; b < blocks; b += THREADS) norm.add(b == tid ? f.x : row[b], b == tid ? f.gamma : gamma[b]);
+        float xg[8], more[8];
+        products(xg, f.x, f.gamma);
+        if (tid < blocks) norm.add(f.x, xg);
+        for (int b = tid + THREADS; b < blocks; b += THREADS) {
+            const uint4 v = row[b];
+            products(more, v, gamma[b]);
+            norm.add(v, more);
+        }
         const Factors by = factors_of<THREADS>(norm, p.K, p.eps, s_norm);
         back = by.back;
         for (int b = tid; b < blocks; b += THREADS) {
-            const uint4 v = b == tid ? f.x : row[b], g = b == tid ? f.gamma : gamma[b];
+            if (b != tid) products(xg, row[b], gamma[b]);
             uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = halves_of(value_of(half_of(v, i)) * value_of(half_of(g, i)) * by.r);
+            for (int i = 0; i < 8; ++i) w[i] = halves_of(xg[i] * by.r);
             reinterpret_cast<uint4 *>(nat)[2 * b] = make_uint4(w[0], w[1], w[2], w[3]);
             reinterpret_cast<uint4 *>(nat)[2 * b + 1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
@@ -283,10 +296,16 @@ void w4a16_rows_kernel(Args p, uint4 *out)
     for (int i = 0; i < 8; ++i) w[i] = half_of(v, i);
     if (p.gamma) {
         Norm norm;
-        for (int j = tid; j < blocks; j += 512) norm.add(reinterpret_cast<const uint4 *>(x)[j], reinterpret_cast<const uint4 *>(p.gamma)[j]);
+        float xg[8];
+        for (int j = tid; j < blocks; j += 512) {
+            const uint4 y = reinterpret_cast<const uint4 *>(x)[j];
+            products(xg, y, reinterpret_cast<const uint4 *>(p.gamma)[j]);
+            norm.add(y, xg);
+        }
         const Factors by = factors_of<512>(norm, p.K, p.eps, s_norm);
+        products(xg, v, g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = halves_of(value_of(w[i]) * value_of(half_of(g, i)) * by.r);
+        for (int i = 0; i < 8; ++i) w[i] = halves_of(xg[i] * by.r);
         if (blockIdx.y == 0 && tid == 0) p.back[m] = by.back;
     }
     if (b >= blocks) return;
