@@ -885,7 +885,7 @@ bool w4a16_fits(int64_t M, int64_t N, int K, int O, bool gated)
     if (M == 0 || N == 0) return true;
     const int64_t G = K / 128, widest = (K - O) / 2 > O ? (K - O) / 2 : O;
     if (N > 0xffffffffLL / (widest > 2 * G ? widest : 2 * G)) return false;           // 32-bit offsets
-    // workgroups: a row each, tiles of outputs (of 128 at least where there are many rows) and rows, 256 outputs of a join each
+    // threads: 1024 for a row, 512 for each of up to 32 parts (as 16 times 1024) of a tile of 128 outputs at least and 32 rows, 256 for as many outputs of a join
     const int64_t most = atom_launch::kMostThreads / 1024;
     return M <= most && (N + 15) / 16 <= most && (N + 127) / 128 * 16 <= most / ((M + 31) / 32) && M <= most * 256 / N;
 }
