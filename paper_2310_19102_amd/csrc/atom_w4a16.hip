@@ -597,7 +597,7 @@ typedef float f16 __attribute__((ext_vector_type(16)));
 // and weights come a unit at a time through LDS, a tile by each wavefront.  `parts` workgroups share a tile's units where the tiles alone do not
 // fill the card; their sums meet in the workspace.  What the L2 delivers to all compute units together (about 8 TB/s) is the tightest bound beside
 // memory, so scales come 64 of a row at a time (by themselves, 2 bytes bring a line each: as much as the weights), and rows behind M are not fetched.
-// 33 rows, 8192 outputs of 28672 channels: 46 us of the call's 51 (2.6 TB/s of weights; a second tile of 32 rows for one); 64 rows, gated 28672 of 8192
+// 33 rows, 8192 outputs of 28672 channels: 42.5 us of the call's 51 (2.9 TB/s of weights; a second tile of 32 rows for one); 64 rows, gated 28672 of 8192
 // behind the norm: 130 of 138, at 920 TFLOP/s with both halves of the activations.  One or two units under way and short code: with three or four, and scales
 // eight rows at a time, 20 rows and 4000 outputs of 8192 channels took 25.2 us, now 20.7.
 template <bool GATED, int RT, int HL>
